@@ -191,6 +191,93 @@ dar_status dar_attn_decode_noalloc(const dar_cache *cache, int32_t Hq, const voi
                                    const float *Uk, const float *Uv, float scale, void *out,
                                    void *stream);
 
+/*
+ * A decode step for a batch whose sequences, in groups, share the first pages of
+ * their contexts (samples of one prompt; requests behind one system prompt or
+ * document).  Sequence b belongs to group[b] (int32[B]; -1 = none, else in
+ * [0, n_groups)), and the first prefix_pages[i] pages (int32[n_groups]) of all
+ * members of group i are the same physical pages: positions
+ * 0 .. 64 prefix_pages[i] - 1.  Results are those of dar_attn_decode; the shared
+ * pages are read once per group and KV head instead of once per member, with the
+ * members' queries as the rows of one product, and joined with each sequence's
+ * own part by log-sum-exp (one softmax, Eq. 4).
+ *  - The shared pages' ids are taken from the block table of a group's first
+ *    member; the others' entries for them are not read.
+ *  - A member for which some of them are not distant yet
+ *    (seq_lens[b] - w < 64 prefix_pages[i]) is attended alone, by its own table.
+ *  - group and prefix_pages are device arrays; both may be NULL when n_groups is 0.
+ *    0 <= n_groups <= B.
+ *  - A group outside [-1, n_groups) sets *status = DAR_ERR_INVALID_ARG (the
+ *    sequence is attended alone), a prefix_pages outside [0, max_pages_per_seq]
+ *    DAR_ERR_CAPACITY (the group shares nothing).  A length outside
+ *    [0, max_pages_per_seq * 64 + w] or a needed block-table entry outside
+ *    [0, num_pages) sets DAR_ERR_CAPACITY; out is then undefined for the
+ *    sequences that need it.
+ * Arguments, sizes and alignment otherwise as dar_attn_decode; two kernels in
+ * order on `stream`, the first after all earlier work on it.  Workspace of
+ * dar_decode_shared_workspace_bytes(cache, Hq) bytes, no initialisation; calls
+ * that share one must not overlap on the device.  Deterministic.
+ */
+size_t dar_decode_shared_workspace_bytes(const dar_cache *cache, int32_t Hq);
+dar_status dar_attn_decode_shared(const dar_cache *cache, int32_t Hq, const void *q, const float *Uk,
+                                  const float *Uv, const int32_t *group, int32_t n_groups,
+                                  const int32_t *prefix_pages, float scale, void *out, void *workspace,
+                                  size_t workspace_bytes, void *stream);
+
+/*
+ * A decode step that also accumulates attention weights: with p_hj the softmax
+ * weight of the token at position j in query head h (Eq. 4),
+ *   weights[b][g][j] = decay * weights[b][g][j] + sum over the heads h of KV head g of p_hj
+ * for j in [0, seq_lens[b]), ring and pages alike; entries behind stay as they are.
+ * weights [B][Hkv][max_pages_per_seq * 64 + w] fp32 belongs to the caller, who
+ * zero-fills a sequence's entries when its context starts (a token that is appended
+ * later finds a zero: dar_cache_evict leaves zeros behind the new end).
+ * 0 <= decay <= 1; decay = 1 accumulates over all steps, and decay = 0 keeps this
+ * step's weights alone, whatever was there.  out is that of dar_attn_decode.
+ * Scores, maxima and sums are fp32.
+ * Arguments, sizes, alignment (weights too) and errors otherwise as
+ * dar_attn_decode; Hq / Hkv <= 1024.  For a sequence with a bad length or page,
+ * out and its weights are undefined.  Two kernels in order on `stream`, the first
+ * after all earlier work on it.  Workspace of
+ * dar_decode_scored_workspace_bytes(cache, Hq) bytes (4 bytes per query head and
+ * position of capacity, and partial results), no initialisation; calls that share
+ * one must not overlap on the device.  Deterministic.
+ */
+size_t dar_decode_scored_workspace_bytes(const dar_cache *cache, int32_t Hq);
+dar_status dar_attn_decode_scored(const dar_cache *cache, int32_t Hq, const void *q, const float *Uk,
+                                  const float *Uv, float scale, float *weights, float decay, void *out,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Eviction of distant tokens by accumulated attention weight, in place.  Let
+ * n = max(0, seq_lens[b] - w) be a sequence's distant tokens and keep[b] (device
+ * int32[B]) its budget.  n <= keep[b]: nothing changes.  Otherwise, for each KV head
+ * on its own: the tokens at positions [0, protect[b]) stay (device int32[B]; NULL =
+ * 0), and of those at [protect[b], n) the keep[b] - protect[b] with the largest
+ * weights[b][g][.] (of equal weights the lower positions; NaN ranks lowest).  The
+ * bottleneck vectors and weights of tokens that stay at positions >= keep[b] move, in
+ * ascending order, into the positions < keep[b] that evicted tokens leave, in
+ * ascending order (attention does not depend on the order of distant tokens).  The
+ * window's tokens stay and come down to positions keep[b] .. keep[b] + w - 1: the ring
+ * turns by (n - keep[b]) mod w slots (a multiple of w moves nothing) and their weights
+ * follow.  Weights at positions [keep[b] + w, old length) become zero, and
+ * seq_lens[b] = keep[b] + w.  Everything else stays as it is: rows of pages behind
+ * keep[b] keep their bytes, and pages from ceil(keep[b] / 64) on are free for reuse.
+ *  - Pages that several sequences list (a shared prefix) have to lie in the protected
+ *    part, which is neither read nor written.
+ *  - keep[b] < 0, protect[b] < 0 or protect[b] > keep[b] sets
+ *    *status = DAR_ERR_INVALID_ARG, a length outside [0, max_pages_per_seq * 64 + w]
+ *    or a page id outside [0, num_pages) among those of positions [protect[b], n)
+ *    DAR_ERR_CAPACITY; such a sequence is left as it is.
+ *  - fp32 and bf16; weights as in dar_attn_decode_scored, 16-byte aligned.
+ * Two kernels in order on `stream`, the first after all earlier work on it.  Workspace
+ * of dar_cache_evict_workspace_bytes(cache) bytes, no initialisation; calls that share
+ * one must not overlap on the device.  Deterministic.
+ */
+size_t dar_cache_evict_workspace_bytes(const dar_cache *cache);
+dar_status dar_cache_evict(const dar_cache *cache, float *weights, const int32_t *keep,
+                           const int32_t *protect, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Bytes of workspace dar_attn_prefill needs (the Eq. 1 vectors of all tokens). */
 size_t dar_prefill_workspace_bytes(dar_dtype dtype, int32_t B, int32_t Hkv, int32_t N,
                                    int32_t d_down);

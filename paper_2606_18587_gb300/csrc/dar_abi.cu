@@ -203,6 +203,59 @@ dar_status prepare_decode(const dar_cache *cache, int32_t Hq, const void *q, con
     return ok();
 }
 
+// Checks what dar_attn_decode_shared and dar_attn_decode_scored have in common and fills *a;
+// *empty = nothing to launch.
+dar_status prepare_segments(const dar_cache *cache, int32_t Hq, const void *q, const float *Uk, const float *Uv,
+                            float scale, void *out, const void *workspace, size_t workspace_bytes, bool scored,
+                            dar::SegmentArgs *a, bool *empty)
+{
+    dar_status s = check_cache(cache);
+    if (s != DAR_OK)
+        return s;
+    if (Hq < cache->Hkv || Hq % cache->Hkv)
+        return fail(DAR_ERR_INVALID_ARG, "Hq=%d is not a multiple of Hkv=%d", Hq, cache->Hkv);
+    if (cache->B > DAR_DECODE_MAX_BATCH)
+        return fail(DAR_ERR_UNSUPPORTED, "decode batch %d > %d", cache->B, DAR_DECODE_MAX_BATCH);
+    *empty = cache->B == 0;
+    if (*empty)
+        return ok();
+    if (!q || !Uk || !Uv || !out || !workspace)
+        return fail(DAR_ERR_INVALID_ARG, "NULL pointer");
+    if (!aligned16(q) || !aligned16(out) || !aligned16(Uk) || !aligned16(Uv) || !aligned16(workspace))
+        return fail(DAR_ERR_INVALID_ARG, "q, out, Uk, Uv and workspace must be 16-byte aligned");
+    // the copies count 128-byte lines of the ring and of the pools, the line of work its stages, in int32
+    const double es = (double)esize(cache->dtype), most = 2147483647.0 - 128.0;
+    if ((double)cache->B * cache->Hkv * cache->w * cache->d * es / 128.0 >= most ||
+        (double)cache->num_pages * cache->Hkv * DAR_PAGE_SIZE * cache->d_down * es / 128.0 >= most ||
+        (double)cache->max_pages_per_seq * DAR_PAGE_SIZE + cache->w >= most ||
+        dar::segments_line_bound(cache->dtype, cache->B, Hq, cache->Hkv, cache->d_down, cache->w,
+                                 cache->max_pages_per_seq) >= most)
+        return fail(DAR_ERR_UNSUPPORTED, "cache too large for int32 line indices");
+    const size_t need = dar::segments_workspace_bytes(cache->B, Hq, cache->Hkv, cache->d_down, cache->w,
+                                                      cache->max_pages_per_seq, scored);
+    if (workspace_bytes < need)
+        return fail(DAR_ERR_CAPACITY, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+    a->q = q;
+    a->out = out;
+    a->win_k = cache->win_k;
+    a->win_v = cache->win_v;
+    a->pool_kd = cache->pool_kd;
+    a->pool_vd = cache->pool_vd;
+    a->block_table = cache->block_table;
+    a->seq_lens = cache->seq_lens;
+    a->status = cache->status;
+    a->Uk = Uk;
+    a->Uv = Uv;
+    a->B = cache->B;
+    a->Hq = Hq;
+    a->Hkv = cache->Hkv;
+    a->w = cache->w;
+    a->maxp = cache->max_pages_per_seq;
+    a->num_pages = cache->num_pages;
+    a->c2 = default_scale(scale, cache->d) * kLog2e;
+    return ok();
+}
+
 struct ChunkLayout {
     size_t pos0, kw, vw, kdt, vdt, total;
 };
@@ -340,6 +393,117 @@ dar_status dar_decode_step(const dar_cache *cache, const void *k_new, const void
         dc.prep = prepared ? dar::kPrepDone : dar::kPrepOverlaps;
     }
     return from_cuda(dar::launch_decode(cache->dtype, cache->d_down, dc, st), "dar_decode_step decode launch");
+}
+
+size_t dar_decode_shared_workspace_bytes(const dar_cache *cache, int32_t Hq)
+{
+    if (check_cache(cache) != DAR_OK || Hq < cache->Hkv || Hq % cache->Hkv)
+        return 0;
+    return dar::segments_workspace_bytes(cache->B, Hq, cache->Hkv, cache->d_down, cache->w, cache->max_pages_per_seq,
+                                         false);
+}
+
+dar_status dar_attn_decode_shared(const dar_cache *cache, int32_t Hq, const void *q, const float *Uk,
+                                  const float *Uv, const int32_t *group, int32_t n_groups,
+                                  const int32_t *prefix_pages, float scale, void *out, void *workspace,
+                                  size_t workspace_bytes, void *stream)
+{
+    dar::SegmentArgs a;
+    bool empty = false;
+    dar_status s = prepare_segments(cache, Hq, q, Uk, Uv, scale, out, workspace, workspace_bytes, false, &a, &empty);
+    if (s != DAR_OK)
+        return s;
+    if (n_groups < 0 || n_groups > cache->B)
+        return fail(DAR_ERR_INVALID_ARG, "n_groups=%d (0 to B=%d)", n_groups, cache->B);
+    if (n_groups > 0 && (!group || !prefix_pages))
+        return fail(DAR_ERR_INVALID_ARG, "group or prefix_pages is NULL");
+    if (empty)
+        return ok();
+    a.group = group;
+    a.prefix_pages = prefix_pages;
+    a.n_groups = n_groups;
+    return from_cuda(dar::launch_segments(cache->dtype, cache->d_down, a, workspace, static_cast<cudaStream_t>(stream)),
+                     "dar_attn_decode_shared launch");
+}
+
+size_t dar_decode_scored_workspace_bytes(const dar_cache *cache, int32_t Hq)
+{
+    if (check_cache(cache) != DAR_OK || Hq < cache->Hkv || Hq % cache->Hkv)
+        return 0;
+    return dar::segments_workspace_bytes(cache->B, Hq, cache->Hkv, cache->d_down, cache->w, cache->max_pages_per_seq,
+                                         true);
+}
+
+dar_status dar_attn_decode_scored(const dar_cache *cache, int32_t Hq, const void *q, const float *Uk,
+                                  const float *Uv, float scale, float *weights, float decay, void *out,
+                                  void *workspace, size_t workspace_bytes, void *stream)
+{
+    dar::SegmentArgs a;
+    bool empty = false;
+    dar_status s = prepare_segments(cache, Hq, q, Uk, Uv, scale, out, workspace, workspace_bytes, true, &a, &empty);
+    if (s != DAR_OK)
+        return s;
+    if (Hq / cache->Hkv > 1024)
+        return fail(DAR_ERR_UNSUPPORTED, "%d query heads per KV head > 1024", Hq / cache->Hkv);
+    if (!(decay >= 0.f && decay <= 1.f))
+        return fail(DAR_ERR_INVALID_ARG, "decay=%g (0 to 1)", (double)decay);
+    if (empty)
+        return ok();
+    if (!weights)
+        return fail(DAR_ERR_INVALID_ARG, "weights is NULL");
+    if (!aligned16(weights))
+        return fail(DAR_ERR_INVALID_ARG, "weights must be 16-byte aligned");
+    a.weights = weights;
+    a.decay = decay;
+    return from_cuda(dar::launch_segments(cache->dtype, cache->d_down, a, workspace, static_cast<cudaStream_t>(stream)),
+                     "dar_attn_decode_scored launch");
+}
+
+size_t dar_cache_evict_workspace_bytes(const dar_cache *cache)
+{
+    if (check_cache(cache) != DAR_OK)
+        return 0;
+    return dar::evict_workspace_bytes(cache->B, cache->Hkv, cache->w, cache->max_pages_per_seq);
+}
+
+dar_status dar_cache_evict(const dar_cache *cache, float *weights, const int32_t *keep, const int32_t *protect,
+                           void *workspace, size_t workspace_bytes, void *stream)
+{
+    dar_status s = check_cache(cache);
+    if (s != DAR_OK)
+        return s;
+    if (cache->B == 0)
+        return ok();
+    if (!weights || !keep || !workspace)
+        return fail(DAR_ERR_INVALID_ARG, "NULL pointer");
+    if (!aligned16(weights) || !aligned16(workspace))
+        return fail(DAR_ERR_INVALID_ARG, "weights and workspace must be 16-byte aligned");
+    if ((double)cache->B * cache->Hkv * 8 >= 2147483647.0 ||
+        (double)cache->max_pages_per_seq * DAR_PAGE_SIZE + cache->w >= 2147483647.0)
+        return fail(DAR_ERR_UNSUPPORTED, "B * Hkv=%lld heads or %lld positions are beyond int32",
+                    (long long)cache->B * cache->Hkv, (long long)cache->max_pages_per_seq * DAR_PAGE_SIZE + cache->w);
+    const size_t need = dar::evict_workspace_bytes(cache->B, cache->Hkv, cache->w, cache->max_pages_per_seq);
+    if (workspace_bytes < need)
+        return fail(DAR_ERR_CAPACITY, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+    dar::EvictArgs a;
+    a.win_k = cache->win_k;
+    a.win_v = cache->win_v;
+    a.pool_kd = cache->pool_kd;
+    a.pool_vd = cache->pool_vd;
+    a.block_table = cache->block_table;
+    a.seq_lens = cache->seq_lens;
+    a.status = cache->status;
+    a.weights = weights;
+    a.keep = keep;
+    a.protect = protect;
+    a.B = cache->B;
+    a.Hkv = cache->Hkv;
+    a.w = cache->w;
+    a.maxp = cache->max_pages_per_seq;
+    a.num_pages = cache->num_pages;
+    a.row_bytes = (int)(cache->d_down * esize(cache->dtype));
+    a.ring_bytes = (int)(cache->d * esize(cache->dtype));
+    return from_cuda(dar::launch_evict(a, workspace, static_cast<cudaStream_t>(stream)), "dar_cache_evict launch");
 }
 
 size_t dar_prefill_chunk_workspace_bytes(const dar_cache *cache, int32_t n)

@@ -161,6 +161,39 @@ cudaError_t launch_latent_absorb(const float *Wup, const float *WK, const float 
                                  int D, int DL, cudaStream_t s);
 cudaError_t launch_latent_decode(const LatentDecodeArgs &a, void *workspace, cudaStream_t s);
 
+// Decode steps in two segments kernels (dar_segments.cu): with groups of sequences that share
+// their first pages, or with every token's attention weight added to `weights`.
+struct SegmentArgs {
+    const void *q;
+    void *out;
+    const void *win_k, *win_v, *pool_kd, *pool_vd;
+    const int32_t *block_table, *seq_lens;
+    int32_t *status;
+    const float *Uk, *Uv;
+    const int32_t *group = nullptr, *prefix_pages = nullptr;  // [B], [n_groups]
+    float *weights = nullptr;                                 // [B][Hkv][maxp * 64 + w]
+    int B, Hq, Hkv, w, maxp, num_pages, n_groups = 0;
+    float c2;           // scale * log2(e)
+    float decay = 0.f;  // what the weights are multiplied by first
+};
+size_t segments_workspace_bytes(int B, int Hq, int Hkv, int dd, int w, int maxp, bool scored);
+double segments_line_bound(dar_dtype dt, int B, int Hq, int Hkv, int dd, int w, int maxp);
+cudaError_t launch_segments(dar_dtype dt, int dd, const SegmentArgs &s, void *workspace, cudaStream_t st);
+
+// Eviction from the cache by accumulated attention weight (dar_evict.cu).
+struct EvictArgs {
+    void *win_k, *win_v, *pool_kd, *pool_vd;
+    const int32_t *block_table;
+    int32_t *seq_lens, *status;
+    float *weights;                  // [B][Hkv][maxp * 64 + w]
+    const int32_t *keep, *protect;   // [B]; protect may be nullptr (0)
+    int B, Hkv, w, maxp, num_pages;
+    int row_bytes;                   // of a bottleneck vector
+    int ring_bytes;                  // of a ring row
+};
+size_t evict_workspace_bytes(int B, int Hkv, int w, int maxp);
+cudaError_t launch_evict(const EvictArgs &a, void *workspace, cudaStream_t st);
+
 // Chunked prefill over a cache: gather kernel, attention (chunk mode), then
 // the cache append of the chunk.  Buffers of the workspace (see dar_abi.cu).
 struct ChunkArgs {

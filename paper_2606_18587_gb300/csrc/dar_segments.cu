@@ -1,0 +1,1015 @@
+// dar_segments.cu -- two decode steps over the mixed-dimension cache that
+// dar_decode.cu does not cover (Eq. 3-4 for the query at position L_b - 1):
+//
+//  shared   the sequences of a group list the same first P pages.  The softmax of
+//           a row over prefix, rest and window is one softmax, so the three can be
+//           computed apart and joined by their maxima and sums:
+//             o = (sum_local p v + (sum_prefix p v^D + sum_rest p v^D) Uv) / sum p.
+//           The prefix part has the same keys for every row of the group: it is a
+//           product of all members' queries with one set of keys, read once.
+//  scored   every token's attention weight, summed over the query heads of its KV
+//           head, is added to a running total.  A weight needs the row's final
+//           maximum and sum, so the scores are kept (4 bytes per query head and
+//           token) and turned into weights by the second kernel.
+//
+// Two kernels on the caller's stream, the second launched programmatically:
+//
+//  segments  The work is a line of stages, cut evenly among the CTAs.  A stage is
+//            8 KB of keys and 8 KB of values: 64 lines of 128 bytes each, whatever
+//            the type and width.  A unit is a run of stages with the same rows:
+//              prefix unit   (group, KV head, up to R rows): the group's prefix;
+//                            rows are (member, head) pairs;
+//              private unit  (sequence, KV head, up to R rows): the ring, then the
+//                            pages behind the prefix.
+//            A CTA's cut of a unit leaves one partial result (m, l, acc) per row and
+//            key warp.  Units are laid end to end, so unit u's cut by CTA k has the
+//            slot u + k, and the joining kernel finds a unit's cuts by arithmetic.
+//            Every CTA builds the same tables from the lengths and groups.  One warp
+//            fills a ring of shared-memory slots by TMA; four warps consume them,
+//            RW of them on different rows and 4 / RW on different keys of a stage.
+//  join      per (sequence, KV head): the partial results of each row are joined by
+//            log-sum-exp and the bottleneck sum is lifted once by Uv.  Scored: the
+//            kept scores become weights, p = 2^(s - m) / l, and are added.
+//
+// Bound: HBM for the rings, the private pages and the weights; a prefix that many
+// rows share is bound by its scores instead (R rows per byte of it).
+#include <cuda.h>
+
+#include "dar_common.cuh"
+#include "dar_launch.h"
+#include "dar_sm100.cuh"
+
+namespace dar {
+namespace seg {
+
+using namespace sm100;
+
+constexpr int kLines = 64;               // 128-byte lines of keys (and of values) in a stage
+constexpr int kHalf = kLines * 128;      // bytes of keys in a stage
+constexpr int kSlot = 2 * kHalf;
+constexpr int kStages = 4;
+constexpr int kWarps = 4;                // consumer warps
+constexpr int kThreads = (kWarps + 1) * 32;
+constexpr int kMaxCtas = 480;            // the workspace holds partial results of this many CTAs
+constexpr int kCostPrivate = 4;          // cost of a private stage
+
+constexpr int kRPW = 4;                  // rows a warp takes
+constexpr int kR = kWarps * kRPW;        // rows of a unit at most
+
+// Rows of a tile of nr rows go to RW warps; the other warps split the keys.
+__host__ __device__ inline int row_warps(int nr) { return nr <= kRPW ? 1 : nr <= 2 * kRPW ? 2 : 4; }
+// Cost of a prefix stage for nr rows, in quarters of a private stage.
+__host__ __device__ inline int prefix_cost(int nr) { return 3 + (nr + 15) / 16; }
+constexpr int kCostMax = 8;
+
+template <typename T>
+__host__ __device__ constexpr int ring_tokens() { return kHalf / (kHeadDim * (int)sizeof(T)); }
+template <typename T, int DD>
+__host__ __device__ constexpr int page_tokens() { return kHalf / (DD * (int)sizeof(T)); }
+
+// What the joining kernel has to know about the line of units.
+struct PlanHead {
+    int total, ctas;  // cost units on the line, CTAs that share it
+};
+struct PlanSeq {
+    int L;             // tokens
+    int start, stages; // its first private unit's place on the line; stages of each private unit
+    int xstart, xstages, xcost, xunit;  // its group's first prefix unit: place, stages, cost of one, index
+    int xrt;           // row tiles of the group (0: not in a group)
+    int row0;          // the sequence's first row among the group's rows of a KV head
+    int xrows;         // rows of the group per KV head
+    int pad[2];
+};
+
+struct Args {
+    const void *q;
+    void *out;
+    const int32_t *block_table, *seq_lens, *group, *prefix_pages;
+    int32_t *status;
+    const float *Uk, *Uv;
+    PlanHead *head;
+    PlanSeq *plan;
+    float *rec_p, *rec_x;  // partial results of private and prefix units
+    float *scores;         // [B][Hq][slots] scaled scores (log2), or nullptr
+    float *weights;        // [B][Hkv][slots], or nullptr
+    long long slots;
+    int B, Hq, Hkv, G, w, maxp, num_pages, ngroups;
+    int RP, RTP;  // rows of a private unit at most, row tiles of a (sequence, KV head)
+    float c2;     // scale * log2(e)
+    float decay;
+};
+
+template <int DD>
+__host__ __device__ constexpr int rec_p_floats() { return 4 + kHeadDim + DD; }
+template <int DD>
+__host__ __device__ constexpr int rec_x_floats() { return 4 + DD; }
+
+// The CTA that owns the stage at place p of the line: the last k with total * k / ctas <= p.
+__device__ __forceinline__ int owner(long long p, int total, int ctas)
+{
+    return (int)(((p + 1) * ctas - 1) / total);
+}
+
+// ------------------------------------------------------------------ tables
+
+struct Tables {  // in shared memory; B or ngroups entries each
+    int *L, *grp, *rank, *start, *members;
+    int *gP, *gcnt, *gmoff, *gxst, *gxu;
+    int *tot;  // [0] cost of the prefix units, [1] of all
+};
+
+__host__ __device__ inline int table_ints(int B, int ngroups) { return 5 * B + 5 * ngroups + 4; }
+
+__device__ __forceinline__ Tables table_ptrs(int *p, int B, int ng)
+{
+    Tables t;
+    t.L = p;
+    t.grp = t.L + B;
+    t.rank = t.grp + B;
+    t.start = t.rank + B;
+    t.members = t.start + B;
+    t.gP = t.members + B;
+    t.gcnt = t.gP + ng;
+    t.gmoff = t.gcnt + ng;
+    t.gxst = t.gmoff + ng;
+    t.gxu = t.gxst + ng;
+    t.tot = t.gxu + ng;
+    return t;
+}
+
+__device__ __forceinline__ int distant(int L, int w) { return L > w ? L - w : 0; }
+
+template <typename T, int DD>
+__device__ __forceinline__ int private_stages(int L, int w, int P)
+{
+    constexpr int TW = ring_tokens<T>(), TP = page_tokens<T, DD>();
+    const int nwin = min(L, w);
+    return (nwin + TW - 1) / TW + (L - nwin - P * kPage + TP - 1) / TP;
+}
+template <typename T, int DD>
+__device__ __forceinline__ int prefix_stages(int P)
+{
+    constexpr int TP = page_tokens<T, DD>();
+    return (P * kPage + TP - 1) / TP;
+}
+
+// Exclusive sums of a[0..n) in place by one warp; returns the total.
+__device__ __forceinline__ int warp_scan(int *a, int n, int lane)
+{
+    int run = 0;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const int v = i0 + lane < n ? a[i0 + lane] : 0;
+        int x = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o)
+                x += y;
+        }
+        if (i0 + lane < n)
+            a[i0 + lane] = run + x - v;
+        run += __shfl_sync(0xffffffffu, x, 31);
+    }
+    __syncwarp();
+    return run;
+}
+
+// The tables of the line of units, the same in every CTA.  A sequence belongs to its group if all
+// of the group's shared pages are distant for it; a group of one is none.
+template <typename T, int DD>
+__device__ void build_tables(const Args &a, const Tables &t, bool first_cta)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ng = a.ngroups;
+    for (int i = tid; i < ng; i += kThreads) {
+        int P = a.prefix_pages[i];
+        if (P < 0 || P > a.maxp) {
+            if (first_cta)
+                report(a.status, DAR_ERR_CAPACITY);
+            P = 0;
+        }
+        t.gP[i] = P;
+        t.gcnt[i] = 0;
+    }
+    for (int b = tid; b < a.B; b += kThreads) {
+        int L = a.seq_lens[b];
+        if (L < 0 || (long long)L > (long long)a.maxp * kPage + a.w) {
+            if (first_cta)
+                report(a.status, DAR_ERR_CAPACITY);
+            L = 0;
+        }
+        int g = ng ? a.group[b] : -1;
+        if (g < -1 || g >= ng) {
+            if (first_cta)
+                report(a.status, DAR_ERR_INVALID_ARG);
+            g = -1;
+        }
+        t.L[b] = L;
+        t.grp[b] = g;
+    }
+    __syncthreads();
+    if (ng) {
+        for (int b = tid; b < a.B; b += kThreads) {
+            const int g = t.grp[b];
+            if (g >= 0 && (t.gP[g] == 0 || distant(t.L[b], a.w) < t.gP[g] * kPage))
+                t.grp[b] = -1;
+        }
+        __syncthreads();
+        if (warp == 0) {  // members are numbered in the order of their sequences
+            for (int b0 = 0; b0 < a.B; b0 += 32) {
+                const int b = b0 + lane;
+                const int g = b < a.B ? t.grp[b] : -1;
+                const unsigned same = __match_any_sync(0xffffffffu, g);
+                const int before = __popc(same & ((1u << lane) - 1u));
+                const int base = g >= 0 ? t.gcnt[g] : 0;
+                __syncwarp();
+                if (g >= 0) {
+                    t.rank[b] = base + before;
+                    if (before == 0)
+                        t.gcnt[g] = base + __popc(same);
+                }
+                __syncwarp();
+            }
+        }
+        __syncthreads();
+    }
+    for (int b = tid; b < a.B; b += kThreads) {
+        int g = t.grp[b];
+        if (g >= 0 && t.gcnt[g] < 2)
+            t.grp[b] = g = -1;
+        t.start[b] = a.Hkv * a.RTP * kCostPrivate * private_stages<T, DD>(t.L[b], a.w, g >= 0 ? t.gP[g] : 0);
+    }
+    for (int i = tid; i < ng; i += kThreads) {
+        const int cnt = t.gcnt[i] < 2 ? 0 : t.gcnt[i];
+        const int rows = cnt * a.G, rt = (rows + kR - 1) / kR;
+        t.gmoff[i] = cnt;
+        t.gxu[i] = a.Hkv * rt;
+        t.gxst[i] = cnt ? a.Hkv * rt * prefix_cost(min(rows, kR)) * prefix_stages<T, DD>(t.gP[i]) : 0;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        const int s = warp_scan(t.start, a.B, lane);
+        if (lane == 0)
+            t.tot[1] = s;
+    } else if (warp == 1) {
+        warp_scan(t.gmoff, ng, lane);
+        warp_scan(t.gxu, ng, lane);
+        const int s = warp_scan(t.gxst, ng, lane);
+        if (lane == 0)
+            t.tot[0] = s;
+    }
+    __syncthreads();
+    for (int b = tid; b < a.B; b += kThreads) {
+        const int g = t.grp[b];
+        if (g >= 0)
+            t.members[t.gmoff[g] + t.rank[b]] = b;
+        t.start[b] += t.tot[0];
+    }
+    __syncthreads();
+}
+
+// A CTA's cut of a unit.
+struct Cut {
+    int b;            // sequence whose block table is read
+    int g;            // KV head
+    int grp;          // group of a prefix unit, or -1
+    int rt;           // row tile
+    int rows;         // rows of this tile
+    int RW;           // warps on different rows (the others split the keys)
+    int slot;         // slot of the partial results
+    int st0, st1;     // stages [st0, st1) of the unit
+    int nwin;         // ring tokens (0 in a prefix unit)
+    int tok0, tok1;   // distant tokens [tok0, tok1) of the whole unit
+    int nsw;          // ring stages of the whole unit
+};
+
+// The cut that begins at place p of the line; *next = where the unit ends.  False when the rest of
+// the unit holds no stage that starts at or after p.
+template <typename T, int DD>
+__device__ bool find_cut(const Args &a, const Tables &t, int p, int hi, int cta, Cut &c, int &next)
+{
+    int start, cost, nst, unit;
+    if (p < t.tot[0]) {
+        int lo = 0, up = a.ngroups - 1;  // the last group that starts at or before p (empty ones share a start)
+        while (lo < up) {
+            const int mid = (lo + up + 1) >> 1;
+            if (t.gxst[mid] <= p)
+                lo = mid;
+            else
+                up = mid - 1;
+        }
+        const int i = lo, rows = t.gcnt[i] * a.G, rts = (rows + kR - 1) / kR;
+        cost = prefix_cost(min(rows, kR));
+        nst = prefix_stages<T, DD>(t.gP[i]);
+        const int u = (p - t.gxst[i]) / (nst * cost);
+        start = t.gxst[i] + u * nst * cost;
+        unit = t.gxu[i] + u;
+        c.grp = i;
+        c.g = u / rts;
+        c.rt = u % rts;
+        c.rows = min(kR, rows - c.rt * kR);
+        c.RW = row_warps(c.rows);
+        c.b = t.members[t.gmoff[i]];
+        c.nwin = c.nsw = 0;
+        c.tok0 = 0;
+        c.tok1 = t.gP[i] * kPage;
+    } else {
+        int lo = 0, up = a.B - 1;
+        while (lo < up) {
+            const int mid = (lo + up + 1) >> 1;
+            if (t.start[mid] <= p)
+                lo = mid;
+            else
+                up = mid - 1;
+        }
+        const int b = lo, P = t.grp[b] >= 0 ? t.gP[t.grp[b]] : 0;
+        cost = kCostPrivate;
+        nst = private_stages<T, DD>(t.L[b], a.w, P);
+        const int u = (p - t.start[b]) / (nst * cost);
+        start = t.start[b] + u * nst * cost;
+        unit = b * a.Hkv * a.RTP + u;
+        c.grp = -1;
+        c.b = b;
+        c.g = u / a.RTP;
+        c.rt = u % a.RTP;
+        c.rows = min(a.RP, a.G - c.rt * kR);
+        c.RW = row_warps(a.RP);
+        c.nwin = min(t.L[b], a.w);
+        c.nsw = (c.nwin + ring_tokens<T>() - 1) / ring_tokens<T>();
+        c.tok0 = P * kPage;
+        c.tok1 = t.L[b] - c.nwin;
+    }
+    c.slot = unit + cta;
+    next = start + nst * cost;
+    c.st0 = (p - start + cost - 1) / cost;
+    c.st1 = min(nst, (hi - start + cost - 1) / cost);
+    return c.st0 < c.st1;
+}
+
+// Query row `row` of a cut: its (sequence, head).
+__device__ __forceinline__ void row_of(const Args &a, const Tables &t, const Cut &c, int row, int &b, int &h)
+{
+    if (c.grp < 0) {
+        b = c.b;
+        h = c.g * a.G + c.rt * kR + row;
+    } else {
+        const int i = c.rt * kR + row;
+        b = t.members[t.gmoff[c.grp] + i / a.G];
+        h = c.g * a.G + i % a.G;
+    }
+}
+
+// Byte of a tile whose 128-byte lines are swizzled in 16-byte chunks.
+__device__ __forceinline__ int swz(int byte)
+{
+    return byte ^ (((byte >> 7) & 7) << 4);
+}
+
+__device__ __forceinline__ void load8(const unsigned char *tile, int byte, float (&x)[8], float)
+{
+    const float4 u = *reinterpret_cast<const float4 *>(tile + swz(byte));
+    const float4 v = *reinterpret_cast<const float4 *>(tile + swz(byte + 16));
+    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
+}
+__device__ __forceinline__ void load8(const unsigned char *tile, int byte, float (&x)[8], bf16)
+{
+    unpack(*reinterpret_cast<const uint4 *>(tile + swz(byte)), x, bf16());
+}
+
+// Running softmax of a warp's rows over the tokens of its lanes: ROW / 8 lanes share a token, each
+// with 8 of its entries; every group of lanes has its own maximum and sum until finish().
+template <int ROW>
+struct Running {
+    static constexpr int LPT = ROW / 8, TPI = 32 / LPT;
+    float m[kRPW], l[kRPW], acc[kRPW][8];
+    __device__ void clear()
+    {
+#pragma unroll
+        for (int r = 0; r < kRPW; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                acc[r][e] = 0.f;
+        }
+    }
+    __device__ void finish()
+    {
+#pragma unroll
+        for (int off = LPT; off < 32; off <<= 1)
+#pragma unroll
+            for (int r = 0; r < kRPW; ++r) {
+                const float mo = __shfl_xor_sync(0xffffffffu, m[r], off);
+                const float lo = __shfl_xor_sync(0xffffffffu, l[r], off);
+                const float mn = fmaxf(m[r], mo);
+                const float fa = mn == -INFINITY ? 1.f : exp2f(m[r] - mn), fb = mn == -INFINITY ? 1.f : exp2f(mo - mn);
+                l[r] = l[r] * fa + lo * fb;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    acc[r][e] = acc[r][e] * fa + __shfl_xor_sync(0xffffffffu, acc[r][e], off) * fb;
+                m[r] = mn;
+            }
+    }
+};
+
+// ntok tokens of a stage; this warp takes those of its key share (kw of kws).  score(r, tok, s): what
+// becomes of the scaled score of a valid token.
+template <typename T, int ROW, typename Score>
+__device__ __forceinline__ void lane_stage(const unsigned char *tile, int ntok, int kw, int kws,
+                                           const float (&q)[kRPW][8], float c2, Running<ROW> &s, int lane, Score score)
+{
+    constexpr int LPT = Running<ROW>::LPT, TPI = Running<ROW>::TPI;
+    const int grp = lane / LPT, sub = lane % LPT;
+    for (int t0 = kw * TPI; t0 < ntok; t0 += kws * TPI) {
+        const int t = t0 + grp;
+        const bool valid = t < ntok;
+        const int byte = (t * ROW + sub * 8) * (int)sizeof(T);
+        float k[8], v[8];
+        load8(tile, byte, k, T());
+        load8(tile + kHalf, byte, v, T());
+        float x[kRPW];
+#pragma unroll
+        for (int r = 0; r < kRPW; ++r) {
+            x[r] = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                x[r] = fmaf(q[r][e], k[e], x[r]);
+        }
+#pragma unroll
+        for (int off = 1; off < LPT; off <<= 1)
+#pragma unroll
+            for (int r = 0; r < kRPW; ++r)
+                x[r] += __shfl_xor_sync(0xffffffffu, x[r], off);
+        if (!valid) {  // whatever the slot holds there must not reach a sum
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e] = 0.f;
+        }
+#pragma unroll
+        for (int r = 0; r < kRPW; ++r) {
+            const float y = valid ? x[r] * c2 : -INFINITY;
+            if (valid && sub == 0)
+                score(r, t, y);
+            const float mn = fmaxf(s.m[r], y);
+            const float base = mn == -INFINITY ? 0.f : mn;
+            const float f = exp2f(s.m[r] - base), p = exp2f(y - base);
+            s.m[r] = mn;
+            s.l[r] = s.l[r] * f + p;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                s.acc[r][e] = fmaf(p, v[e], s.acc[r][e] * f);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ segments
+
+__host__ __device__ constexpr int align1k(int x) { return (x + 1023) & ~1023; }
+// Shared memory: the slots (1024-byte aligned, as the swizzle wants), query rows, tables, barriers.
+constexpr int kQBytes = 2 * kR * kHeadDim * 4;
+inline size_t segments_smem(int B, int ngroups)
+{
+    return 1024 + (size_t)kStages * kSlot + kQBytes + (size_t)table_ints(B, ngroups) * 4 + 2 * kStages * 8 + 16;
+}
+
+template <typename T, int DD, bool SCORED>
+__global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constant__ CUtensorMap m_wk,
+                                                            const __grid_constant__ CUtensorMap m_wv,
+                                                            const __grid_constant__ CUtensorMap m_pk,
+                                                            const __grid_constant__ CUtensorMap m_pv, Args a)
+{
+    constexpr int TW = ring_tokens<T>(), TP = page_tokens<T, DD>();
+    constexpr int PL = kPage * DD * (int)sizeof(T) / 128;  // lines of a head's page
+    constexpr int BOX = PL < kLines ? PL : kLines;         // lines of one copy
+    constexpr int WL = kHeadDim * (int)sizeof(T) / 128;    // lines of a ring row
+    extern __shared__ unsigned char raw[];
+    unsigned char *slots = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    float *qs = reinterpret_cast<float *>(slots + kStages * kSlot);  // [kR][64] query rows
+    float *qt = qs + kR * kHeadDim;                                  // [kR][DD] absorbed rows
+    uint64_t *full = reinterpret_cast<uint64_t *>(qt + kR * kHeadDim);
+    uint64_t *empty = full + kStages;
+    int *ints = reinterpret_cast<int *>(empty + kStages);
+    volatile int *gave_up = ints;
+    const Tables t = table_ptrs(ints + 1, a.B, a.ngroups);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    if (tid == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], kWarps);
+        }
+        *gave_up = 0;
+        mbar_init_fence();
+    }
+    build_tables<T, DD>(a, t, blockIdx.x == 0);  // its barriers also publish the mbarriers
+    const int total = t.tot[0] + t.tot[1];
+    // a CTA's share holds a whole stage at least, so every CTA between a unit's first and last has one of it
+    const int ctas = max(1, min((int)gridDim.x, total / (t.tot[0] ? kCostMax : kCostPrivate)));
+    if (blockIdx.x == 0) {
+        if (tid == 0)
+            *a.head = PlanHead{total, ctas};
+        for (int b = tid; b < a.B; b += kThreads) {
+            PlanSeq s;
+            const int g = t.grp[b];
+            s.L = t.L[b];
+            s.start = t.start[b];
+            s.stages = private_stages<T, DD>(s.L, a.w, g >= 0 ? t.gP[g] : 0);
+            s.xrt = 0;
+            s.xstart = s.xstages = s.xcost = s.xunit = s.row0 = s.xrows = 0;
+            if (g >= 0) {
+                s.xrows = t.gcnt[g] * a.G;
+                s.xrt = (s.xrows + kR - 1) / kR;
+                s.xstart = t.gxst[g];
+                s.xstages = prefix_stages<T, DD>(t.gP[g]);
+                s.xcost = prefix_cost(min(s.xrows, kR));
+                s.xunit = t.gxu[g];
+                s.row0 = t.rank[b] * a.G;
+            }
+            a.plan[b] = s;
+        }
+    }
+    const int cta = blockIdx.x;
+    const int lo = cta < ctas ? (int)((long long)total * cta / ctas) : total;
+    const int hi = cta < ctas ? (int)((long long)total * (cta + 1) / ctas) : total;
+
+    if (warp == kWarps) {
+        // ---- one warp fills the slots
+        int n = 0;
+        bool alive = true;
+        for (int p = lo, next; alive && p < hi; p = next) {
+            Cut c;
+            if (!find_cut<T, DD>(a, t, p, hi, cta, c, next))
+                continue;
+            const int32_t *table = a.block_table + (size_t)c.b * a.maxp;
+            const int ring0 = (c.b * a.Hkv + c.g) * a.w;
+            int ids0 = -1, ids = -1;  // block-table entries ids0 .. ids0 + 31, one per lane
+            for (int st = c.st0; st < c.st1; ++st, ++n) {
+                const int s = n % kStages;
+                if (n >= kStages && !mbar_wait(&empty[s], (unsigned)((n / kStages - 1) & 1), gave_up)) {
+                    alive = false;
+                    break;
+                }
+                unsigned char *dst = slots + s * kSlot;
+                if (st < c.nsw) {
+                    if (lane == 0) {
+                        mbar_expect_tx(&full[s], kSlot);
+                        const int y = (ring0 + st * TW) * WL;
+                        tma_load_2d(dst, &m_wk, 0, y, &full[s]);
+                        tma_load_2d(dst + kHalf, &m_wv, 0, y, &full[s]);
+                    }
+                    continue;
+                }
+                const int tok = c.tok0 + (st - c.nsw) * TP;
+                const int end = min(c.tok1, tok + TP);
+                const int pg0 = tok / kPage, pg1 = (end + kPage - 1) / kPage;
+                if (ids0 < 0 || pg1 > ids0 + 32 || pg0 < ids0) {
+                    ids0 = pg0;
+                    ids = ids0 + lane < a.maxp ? __ldg(table + ids0 + lane) : -1;
+                }
+                unsigned bytes = 0;
+                for (int pg = pg0; pg < pg1; ++pg) {
+                    const int id = __shfl_sync(0xffffffffu, ids, pg - ids0);
+                    bytes += id >= 0 && id < a.num_pages ? 2u * BOX * 128u : 0u;
+                }
+                if (lane == 0)
+                    mbar_expect_tx(&full[s], bytes);
+                for (int pg = pg0; pg < pg1; ++pg) {
+                    const int id = __shfl_sync(0xffffffffu, ids, pg - ids0);
+                    if (lane != 0)
+                        continue;
+                    if (id < 0 || id >= a.num_pages) {
+                        report(a.status, DAR_ERR_CAPACITY);
+                        continue;
+                    }
+                    const int y = (id * a.Hkv + c.g) * PL + (tok % kPage) * PL / kPage;
+                    const int off = (pg - pg0) * BOX * 128;
+                    tma_load_2d(dst + off, &m_pk, 0, y, &full[s]);
+                    tma_load_2d(dst + kHalf + off, &m_pv, 0, y, &full[s]);
+                }
+            }
+        }
+        if (!alive) {
+            // a wait gave up: the copies in flight land (again a bounded wait) before the block leaves
+            if (lane == 0)
+                report(a.status, DAR_ERR_DEVICE);
+            for (int r = max(0, n - kStages); r < n; ++r)
+                mbar_wait(&full[r % kStages], (unsigned)((r / kStages) & 1), nullptr);
+        }
+        return;
+    }
+
+    // ---- four warps consume them
+    int n = 0;
+    bool alive = true;
+    for (int p = lo, next; p < hi; p = next) {
+        Cut c;
+        if (!find_cut<T, DD>(a, t, p, hi, cta, c, next))
+            continue;
+        // query rows of the cut, and q~ = q Uk^T
+        asm volatile("bar.sync 1, 128;" ::: "memory");  // the rows of the cut before are read
+        for (int i = tid; i < kR * kHeadDim; i += kWarps * 32) {
+            const int row = i / kHeadDim;
+            float x = 0.f;
+            if (row < c.rows) {
+                int b, h;
+                row_of(a, t, c, row, b, h);
+                x = to_f32(static_cast<const T *>(a.q)[((size_t)b * a.Hq + h) * kHeadDim + i % kHeadDim]);
+            }
+            qs[i] = x;
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        for (int i = tid; i < kR * DD; i += kWarps * 32) {
+            const int row = i / DD, e = i % DD;
+            const float4 *u = reinterpret_cast<const float4 *>(a.Uk + ((size_t)c.g * DD + e) * kHeadDim);
+            const float4 *x = reinterpret_cast<const float4 *>(qs + row * kHeadDim);
+            float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+            if (row < c.rows) {
+#pragma unroll
+                for (int k = 0; k < kHeadDim / 4; ++k) {
+                    const float4 uu = __ldg(u + k), xx = x[k];
+                    s0 = fmaf(uu.x, xx.x, s0);
+                    s1 = fmaf(uu.y, xx.y, s1);
+                    s2 = fmaf(uu.z, xx.z, s2);
+                    s3 = fmaf(uu.w, xx.w, s3);
+                }
+            }
+            qt[i] = (s0 + s1) + (s2 + s3);
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        const int RW = c.RW, KW = kWarps / RW, rw = warp % RW, kw = warp / RW;
+        const int r0 = rw * kRPW;
+        Running<kHeadDim> sl;
+        Running<DD> sd;
+        sl.clear();
+        sd.clear();
+        float ql[kRPW][8], qd[kRPW][8];
+#pragma unroll
+        for (int r = 0; r < kRPW; ++r)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                ql[r][e] = qs[(r0 + r) * kHeadDim + (lane % 8) * 8 + e];
+                qd[r][e] = qt[(r0 + r) * DD + (lane % (DD / 8)) * 8 + e];
+            }
+        float *srow = nullptr;  // scores of the warp's first row
+        if constexpr (SCORED)
+            srow = a.scores + ((size_t)c.b * a.Hq + c.g * a.G + c.rt * kR + r0) * a.slots;
+        const int L = c.tok1 + c.nwin;
+        for (int st = c.st0; st < c.st1; ++st, ++n) {
+            const int s = n % kStages;
+            // a warp that gave up computes nothing more, but still meets the others at the barriers
+            if (!alive || !mbar_wait(&full[s], (unsigned)((n / kStages) & 1), gave_up)) {
+                if (alive && lane == 0)
+                    report(a.status, DAR_ERR_DEVICE);
+                alive = false;
+                continue;
+            }
+            const unsigned char *tile = slots + s * kSlot;
+            if (st < c.nsw) {
+                const int t0 = st * TW;
+                lane_stage<T, kHeadDim>(tile, min(TW, c.nwin - t0), kw, KW, ql, a.c2, sl, lane,
+                                        [&](int r, int tok, float y) {
+                                            if constexpr (SCORED) {
+                                                // the position that a ring slot holds
+                                                const int slot = t0 + tok, pos = (L - 1) - ((L - 1 - slot) % a.w);
+                                                if (r0 + r < c.rows)
+                                                    srow[(size_t)r * a.slots + pos] = y;
+                                            }
+                                        });
+            } else {
+                const int t0 = c.tok0 + (st - c.nsw) * TP;
+                lane_stage<T, DD>(tile, min(TP, c.tok1 - t0), kw, KW, qd, a.c2, sd, lane,
+                                  [&](int r, int tok, float y) {
+                                      if constexpr (SCORED) {
+                                          if (r0 + r < c.rows)
+                                              srow[(size_t)r * a.slots + t0 + tok] = y;
+                                      }
+                                  });
+            }
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(&empty[s]);
+        }
+        sl.finish();
+        sd.finish();
+#pragma unroll
+        for (int r = 0; r < kRPW; ++r) {
+            if (r0 + r >= c.rows)
+                continue;
+            const float m = fmaxf(sl.m[r], sd.m[r]);
+            const float base = m == -INFINITY ? 0.f : m;
+            const float fl = exp2f(sl.m[r] - base), fd = exp2f(sd.m[r] - base);
+            float *rec;
+            if (c.grp < 0) {
+                rec = a.rec_p + ((size_t)c.slot * (KW * a.RP) + kw * a.RP + r0 + r) * rec_p_floats<DD>();
+                if (lane < 8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        rec[4 + lane * 8 + e] = sl.acc[r][e] * fl;
+                if (lane < DD / 8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        rec[4 + kHeadDim + lane * 8 + e] = sd.acc[r][e] * fd;
+            } else {
+                rec = a.rec_x + ((size_t)c.slot * kR + kw * (RW * kRPW) + r0 + r) * rec_x_floats<DD>();
+                if (lane < DD / 8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        rec[4 + lane * 8 + e] = sd.acc[r][e] * fd;
+            }
+            if (lane == 0) {
+                rec[0] = m;
+                rec[1] = sl.l[r] * fl + sd.l[r] * fd;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ join
+
+// Where the partial results of a row are: n runs of `stride` floats from `base`.
+struct RecRun {
+    const float *base;
+    int n, stride;
+};
+
+template <int DD>
+__device__ __forceinline__ RecRun private_run(const Args &a, const PlanHead &hd, const PlanSeq &s, int b, int g, int j)
+{
+    RecRun r{nullptr, 0, 0};
+    if (s.stages == 0)
+        return r;
+    const int rt = j / kR, row = j % kR, KW = kWarps / row_warps(a.RP);
+    const int u = g * a.RTP + rt;
+    const long long p0 = s.start + (long long)u * s.stages * kCostPrivate;
+    const int k0 = owner(p0, hd.total, hd.ctas), k1 = owner(p0 + (s.stages - 1) * kCostPrivate, hd.total, hd.ctas);
+    const size_t slot = (size_t)b * a.Hkv * a.RTP + u + k0;
+    r.stride = a.RP * rec_p_floats<DD>();
+    r.base = a.rec_p + (slot * (KW * a.RP) + row) * rec_p_floats<DD>();
+    r.n = (k1 - k0 + 1) * KW;
+    return r;
+}
+
+template <int DD>
+__device__ __forceinline__ int prefix_runs(const Args &a, const PlanHead &hd, const PlanSeq &s, int g, int j, int &kws,
+                                           const float *&base)
+{
+    if (s.xrt == 0)
+        return 0;
+    const int i = s.row0 + j, rt = i / kR, row = i % kR, rows = min(kR, s.xrows - rt * kR), RW = row_warps(rows);
+    const int u = g * s.xrt + rt;
+    const long long p0 = s.xstart + (long long)u * s.xstages * s.xcost;
+    const int k0 = owner(p0, hd.total, hd.ctas), k1 = owner(p0 + (s.xstages - 1) * s.xcost, hd.total, hd.ctas);
+    kws = kWarps / RW;
+    base = a.rec_x + ((size_t)(s.xunit + u + k0) * kR + row) * rec_x_floats<DD>();
+    return k1 - k0 + 1;
+}
+
+constexpr int kJoinThreads = 128;
+constexpr int kJoinTokens = 2048;  // tokens whose weights a block updates
+
+// Block (b * Hkv + g, chunk): the rows of a (sequence, KV head); chunk 0 writes their outputs, and
+// every chunk the weights of its tokens.
+template <typename T, int DD, bool SCORED>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a)
+{
+    extern __shared__ float stat[];  // SCORED: [G][2] m and 1 / l
+    grid_dep_wait();
+    const int bg = blockIdx.x, b = bg / a.Hkv, g = bg % a.Hkv, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const PlanSeq s = a.plan[b];
+    const PlanHead hd = *a.head;
+    const int chunk = blockIdx.y;
+    if (chunk > 0 && (long long)chunk * kJoinTokens >= s.L)
+        return;
+    for (int j = warp; j < a.G; j += kJoinThreads / 32) {
+        const size_t row = (size_t)b * a.Hq + g * a.G + j;
+        T *o = static_cast<T *>(a.out) + row * kHeadDim;
+        if (s.L == 0) {
+            if (chunk == 0) {
+                o[lane] = from_f32<T>(0.f);
+                o[lane + 32] = from_f32<T>(0.f);
+            }
+            continue;
+        }
+        const RecRun pr = private_run<DD>(a, hd, s, b, g, j);
+        int kws = 1;
+        const float *xb = nullptr;
+        const int xn = prefix_runs<DD>(a, hd, s, g, j, kws, xb);
+        const int xrow = kR / kws * rec_x_floats<DD>();  // from one key warp's row to the next one's
+        float m = -INFINITY;
+        for (int i = lane; i < pr.n; i += 32)
+            m = fmaxf(m, pr.base[(size_t)i * pr.stride]);
+        for (int i = lane; i < xn * kws; i += 32)
+            m = fmaxf(m, xb[(size_t)(i / kws) * kR * rec_x_floats<DD>() + (size_t)(i % kws) * xrow]);
+#pragma unroll
+        for (int off = 16; off; off >>= 1)
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+        const float base = m == -INFINITY ? 0.f : m;
+        float l = 0.f;
+        for (int i = lane; i < pr.n; i += 32)
+            l += pr.base[(size_t)i * pr.stride + 1] * exp2f(pr.base[(size_t)i * pr.stride] - base);
+        for (int i = lane; i < xn * kws; i += 32) {
+            const float *r = xb + (size_t)(i / kws) * kR * rec_x_floats<DD>() + (size_t)(i % kws) * xrow;
+            l += r[1] * exp2f(r[0] - base);
+        }
+#pragma unroll
+        for (int off = 16; off; off >>= 1)
+            l += __shfl_xor_sync(0xffffffffu, l, off);
+        if constexpr (SCORED) {
+            if (lane == 0) {
+                stat[2 * j] = base;
+                stat[2 * j + 1] = 1.f / l;
+            }
+        }
+        if (chunk > 0)
+            continue;
+        float o0 = 0.f, o1 = 0.f, d0 = 0.f, d1 = 0.f;  // entries lane, lane + 32 of both sums
+        for (int i = 0; i < pr.n; ++i) {
+            const float *r = pr.base + (size_t)i * pr.stride;
+            const float f = exp2f(r[0] - base);
+            o0 = fmaf(f, r[4 + lane], o0);
+            o1 = fmaf(f, r[36 + lane], o1);
+            if (lane < DD)
+                d0 = fmaf(f, r[4 + kHeadDim + lane], d0);
+            if (DD > 32)
+                d1 = fmaf(f, r[4 + kHeadDim + 32 + lane], d1);
+        }
+        for (int i = 0; i < xn * kws; ++i) {
+            const float *r = xb + (size_t)(i / kws) * kR * rec_x_floats<DD>() + (size_t)(i % kws) * xrow;
+            const float f = exp2f(r[0] - base);
+            if (lane < DD)
+                d0 = fmaf(f, r[4 + lane], d0);
+            if (DD > 32)
+                d1 = fmaf(f, r[4 + 32 + lane], d1);
+        }
+        const float *Uv = a.Uv + (size_t)g * DD * kHeadDim;
+#pragma unroll
+        for (int e = 0; e < DD; ++e) {
+            const float x = __shfl_sync(0xffffffffu, e < 32 ? d0 : d1, e & 31);
+            o0 = fmaf(x, __ldg(Uv + e * kHeadDim + lane), o0);
+            o1 = fmaf(x, __ldg(Uv + e * kHeadDim + lane + 32), o1);
+        }
+        o[lane] = from_f32<T>(o0 / l);
+        o[lane + 32] = from_f32<T>(o1 / l);
+    }
+    if constexpr (SCORED) {
+        __syncthreads();
+        float *w = a.weights + (size_t)bg * a.slots;
+        const float *x = a.scores + ((size_t)b * a.Hq + (size_t)g * a.G) * a.slots;
+        const int t1 = (int)min((long long)s.L, (long long)(chunk + 1) * kJoinTokens);
+        for (int t = chunk * kJoinTokens + threadIdx.x; t < t1; t += kJoinThreads) {
+            float p = 0.f;
+            for (int j = 0; j < a.G; ++j)
+                p += exp2f(x[(size_t)j * a.slots + t] - stat[2 * j]) * stat[2 * j + 1];
+            w[t] = a.decay != 0.f ? fmaf(a.decay, w[t], p) : p;
+        }
+    }
+}
+
+// ------------------------------------------------------------------ launch
+
+struct Layout {
+    size_t head, plan, rec_p, rec_x, scores, total;
+    int RP, RTP;
+};
+
+static size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
+
+static Layout layout(int B, int Hq, int Hkv, int dd, int w, int maxp, bool scored)
+{
+    Layout y;
+    const int G = Hq / Hkv;
+    y.RP = G < kR ? G : kR;
+    y.RTP = (G + kR - 1) / kR;
+    const size_t units = (size_t)B * Hkv * y.RTP + kMaxCtas;
+    const size_t rows_p = (size_t)(kWarps / row_warps(y.RP)) * y.RP;
+    // a group of n rows has ceil(n / R) tiles, and there are at most B / 2 groups of two or more
+    const size_t units_x = (size_t)Hkv * ((size_t)B * G / kR + B / 2 + 1) + kMaxCtas;
+    const size_t slots = (size_t)maxp * kPage + w;
+    y.head = 0;
+    y.plan = 256;
+    y.rec_p = y.plan + up256((size_t)B * sizeof(PlanSeq));
+    y.rec_x = y.rec_p + up256(units * rows_p * (4 + kHeadDim + dd) * sizeof(float));
+    y.scores = y.rec_x + (scored ? 0 : up256(units_x * kR * (4 + dd) * sizeof(float)));
+    y.total = y.scores + (scored ? up256((size_t)B * Hq * slots * sizeof(float)) : 0);
+    return y;
+}
+
+template <typename T, int DD, bool SCORED>
+static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t st)
+{
+    const Layout y = layout(s.B, s.Hq, s.Hkv, DD, s.w, s.maxp, SCORED);
+    char *ws = static_cast<char *>(workspace);
+    Args a;
+    a.q = s.q;
+    a.out = s.out;
+    a.block_table = s.block_table;
+    a.seq_lens = s.seq_lens;
+    a.group = s.group;
+    a.prefix_pages = s.prefix_pages;
+    a.status = s.status;
+    a.Uk = s.Uk;
+    a.Uv = s.Uv;
+    a.head = reinterpret_cast<PlanHead *>(ws + y.head);
+    a.plan = reinterpret_cast<PlanSeq *>(ws + y.plan);
+    a.rec_p = reinterpret_cast<float *>(ws + y.rec_p);
+    a.rec_x = reinterpret_cast<float *>(ws + y.rec_x);
+    a.scores = SCORED ? reinterpret_cast<float *>(ws + y.scores) : nullptr;
+    a.weights = s.weights;
+    a.slots = (long long)s.maxp * kPage + s.w;
+    a.B = s.B;
+    a.Hq = s.Hq;
+    a.Hkv = s.Hkv;
+    a.G = s.Hq / s.Hkv;
+    a.w = s.w;
+    a.maxp = s.maxp;
+    a.num_pages = s.num_pages;
+    a.ngroups = s.n_groups;
+    a.RP = y.RP;
+    a.RTP = y.RTP;
+    a.c2 = s.c2;
+    a.decay = s.decay;
+    constexpr int PL = kPage * DD * (int)sizeof(T) / 128;
+    const unsigned long long ring_lines = (unsigned long long)s.B * s.Hkv * s.w * kHeadDim * sizeof(T) / 128;
+    const unsigned long long pool_lines = (unsigned long long)(s.num_pages > 0 ? s.num_pages : 1) * s.Hkv * PL;
+    const int box = PL < kLines ? PL : kLines;
+    // 128-byte lines whatever the type: 64 two-byte elements each
+    CUtensorMap wk, wv, pk{}, pv{};
+    if (!make_tma_2d_bf16(&wk, s.win_k, ring_lines, 64, kLines) || !make_tma_2d_bf16(&wv, s.win_v, ring_lines, 64, kLines))
+        return cudaErrorInvalidValue;
+    if (s.maxp > 0 && (!make_tma_2d_bf16(&pk, s.pool_kd, pool_lines, 64, box) ||
+                       !make_tma_2d_bf16(&pv, s.pool_vd, pool_lines, 64, box)))
+        return cudaErrorInvalidValue;
+    auto kern = segments_kernel<T, DD, SCORED>;
+    static PerDeviceOnce once;
+    int sms = 0;
+    cudaError_t e = per_device_once(
+        once,
+        [&](int dev) {
+            cudaError_t e2 = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                  (int)segments_smem(DAR_DECODE_MAX_BATCH, DAR_DECODE_MAX_BATCH));
+            int n = 0;
+            if (e2 == cudaSuccess)
+                e2 = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+            once.value[dev] = n;
+            return e2;
+        },
+        &sms);
+    if (e != cudaSuccess)
+        return e;
+    const int grid = 2 * sms < kMaxCtas ? 2 * sms : kMaxCtas;
+    kern<<<grid, kThreads, segments_smem(s.B, s.n_groups), st>>>(wk, wv, pk, pv, a);
+    e = cudaGetLastError();
+    if (e != cudaSuccess)
+        return e;
+    cudaLaunchAttribute pdl[1];
+    pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    pdl[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.stream = st;
+    cfg.attrs = pdl;
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3(s.B * s.Hkv, SCORED ? (unsigned)((a.slots + kJoinTokens - 1) / kJoinTokens) : 1u);
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.dynamicSmemBytes = SCORED ? a.G * 2 * sizeof(float) : 0;
+    return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, SCORED>, a);
+}
+
+template <typename T, bool SCORED>
+static cudaError_t launch_dd(int dd, const SegmentArgs &s, void *ws, cudaStream_t st)
+{
+    switch (dd) {
+    case 8: return launch_t<T, 8, SCORED>(s, ws, st);
+    case 16: return launch_t<T, 16, SCORED>(s, ws, st);
+    case 32: return launch_t<T, 32, SCORED>(s, ws, st);
+    case 64: return launch_t<T, 64, SCORED>(s, ws, st);
+    default: return cudaErrorInvalidValue;
+    }
+}
+
+}  // namespace seg
+
+size_t segments_workspace_bytes(int B, int Hq, int Hkv, int dd, int w, int maxp, bool scored)
+{
+    return seg::layout(B, Hq, Hkv, dd, w, maxp, scored).total;
+}
+
+// Upper bound of the line's length: every sequence at capacity, as private units and once more as
+// prefix units.
+double segments_line_bound(dar_dtype dt, int B, int Hq, int Hkv, int dd, int w, int maxp)
+{
+    const int es = dt == DAR_F32 ? 4 : 2, G = Hq / Hkv;
+    const double stages = (double)w * kHeadDim * es / seg::kHalf + (double)maxp * kPage * dd * es / seg::kHalf + 2;
+    return (double)B * Hkv * ((G + seg::kR - 1) / seg::kR) * stages * (seg::kCostPrivate + seg::kCostMax);
+}
+
+cudaError_t launch_segments(dar_dtype dt, int dd, const SegmentArgs &s, void *workspace, cudaStream_t st)
+{
+    if (s.B == 0)
+        return cudaSuccess;
+    if (s.weights)
+        return dt == DAR_F32 ? seg::launch_dd<float, true>(dd, s, workspace, st)
+                             : seg::launch_dd<bf16, true>(dd, s, workspace, st);
+    return dt == DAR_F32 ? seg::launch_dd<float, false>(dd, s, workspace, st)
+                         : seg::launch_dd<bf16, false>(dd, s, workspace, st);
+}
+
+}  // namespace dar

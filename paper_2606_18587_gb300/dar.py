@@ -75,6 +75,12 @@ def load_library(path: str = LIB_PATH):
         "dar_attn_decode": ([CP, I32, P, P, P, F, P, P, SZ, P], ctypes.c_int),
         "dar_attn_decode_noalloc": ([CP, I32, P, P, P, F, P, P], ctypes.c_int),
         "dar_decode_step": ([CP, P, P, I32, P, P, P, I32, P, P, P, F, P, P, SZ, P], ctypes.c_int),
+        "dar_decode_shared_workspace_bytes": ([CP, I32], SZ),
+        "dar_attn_decode_shared": ([CP, I32, P, P, P, P, I32, P, F, P, P, SZ, P], ctypes.c_int),
+        "dar_decode_scored_workspace_bytes": ([CP, I32], SZ),
+        "dar_attn_decode_scored": ([CP, I32, P, P, P, F, P, F, P, P, SZ, P], ctypes.c_int),
+        "dar_cache_evict_workspace_bytes": ([CP], SZ),
+        "dar_cache_evict": ([CP, P, P, P, P, SZ, P], ctypes.c_int),
         "dar_check_bounded_wait": ([P, ctypes.c_uint32, P], ctypes.c_int),
         "dar_prefill_workspace_bytes": ([ctypes.c_int, I32, I32, I32, I32], SZ),
         "dar_prefill_chunk_workspace_bytes": ([CP, I32], SZ),
@@ -288,6 +294,111 @@ def dar_attn_decode_noalloc(cache: DarCache, q, Uk, Uv, scale=0.0, out=None, str
     _check(load_library().dar_attn_decode_noalloc(cache.struct, q.shape[1], _ptr(q), _ptr(Uk), _ptr(Uv),
                                                   float(scale), _ptr(out), _stream(stream)))
     return out
+
+
+# --------------------------------------------------------------------------- shared prefixes, weights, eviction
+
+def _operand(t, name, dtype, shape, cache):
+    """A contiguous tensor on the cache's device, of this dtype and shape (None: any)."""
+    _dev(t, name, dtype)
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.device != cache.win_k.device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {cache.win_k.device}")
+
+
+def _on_current_device(cache):
+    """Kernels are launched on the current device's stream: the cache has to be there."""
+    if cache.win_k.device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {cache.win_k.device}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+
+
+def _step_operands(cache, q, Uk, Uv, workspace, out):
+    """Checks of a decode step's operands; returns (Hq, out)."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a tensor [B, Hq, d]")
+    Hq = q.shape[1]
+    _on_current_device(cache)
+    _operand(q, "q", cache.dtype, (cache.B, Hq, cache.d), cache)
+    for name, t in (("Uk", Uk), ("Uv", Uv)):
+        _operand(t, name, torch.float32, (cache.Hkv, cache.d_down, cache.d), cache)
+    _operand(workspace, "workspace", None, None, cache)
+    if out is None:
+        out = torch.empty_like(q)
+    _operand(out, "out", cache.dtype, q.shape, cache)
+    return Hq, out
+
+
+def _new_workspace(cache, nbytes):
+    if nbytes == 0 and cache.B > 0:
+        raise DarError(DAR_ERR_INVALID_ARG, dar_last_error() or "bad cache/Hq")
+    return torch.empty(max(1, nbytes), dtype=torch.uint8, device=cache.win_k.device)
+
+
+def shared_decode_workspace(cache: DarCache, Hq: int):
+    """A workspace of the size dar_attn_decode_shared needs (no initialisation needed)."""
+    return _new_workspace(cache, int(load_library().dar_decode_shared_workspace_bytes(cache.struct, Hq)))
+
+
+def dar_attn_decode_shared(cache: DarCache, q, Uk, Uv, group, prefix_pages, workspace, scale=0.0, out=None,
+                           stream=None):
+    """One decode step for sequences that share their first pages in groups: sequence b belongs to
+    ``group[b]`` (int32 ``[B]``, -1 = none), whose members share their first ``prefix_pages[group[b]]`` pages
+    (int32 ``[n_groups]``).  Results as :func:`dar_attn_decode`; the shared pages are read once per group."""
+    Hq, out = _step_operands(cache, q, Uk, Uv, workspace, out)
+    _operand(group, "group", torch.int32, (cache.B,), cache)
+    _operand(prefix_pages, "prefix_pages", torch.int32, (prefix_pages.numel(),), cache)
+    _check(load_library().dar_attn_decode_shared(
+        cache.struct, Hq, _ptr(q), _ptr(Uk), _ptr(Uv), _ptr(group), prefix_pages.numel(), _ptr(prefix_pages),
+        float(scale), _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
+
+
+def attention_weights(cache: DarCache):
+    """Zeroed totals for dar_attn_decode_scored and dar_cache_evict: one per sequence, KV head and position."""
+    return torch.zeros((cache.B, cache.Hkv, cache.max_pages_per_seq * PAGE_SIZE + cache.w), dtype=torch.float32,
+                       device=cache.win_k.device)
+
+
+def scored_decode_workspace(cache: DarCache, Hq: int):
+    """A workspace of the size dar_attn_decode_scored needs (no initialisation needed)."""
+    return _new_workspace(cache, int(load_library().dar_decode_scored_workspace_bytes(cache.struct, Hq)))
+
+
+def _totals(cache, weights):
+    _operand(weights, "weights", torch.float32, (cache.B, cache.Hkv, cache.max_pages_per_seq * PAGE_SIZE + cache.w),
+             cache)
+
+
+def dar_attn_decode_scored(cache: DarCache, q, Uk, Uv, weights, workspace, decay=1.0, scale=0.0, out=None,
+                           stream=None):
+    """One decode step that also sets ``weights`` (see :func:`attention_weights`) to ``decay * weights`` plus each
+    token's attention weight, summed over the query heads of its KV head."""
+    Hq, out = _step_operands(cache, q, Uk, Uv, workspace, out)
+    _totals(cache, weights)
+    _check(load_library().dar_attn_decode_scored(
+        cache.struct, Hq, _ptr(q), _ptr(Uk), _ptr(Uv), float(scale), _ptr(weights), float(decay), _ptr(out),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
+
+
+def evict_workspace(cache: DarCache):
+    """A workspace of the size dar_cache_evict needs (no initialisation needed)."""
+    return _new_workspace(cache, int(load_library().dar_cache_evict_workspace_bytes(cache.struct)))
+
+
+def dar_cache_evict(cache: DarCache, weights, keep, workspace, protect=None, stream=None):
+    """Eviction in place: every sequence b with more than ``keep[b]`` distant tokens (int32 ``[B]``) keeps, per KV
+    head, its first ``protect[b]`` (int32 ``[B]``; none: 0) and those with the largest ``weights``."""
+    _on_current_device(cache)
+    _totals(cache, weights)
+    _operand(keep, "keep", torch.int32, (cache.B,), cache)
+    if protect is not None:
+        _operand(protect, "protect", torch.int32, (cache.B,), cache)
+    _operand(workspace, "workspace", None, None, cache)
+    _check(load_library().dar_cache_evict(cache.struct, _ptr(weights), _ptr(keep), _ptr(protect), _ptr(workspace),
+                                          workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 # --------------------------------------------------------------------------- prefill
