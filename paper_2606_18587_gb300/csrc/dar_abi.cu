@@ -231,7 +231,7 @@ dar_status prepare_segments(const dar_cache *cache, int32_t Hq, const void *q, c
         dar::segments_line_bound(cache->dtype, cache->B, Hq, cache->Hkv, cache->d_down, cache->w,
                                  cache->max_pages_per_seq) >= most)
         return fail(DAR_ERR_UNSUPPORTED, "cache too large for int32 line indices");
-    const size_t need = dar::segments_workspace_bytes(cache->B, Hq, cache->Hkv, cache->d_down, cache->w,
+    const size_t need = dar::segments_workspace_bytes(cache->dtype, cache->B, Hq, cache->Hkv, cache->d_down, cache->w,
                                                       cache->max_pages_per_seq, scored);
     if (workspace_bytes < need)
         return fail(DAR_ERR_CAPACITY, "workspace %zu bytes < %zu needed", workspace_bytes, need);
@@ -399,7 +399,7 @@ size_t dar_decode_shared_workspace_bytes(const dar_cache *cache, int32_t Hq)
 {
     if (check_cache(cache) != DAR_OK || Hq < cache->Hkv || Hq % cache->Hkv)
         return 0;
-    return dar::segments_workspace_bytes(cache->B, Hq, cache->Hkv, cache->d_down, cache->w, cache->max_pages_per_seq,
+    return dar::segments_workspace_bytes(cache->dtype, cache->B, Hq, cache->Hkv, cache->d_down, cache->w, cache->max_pages_per_seq,
                                          false);
 }
 
@@ -430,7 +430,7 @@ size_t dar_decode_scored_workspace_bytes(const dar_cache *cache, int32_t Hq)
 {
     if (check_cache(cache) != DAR_OK || Hq < cache->Hkv || Hq % cache->Hkv)
         return 0;
-    return dar::segments_workspace_bytes(cache->B, Hq, cache->Hkv, cache->d_down, cache->w, cache->max_pages_per_seq,
+    return dar::segments_workspace_bytes(cache->dtype, cache->B, Hq, cache->Hkv, cache->d_down, cache->w, cache->max_pages_per_seq,
                                          true);
 }
 

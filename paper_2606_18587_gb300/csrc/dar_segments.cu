@@ -53,13 +53,18 @@ constexpr int kThreads = (kWarps + 1) * 32;
 constexpr int kMaxCtas = 480;            // the workspace holds partial results of this many CTAs
 constexpr int kCostPrivate = 4;          // cost of a private stage
 
-constexpr int kRPW = 4;                  // rows a warp takes
-constexpr int kR = kWarps * kRPW;        // rows of a unit at most
+// Rows a warp takes (a tensor-core tile; registers in fp32), and rows of a unit at most.
+template <typename T>
+__host__ __device__ constexpr int rpw() { return sizeof(T) == 2 ? 16 : 4; }
+template <typename T>
+__host__ __device__ constexpr int unit_rows() { return kWarps * rpw<T>(); }
 
 // Rows of a tile of nr rows go to RW warps; the other warps split the keys.
-__host__ __device__ inline int row_warps(int nr) { return nr <= kRPW ? 1 : nr <= 2 * kRPW ? 2 : 4; }
+template <typename T>
+__host__ __device__ inline int row_warps(int nr) { return nr <= rpw<T>() ? 1 : nr <= 2 * rpw<T>() ? 2 : 4; }
 // Cost of a prefix stage for nr rows, in quarters of a private stage.
-__host__ __device__ inline int prefix_cost(int nr) { return 3 + (nr + 15) / 16; }
+template <typename T>
+__host__ __device__ inline int prefix_cost(int nr) { return 3 + (nr + rpw<T>() - 1) / rpw<T>(); }
 constexpr int kCostMax = 8;
 
 template <typename T>
@@ -90,9 +95,9 @@ struct Args {
     PlanHead *head;
     PlanSeq *plan;
     float *rec_p, *rec_x;  // partial results of private and prefix units
-    float *scores;         // [B][Hq][slots] scaled scores (log2), or nullptr
+    float *scores;         // [B][Hq][score_stride] scaled scores (log2), or nullptr
     float *weights;        // [B][Hkv][slots], or nullptr
-    long long slots;
+    long long slots, score_stride;  // positions of a sequence at capacity, and rounded up to whole 16 bytes
     int B, Hq, Hkv, G, w, maxp, num_pages, ngroups;
     int RP, RTP;  // rows of a private unit at most, row tiles of a (sequence, KV head)
     float c2;     // scale * log2(e)
@@ -179,6 +184,7 @@ __device__ __forceinline__ int warp_scan(int *a, int n, int lane)
 template <typename T, int DD>
 __device__ void build_tables(const Args &a, const Tables &t, bool first_cta)
 {
+    constexpr int kR = unit_rows<T>();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ng = a.ngroups;
     for (int i = tid; i < ng; i += kThreads) {
         int P = a.prefix_pages[i];
@@ -243,7 +249,7 @@ __device__ void build_tables(const Args &a, const Tables &t, bool first_cta)
         const int rows = cnt * a.G, rt = (rows + kR - 1) / kR;
         t.gmoff[i] = cnt;
         t.gxu[i] = a.Hkv * rt;
-        t.gxst[i] = cnt ? a.Hkv * rt * prefix_cost(min(rows, kR)) * prefix_stages<T, DD>(t.gP[i]) : 0;
+        t.gxst[i] = cnt ? a.Hkv * rt * prefix_cost<T>(min(rows, kR)) * prefix_stages<T, DD>(t.gP[i]) : 0;
     }
     __syncthreads();
     if (warp == 0) {
@@ -287,6 +293,7 @@ struct Cut {
 template <typename T, int DD>
 __device__ bool find_cut(const Args &a, const Tables &t, int p, int hi, int cta, Cut &c, int &next)
 {
+    constexpr int kR = unit_rows<T>();
     int start, cost, nst, unit;
     if (p < t.tot[0]) {
         int lo = 0, up = a.ngroups - 1;  // the last group that starts at or before p (empty ones share a start)
@@ -298,7 +305,7 @@ __device__ bool find_cut(const Args &a, const Tables &t, int p, int hi, int cta,
                 up = mid - 1;
         }
         const int i = lo, rows = t.gcnt[i] * a.G, rts = (rows + kR - 1) / kR;
-        cost = prefix_cost(min(rows, kR));
+        cost = prefix_cost<T>(min(rows, kR));
         nst = prefix_stages<T, DD>(t.gP[i]);
         const int u = (p - t.gxst[i]) / (nst * cost);
         start = t.gxst[i] + u * nst * cost;
@@ -307,7 +314,7 @@ __device__ bool find_cut(const Args &a, const Tables &t, int p, int hi, int cta,
         c.g = u / rts;
         c.rt = u % rts;
         c.rows = min(kR, rows - c.rt * kR);
-        c.RW = row_warps(c.rows);
+        c.RW = row_warps<T>(c.rows);
         c.b = t.members[t.gmoff[i]];
         c.nwin = c.nsw = 0;
         c.tok0 = 0;
@@ -332,7 +339,7 @@ __device__ bool find_cut(const Args &a, const Tables &t, int p, int hi, int cta,
         c.g = u / a.RTP;
         c.rt = u % a.RTP;
         c.rows = min(a.RP, a.G - c.rt * kR);
-        c.RW = row_warps(a.RP);
+        c.RW = row_warps<T>(a.RP);
         c.nwin = min(t.L[b], a.w);
         c.nsw = (c.nwin + ring_tokens<T>() - 1) / ring_tokens<T>();
         c.tok0 = P * kPage;
@@ -346,6 +353,7 @@ __device__ bool find_cut(const Args &a, const Tables &t, int p, int hi, int cta,
 }
 
 // Query row `row` of a cut: its (sequence, head).
+template <int kR>
 __device__ __forceinline__ void row_of(const Args &a, const Tables &t, const Cut &c, int row, int &b, int &h)
 {
     if (c.grp < 0) {
@@ -377,6 +385,8 @@ __device__ __forceinline__ void load8(const unsigned char *tile, int byte, float
 
 // Running softmax of a warp's rows over the tokens of its lanes: ROW / 8 lanes share a token, each
 // with 8 of its entries; every group of lanes has its own maximum and sum until finish().
+constexpr int kRPW = rpw<float>();
+
 template <int ROW>
 struct Running {
     static constexpr int LPT = ROW / 8, TPI = 32 / LPT;
@@ -465,10 +475,493 @@ __device__ __forceinline__ void lane_stage(const unsigned char *tile, int ntok, 
 
 __host__ __device__ constexpr int align1k(int x) { return (x + 1023) & ~1023; }
 // Shared memory: the slots (1024-byte aligned, as the swizzle wants), query rows, tables, barriers.
-constexpr int kQBytes = 2 * kR * kHeadDim * 4;
+constexpr int kQBytes = 2 * unit_rows<float>() * kHeadDim * 4;  // fp32
+template <typename T>
 inline size_t segments_smem(int B, int ngroups)
 {
-    return 1024 + (size_t)kStages * kSlot + kQBytes + (size_t)table_ints(B, ngroups) * 4 + 2 * kStages * 8 + 16;
+    return 1024 + (size_t)kStages * kSlot + (sizeof(T) == 4 ? kQBytes : 0) + (size_t)table_ints(B, ngroups) * 4 + 2 * kStages * 8 + 16;
+}
+
+// ---- the four warps that consume the stages, fp32: CUDA cores
+template <typename T, int DD, bool SCORED>
+__device__ __forceinline__ void consume_lanes(const Args &a, const Tables &t, const unsigned char *slots, float *qs,
+                                              uint64_t *full, uint64_t *empty, volatile int *gave_up, int cta, int lo,
+                                              int hi)
+{
+    constexpr int TW = ring_tokens<T>(), TP = page_tokens<T, DD>(), kR = unit_rows<T>();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    float *qt = qs + kR * kHeadDim;  // [kR][64] query rows, then [kR][DD] absorbed rows
+    int n = 0;
+    bool alive = true;
+    for (int p = lo, next; p < hi; p = next) {
+        Cut c;
+        if (!find_cut<T, DD>(a, t, p, hi, cta, c, next))
+            continue;
+        // query rows of the cut, and q~ = q Uk^T
+        asm volatile("bar.sync 1, 128;" ::: "memory");  // the rows of the cut before are read
+        for (int i = tid; i < kR * kHeadDim; i += kWarps * 32) {
+            const int row = i / kHeadDim;
+            float x = 0.f;
+            if (row < c.rows) {
+                int b, h;
+                row_of<kR>(a, t, c, row, b, h);
+                x = to_f32(static_cast<const T *>(a.q)[((size_t)b * a.Hq + h) * kHeadDim + i % kHeadDim]);
+            }
+            qs[i] = x;
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        for (int i = tid; i < kR * DD; i += kWarps * 32) {
+            const int row = i / DD, e = i % DD;
+            const float4 *u = reinterpret_cast<const float4 *>(a.Uk + ((size_t)c.g * DD + e) * kHeadDim);
+            const float4 *x = reinterpret_cast<const float4 *>(qs + row * kHeadDim);
+            float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+            if (row < c.rows) {
+#pragma unroll
+                for (int k = 0; k < kHeadDim / 4; ++k) {
+                    const float4 uu = __ldg(u + k), xx = x[k];
+                    s0 = fmaf(uu.x, xx.x, s0);
+                    s1 = fmaf(uu.y, xx.y, s1);
+                    s2 = fmaf(uu.z, xx.z, s2);
+                    s3 = fmaf(uu.w, xx.w, s3);
+                }
+            }
+            qt[i] = (s0 + s1) + (s2 + s3);
+        }
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        const int RW = c.RW, KW = kWarps / RW, rw = warp % RW, kw = warp / RW;
+        const int r0 = rw * kRPW;
+        Running<kHeadDim> sl;
+        Running<DD> sd;
+        sl.clear();
+        sd.clear();
+        float ql[kRPW][8], qd[kRPW][8];
+#pragma unroll
+        for (int r = 0; r < kRPW; ++r)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                ql[r][e] = qs[(r0 + r) * kHeadDim + (lane % 8) * 8 + e];
+                qd[r][e] = qt[(r0 + r) * DD + (lane % (DD / 8)) * 8 + e];
+            }
+        float *srow = nullptr;  // scores of the warp's first row
+        if constexpr (SCORED)
+            srow = a.scores + ((size_t)c.b * a.Hq + c.g * a.G + c.rt * kR + r0) * a.score_stride;
+        const int L = c.tok1 + c.nwin;
+        for (int st = c.st0; st < c.st1; ++st, ++n) {
+            const int s = n % kStages;
+            // a warp that gave up computes nothing more, but still meets the others at the barriers
+            if (!alive || !mbar_wait(&full[s], (unsigned)((n / kStages) & 1), gave_up)) {
+                if (alive && lane == 0)
+                    report(a.status, DAR_ERR_DEVICE);
+                alive = false;
+                continue;
+            }
+            const unsigned char *tile = slots + s * kSlot;
+            if (st < c.nsw) {
+                const int t0 = st * TW;
+                lane_stage<T, kHeadDim>(tile, min(TW, c.nwin - t0), kw, KW, ql, a.c2, sl, lane,
+                                        [&](int r, int tok, float y) {
+                                            if constexpr (SCORED) {
+                                                // the position that a ring slot holds
+                                                const int slot = t0 + tok, pos = (L - 1) - ((L - 1 - slot) % a.w);
+                                                if (r0 + r < c.rows)
+                                                    srow[(size_t)r * a.score_stride + pos] = y;
+                                            }
+                                        });
+            } else {
+                const int t0 = c.tok0 + (st - c.nsw) * TP;
+                lane_stage<T, DD>(tile, min(TP, c.tok1 - t0), kw, KW, qd, a.c2, sd, lane,
+                                  [&](int r, int tok, float y) {
+                                      if constexpr (SCORED) {
+                                          if (r0 + r < c.rows)
+                                              srow[(size_t)r * a.score_stride + t0 + tok] = y;
+                                      }
+                                  });
+            }
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(&empty[s]);
+        }
+        sl.finish();
+        sd.finish();
+#pragma unroll
+        for (int r = 0; r < kRPW; ++r) {
+            if (r0 + r >= c.rows)
+                continue;
+            const float m = fmaxf(sl.m[r], sd.m[r]);
+            const float base = m == -INFINITY ? 0.f : m;
+            const float fl = exp2f(sl.m[r] - base), fd = exp2f(sd.m[r] - base);
+            float *rec;
+            if (c.grp < 0) {
+                rec = a.rec_p + ((size_t)c.slot * (KW * a.RP) + kw * a.RP + r0 + r) * rec_p_floats<DD>();
+                if (lane < 8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        rec[4 + lane * 8 + e] = sl.acc[r][e] * fl;
+                if (lane < DD / 8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        rec[4 + kHeadDim + lane * 8 + e] = sd.acc[r][e] * fd;
+            } else {
+                rec = a.rec_x + ((size_t)c.slot * kR + kw * (RW * kRPW) + r0 + r) * rec_x_floats<DD>();
+                if (lane < DD / 8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        rec[4 + lane * 8 + e] = sd.acc[r][e] * fd;
+            }
+            if (lane == 0) {
+                rec[0] = m;
+                rec[1] = sl.l[r] * fl + sd.l[r] * fd;
+            }
+        }
+    }
+}
+
+// ---- the same, bf16: tensor cores (mma.sync m16n8k16; a tile has few rows in most calls, and tcgen05
+// products of 128 rows would be mostly padding).  A warp holds 16 rows: their queries are the A operand
+// of the scores, and the weights, rounded to bf16, that of the value sums.  Lane 4 i + c holds rows i and
+// i + 8, columns 2 c and 2 c + 1 of every 8-column tile.
+
+// Two fp32 values as NT bf16 terms each: x = t0 + t1 (+ t2) but for 2^-16 (2^-24) of it.
+template <int NT>
+__device__ __forceinline__ void split2(float x, float y, uint32_t (&t)[NT])
+{
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        t[i] = cvt_bf16x2(x, y);
+        x -= bf16lo(t[i]);
+        y -= bf16hi(t[i]);
+    }
+}
+
+// Scores and value sums of a step of NB * 16 keys from token tok0 of the tile; keys >= ntok do not count.
+// QA: A operands of the scores (KS products of 16 entries each; entries of a key repeat every ROW).
+template <int ROW, int KS, int NB, bool MASK, typename Keep, typename Rescale>
+__device__ __forceinline__ void mma_step(uint32_t tile, int tok0, int ntok, const uint32_t (&qa)[KS][4], float c2,
+                                         float (&acc)[ROW / 8][4], float (&ms)[2], float (&l)[2], int lane, Keep keep,
+                                         Rescale rescale)
+{
+    constexpr int RB = ROW * 2;  // bytes of a row
+    float s[2 * NB][4];
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i)
+        s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+    const int mat = lane >> 3, mrow = lane & 7;
+    if constexpr (ROW == 8) {  // a key is one 16-byte chunk: both halves of the product's 16 entries
+#pragma unroll
+        for (int i = 0; i < NB; i += 2) {
+            uint32_t k[4];
+            ldsm_x4(tile + swz((tok0 + 16 * i + 8 * mat + mrow) * RB), k);
+#pragma unroll
+            for (int x = 0; x < KS; ++x)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    mma_bf16_acc(s[2 * i + j], qa[x], k[j], k[j]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int e = 0; e < ROW / 16; ++e) {
+                uint32_t k[4];
+                ldsm_x4(tile + swz((tok0 + 16 * i + 8 * (mat >> 1) + mrow) * RB + 32 * e + 16 * (mat & 1)), k);
+#pragma unroll
+                for (int x = e; x < KS; x += ROW / 16) {
+                    mma_bf16_acc(s[2 * i], qa[x], k[0], k[1]);
+                    mma_bf16_acc(s[2 * i + 1], qa[x], k[2], k[3]);
+                }
+            }
+    }
+    if constexpr (MASK) {
+#pragma unroll
+        for (int i = 0; i < 2 * NB; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (tok0 + 8 * i + 2 * (lane & 3) + (e & 1) >= ntok)
+                    s[i][e] = -INFINITY;
+    }
+    keep(tok0, s);
+    float m0 = s[0][0], m1 = s[0][2];
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) {
+        m0 = max3(m0, s[i][0], s[i][1]);
+        m1 = max3(m1, s[i][2], s[i][3]);
+    }
+    m0 *= c2;
+    m1 *= c2;
+    if (__any_sync(0xffffffffu, m0 > ms[0] || m1 > ms[1])) {
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
+            m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, o));
+        }
+        m0 = fmaxf(ms[0], m0);
+        m1 = fmaxf(ms[1], m1);
+        rescale(m0 == -INFINITY ? 1.f : ex2_approx(ms[0] - m0), m1 == -INFINITY ? 1.f : ex2_approx(ms[1] - m1));
+        ms[0] = m0;
+        ms[1] = m1;
+    }
+    const float b0 = ms[0] == -INFINITY ? 0.f : ms[0], b1 = ms[1] == -INFINITY ? 0.f : ms[1];
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) {
+        float x0, x1, x2, x3;
+        ffma2(x0, x1, s[i][0], s[i][1], c2, c2, -b0, -b0);
+        ffma2(x2, x3, s[i][2], s[i][3], c2, c2, -b1, -b1);
+        s[i][0] = ex2_approx(x0);
+        s[i][1] = ex2_approx(x1);
+        s[i][2] = ex2_approx(x2);
+        s[i][3] = ex2_approx(x3);
+        l[0] += s[i][0] + s[i][1];
+        l[1] += s[i][2] + s[i][3];
+    }
+    // bytes behind the last key must not reach a sum: 0 * NaN is NaN
+    auto key_mask = [&](int key) {
+        return (key < ntok ? 0xffffu : 0u) | (key + 1 < ntok ? 0xffff0000u : 0u);
+    };
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        // the weights as bf16 operands: 2^-9 of each at most, beside an output that is rounded as much
+        const uint32_t p[4] = {cvt_bf16x2(s[2 * i][0], s[2 * i][1]), cvt_bf16x2(s[2 * i][2], s[2 * i][3]),
+                               cvt_bf16x2(s[2 * i + 1][0], s[2 * i + 1][1]),
+                               cvt_bf16x2(s[2 * i + 1][2], s[2 * i + 1][3])};
+        uint32_t mk0 = ~0u, mk1 = ~0u;
+        if constexpr (MASK) {
+            mk0 = key_mask(tok0 + 16 * i + 2 * (lane & 3));
+            mk1 = key_mask(tok0 + 16 * i + 8 + 2 * (lane & 3));
+        }
+        if constexpr (ROW == 8) {
+            uint32_t v[2];
+            asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];"
+                         : "=r"(v[0]), "=r"(v[1])
+                         : "r"(tile + kHalf + swz((tok0 + 16 * i + 8 * (mat & 1) + mrow) * RB)));
+            mma_bf16_acc(acc[0], p, v[0] & mk0, v[1] & mk1);
+        } else {
+#pragma unroll
+            for (int e = 0; e < ROW / 16; ++e) {
+                uint32_t v[4];
+                ldsm_x4_t(tile + kHalf + swz((tok0 + 16 * i + 8 * (mat & 1) + mrow) * RB + 32 * e + 16 * (mat >> 1)), v);
+                mma_bf16_acc(acc[2 * e], p, v[0] & mk0, v[1] & mk1);
+                mma_bf16_acc(acc[2 * e + 1], p, v[2] & mk0, v[3] & mk1);
+            }
+        }
+    }
+}
+
+template <int DD, bool SCORED>
+__device__ __forceinline__ void consume_mma(const Args &a, const Tables &t, const unsigned char *slots, uint64_t *full,
+                                            uint64_t *empty, volatile int *gave_up, int cta, int lo, int hi)
+{
+    constexpr int TW = ring_tokens<bf16>(), TP = page_tokens<bf16, DD>(), kR = unit_rows<bf16>();
+    // q~ in bf16 terms: two leave 2^-16 of it, beside weights rounded to 2^-9; weights that are results take three
+    constexpr int NT = SCORED ? 3 : 2;
+    constexpr int KS = DD == 8 ? (NT + 1) / 2 : NT * DD / 16;  // products of 16 entries in a global score
+    constexpr int NBP = TP / kWarps >= 64 ? 4 : TP / kWarps / 16, NBW = TW / kWarps / 16;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i0 = lane >> 2, c0 = lane & 3;
+    int n = 0;
+    bool alive = true;
+    for (int p = lo, next; p < hi; p = next) {
+        Cut c;
+        if (!find_cut<bf16, DD>(a, t, p, hi, cta, c, next))
+            continue;
+        const int RW = c.RW, KW = kWarps / RW, rw = warp % RW, kw = warp / RW;
+        const int r0 = rw * 16 + i0, r1 = r0 + 8;  // this lane's rows
+        // queries (entries 16 e + 2 c, + 1 and 16 e + 8 + 2 c, + 1 of either row)
+        uint32_t qa[4][4];
+        {
+            const uint32_t *q0 = nullptr, *q1 = nullptr;
+            int b, h;
+            if (r0 < c.rows) {
+                row_of<kR>(a, t, c, r0, b, h);
+                q0 = static_cast<const uint32_t *>(a.q) + ((size_t)b * a.Hq + h) * (kHeadDim / 2) + c0;
+            }
+            if (r1 < c.rows) {
+                row_of<kR>(a, t, c, r1, b, h);
+                q1 = static_cast<const uint32_t *>(a.q) + ((size_t)b * a.Hq + h) * (kHeadDim / 2) + c0;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                qa[e][0] = q0 ? __ldg(q0 + 8 * e) : 0u;
+                qa[e][1] = q1 ? __ldg(q1 + 8 * e) : 0u;
+                qa[e][2] = q0 ? __ldg(q0 + 8 * e + 4) : 0u;
+                qa[e][3] = q1 ? __ldg(q1 + 8 * e + 4) : 0u;
+            }
+        }
+        // q~ = q Uk^T: Uk in three bf16 terms, so that the products are fp32 ones but for 2^-24
+        uint32_t qt[KS][4];
+        {
+            const float *u = a.Uk + ((size_t)c.g * DD + i0) * kHeadDim + 2 * c0;
+            uint32_t prev[NT][2];  // terms of the tile of 8 entries before
+#pragma unroll
+            for (int j = 0; j < DD / 8; ++j) {
+                float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 u0 = __ldg(reinterpret_cast<const float2 *>(u + j * 8 * kHeadDim + 16 * e));
+                    const float2 u1 = __ldg(reinterpret_cast<const float2 *>(u + j * 8 * kHeadDim + 16 * e + 8));
+                    uint32_t t0[3], t1[3];
+                    split2<3>(u0.x, u0.y, t0);
+                    split2<3>(u1.x, u1.y, t1);
+#pragma unroll
+                    for (int y = 2; y >= 0; --y)
+                        mma_bf16_acc(x, qa[e], t0[y], t1[y]);
+                }
+                uint32_t lo8[NT], hi8[NT];  // terms of rows i and i + 8
+                split2<NT>(x[0], x[1], lo8);
+                split2<NT>(x[2], x[3], hi8);
+                if constexpr (DD == 8) {
+#pragma unroll
+                    for (int y = 0; y < KS; ++y) {
+                        qt[y][0] = lo8[2 * y];
+                        qt[y][1] = hi8[2 * y];
+                        qt[y][2] = 2 * y + 1 < NT ? lo8[2 * y + 1 < NT ? 2 * y + 1 : 0] : 0u;
+                        qt[y][3] = 2 * y + 1 < NT ? hi8[2 * y + 1 < NT ? 2 * y + 1 : 0] : 0u;
+                    }
+                } else if (j % 2 == 0) {
+#pragma unroll
+                    for (int y = 0; y < NT; ++y) {
+                        prev[y][0] = lo8[y];
+                        prev[y][1] = hi8[y];
+                    }
+                } else {
+#pragma unroll
+                    for (int y = 0; y < NT; ++y) {  // term y of entries 16 (j / 2) ..: product y * DD / 16 + j / 2
+                        uint32_t *o = qt[y * (DD / 16) + j / 2];
+                        o[0] = prev[y][0];
+                        o[1] = prev[y][1];
+                        o[2] = lo8[y];
+                        o[3] = hi8[y];
+                    }
+                }
+            }
+        }
+        float ol[kHeadDim / 8][4], od[DD / 8][4], ms[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < kHeadDim / 8; ++j)
+            ol[j][0] = ol[j][1] = ol[j][2] = ol[j][3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < DD / 8; ++j)
+            od[j][0] = od[j][1] = od[j][2] = od[j][3] = 0.f;
+        const bool ring = c.st0 < c.nsw;  // the cut holds ring stages
+        auto rescale = [&](float f0, float f1) {
+            l[0] *= f0;
+            l[1] *= f1;
+            if (ring)
+#pragma unroll
+                for (int j = 0; j < kHeadDim / 8; ++j) {
+                    ol[j][0] *= f0;
+                    ol[j][1] *= f0;
+                    ol[j][2] *= f1;
+                    ol[j][3] *= f1;
+                }
+#pragma unroll
+            for (int j = 0; j < DD / 8; ++j) {
+                od[j][0] *= f0;
+                od[j][1] *= f0;
+                od[j][2] *= f1;
+                od[j][3] *= f1;
+            }
+        };
+        float *s0 = nullptr, *s1 = nullptr;  // scores of the lane's rows
+        if constexpr (SCORED) {
+            float *x = a.scores + ((size_t)c.b * a.Hq + c.g * a.G + c.rt * kR) * a.score_stride;
+            s0 = r0 < c.rows ? x + (size_t)r0 * a.score_stride : nullptr;
+            s1 = r1 < c.rows ? x + (size_t)r1 * a.score_stride : nullptr;
+        }
+        const int L = c.tok1 + c.nwin;
+        for (int st = c.st0; st < c.st1; ++st, ++n) {
+            const int s = n % kStages;
+            if (!alive || !mbar_wait(&full[s], (unsigned)((n / kStages) & 1), gave_up)) {
+                if (alive && lane == 0)
+                    report(a.status, DAR_ERR_DEVICE);
+                alive = false;
+                continue;
+            }
+            const uint32_t tile = smem_u32(slots + s * kSlot);
+            if (st < c.nsw) {
+                const int t0 = st * TW, ntok = min(TW, c.nwin - t0);
+                auto keep = [&](int tok, const float (&x)[2 * NBW][4]) {
+                    if constexpr (SCORED) {
+#pragma unroll
+                        for (int i = 0; i < 2 * NBW; ++i)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int k = tok + 8 * i + 2 * c0 + e;
+                                if (k >= ntok)
+                                    continue;
+                                const int pos = (L - 1) - ((L - 1 - (t0 + k)) % a.w);  // held by ring slot t0 + k
+                                if (s0)
+                                    s0[pos] = x[i][e] * a.c2;
+                                if (s1)
+                                    s1[pos] = x[i][2 + e] * a.c2;
+                            }
+                    }
+                };
+                for (int k = kw * (TW / KW); k < min(ntok, (kw + 1) * (TW / KW)); k += 16 * NBW) {
+                    if (k + 16 * NBW <= ntok)
+                        mma_step<kHeadDim, 4, NBW, false>(tile, k, ntok, qa, a.c2, ol, ms, l, lane, keep, rescale);
+                    else
+                        mma_step<kHeadDim, 4, NBW, true>(tile, k, ntok, qa, a.c2, ol, ms, l, lane, keep, rescale);
+                }
+            } else {
+                const int t0 = c.tok0 + (st - c.nsw) * TP, ntok = min(TP, c.tok1 - t0);
+                auto keep = [&](int tok, const float (&x)[2 * NBP][4]) {
+                    if constexpr (SCORED) {
+#pragma unroll
+                        for (int i = 0; i < 2 * NBP; ++i) {
+                            const int k = tok + 8 * i + 2 * c0;
+                            auto put = [&](float *row, float x0, float x1) {
+                                if (k + 1 < ntok)
+                                    *reinterpret_cast<float2 *>(row + t0 + k) = make_float2(x0 * a.c2, x1 * a.c2);
+                                else if (k < ntok)  // the next position is the ring's
+                                    row[t0 + k] = x0 * a.c2;
+                            };
+                            if (s0)
+                                put(s0, x[i][0], x[i][1]);
+                            if (s1)
+                                put(s1, x[i][2], x[i][3]);
+                        }
+                    }
+                };
+                for (int k = kw * (TP / KW); k < min(ntok, (kw + 1) * (TP / KW)); k += 16 * NBP) {
+                    if (k + 16 * NBP <= ntok)
+                        mma_step<DD, KS, NBP, false>(tile, k, ntok, qt, a.c2, od, ms, l, lane, keep, rescale);
+                    else
+                        mma_step<DD, KS, NBP, true>(tile, k, ntok, qt, a.c2, od, ms, l, lane, keep, rescale);
+                }
+            }
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(&empty[s]);
+        }
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            l[0] += __shfl_xor_sync(0xffffffffu, l[0], o);
+            l[1] += __shfl_xor_sync(0xffffffffu, l[1], o);
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const int row = y ? r1 : r0;
+            if (row >= c.rows)
+                continue;
+            float *rec;
+            if (c.grp < 0) {
+                rec = a.rec_p + ((size_t)c.slot * (KW * a.RP) + kw * a.RP + row) * rec_p_floats<DD>();
+#pragma unroll
+                for (int j = 0; j < kHeadDim / 8; ++j)
+                    *reinterpret_cast<float2 *>(rec + 4 + 8 * j + 2 * c0) = make_float2(ol[j][2 * y], ol[j][2 * y + 1]);
+#pragma unroll
+                for (int j = 0; j < DD / 8; ++j)
+                    *reinterpret_cast<float2 *>(rec + 4 + kHeadDim + 8 * j + 2 * c0) =
+                        make_float2(od[j][2 * y], od[j][2 * y + 1]);
+            } else {
+                rec = a.rec_x + ((size_t)c.slot * kR + kw * (RW * 16) + row) * rec_x_floats<DD>();
+#pragma unroll
+                for (int j = 0; j < DD / 8; ++j)
+                    *reinterpret_cast<float2 *>(rec + 4 + 8 * j + 2 * c0) = make_float2(od[j][2 * y], od[j][2 * y + 1]);
+            }
+            if (c0 == 0)
+                *reinterpret_cast<float2 *>(rec) = make_float2(ms[y], l[y]);
+        }
+    }
 }
 
 template <typename T, int DD, bool SCORED>
@@ -483,9 +976,8 @@ __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constan
     constexpr int WL = kHeadDim * (int)sizeof(T) / 128;    // lines of a ring row
     extern __shared__ unsigned char raw[];
     unsigned char *slots = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-    float *qs = reinterpret_cast<float *>(slots + kStages * kSlot);  // [kR][64] query rows
-    float *qt = qs + kR * kHeadDim;                                  // [kR][DD] absorbed rows
-    uint64_t *full = reinterpret_cast<uint64_t *>(qt + kR * kHeadDim);
+    unsigned char *rows_at = slots + kStages * kSlot;  // fp32: query rows
+    uint64_t *full = reinterpret_cast<uint64_t *>(rows_at + (sizeof(T) == 4 ? kQBytes : 0));
     uint64_t *empty = full + kStages;
     int *ints = reinterpret_cast<int *>(empty + kStages);
     volatile int *gave_up = ints;
@@ -517,10 +1009,10 @@ __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constan
             s.xstart = s.xstages = s.xcost = s.xunit = s.row0 = s.xrows = 0;
             if (g >= 0) {
                 s.xrows = t.gcnt[g] * a.G;
-                s.xrt = (s.xrows + kR - 1) / kR;
+                s.xrt = (s.xrows + unit_rows<T>() - 1) / unit_rows<T>();
                 s.xstart = t.gxst[g];
                 s.xstages = prefix_stages<T, DD>(t.gP[g]);
-                s.xcost = prefix_cost(min(s.xrows, kR));
+                s.xcost = prefix_cost<T>(min(s.xrows, unit_rows<T>()));
                 s.xunit = t.gxu[g];
                 s.row0 = t.rank[b] * a.G;
             }
@@ -598,129 +1090,10 @@ __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constan
     }
 
     // ---- four warps consume them
-    int n = 0;
-    bool alive = true;
-    for (int p = lo, next; p < hi; p = next) {
-        Cut c;
-        if (!find_cut<T, DD>(a, t, p, hi, cta, c, next))
-            continue;
-        // query rows of the cut, and q~ = q Uk^T
-        asm volatile("bar.sync 1, 128;" ::: "memory");  // the rows of the cut before are read
-        for (int i = tid; i < kR * kHeadDim; i += kWarps * 32) {
-            const int row = i / kHeadDim;
-            float x = 0.f;
-            if (row < c.rows) {
-                int b, h;
-                row_of(a, t, c, row, b, h);
-                x = to_f32(static_cast<const T *>(a.q)[((size_t)b * a.Hq + h) * kHeadDim + i % kHeadDim]);
-            }
-            qs[i] = x;
-        }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        for (int i = tid; i < kR * DD; i += kWarps * 32) {
-            const int row = i / DD, e = i % DD;
-            const float4 *u = reinterpret_cast<const float4 *>(a.Uk + ((size_t)c.g * DD + e) * kHeadDim);
-            const float4 *x = reinterpret_cast<const float4 *>(qs + row * kHeadDim);
-            float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-            if (row < c.rows) {
-#pragma unroll
-                for (int k = 0; k < kHeadDim / 4; ++k) {
-                    const float4 uu = __ldg(u + k), xx = x[k];
-                    s0 = fmaf(uu.x, xx.x, s0);
-                    s1 = fmaf(uu.y, xx.y, s1);
-                    s2 = fmaf(uu.z, xx.z, s2);
-                    s3 = fmaf(uu.w, xx.w, s3);
-                }
-            }
-            qt[i] = (s0 + s1) + (s2 + s3);
-        }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        const int RW = c.RW, KW = kWarps / RW, rw = warp % RW, kw = warp / RW;
-        const int r0 = rw * kRPW;
-        Running<kHeadDim> sl;
-        Running<DD> sd;
-        sl.clear();
-        sd.clear();
-        float ql[kRPW][8], qd[kRPW][8];
-#pragma unroll
-        for (int r = 0; r < kRPW; ++r)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                ql[r][e] = qs[(r0 + r) * kHeadDim + (lane % 8) * 8 + e];
-                qd[r][e] = qt[(r0 + r) * DD + (lane % (DD / 8)) * 8 + e];
-            }
-        float *srow = nullptr;  // scores of the warp's first row
-        if constexpr (SCORED)
-            srow = a.scores + ((size_t)c.b * a.Hq + c.g * a.G + c.rt * kR + r0) * a.slots;
-        const int L = c.tok1 + c.nwin;
-        for (int st = c.st0; st < c.st1; ++st, ++n) {
-            const int s = n % kStages;
-            // a warp that gave up computes nothing more, but still meets the others at the barriers
-            if (!alive || !mbar_wait(&full[s], (unsigned)((n / kStages) & 1), gave_up)) {
-                if (alive && lane == 0)
-                    report(a.status, DAR_ERR_DEVICE);
-                alive = false;
-                continue;
-            }
-            const unsigned char *tile = slots + s * kSlot;
-            if (st < c.nsw) {
-                const int t0 = st * TW;
-                lane_stage<T, kHeadDim>(tile, min(TW, c.nwin - t0), kw, KW, ql, a.c2, sl, lane,
-                                        [&](int r, int tok, float y) {
-                                            if constexpr (SCORED) {
-                                                // the position that a ring slot holds
-                                                const int slot = t0 + tok, pos = (L - 1) - ((L - 1 - slot) % a.w);
-                                                if (r0 + r < c.rows)
-                                                    srow[(size_t)r * a.slots + pos] = y;
-                                            }
-                                        });
-            } else {
-                const int t0 = c.tok0 + (st - c.nsw) * TP;
-                lane_stage<T, DD>(tile, min(TP, c.tok1 - t0), kw, KW, qd, a.c2, sd, lane,
-                                  [&](int r, int tok, float y) {
-                                      if constexpr (SCORED) {
-                                          if (r0 + r < c.rows)
-                                              srow[(size_t)r * a.slots + t0 + tok] = y;
-                                      }
-                                  });
-            }
-            __syncwarp();
-            if (lane == 0)
-                mbar_arrive(&empty[s]);
-        }
-        sl.finish();
-        sd.finish();
-#pragma unroll
-        for (int r = 0; r < kRPW; ++r) {
-            if (r0 + r >= c.rows)
-                continue;
-            const float m = fmaxf(sl.m[r], sd.m[r]);
-            const float base = m == -INFINITY ? 0.f : m;
-            const float fl = exp2f(sl.m[r] - base), fd = exp2f(sd.m[r] - base);
-            float *rec;
-            if (c.grp < 0) {
-                rec = a.rec_p + ((size_t)c.slot * (KW * a.RP) + kw * a.RP + r0 + r) * rec_p_floats<DD>();
-                if (lane < 8)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        rec[4 + lane * 8 + e] = sl.acc[r][e] * fl;
-                if (lane < DD / 8)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        rec[4 + kHeadDim + lane * 8 + e] = sd.acc[r][e] * fd;
-            } else {
-                rec = a.rec_x + ((size_t)c.slot * kR + kw * (RW * kRPW) + r0 + r) * rec_x_floats<DD>();
-                if (lane < DD / 8)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        rec[4 + lane * 8 + e] = sd.acc[r][e] * fd;
-            }
-            if (lane == 0) {
-                rec[0] = m;
-                rec[1] = sl.l[r] * fl + sd.l[r] * fd;
-            }
-        }
-    }
+    if constexpr (sizeof(T) == 2)
+        consume_mma<DD, SCORED>(a, t, slots, full, empty, gave_up, cta, lo, hi);
+    else
+        consume_lanes<T, DD, SCORED>(a, t, slots, reinterpret_cast<float *>(rows_at), full, empty, gave_up, cta, lo, hi);
 }
 
 // ------------------------------------------------------------------ join
@@ -731,13 +1104,14 @@ struct RecRun {
     int n, stride;
 };
 
-template <int DD>
+template <typename T, int DD>
 __device__ __forceinline__ RecRun private_run(const Args &a, const PlanHead &hd, const PlanSeq &s, int b, int g, int j)
 {
+    constexpr int kR = unit_rows<T>();
     RecRun r{nullptr, 0, 0};
     if (s.stages == 0)
         return r;
-    const int rt = j / kR, row = j % kR, KW = kWarps / row_warps(a.RP);
+    const int rt = j / kR, row = j % kR, KW = kWarps / row_warps<T>(a.RP);
     const int u = g * a.RTP + rt;
     const long long p0 = s.start + (long long)u * s.stages * kCostPrivate;
     const int k0 = owner(p0, hd.total, hd.ctas), k1 = owner(p0 + (s.stages - 1) * kCostPrivate, hd.total, hd.ctas);
@@ -748,13 +1122,14 @@ __device__ __forceinline__ RecRun private_run(const Args &a, const PlanHead &hd,
     return r;
 }
 
-template <int DD>
+template <typename T, int DD>
 __device__ __forceinline__ int prefix_runs(const Args &a, const PlanHead &hd, const PlanSeq &s, int g, int j, int &kws,
                                            const float *&base)
 {
+    constexpr int kR = unit_rows<T>();
     if (s.xrt == 0)
         return 0;
-    const int i = s.row0 + j, rt = i / kR, row = i % kR, rows = min(kR, s.xrows - rt * kR), RW = row_warps(rows);
+    const int i = s.row0 + j, rt = i / kR, row = i % kR, rows = min(kR, s.xrows - rt * kR), RW = row_warps<T>(rows);
     const int u = g * s.xrt + rt;
     const long long p0 = s.xstart + (long long)u * s.xstages * s.xcost;
     const int k0 = owner(p0, hd.total, hd.ctas), k1 = owner(p0 + (s.xstages - 1) * s.xcost, hd.total, hd.ctas);
@@ -772,6 +1147,7 @@ template <typename T, int DD, bool SCORED>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a)
 {
     extern __shared__ float stat[];  // SCORED: [G][2] m and 1 / l
+    constexpr int kR = unit_rows<T>();
     grid_dep_wait();
     const int bg = blockIdx.x, b = bg / a.Hkv, g = bg % a.Hkv, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const PlanSeq s = a.plan[b];
@@ -789,10 +1165,10 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a)
             }
             continue;
         }
-        const RecRun pr = private_run<DD>(a, hd, s, b, g, j);
+        const RecRun pr = private_run<T, DD>(a, hd, s, b, g, j);
         int kws = 1;
         const float *xb = nullptr;
-        const int xn = prefix_runs<DD>(a, hd, s, g, j, kws, xb);
+        const int xn = prefix_runs<T, DD>(a, hd, s, g, j, kws, xb);
         const int xrow = kR / kws * rec_x_floats<DD>();  // from one key warp's row to the next one's
         float m = -INFINITY;
         for (int i = lane; i < pr.n; i += 32)
@@ -853,12 +1229,12 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a)
     if constexpr (SCORED) {
         __syncthreads();
         float *w = a.weights + (size_t)bg * a.slots;
-        const float *x = a.scores + ((size_t)b * a.Hq + (size_t)g * a.G) * a.slots;
+        const float *x = a.scores + ((size_t)b * a.Hq + (size_t)g * a.G) * a.score_stride;
         const int t1 = (int)min((long long)s.L, (long long)(chunk + 1) * kJoinTokens);
         for (int t = chunk * kJoinTokens + threadIdx.x; t < t1; t += kJoinThreads) {
             float p = 0.f;
             for (int j = 0; j < a.G; ++j)
-                p += exp2f(x[(size_t)j * a.slots + t] - stat[2 * j]) * stat[2 * j + 1];
+                p += exp2f(x[(size_t)j * a.score_stride + t] - stat[2 * j]) * stat[2 * j + 1];
             w[t] = a.decay != 0.f ? fmaf(a.decay, w[t], p) : p;
         }
     }
@@ -873,17 +1249,19 @@ struct Layout {
 
 static size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
+template <typename T>
 static Layout layout(int B, int Hq, int Hkv, int dd, int w, int maxp, bool scored)
 {
+    constexpr int kR = unit_rows<T>();
     Layout y;
     const int G = Hq / Hkv;
     y.RP = G < kR ? G : kR;
     y.RTP = (G + kR - 1) / kR;
     const size_t units = (size_t)B * Hkv * y.RTP + kMaxCtas;
-    const size_t rows_p = (size_t)(kWarps / row_warps(y.RP)) * y.RP;
+    const size_t rows_p = (size_t)(kWarps / row_warps<T>(y.RP)) * y.RP;
     // a group of n rows has ceil(n / R) tiles, and there are at most B / 2 groups of two or more
     const size_t units_x = (size_t)Hkv * ((size_t)B * G / kR + B / 2 + 1) + kMaxCtas;
-    const size_t slots = (size_t)maxp * kPage + w;
+    const size_t slots = ((size_t)maxp * kPage + w + 3) / 4 * 4;
     y.head = 0;
     y.plan = 256;
     y.rec_p = y.plan + up256((size_t)B * sizeof(PlanSeq));
@@ -896,7 +1274,7 @@ static Layout layout(int B, int Hq, int Hkv, int dd, int w, int maxp, bool score
 template <typename T, int DD, bool SCORED>
 static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t st)
 {
-    const Layout y = layout(s.B, s.Hq, s.Hkv, DD, s.w, s.maxp, SCORED);
+    const Layout y = layout<T>(s.B, s.Hq, s.Hkv, DD, s.w, s.maxp, SCORED);
     char *ws = static_cast<char *>(workspace);
     Args a;
     a.q = s.q;
@@ -915,6 +1293,7 @@ static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t 
     a.scores = SCORED ? reinterpret_cast<float *>(ws + y.scores) : nullptr;
     a.weights = s.weights;
     a.slots = (long long)s.maxp * kPage + s.w;
+    a.score_stride = (a.slots + 3) / 4 * 4;
     a.B = s.B;
     a.Hq = s.Hq;
     a.Hkv = s.Hkv;
@@ -945,7 +1324,7 @@ static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t 
         once,
         [&](int dev) {
             cudaError_t e2 = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                  (int)segments_smem(DAR_DECODE_MAX_BATCH, DAR_DECODE_MAX_BATCH));
+                                                  (int)segments_smem<T>(DAR_DECODE_MAX_BATCH, DAR_DECODE_MAX_BATCH));
             int n = 0;
             if (e2 == cudaSuccess)
                 e2 = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
@@ -956,7 +1335,7 @@ static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t 
     if (e != cudaSuccess)
         return e;
     const int grid = 2 * sms < kMaxCtas ? 2 * sms : kMaxCtas;
-    kern<<<grid, kThreads, segments_smem(s.B, s.n_groups), st>>>(wk, wv, pk, pv, a);
+    kern<<<grid, kThreads, segments_smem<T>(s.B, s.n_groups), st>>>(wk, wv, pk, pv, a);
     e = cudaGetLastError();
     if (e != cudaSuccess)
         return e;
@@ -987,9 +1366,10 @@ static cudaError_t launch_dd(int dd, const SegmentArgs &s, void *ws, cudaStream_
 
 }  // namespace seg
 
-size_t segments_workspace_bytes(int B, int Hq, int Hkv, int dd, int w, int maxp, bool scored)
+size_t segments_workspace_bytes(dar_dtype dt, int B, int Hq, int Hkv, int dd, int w, int maxp, bool scored)
 {
-    return seg::layout(B, Hq, Hkv, dd, w, maxp, scored).total;
+    return dt == DAR_F32 ? seg::layout<float>(B, Hq, Hkv, dd, w, maxp, scored).total
+                         : seg::layout<bf16>(B, Hq, Hkv, dd, w, maxp, scored).total;
 }
 
 // Upper bound of the line's length: every sequence at capacity, as private units and once more as
@@ -998,7 +1378,8 @@ double segments_line_bound(dar_dtype dt, int B, int Hq, int Hkv, int dd, int w, 
 {
     const int es = dt == DAR_F32 ? 4 : 2, G = Hq / Hkv;
     const double stages = (double)w * kHeadDim * es / seg::kHalf + (double)maxp * kPage * dd * es / seg::kHalf + 2;
-    return (double)B * Hkv * ((G + seg::kR - 1) / seg::kR) * stages * (seg::kCostPrivate + seg::kCostMax);
+    const int R = dt == DAR_F32 ? seg::unit_rows<float>() : seg::unit_rows<bf16>();
+    return (double)B * Hkv * ((G + R - 1) / R) * stages * (seg::kCostPrivate + seg::kCostMax);
 }
 
 cudaError_t launch_segments(dar_dtype dt, int dd, const SegmentArgs &s, void *workspace, cudaStream_t st)
