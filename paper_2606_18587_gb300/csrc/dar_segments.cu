@@ -50,6 +50,7 @@ constexpr int kSlot = 2 * kHalf;
 constexpr int kStages = 4;
 constexpr int kWarps = 4;                // consumer warps
 constexpr int kThreads = (kWarps + 1) * 32;
+constexpr int kSmemPerSm = 228 * 1024;  // of which a CTA's share is its own and 1 KB
 constexpr int kMaxCtas = 480;            // the workspace holds partial results of this many CTAs
 constexpr int kCostPrivate = 4;          // cost of a private stage
 
@@ -95,7 +96,7 @@ struct Args {
     PlanHead *head;
     PlanSeq *plan;
     float *rec_p, *rec_x;  // partial results of private and prefix units
-    float *scores;         // [B][Hq][score_stride] scaled scores (log2), or nullptr
+    float *scores;         // [B][Hq][score_stride] scores, unscaled, or nullptr
     float *weights;        // [B][Hkv][slots], or nullptr
     long long slots, score_stride;  // positions of a sequence at capacity, and rounded up to whole 16 bytes
     int B, Hq, Hkv, G, w, maxp, num_pages, ngroups;
@@ -422,7 +423,7 @@ struct Running {
 };
 
 // ntok tokens of a stage; this warp takes those of its key share (kw of kws).  score(r, tok, s): what
-// becomes of the scaled score of a valid token.
+// becomes of the score of a valid token.
 template <typename T, int ROW, typename Score>
 __device__ __forceinline__ void lane_stage(const unsigned char *tile, int ntok, int kw, int kws,
                                            const float (&q)[kRPW][8], float c2, Running<ROW> &s, int lane, Score score)
@@ -458,7 +459,7 @@ __device__ __forceinline__ void lane_stage(const unsigned char *tile, int ntok, 
         for (int r = 0; r < kRPW; ++r) {
             const float y = valid ? x[r] * c2 : -INFINITY;
             if (valid && sub == 0)
-                score(r, t, y);
+                score(r, t, x[r]);
             const float mn = fmaxf(s.m[r], y);
             const float base = mn == -INFINITY ? 0.f : mn;
             const float f = exp2f(s.m[r] - base), p = exp2f(y - base);
@@ -617,9 +618,14 @@ __device__ __forceinline__ void consume_lanes(const Args &a, const Tables &t, co
 }
 
 // ---- the same, bf16: tensor cores (mma.sync m16n8k16; a tile has few rows in most calls, and tcgen05
-// products of 128 rows would be mostly padding).  A warp holds 16 rows: their queries are the A operand
-// of the scores, and the weights, rounded to bf16, that of the value sums.  Lane 4 i + c holds rows i and
-// i + 8, columns 2 c and 2 c + 1 of every 8-column tile.
+// products of 128 rows would be mostly padding).
+//
+// Two forms.  cut16: a warp holds 16 rows, which are the M side of the scores (A = queries, B = keys);
+// lane 4 i + c holds rows i and i + 8 and columns 2 c, 2 c + 1 of every 8-column tile.  cut8: a warp holds
+// up to 8 rows, which are the N side (A = keys, B = queries), so that a product has no idle rows; lane
+// 4 i + c holds keys i and i + 8 of a block of 16 and rows 2 c, 2 c + 1, and the weights become a B
+// operand by two 8 x 8 transpositions.  Rows up to 8 in a private unit take cut8 (half the products,
+// exponentials and accumulators of cut16).
 
 // Two fp32 values as NT bf16 terms each: x = t0 + t1 (+ t2) but for 2^-16 (2^-24) of it.
 template <int NT>
@@ -633,112 +639,176 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t (&t)[NT])
     }
 }
 
-// Scores and value sums of a step of NB * 16 keys from token tok0 of the tile; keys >= ntok do not count.
-// QA: A operands of the scores (KS products of 16 entries each; entries of a key repeat every ROW).
-template <int ROW, int KS, int NB, bool MASK, typename Keep, typename Rescale>
-__device__ __forceinline__ void mma_step(uint32_t tile, int tok0, int ntok, const uint32_t (&qa)[KS][4], float c2,
-                                         float (&acc)[ROW / 8][4], float (&ms)[2], float (&l)[2], int lane, Keep keep,
-                                         Rescale rescale)
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
-    constexpr int RB = ROW * 2;  // bytes of a row
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// 0xffff in the halves whose key (key, key + 1) is below ntok.
+__device__ __forceinline__ uint32_t key_mask(int key, int ntok)
+{
+    return (key < ntok ? 0xffffu : 0u) | (key + 1 < ntok ? 0xffff0000u : 0u);
+}
+
+// Shared-memory address of a lane's row in an ldmatrix: block i (16 keys) of the step at `base`, 16-entry
+// piece e.  `lane0` is the lane's swizzled place in block 0, piece 0; steps start on 1024-byte boundaries,
+// so the swizzle of later blocks and pieces differs by constants (see swz).
+template <int ROW>
+__device__ __forceinline__ uint32_t frag(uint32_t base, uint32_t lane0, int i, int e)
+{
+    const uint32_t flip = ROW == 8 ? (uint32_t)(i & 3) << 5 : ROW == 16 ? (uint32_t)(i & 1) << 6 : (uint32_t)e << 5;
+    return base + (uint32_t)(i * 16 * ROW * 2) + (lane0 ^ flip);
+}
+
+struct Soft {
+    float ms[2], l[2][2];  // running maximum of the lane's two rows, and its share of their sums
+    __device__ void clear()
+    {
+        ms[0] = ms[1] = -INFINITY;
+        l[0][0] = l[0][1] = l[1][0] = l[1][1] = 0.f;
+    }
+};
+
+// Turns the scores of a step into weights relative to the running maximum of their row.  BYKEY: the layout of
+// cut8, s[i] = (key, row 0), (key, row 1), (key + 8, row 0), (key + 8, row 1); else that of cut16, rows 0 0 1 1.
+template <int TILES, bool BYKEY, typename Rescale>
+__device__ __forceinline__ void soft_step(float (&s)[TILES][4], float c2, Soft &f, const Rescale &rescale)
+{
+    constexpr int P0 = 0, P1 = BYKEY ? 2 : 1, Q0 = BYKEY ? 1 : 2, Q1 = 3;
+    float m0 = s[0][P0], m1 = s[0][Q0];
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+        m0 = max3(m0, s[i][P0], s[i][P1]);
+        m1 = max3(m1, s[i][Q0], s[i][Q1]);
+    }
+    m0 *= c2;
+    m1 *= c2;
+    if (__any_sync(0xffffffffu, m0 > f.ms[0] || m1 > f.ms[1])) {
+#pragma unroll
+        for (int o = BYKEY ? 4 : 1; o < (BYKEY ? 32 : 4); o <<= 1) {
+            m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
+            m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, o));
+        }
+        m0 = fmaxf(f.ms[0], m0);
+        m1 = fmaxf(f.ms[1], m1);
+        const float r0 = m0 == -INFINITY ? 1.f : ex2_approx(f.ms[0] - m0);
+        const float r1 = m1 == -INFINITY ? 1.f : ex2_approx(f.ms[1] - m1);
+        f.l[0][0] *= r0;
+        f.l[0][1] *= r0;
+        f.l[1][0] *= r1;
+        f.l[1][1] *= r1;
+        rescale(r0, r1);
+        f.ms[0] = m0;
+        f.ms[1] = m1;
+    }
+    const float b0 = f.ms[0] == -INFINITY ? 0.f : -f.ms[0], b1 = f.ms[1] == -INFINITY ? 0.f : -f.ms[1];
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+        float x0, x1, y0, y1;
+        ffma2(x0, x1, s[i][P0], s[i][P1], c2, c2, b0, b0);
+        ffma2(y0, y1, s[i][Q0], s[i][Q1], c2, c2, b1, b1);
+        s[i][P0] = ex2_approx(x0);
+        s[i][P1] = ex2_approx(x1);
+        s[i][Q0] = ex2_approx(y0);
+        s[i][Q1] = ex2_approx(y1);
+        add2(f.l[0][0], f.l[0][1], f.l[0][0], f.l[0][1], s[i][P0], s[i][P1]);
+        add2(f.l[1][0], f.l[1][1], f.l[1][0], f.l[1][1], s[i][Q0], s[i][Q1]);
+    }
+}
+
+// Lane's place of an ldmatrix.x4 whose matrices are ordered keys first (0-7 and 8-15, then the next 8
+// entries) or entries first.  ROW 8: a row is one 16-byte chunk, so the matrices are four times 8 keys.
+template <int ROW, bool KEYS_FIRST>
+__device__ __forceinline__ uint32_t lane_place(int lane)
+{
+    const int mat = lane >> 3, r = lane & 7;
+    if (ROW == 8)
+        return (uint32_t)swz((8 * mat + r) * 16);
+    const int key = 8 * (KEYS_FIRST ? mat & 1 : mat >> 1) + r, half = KEYS_FIRST ? mat >> 1 : mat & 1;
+    return (uint32_t)swz(key * ROW * 2 + 16 * half);
+}
+
+// Scores and value sums of NB blocks of 16 keys, rows on the M side.  Keys from ntok on (counted from the
+// step) do not count.  qa: KS products of 16 entries each; a key's entries repeat every ROW.
+template <int ROW, int KS, int NB, bool MASK, typename Keep, typename Rescale>
+__device__ __forceinline__ void step16(uint32_t base, int ntok, const uint32_t (&qa)[KS][4], float c2,
+                                       float (&acc)[ROW / 8][4], Soft &f, int lane, const Keep &keep, const Rescale &rescale)
+{
+    const uint32_t lk = lane_place<ROW, false>(lane), lv = lane_place<ROW, true>(lane);
+    const int c0 = lane & 3;
     float s[2 * NB][4];
 #pragma unroll
     for (int i = 0; i < 2 * NB; ++i)
         s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
-    const int mat = lane >> 3, mrow = lane & 7;
-    if constexpr (ROW == 8) {  // a key is one 16-byte chunk: both halves of the product's 16 entries
 #pragma unroll
-        for (int i = 0; i < NB; i += 2) {
-            uint32_t k[4];
-            ldsm_x4(tile + swz((tok0 + 16 * i + 8 * mat + mrow) * RB), k);
+    for (int i = 0; i < NB; ++i) {
+        if constexpr (ROW == 8) {  // both halves of the product's 16 entries are the key's 8
+            if (i % 2 == 0) {
+                uint32_t k[4];
+                ldsm_x4(frag<ROW>(base, lk, i, 0), k);
 #pragma unroll
-            for (int x = 0; x < KS; ++x)
+                for (int x = 0; x < KS; ++x)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    mma_bf16_acc(s[2 * i + j], qa[x], k[j], k[j]);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < NB; ++i)
+                    for (int j = 0; j < 4; ++j)
+                        mma_bf16_acc(s[2 * i + j], qa[x], k[j], k[j]);
+            }
+        } else {
 #pragma unroll
             for (int e = 0; e < ROW / 16; ++e) {
                 uint32_t k[4];
-                ldsm_x4(tile + swz((tok0 + 16 * i + 8 * (mat >> 1) + mrow) * RB + 32 * e + 16 * (mat & 1)), k);
+                ldsm_x4(frag<ROW>(base, lk, i, e), k);
 #pragma unroll
                 for (int x = e; x < KS; x += ROW / 16) {
                     mma_bf16_acc(s[2 * i], qa[x], k[0], k[1]);
                     mma_bf16_acc(s[2 * i + 1], qa[x], k[2], k[3]);
                 }
             }
+        }
     }
     if constexpr (MASK) {
 #pragma unroll
         for (int i = 0; i < 2 * NB; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (tok0 + 8 * i + 2 * (lane & 3) + (e & 1) >= ntok)
+                if (8 * i + 2 * c0 + (e & 1) >= ntok)
                     s[i][e] = -INFINITY;
     }
-    keep(tok0, s);
-    float m0 = s[0][0], m1 = s[0][2];
-#pragma unroll
-    for (int i = 0; i < 2 * NB; ++i) {
-        m0 = max3(m0, s[i][0], s[i][1]);
-        m1 = max3(m1, s[i][2], s[i][3]);
-    }
-    m0 *= c2;
-    m1 *= c2;
-    if (__any_sync(0xffffffffu, m0 > ms[0] || m1 > ms[1])) {
-#pragma unroll
-        for (int o = 1; o < 4; o <<= 1) {
-            m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, o));
-            m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, o));
-        }
-        m0 = fmaxf(ms[0], m0);
-        m1 = fmaxf(ms[1], m1);
-        rescale(m0 == -INFINITY ? 1.f : ex2_approx(ms[0] - m0), m1 == -INFINITY ? 1.f : ex2_approx(ms[1] - m1));
-        ms[0] = m0;
-        ms[1] = m1;
-    }
-    const float b0 = ms[0] == -INFINITY ? 0.f : ms[0], b1 = ms[1] == -INFINITY ? 0.f : ms[1];
-#pragma unroll
-    for (int i = 0; i < 2 * NB; ++i) {
-        float x0, x1, x2, x3;
-        ffma2(x0, x1, s[i][0], s[i][1], c2, c2, -b0, -b0);
-        ffma2(x2, x3, s[i][2], s[i][3], c2, c2, -b1, -b1);
-        s[i][0] = ex2_approx(x0);
-        s[i][1] = ex2_approx(x1);
-        s[i][2] = ex2_approx(x2);
-        s[i][3] = ex2_approx(x3);
-        l[0] += s[i][0] + s[i][1];
-        l[1] += s[i][2] + s[i][3];
-    }
-    // bytes behind the last key must not reach a sum: 0 * NaN is NaN
-    auto key_mask = [&](int key) {
-        return (key < ntok ? 0xffffu : 0u) | (key + 1 < ntok ? 0xffff0000u : 0u);
-    };
+    keep(s, !MASK);
+    soft_step<2 * NB, false>(s, c2, f, rescale);
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-        // the weights as bf16 operands: 2^-9 of each at most, beside an output that is rounded as much
+        // the weights as bf16 operands: 2^-8 of each at most, beside an output that is rounded as much
         const uint32_t p[4] = {cvt_bf16x2(s[2 * i][0], s[2 * i][1]), cvt_bf16x2(s[2 * i][2], s[2 * i][3]),
                                cvt_bf16x2(s[2 * i + 1][0], s[2 * i + 1][1]),
                                cvt_bf16x2(s[2 * i + 1][2], s[2 * i + 1][3])};
-        uint32_t mk0 = ~0u, mk1 = ~0u;
+        uint32_t mk0 = ~0u, mk1 = ~0u;  // bytes behind the last key must not reach a sum: 0 * NaN is NaN
         if constexpr (MASK) {
-            mk0 = key_mask(tok0 + 16 * i + 2 * (lane & 3));
-            mk1 = key_mask(tok0 + 16 * i + 8 + 2 * (lane & 3));
+            mk0 = key_mask(16 * i + 2 * c0, ntok);
+            mk1 = key_mask(16 * i + 8 + 2 * c0, ntok);
         }
         if constexpr (ROW == 8) {
-            uint32_t v[2];
-            asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];"
-                         : "=r"(v[0]), "=r"(v[1])
-                         : "r"(tile + kHalf + swz((tok0 + 16 * i + 8 * (mat & 1) + mrow) * RB)));
-            mma_bf16_acc(acc[0], p, v[0] & mk0, v[1] & mk1);
+            if (i % 2 == 0) {
+                uint32_t v[4];
+                ldsm_x4_t(frag<ROW>(base + kHalf, lv, i, 0), v);
+                const uint32_t p2[4] = {cvt_bf16x2(s[2 * i + 2][0], s[2 * i + 2][1]),
+                                        cvt_bf16x2(s[2 * i + 2][2], s[2 * i + 2][3]),
+                                        cvt_bf16x2(s[2 * i + 3][0], s[2 * i + 3][1]),
+                                        cvt_bf16x2(s[2 * i + 3][2], s[2 * i + 3][3])};
+                uint32_t mk2 = ~0u, mk3 = ~0u;
+                if constexpr (MASK) {
+                    mk2 = key_mask(16 * i + 16 + 2 * c0, ntok);
+                    mk3 = key_mask(16 * i + 24 + 2 * c0, ntok);
+                }
+                mma_bf16_acc(acc[0], p, v[0] & mk0, v[1] & mk1);
+                mma_bf16_acc(acc[0], p2, v[2] & mk2, v[3] & mk3);
+            }
         } else {
 #pragma unroll
             for (int e = 0; e < ROW / 16; ++e) {
                 uint32_t v[4];
-                ldsm_x4_t(tile + kHalf + swz((tok0 + 16 * i + 8 * (mat & 1) + mrow) * RB + 32 * e + 16 * (mat >> 1)), v);
+                ldsm_x4_t(frag<ROW>(base + kHalf, lv, i, e), v);
                 mma_bf16_acc(acc[2 * e], p, v[0] & mk0, v[1] & mk1);
                 mma_bf16_acc(acc[2 * e + 1], p, v[2] & mk0, v[3] & mk1);
             }
@@ -746,225 +816,540 @@ __device__ __forceinline__ void mma_step(uint32_t tile, int tok0, int ntok, cons
     }
 }
 
-template <int DD, bool SCORED>
-__device__ __forceinline__ void consume_mma(const Args &a, const Tables &t, const unsigned char *slots, uint64_t *full,
-                                            uint64_t *empty, volatile int *gave_up, int cta, int lo, int hi)
+// The same with up to 8 rows on the N side.  qb: B operands; acc: [16 entries][8 rows] tiles.
+template <int ROW, int KS, int NB, bool MASK, typename Keep, typename Rescale>
+__device__ __forceinline__ void step8(uint32_t base, int ntok, const uint32_t (&qb)[KS][2], float c2,
+                                      float (&acc)[(ROW + 15) / 16][4], Soft &f, int lane, const Keep &keep,
+                                      const Rescale &rescale)
 {
-    constexpr int TW = ring_tokens<bf16>(), TP = page_tokens<bf16, DD>(), kR = unit_rows<bf16>();
-    // q~ in bf16 terms: two leave 2^-16 of it, beside weights rounded to 2^-9; weights that are results take three
-    constexpr int NT = SCORED ? 3 : 2;
-    constexpr int KS = DD == 8 ? (NT + 1) / 2 : NT * DD / 16;  // products of 16 entries in a global score
-    constexpr int NBP = TP / kWarps >= 64 ? 4 : TP / kWarps / 16, NBW = TW / kWarps / 16;
+    const uint32_t lk = lane_place<ROW, true>(lane), lv = lane_place<ROW, false>(lane);
+    const int i0 = lane >> 2, c0 = lane & 3;
+    float s[NB][4];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+        s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        if constexpr (ROW == 8) {
+            if (i % 2 == 0) {
+                uint32_t k[4];
+                ldsm_x4(frag<ROW>(base, lk, i, 0), k);
+                const uint32_t ka[4] = {k[0], k[1], k[0], k[1]}, kb[4] = {k[2], k[3], k[2], k[3]};
+#pragma unroll
+                for (int x = 0; x < KS; ++x) {
+                    mma_bf16_acc(s[i], ka, qb[x][0], qb[x][1]);
+                    mma_bf16_acc(s[i + 1], kb, qb[x][0], qb[x][1]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < ROW / 16; ++e) {
+                uint32_t k[4];
+                ldsm_x4(frag<ROW>(base, lk, i, e), k);
+#pragma unroll
+                for (int x = e; x < KS; x += ROW / 16)
+                    mma_bf16_acc(s[i], k, qb[x][0], qb[x][1]);
+            }
+        }
+    }
+    if constexpr (MASK) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (16 * i + i0 + 8 * (e >> 1) >= ntok)
+                    s[i][e] = -INFINITY;
+    }
+    keep(s, !MASK);
+    soft_step<NB, true>(s, c2, f, rescale);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        // weights rounded as in step16
+        const uint32_t p0 = transpose8(cvt_bf16x2(s[i][0], s[i][1])), p1 = transpose8(cvt_bf16x2(s[i][2], s[i][3]));
+        uint32_t mk0 = ~0u, mk1 = ~0u;
+        if constexpr (MASK) {
+            mk0 = key_mask(16 * i + 2 * c0, ntok);
+            mk1 = key_mask(16 * i + 8 + 2 * c0, ntok);
+        }
+        if constexpr (ROW == 8) {
+            if (i % 2 == 0) {
+                uint32_t v[4], mk2 = ~0u, mk3 = ~0u;
+                ldsm_x4_t(frag<ROW>(base + kHalf, lv, i, 0), v);
+                if constexpr (MASK) {
+                    mk2 = key_mask(16 * i + 16 + 2 * c0, ntok);
+                    mk3 = key_mask(16 * i + 24 + 2 * c0, ntok);
+                }
+                const uint32_t va[4] = {v[0] & mk0, 0u, v[1] & mk1, 0u}, vb[4] = {v[2] & mk2, 0u, v[3] & mk3, 0u};
+                mma_bf16_acc(acc[0], va, p0, p1);
+                mma_bf16_acc(acc[0], vb, transpose8(cvt_bf16x2(s[i + 1][0], s[i + 1][1])),
+                             transpose8(cvt_bf16x2(s[i + 1][2], s[i + 1][3])));
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < ROW / 16; ++e) {
+                uint32_t v[4];
+                ldsm_x4_t(frag<ROW>(base + kHalf, lv, i, e), v);
+                const uint32_t vm[4] = {v[0] & mk0, v[1] & mk0, v[2] & mk1, v[3] & mk1};
+                mma_bf16_acc(acc[e], vm, p0, p1);
+            }
+        }
+    }
+}
+
+// What a consumer warp carries from cut to cut.
+struct Consumer {
+    const Args &a;
+    const Tables &t;
+    const unsigned char *slots;
+    uint64_t *full, *empty;
+    volatile int *gave_up;
+    int n;       // stages taken
+    bool alive;  // false once a wait gave up: nothing more is computed
+    // The next stage's slot, or nullptr.
+    __device__ __forceinline__ const unsigned char *take(int lane)
+    {
+        const int s = n % kStages;
+        if (!alive || !mbar_wait(&full[s], (unsigned)((n / kStages) & 1), gave_up)) {
+            if (alive && lane == 0)
+                report(a.status, DAR_ERR_DEVICE);
+            alive = false;
+            ++n;
+            return nullptr;
+        }
+        return slots + s * kSlot;
+    }
+    __device__ __forceinline__ void give(int lane)
+    {
+        __syncwarp();
+        if (lane == 0)
+            mbar_arrive(&empty[n % kStages]);
+        ++n;
+    }
+};
+
+// Steps of a page stage (of 16 * NBP keys) and of a ring stage, and products of a global score.  q~ in bf16
+// terms: two leave 2^-16 of it, beside weights rounded to 2^-8; weights that are results take three.
+template <int DD, bool SCORED>
+struct Shape {
+    static constexpr int TW = ring_tokens<bf16>(), TP = page_tokens<bf16, DD>();
+    static constexpr int NT = SCORED ? 3 : 2;
+    static constexpr int KS = DD == 8 ? (NT + 1) / 2 : NT * DD / 16;
+    static constexpr int NBP = TP / kWarps >= 64 ? 4 : TP / kWarps / 16, NBW = TW / kWarps / 16;
+};
+
+// The query rows r0, r1 of a cut (nullptr: none), as pairs of entries from 2 c0 on.
+template <int kR>
+__device__ __forceinline__ const uint32_t *query_row(const Args &a, const Tables &t, const Cut &c, int row, int c0)
+{
+    if (row >= c.rows)
+        return nullptr;
+    int b, h;
+    row_of<kR>(a, t, c, row, b, h);
+    return static_cast<const uint32_t *>(a.q) + ((size_t)b * a.Hq + h) * (kHeadDim / 2) + c0;
+}
+
+// RING: the cut may hold ring stages (private units).
+template <int DD, bool SCORED, bool RING>
+__device__ __forceinline__ void cut16(Consumer &w, const Cut &c)
+{
+    using S = Shape<DD, SCORED>;
+    constexpr int TW = S::TW, TP = S::TP, NT = S::NT, KS = S::KS, NBP = S::NBP, NBW = S::NBW, kR = unit_rows<bf16>();
+    constexpr int NL = RING ? kHeadDim / 8 : 1;
+    const Args &a = w.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i0 = lane >> 2, c0 = lane & 3;
-    int n = 0;
-    bool alive = true;
-    for (int p = lo, next; p < hi; p = next) {
-        Cut c;
-        if (!find_cut<bf16, DD>(a, t, p, hi, cta, c, next))
-            continue;
-        const int RW = c.RW, KW = kWarps / RW, rw = warp % RW, kw = warp / RW;
-        const int r0 = rw * 16 + i0, r1 = r0 + 8;  // this lane's rows
-        // queries (entries 16 e + 2 c, + 1 and 16 e + 8 + 2 c, + 1 of either row)
-        uint32_t qa[4][4];
-        {
-            const uint32_t *q0 = nullptr, *q1 = nullptr;
-            int b, h;
-            if (r0 < c.rows) {
-                row_of<kR>(a, t, c, r0, b, h);
-                q0 = static_cast<const uint32_t *>(a.q) + ((size_t)b * a.Hq + h) * (kHeadDim / 2) + c0;
-            }
-            if (r1 < c.rows) {
-                row_of<kR>(a, t, c, r1, b, h);
-                q1 = static_cast<const uint32_t *>(a.q) + ((size_t)b * a.Hq + h) * (kHeadDim / 2) + c0;
-            }
+    const int RW = c.RW, KW = kWarps / RW, rw = warp % RW, kw = warp / RW;
+    const int r0 = rw * 16 + i0, r1 = r0 + 8;  // this lane's rows
+    // queries: entries 16 e + 2 c, + 1 and 16 e + 8 + 2 c, + 1 of either row
+    uint32_t qa[4][4];
+    {
+        const uint32_t *q0 = query_row<kR>(a, w.t, c, r0, c0), *q1 = query_row<kR>(a, w.t, c, r1, c0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            qa[e][0] = q0 ? __ldg(q0 + 8 * e) : 0u;
+            qa[e][1] = q1 ? __ldg(q1 + 8 * e) : 0u;
+            qa[e][2] = q0 ? __ldg(q0 + 8 * e + 4) : 0u;
+            qa[e][3] = q1 ? __ldg(q1 + 8 * e + 4) : 0u;
+        }
+    }
+    // q~ = q Uk^T: Uk in three bf16 terms, so that the products are fp32 ones but for 2^-24
+    uint32_t qt[KS][4];
+    {
+        const float *u = a.Uk + ((size_t)c.g * DD + i0) * kHeadDim + 2 * c0;
+        uint32_t prev[NT][2];  // terms of the tile of 8 entries before
+#pragma unroll
+        for (int j = 0; j < DD / 8; ++j) {
+            float x[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                qa[e][0] = q0 ? __ldg(q0 + 8 * e) : 0u;
-                qa[e][1] = q1 ? __ldg(q1 + 8 * e) : 0u;
-                qa[e][2] = q0 ? __ldg(q0 + 8 * e + 4) : 0u;
-                qa[e][3] = q1 ? __ldg(q1 + 8 * e + 4) : 0u;
+                const float2 u0 = __ldg(reinterpret_cast<const float2 *>(u + j * 8 * kHeadDim + 16 * e));
+                const float2 u1 = __ldg(reinterpret_cast<const float2 *>(u + j * 8 * kHeadDim + 16 * e + 8));
+                uint32_t t0[3], t1[3];
+                split2<3>(u0.x, u0.y, t0);
+                split2<3>(u1.x, u1.y, t1);
+#pragma unroll
+                for (int y = 2; y >= 0; --y)
+                    mma_bf16_acc(x, qa[e], t0[y], t1[y]);
             }
-        }
-        // q~ = q Uk^T: Uk in three bf16 terms, so that the products are fp32 ones but for 2^-24
-        uint32_t qt[KS][4];
-        {
-            const float *u = a.Uk + ((size_t)c.g * DD + i0) * kHeadDim + 2 * c0;
-            uint32_t prev[NT][2];  // terms of the tile of 8 entries before
+            uint32_t lo8[NT], hi8[NT];  // terms of rows i and i + 8
+            split2<NT>(x[0], x[1], lo8);
+            split2<NT>(x[2], x[3], hi8);
+            if constexpr (DD == 8) {
 #pragma unroll
-            for (int j = 0; j < DD / 8; ++j) {
-                float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 u0 = __ldg(reinterpret_cast<const float2 *>(u + j * 8 * kHeadDim + 16 * e));
-                    const float2 u1 = __ldg(reinterpret_cast<const float2 *>(u + j * 8 * kHeadDim + 16 * e + 8));
-                    uint32_t t0[3], t1[3];
-                    split2<3>(u0.x, u0.y, t0);
-                    split2<3>(u1.x, u1.y, t1);
-#pragma unroll
-                    for (int y = 2; y >= 0; --y)
-                        mma_bf16_acc(x, qa[e], t0[y], t1[y]);
+                for (int y = 0; y < KS; ++y) {
+                    qt[y][0] = lo8[2 * y];
+                    qt[y][1] = hi8[2 * y];
+                    qt[y][2] = 2 * y + 1 < NT ? lo8[2 * y + 1 < NT ? 2 * y + 1 : 0] : 0u;
+                    qt[y][3] = 2 * y + 1 < NT ? hi8[2 * y + 1 < NT ? 2 * y + 1 : 0] : 0u;
                 }
-                uint32_t lo8[NT], hi8[NT];  // terms of rows i and i + 8
-                split2<NT>(x[0], x[1], lo8);
-                split2<NT>(x[2], x[3], hi8);
-                if constexpr (DD == 8) {
+            } else if (j % 2 == 0) {
 #pragma unroll
-                    for (int y = 0; y < KS; ++y) {
-                        qt[y][0] = lo8[2 * y];
-                        qt[y][1] = hi8[2 * y];
-                        qt[y][2] = 2 * y + 1 < NT ? lo8[2 * y + 1 < NT ? 2 * y + 1 : 0] : 0u;
-                        qt[y][3] = 2 * y + 1 < NT ? hi8[2 * y + 1 < NT ? 2 * y + 1 : 0] : 0u;
-                    }
-                } else if (j % 2 == 0) {
+                for (int y = 0; y < NT; ++y) {
+                    prev[y][0] = lo8[y];
+                    prev[y][1] = hi8[y];
+                }
+            } else {
 #pragma unroll
-                    for (int y = 0; y < NT; ++y) {
-                        prev[y][0] = lo8[y];
-                        prev[y][1] = hi8[y];
-                    }
-                } else {
-#pragma unroll
-                    for (int y = 0; y < NT; ++y) {  // term y of entries 16 (j / 2) ..: product y * DD / 16 + j / 2
-                        uint32_t *o = qt[y * (DD / 16) + j / 2];
-                        o[0] = prev[y][0];
-                        o[1] = prev[y][1];
-                        o[2] = lo8[y];
-                        o[3] = hi8[y];
-                    }
+                for (int y = 0; y < NT; ++y) {  // term y of entries 16 (j / 2) ..: product y * DD / 16 + j / 2
+                    uint32_t *o = qt[y * (DD / 16) + j / 2];
+                    o[0] = prev[y][0];
+                    o[1] = prev[y][1];
+                    o[2] = lo8[y];
+                    o[3] = hi8[y];
                 }
             }
         }
-        float ol[kHeadDim / 8][4], od[DD / 8][4], ms[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    }
+    float ol[NL][4], od[DD / 8][4];
+    Soft f;
+    f.clear();
 #pragma unroll
-        for (int j = 0; j < kHeadDim / 8; ++j)
-            ol[j][0] = ol[j][1] = ol[j][2] = ol[j][3] = 0.f;
+    for (int j = 0; j < NL; ++j)
+        ol[j][0] = ol[j][1] = ol[j][2] = ol[j][3] = 0.f;
 #pragma unroll
-        for (int j = 0; j < DD / 8; ++j)
-            od[j][0] = od[j][1] = od[j][2] = od[j][3] = 0.f;
-        const bool ring = c.st0 < c.nsw;  // the cut holds ring stages
-        auto rescale = [&](float f0, float f1) {
-            l[0] *= f0;
-            l[1] *= f1;
-            if (ring)
+    for (int j = 0; j < DD / 8; ++j)
+        od[j][0] = od[j][1] = od[j][2] = od[j][3] = 0.f;
+    const bool ring = RING && c.st0 < c.nsw;  // the cut holds ring stages
+    auto rescale = [&](float f0, float f1) {
+        if (ring)
 #pragma unroll
-                for (int j = 0; j < kHeadDim / 8; ++j) {
-                    ol[j][0] *= f0;
-                    ol[j][1] *= f0;
-                    ol[j][2] *= f1;
-                    ol[j][3] *= f1;
-                }
-#pragma unroll
-            for (int j = 0; j < DD / 8; ++j) {
-                od[j][0] *= f0;
-                od[j][1] *= f0;
-                od[j][2] *= f1;
-                od[j][3] *= f1;
+            for (int j = 0; j < NL; ++j) {
+                ol[j][0] *= f0;
+                ol[j][1] *= f0;
+                ol[j][2] *= f1;
+                ol[j][3] *= f1;
             }
-        };
-        float *s0 = nullptr, *s1 = nullptr;  // scores of the lane's rows
-        if constexpr (SCORED) {
-            float *x = a.scores + ((size_t)c.b * a.Hq + c.g * a.G + c.rt * kR) * a.score_stride;
-            s0 = r0 < c.rows ? x + (size_t)r0 * a.score_stride : nullptr;
-            s1 = r1 < c.rows ? x + (size_t)r1 * a.score_stride : nullptr;
+#pragma unroll
+        for (int j = 0; j < DD / 8; ++j) {
+            od[j][0] *= f0;
+            od[j][1] *= f0;
+            od[j][2] *= f1;
+            od[j][3] *= f1;
         }
-        const int L = c.tok1 + c.nwin;
-        for (int st = c.st0; st < c.st1; ++st, ++n) {
-            const int s = n % kStages;
-            if (!alive || !mbar_wait(&full[s], (unsigned)((n / kStages) & 1), gave_up)) {
-                if (alive && lane == 0)
-                    report(a.status, DAR_ERR_DEVICE);
-                alive = false;
+    };
+    float *s0 = nullptr, *s1 = nullptr;  // scores of the lane's rows
+    if constexpr (SCORED) {
+        float *x = a.scores + ((size_t)c.b * a.Hq + c.g * a.G + c.rt * kR) * a.score_stride;
+        s0 = r0 < c.rows ? x + (size_t)r0 * a.score_stride : nullptr;
+        s1 = r1 < c.rows ? x + (size_t)r1 * a.score_stride : nullptr;
+    }
+    const int L = c.tok1 + c.nwin;
+    int st = c.st0;
+    if constexpr (RING) {
+        for (; st < min(c.st1, c.nsw); ++st) {
+            const unsigned char *slot = w.take(lane);
+            if (!slot)
                 continue;
-            }
-            const uint32_t tile = smem_u32(slots + s * kSlot);
-            if (st < c.nsw) {
-                const int t0 = st * TW, ntok = min(TW, c.nwin - t0);
-                auto keep = [&](int tok, const float (&x)[2 * NBW][4]) {
+            const uint32_t tile = smem_u32(slot);
+            const int t0 = st * TW, ntok = min(TW, c.nwin - t0);
+            for (int k = kw * (TW / KW); k < min(ntok, (kw + 1) * (TW / KW)); k += 16 * NBW) {
+                auto keep = [&](const float (&x)[2 * NBW][4], bool) {
                     if constexpr (SCORED) {
 #pragma unroll
                         for (int i = 0; i < 2 * NBW; ++i)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const int k = tok + 8 * i + 2 * c0 + e;
-                                if (k >= ntok)
+                                const int kk = k + 8 * i + 2 * c0 + e;
+                                if (kk >= ntok)
                                     continue;
-                                const int pos = (L - 1) - ((L - 1 - (t0 + k)) % a.w);  // held by ring slot t0 + k
+                                const int pos = (L - 1) - ((L - 1 - (t0 + kk)) % a.w);  // held by ring slot t0 + kk
                                 if (s0)
-                                    s0[pos] = x[i][e] * a.c2;
+                                    s0[pos] = x[i][e];
                                 if (s1)
-                                    s1[pos] = x[i][2 + e] * a.c2;
+                                    s1[pos] = x[i][2 + e];
                             }
                     }
                 };
-                for (int k = kw * (TW / KW); k < min(ntok, (kw + 1) * (TW / KW)); k += 16 * NBW) {
-                    if (k + 16 * NBW <= ntok)
-                        mma_step<kHeadDim, 4, NBW, false>(tile, k, ntok, qa, a.c2, ol, ms, l, lane, keep, rescale);
-                    else
-                        mma_step<kHeadDim, 4, NBW, true>(tile, k, ntok, qa, a.c2, ol, ms, l, lane, keep, rescale);
-                }
-            } else {
-                const int t0 = c.tok0 + (st - c.nsw) * TP, ntok = min(TP, c.tok1 - t0);
-                auto keep = [&](int tok, const float (&x)[2 * NBP][4]) {
-                    if constexpr (SCORED) {
+                const uint32_t base = tile + k * kHeadDim * 2;
+                if (k + 16 * NBW <= ntok)
+                    step16<kHeadDim, 4, NBW, false>(base, ntok - k, qa, a.c2, ol, f, lane, keep, rescale);
+                else
+                    step16<kHeadDim, 4, NBW, true>(base, ntok - k, qa, a.c2, ol, f, lane, keep, rescale);
+            }
+            w.give(lane);
+        }
+    }
+    for (; st < c.st1; ++st) {
+        const unsigned char *slot = w.take(lane);
+        if (!slot)
+            continue;
+        const uint32_t tile = smem_u32(slot);
+        const int t0 = c.tok0 + (st - c.nsw) * TP, ntok = min(TP, c.tok1 - t0);
+        for (int k = kw * (TP / KW); k < min(ntok, (kw + 1) * (TP / KW)); k += 16 * NBP) {
+            auto keep = [&](const float (&x)[2 * NBP][4], bool) {
+                if constexpr (SCORED) {
 #pragma unroll
-                        for (int i = 0; i < 2 * NBP; ++i) {
-                            const int k = tok + 8 * i + 2 * c0;
-                            auto put = [&](float *row, float x0, float x1) {
-                                if (k + 1 < ntok)
-                                    *reinterpret_cast<float2 *>(row + t0 + k) = make_float2(x0 * a.c2, x1 * a.c2);
-                                else if (k < ntok)  // the next position is the ring's
-                                    row[t0 + k] = x0 * a.c2;
-                            };
-                            if (s0)
-                                put(s0, x[i][0], x[i][1]);
-                            if (s1)
-                                put(s1, x[i][2], x[i][3]);
-                        }
+                    for (int i = 0; i < 2 * NBP; ++i) {
+                        const int kk = k + 8 * i + 2 * c0;
+                        auto put = [&](float *row, float x0, float x1) {
+                            if (kk + 1 < ntok)
+                                *reinterpret_cast<float2 *>(row + t0 + kk) = make_float2(x0, x1);
+                            else if (kk < ntok)  // the next position is the ring's
+                                row[t0 + kk] = x0;
+                        };
+                        if (s0)
+                            put(s0, x[i][0], x[i][1]);
+                        if (s1)
+                            put(s1, x[i][2], x[i][3]);
                     }
-                };
-                for (int k = kw * (TP / KW); k < min(ntok, (kw + 1) * (TP / KW)); k += 16 * NBP) {
-                    if (k + 16 * NBP <= ntok)
-                        mma_step<DD, KS, NBP, false>(tile, k, ntok, qt, a.c2, od, ms, l, lane, keep, rescale);
-                    else
-                        mma_step<DD, KS, NBP, true>(tile, k, ntok, qt, a.c2, od, ms, l, lane, keep, rescale);
                 }
-            }
-            __syncwarp();
-            if (lane == 0)
-                mbar_arrive(&empty[s]);
+            };
+            const uint32_t base = tile + k * DD * 2;
+            if (k + 16 * NBP <= ntok)
+                step16<DD, KS, NBP, false>(base, ntok - k, qt, a.c2, od, f, lane, keep, rescale);
+            else
+                step16<DD, KS, NBP, true>(base, ntok - k, qt, a.c2, od, f, lane, keep, rescale);
         }
+        w.give(lane);
+    }
 #pragma unroll
-        for (int o = 1; o < 4; o <<= 1) {
-            l[0] += __shfl_xor_sync(0xffffffffu, l[0], o);
-            l[1] += __shfl_xor_sync(0xffffffffu, l[1], o);
+    for (int y = 0; y < 2; ++y) {
+        float l = f.l[y][0] + f.l[y][1];
+        l += __shfl_xor_sync(0xffffffffu, l, 1);
+        l += __shfl_xor_sync(0xffffffffu, l, 2);
+        const int row = y ? r1 : r0;
+        if (row >= c.rows)
+            continue;
+        float *rec;
+        if (RING && c.grp < 0) {
+            rec = a.rec_p + ((size_t)c.slot * (KW * a.RP) + kw * a.RP + row) * rec_p_floats<DD>();
+#pragma unroll
+            for (int j = 0; j < NL; ++j)
+                *reinterpret_cast<float2 *>(rec + 4 + 8 * j + 2 * c0) = make_float2(ol[j][2 * y], ol[j][2 * y + 1]);
+#pragma unroll
+            for (int j = 0; j < DD / 8; ++j)
+                *reinterpret_cast<float2 *>(rec + 4 + kHeadDim + 8 * j + 2 * c0) =
+                    make_float2(od[j][2 * y], od[j][2 * y + 1]);
+        } else {
+            rec = a.rec_x + ((size_t)c.slot * kR + kw * (RW * 16) + row) * rec_x_floats<DD>();
+#pragma unroll
+            for (int j = 0; j < DD / 8; ++j)
+                *reinterpret_cast<float2 *>(rec + 4 + 8 * j + 2 * c0) = make_float2(od[j][2 * y], od[j][2 * y + 1]);
         }
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int row = y ? r1 : r0;
-            if (row >= c.rows)
-                continue;
-            float *rec;
-            if (c.grp < 0) {
-                rec = a.rec_p + ((size_t)c.slot * (KW * a.RP) + kw * a.RP + row) * rec_p_floats<DD>();
-#pragma unroll
-                for (int j = 0; j < kHeadDim / 8; ++j)
-                    *reinterpret_cast<float2 *>(rec + 4 + 8 * j + 2 * c0) = make_float2(ol[j][2 * y], ol[j][2 * y + 1]);
-#pragma unroll
-                for (int j = 0; j < DD / 8; ++j)
-                    *reinterpret_cast<float2 *>(rec + 4 + kHeadDim + 8 * j + 2 * c0) =
-                        make_float2(od[j][2 * y], od[j][2 * y + 1]);
-            } else {
-                rec = a.rec_x + ((size_t)c.slot * kR + kw * (RW * 16) + row) * rec_x_floats<DD>();
-#pragma unroll
-                for (int j = 0; j < DD / 8; ++j)
-                    *reinterpret_cast<float2 *>(rec + 4 + 8 * j + 2 * c0) = make_float2(od[j][2 * y], od[j][2 * y + 1]);
-            }
-            if (c0 == 0)
-                *reinterpret_cast<float2 *>(rec) = make_float2(ms[y], l[y]);
-        }
+        if (c0 == 0)
+            *reinterpret_cast<float2 *>(rec) = make_float2(f.ms[y], l);
     }
 }
 
-template <typename T, int DD, bool SCORED>
+// A private unit's cut of up to 8 rows; the four warps share its keys.
+template <int DD, bool SCORED>
+__device__ __forceinline__ void cut8(Consumer &w, const Cut &c)
+{
+    using S = Shape<DD, SCORED>;
+    constexpr int TW = S::TW, TP = S::TP, NT = S::NT, KS = S::KS, NBP = S::NBP, NBW = S::NBW, kR = unit_rows<bf16>();
+    constexpr int ND = (DD + 15) / 16;
+    const Args &a = w.a;
+    const int lane = threadIdx.x & 31, kw = threadIdx.x >> 5, i0 = lane >> 2, c0 = lane & 3;
+    // queries as B operands: row i0, entries 16 e + 2 c, + 1 and 16 e + 8 + 2 c, + 1
+    uint32_t qb[4][2];
+    {
+        const uint32_t *q0 = query_row<kR>(a, w.t, c, i0, c0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            qb[e][0] = q0 ? __ldg(q0 + 8 * e) : 0u;
+            qb[e][1] = q0 ? __ldg(q0 + 8 * e + 4) : 0u;
+        }
+    }
+    // q~^T = Uk q^T, 16 entries at a time, as in cut16; its terms turned into B operands
+    uint32_t qt[KS][2];
+#pragma unroll
+    for (int j = 0; j < ND; ++j) {
+        const float *u = a.Uk + ((size_t)c.g * DD + 16 * j + i0) * kHeadDim + 2 * c0;
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t t[4][3];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {  // entries i0, i0 + 8 and inputs 2 c, 2 c + 8
+                float2 v = make_float2(0.f, 0.f);
+                if (DD >= 16 || y % 2 == 0)
+                    v = __ldg(reinterpret_cast<const float2 *>(u + (y & 1) * 8 * kHeadDim + 16 * e + 8 * (y >> 1)));
+                split2<3>(v.x, v.y, t[y]);
+            }
+#pragma unroll
+            for (int y = 2; y >= 0; --y) {
+                const uint32_t ua[4] = {t[0][y], t[1][y], t[2][y], t[3][y]};
+                mma_bf16_acc(x, ua, qb[e][0], qb[e][1]);
+            }
+        }
+        uint32_t lo8[NT], hi8[NT];  // terms of entries i0 and i0 + 8, rows 2 c, 2 c + 1
+        split2<NT>(x[0], x[1], lo8);
+        split2<NT>(x[2], x[3], hi8);
+        if constexpr (DD == 8) {
+#pragma unroll
+            for (int y = 0; y < KS; ++y) {
+                qt[y][0] = transpose8(lo8[2 * y]);
+                qt[y][1] = 2 * y + 1 < NT ? transpose8(lo8[2 * y + 1 < NT ? 2 * y + 1 : 0]) : 0u;
+            }
+        } else {
+#pragma unroll
+            for (int y = 0; y < NT; ++y) {
+                qt[y * ND + j][0] = transpose8(lo8[y]);
+                qt[y * ND + j][1] = transpose8(hi8[y]);
+            }
+        }
+    }
+    float ol[kHeadDim / 16][4], od[ND][4];
+    Soft f;
+    f.clear();
+#pragma unroll
+    for (int j = 0; j < kHeadDim / 16; ++j)
+        ol[j][0] = ol[j][1] = ol[j][2] = ol[j][3] = 0.f;
+#pragma unroll
+    for (int j = 0; j < ND; ++j)
+        od[j][0] = od[j][1] = od[j][2] = od[j][3] = 0.f;
+    auto rescale = [&](float f0, float f1) {
+#pragma unroll
+        for (int j = 0; j < kHeadDim / 16; ++j) {
+            ol[j][0] *= f0;
+            ol[j][1] *= f1;
+            ol[j][2] *= f0;
+            ol[j][3] *= f1;
+        }
+#pragma unroll
+        for (int j = 0; j < ND; ++j) {
+            od[j][0] *= f0;
+            od[j][1] *= f1;
+            od[j][2] *= f0;
+            od[j][3] *= f1;
+        }
+    };
+    float *s0 = nullptr, *s1 = nullptr;  // scores of the lane's rows 2 c, 2 c + 1
+    if constexpr (SCORED) {
+        float *x = a.scores + ((size_t)c.b * a.Hq + c.g * a.G) * a.score_stride;
+        s0 = 2 * c0 < c.rows ? x + (size_t)(2 * c0) * a.score_stride : nullptr;
+        s1 = 2 * c0 + 1 < c.rows ? x + (size_t)(2 * c0 + 1) * a.score_stride : nullptr;
+    }
+    const int L = c.tok1 + c.nwin;
+    int st = c.st0;
+    for (; st < min(c.st1, c.nsw); ++st) {
+        const unsigned char *slot = w.take(lane);
+        if (!slot)
+            continue;
+        const int k = kw * (TW / kWarps), t0 = st * TW, ntok = min(TW, c.nwin - t0) - k;
+        auto keep = [&](const float (&x)[NBW][4], bool) {
+            if constexpr (SCORED) {
+#pragma unroll
+                for (int i = 0; i < NBW; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int kk = 16 * i + 8 * e + i0;
+                        if (kk >= ntok)
+                            continue;
+                        const int pos = (L - 1) - ((L - 1 - (t0 + k + kk)) % a.w);  // held by that ring slot
+                        if (s0)
+                            s0[pos] = x[i][2 * e];
+                        if (s1)
+                            s1[pos] = x[i][2 * e + 1];
+                    }
+            }
+        };
+        const uint32_t base = smem_u32(slot) + k * kHeadDim * 2;
+        if (16 * NBW <= ntok)
+            step8<kHeadDim, 4, NBW, false>(base, ntok, qb, a.c2, ol, f, lane, keep, rescale);
+        else if (ntok > 0)
+            step8<kHeadDim, 4, NBW, true>(base, ntok, qb, a.c2, ol, f, lane, keep, rescale);
+        w.give(lane);
+    }
+    for (; st < c.st1; ++st) {
+        const unsigned char *slot = w.take(lane);
+        if (!slot)
+            continue;
+        const int t0 = c.tok0 + (st - c.nsw) * TP, nstage = min(TP, c.tok1 - t0);
+#pragma unroll 1
+        for (int k = kw * (TP / kWarps); k < (kw + 1) * (TP / kWarps); k += 16 * NBP) {
+            const int ntok = nstage - k;
+            auto keep = [&](const float (&x)[NBP][4], bool whole) {
+                if constexpr (SCORED) {
+#pragma unroll
+                    for (int i = 0; i < NBP; ++i)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int kk = 16 * i + 8 * e + i0;
+                            if (whole || kk < ntok) {
+                                if (s0)
+                                    s0[t0 + k + kk] = x[i][2 * e];
+                                if (s1)
+                                    s1[t0 + k + kk] = x[i][2 * e + 1];
+                            }
+                        }
+                }
+            };
+            const uint32_t base = smem_u32(slot) + k * DD * 2;
+            if (16 * NBP <= ntok)
+                step8<DD, KS, NBP, false>(base, ntok, qt, a.c2, od, f, lane, keep, rescale);
+            else if (ntok > 0)
+                step8<DD, KS, NBP, true>(base, ntok, qt, a.c2, od, f, lane, keep, rescale);
+        }
+        w.give(lane);
+    }
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+        float l = f.l[y][0] + f.l[y][1];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1)
+            l += __shfl_xor_sync(0xffffffffu, l, o);
+        const int row = 2 * c0 + y;
+        if (row >= c.rows)
+            continue;
+        float *rec = a.rec_p + ((size_t)c.slot * (kWarps * a.RP) + kw * a.RP + row) * rec_p_floats<DD>();
+#pragma unroll
+        for (int j = 0; j < kHeadDim / 16; ++j) {
+            rec[4 + 16 * j + i0] = ol[j][y];
+            rec[4 + 16 * j + 8 + i0] = ol[j][2 + y];
+        }
+#pragma unroll
+        for (int j = 0; j < ND; ++j) {
+            rec[4 + kHeadDim + 16 * j + i0] = od[j][y];
+            if (DD >= 16)
+                rec[4 + kHeadDim + 16 * j + 8 + i0] = od[j][2 + y];
+        }
+        if (i0 == 0)
+            *reinterpret_cast<float2 *>(rec) = make_float2(f.ms[y], l);
+    }
+}
+
+// SMALL: private units have at most 8 rows.
+template <int DD, bool SCORED, bool SMALL>
+__device__ __forceinline__ void consume_mma(const Args &a, const Tables &t, const unsigned char *slots, uint64_t *full,
+                                            uint64_t *empty, volatile int *gave_up, int cta, int lo, int hi)
+{
+    Consumer w{a, t, slots, full, empty, gave_up, 0, true};
+    for (int p = lo, next; p < hi; p = next) {
+        Cut c;
+        if (!find_cut<bf16, DD>(a, t, p, hi, cta, c, next))
+            continue;
+        if constexpr (!SMALL)
+            cut16<DD, SCORED, true>(w, c);
+        else if constexpr (SCORED)
+            cut8<DD, SCORED>(w, c);
+        else if (c.grp < 0)
+            cut8<DD, SCORED>(w, c);
+        else
+            cut16<DD, SCORED, false>(w, c);
+    }
+}
+
+template <typename T, int DD, bool SCORED, bool SMALL>
 __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constant__ CUtensorMap m_wk,
                                                             const __grid_constant__ CUtensorMap m_wv,
                                                             const __grid_constant__ CUtensorMap m_pk,
@@ -1091,7 +1476,7 @@ __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constan
 
     // ---- four warps consume them
     if constexpr (sizeof(T) == 2)
-        consume_mma<DD, SCORED>(a, t, slots, full, empty, gave_up, cta, lo, hi);
+        consume_mma<DD, SCORED, SMALL>(a, t, slots, full, empty, gave_up, cta, lo, hi);
     else
         consume_lanes<T, DD, SCORED>(a, t, slots, reinterpret_cast<float *>(rows_at), full, empty, gave_up, cta, lo, hi);
 }
@@ -1234,7 +1619,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a)
         for (int t = chunk * kJoinTokens + threadIdx.x; t < t1; t += kJoinThreads) {
             float p = 0.f;
             for (int j = 0; j < a.G; ++j)
-                p += exp2f(x[(size_t)j * a.score_stride + t] - stat[2 * j]) * stat[2 * j + 1];
+                p += ex2_approx(fmaf(x[(size_t)j * a.score_stride + t], a.c2, -stat[2 * j])) * stat[2 * j + 1];
             w[t] = a.decay != 0.f ? fmaf(a.decay, w[t], p) : p;
         }
     }
@@ -1271,7 +1656,7 @@ static Layout layout(int B, int Hq, int Hkv, int dd, int w, int maxp, bool score
     return y;
 }
 
-template <typename T, int DD, bool SCORED>
+template <typename T, int DD, bool SCORED, bool SMALL>
 static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t st)
 {
     const Layout y = layout<T>(s.B, s.Hq, s.Hkv, DD, s.w, s.maxp, SCORED);
@@ -1317,25 +1702,30 @@ static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t 
     if (s.maxp > 0 && (!make_tma_2d_bf16(&pk, s.pool_kd, pool_lines, 64, box) ||
                        !make_tma_2d_bf16(&pv, s.pool_vd, pool_lines, 64, box)))
         return cudaErrorInvalidValue;
-    auto kern = segments_kernel<T, DD, SCORED>;
+    auto kern = segments_kernel<T, DD, SCORED, SMALL>;
+    // CTAs per SM by registers (once per device); by shared memory below
     static PerDeviceOnce once;
-    int sms = 0;
+    int fit = 0, sms = 0, dev = 0;
     cudaError_t e = per_device_once(
         once,
-        [&](int dev) {
+        [&](int d) {
             cudaError_t e2 = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                   (int)segments_smem<T>(DAR_DECODE_MAX_BATCH, DAR_DECODE_MAX_BATCH));
-            int n = 0;
             if (e2 == cudaSuccess)
-                e2 = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-            once.value[dev] = n;
+                e2 = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&once.value[d], kern, kThreads, 0);
             return e2;
         },
-        &sms);
+        &fit);
+    if (e == cudaSuccess)
+        e = cudaGetDevice(&dev);
+    if (e == cudaSuccess)
+        e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess)
         return e;
-    const int grid = 2 * sms < kMaxCtas ? 2 * sms : kMaxCtas;
-    kern<<<grid, kThreads, segments_smem<T>(s.B, s.n_groups), st>>>(wk, wv, pk, pv, a);
+    const size_t smem = segments_smem<T>(s.B, s.n_groups);
+    const int per_sm = min(min(max(fit, 1), 3), max(1, (int)(kSmemPerSm / (smem + 1024))));
+    const int grid = min(per_sm * sms, kMaxCtas);
+    kern<<<grid, kThreads, smem, st>>>(wk, wv, pk, pv, a);
     e = cudaGetLastError();
     if (e != cudaSuccess)
         return e;
@@ -1352,14 +1742,22 @@ static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t 
     return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, SCORED>, a);
 }
 
+template <typename T, int DD, bool SCORED>
+static cudaError_t launch_rows(const SegmentArgs &s, void *ws, cudaStream_t st)
+{
+    if (sizeof(T) == 2 && s.Hq / s.Hkv <= 8)
+        return launch_t<T, DD, SCORED, sizeof(T) == 2>(s, ws, st);
+    return launch_t<T, DD, SCORED, false>(s, ws, st);
+}
+
 template <typename T, bool SCORED>
 static cudaError_t launch_dd(int dd, const SegmentArgs &s, void *ws, cudaStream_t st)
 {
     switch (dd) {
-    case 8: return launch_t<T, 8, SCORED>(s, ws, st);
-    case 16: return launch_t<T, 16, SCORED>(s, ws, st);
-    case 32: return launch_t<T, 32, SCORED>(s, ws, st);
-    case 64: return launch_t<T, 64, SCORED>(s, ws, st);
+    case 8: return launch_rows<T, 8, SCORED>(s, ws, st);
+    case 16: return launch_rows<T, 16, SCORED>(s, ws, st);
+    case 32: return launch_rows<T, 32, SCORED>(s, ws, st);
+    case 64: return launch_rows<T, 64, SCORED>(s, ws, st);
     default: return cudaErrorInvalidValue;
     }
 }
