@@ -445,6 +445,10 @@ dar_status dar_attn_decode_scored(const dar_cache *cache, int32_t Hq, const void
         return s;
     if (Hq / cache->Hkv > 1024)
         return fail(DAR_ERR_UNSUPPORTED, "%d query heads per KV head > 1024", Hq / cache->Hkv);
+    if ((double)cache->B * cache->Hkv * (((double)cache->max_pages_per_seq * DAR_PAGE_SIZE + cache->w) / 512.0 + 1.0) +
+            (double)cache->B * Hq >= 2147483647.0)
+        return fail(DAR_ERR_UNSUPPORTED, "B * Hkv=%d * %d heads of this capacity are too many blocks", cache->B,
+                    cache->Hkv);
     if (!(decay >= 0.f && decay <= 1.f))
         return fail(DAR_ERR_INVALID_ARG, "decay=%g (0 to 1)", (double)decay);
     if (empty)

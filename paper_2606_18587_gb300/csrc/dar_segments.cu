@@ -1483,144 +1483,245 @@ __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constan
 
 // ------------------------------------------------------------------ join
 
-// Where the partial results of a row are: n runs of `stride` floats from `base`.
-struct RecRun {
+// Where the partial results of a row are: result i of n at base + (i / per) * far + (i % per) * near floats.
+struct Parts {
     const float *base;
-    int n, stride;
+    int n, per;
+    size_t far, near;
+    __device__ __forceinline__ const float *at(int i) const { return base + (i / per) * far + (i % per) * near; }
 };
 
 template <typename T, int DD>
-__device__ __forceinline__ RecRun private_run(const Args &a, const PlanHead &hd, const PlanSeq &s, int b, int g, int j)
+__device__ __forceinline__ Parts private_parts(const Args &a, const PlanHead &hd, const PlanSeq &s, int b, int g, int j)
 {
     constexpr int kR = unit_rows<T>();
-    RecRun r{nullptr, 0, 0};
+    Parts r{nullptr, 0, 1, 0, 0};
     if (s.stages == 0)
         return r;
-    const int rt = j / kR, row = j % kR, KW = kWarps / row_warps<T>(a.RP);
-    const int u = g * a.RTP + rt;
+    const int rt = j / kR, row = j % kR, KW = kWarps / row_warps<T>(a.RP), u = g * a.RTP + rt;
     const long long p0 = s.start + (long long)u * s.stages * kCostPrivate;
     const int k0 = owner(p0, hd.total, hd.ctas), k1 = owner(p0 + (s.stages - 1) * kCostPrivate, hd.total, hd.ctas);
     const size_t slot = (size_t)b * a.Hkv * a.RTP + u + k0;
-    r.stride = a.RP * rec_p_floats<DD>();
-    r.base = a.rec_p + (slot * (KW * a.RP) + row) * rec_p_floats<DD>();
+    r.near = (size_t)a.RP * rec_p_floats<DD>();
+    r.far = KW * r.near;
+    r.per = KW;
     r.n = (k1 - k0 + 1) * KW;
+    r.base = a.rec_p + slot * r.far + (size_t)row * rec_p_floats<DD>();
     return r;
 }
 
 template <typename T, int DD>
-__device__ __forceinline__ int prefix_runs(const Args &a, const PlanHead &hd, const PlanSeq &s, int g, int j, int &kws,
-                                           const float *&base)
+__device__ __forceinline__ Parts prefix_parts(const Args &a, const PlanHead &hd, const PlanSeq &s, int g, int j)
 {
     constexpr int kR = unit_rows<T>();
+    Parts r{nullptr, 0, 1, 0, 0};
     if (s.xrt == 0)
-        return 0;
-    const int i = s.row0 + j, rt = i / kR, row = i % kR, rows = min(kR, s.xrows - rt * kR), RW = row_warps<T>(rows);
-    const int u = g * s.xrt + rt;
+        return r;
+    const int i = s.row0 + j, rt = i / kR, row = i % kR, rows = min(kR, s.xrows - rt * kR);
+    const int RW = row_warps<T>(rows), u = g * s.xrt + rt;
     const long long p0 = s.xstart + (long long)u * s.xstages * s.xcost;
     const int k0 = owner(p0, hd.total, hd.ctas), k1 = owner(p0 + (s.xstages - 1) * s.xcost, hd.total, hd.ctas);
-    kws = kWarps / RW;
-    base = a.rec_x + ((size_t)(s.xunit + u + k0) * kR + row) * rec_x_floats<DD>();
-    return k1 - k0 + 1;
+    r.per = kWarps / RW;
+    r.near = (size_t)(RW * rpw<T>()) * rec_x_floats<DD>();
+    r.far = (size_t)kR * rec_x_floats<DD>();
+    r.n = (k1 - k0 + 1) * r.per;
+    r.base = a.rec_x + (size_t)(s.xunit + u + k0) * r.far + (size_t)row * rec_x_floats<DD>();
+    return r;
 }
 
-constexpr int kJoinThreads = 128;
-constexpr int kJoinTokens = 2048;  // tokens whose weights a block updates
+constexpr int kJoinWarps = 4;
+constexpr int kJoinThreads = kJoinWarps * 32;
+constexpr int kJoinPer = 8;                            // tokens of a thread
+constexpr int kJoinTokens = kJoinThreads * kJoinPer;   // tokens whose weights a block updates
 
-// Block (b * Hkv + g, chunk): the rows of a (sequence, KV head); chunk 0 writes their outputs, and
-// every chunk the weights of its tokens.
-template <typename T, int DD, bool SCORED>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a)
-{
-    extern __shared__ float stat[];  // SCORED: [G][2] m and 1 / l
-    constexpr int kR = unit_rows<T>();
-    grid_dep_wait();
-    const int bg = blockIdx.x, b = bg / a.Hkv, g = bg % a.Hkv, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const PlanSeq s = a.plan[b];
-    const PlanHead hd = *a.head;
-    const int chunk = blockIdx.y;
-    if (chunk > 0 && (long long)chunk * kJoinTokens >= s.L)
-        return;
-    for (int j = warp; j < a.G; j += kJoinThreads / 32) {
-        const size_t row = (size_t)b * a.Hq + g * a.G + j;
-        T *o = static_cast<T *>(a.out) + row * kHeadDim;
-        if (s.L == 0) {
-            if (chunk == 0) {
-                o[lane] = from_f32<T>(0.f);
-                o[lane + 32] = from_f32<T>(0.f);
+// The entries lane, lane + 32 (and so on) of a run of partial results, joined on the way: NLOC and NDOWN
+// registers of the full-width and of the bottleneck sum.
+template <int NLOC, int DD>
+struct Joined {
+    static constexpr int ND = (DD + 31) / 32;
+    float m, l, x[NLOC + ND];
+    __device__ void clear()
+    {
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int i = 0; i < NLOC + ND; ++i)
+            x[i] = 0.f;
+    }
+    __device__ void fold(float mo, float lo, const float (&o)[NLOC + ND])
+    {
+        const float mn = fmaxf(m, mo), base = mn == -INFINITY ? 0.f : mn;
+        const float f = exp2f(m - base), fo = exp2f(mo - base);
+        m = mn;
+        l = l * f + lo * fo;
+#pragma unroll
+        for (int i = 0; i < NLOC + ND; ++i)
+            x[i] = x[i] * f + o[i] * fo;
+    }
+    // parts first, first + step, ..; LOC: they hold full-width sums before the others
+    template <bool LOC>
+    __device__ void add(const Parts &r, int first, int step, int lane)
+    {
+        constexpr int U = 4;  // in flight together
+        for (int i0 = first; i0 < r.n; i0 += U * step) {
+            float mo[U], lo[U], o[U][NLOC + ND];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * step;
+                mo[u] = -INFINITY;
+                lo[u] = 0.f;
+#pragma unroll
+                for (int e = 0; e < NLOC + ND; ++e)
+                    o[u][e] = 0.f;
+                if (i >= r.n)
+                    continue;
+                const float *p = r.at(i);
+                mo[u] = p[0];
+                lo[u] = p[1];
+                if (LOC)
+#pragma unroll
+                    for (int e = 0; e < NLOC; ++e)
+                        o[u][e] = p[4 + 32 * e + lane];
+                const float *d = p + 4 + (LOC ? kHeadDim : 0);
+#pragma unroll
+                for (int e = 0; e < ND; ++e)
+                    if (32 * e + lane < DD)
+                        o[u][NLOC + e] = d[32 * e + lane];
             }
-            continue;
-        }
-        const RecRun pr = private_run<T, DD>(a, hd, s, b, g, j);
-        int kws = 1;
-        const float *xb = nullptr;
-        const int xn = prefix_runs<T, DD>(a, hd, s, g, j, kws, xb);
-        const int xrow = kR / kws * rec_x_floats<DD>();  // from one key warp's row to the next one's
-        float m = -INFINITY;
-        for (int i = lane; i < pr.n; i += 32)
-            m = fmaxf(m, pr.base[(size_t)i * pr.stride]);
-        for (int i = lane; i < xn * kws; i += 32)
-            m = fmaxf(m, xb[(size_t)(i / kws) * kR * rec_x_floats<DD>() + (size_t)(i % kws) * xrow]);
 #pragma unroll
-        for (int off = 16; off; off >>= 1)
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
-        const float base = m == -INFINITY ? 0.f : m;
-        float l = 0.f;
-        for (int i = lane; i < pr.n; i += 32)
-            l += pr.base[(size_t)i * pr.stride + 1] * exp2f(pr.base[(size_t)i * pr.stride] - base);
-        for (int i = lane; i < xn * kws; i += 32) {
-            const float *r = xb + (size_t)(i / kws) * kR * rec_x_floats<DD>() + (size_t)(i % kws) * xrow;
-            l += r[1] * exp2f(r[0] - base);
+            for (int u = 0; u < U; ++u)
+                fold(mo[u], lo[u], o[u]);
+        }
+    }
+};
+
+// Blocks 0 .. B * Hq - 1 write one output row each: the warps take the row's partial results in turn, the
+// first warp joins the four and lifts the bottleneck sum.  Scored: the other blocks update the weights of
+// kJoinTokens tokens of a (sequence, KV head) each.
+template <typename T, int DD, bool SCORED>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
+{
+    constexpr int NLOC = kHeadDim / 32;
+    using J = Joined<NLOC, DD>;
+    __shared__ float part[kJoinWarps][2 + 32 * (NLOC + J::ND)];
+    extern __shared__ float stat[];  // SCORED: [G][2] m and 1 / l
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int rows = a.B * a.Hq;
+    if (!SCORED || (int)blockIdx.x < rows) {
+        const int row = blockIdx.x, b = row / a.Hq, h = row % a.Hq, g = h / a.G, j = h % a.G;
+        // the lift's columns are the caller's: nothing on the stream before writes them any more
+        float uv[DD >= 32 ? 1 : DD];
+        if constexpr (DD < 32) {
+            if (threadIdx.x < kHeadDim)
+#pragma unroll
+                for (int e = 0; e < DD; ++e)
+                    uv[e] = __ldg(a.Uv + ((size_t)g * DD + e) * kHeadDim + threadIdx.x);
+        }
+        grid_dep_wait();
+        const PlanSeq s = a.plan[b];
+        const PlanHead hd = *a.head;
+        J x;
+        x.clear();
+        x.template add<true>(private_parts<T, DD>(a, hd, s, b, g, j), warp, kJoinWarps, lane);
+        if constexpr (!SCORED)
+            x.template add<false>(prefix_parts<T, DD>(a, hd, s, g, j), warp, kJoinWarps, lane);
+        float *p = part[warp];
+        if (lane == 0) {
+            p[0] = x.m;
+            p[1] = x.l;
         }
 #pragma unroll
-        for (int off = 16; off; off >>= 1)
-            l += __shfl_xor_sync(0xffffffffu, l, off);
-        if constexpr (SCORED) {
+        for (int e = 0; e < NLOC + J::ND; ++e)
+            p[2 + 32 * e + lane] = x.x[e];
+        __syncthreads();
+        float m = -INFINITY, f[kJoinWarps], l = 0.f;
+#pragma unroll
+        for (int i = 0; i < kJoinWarps; ++i)
+            m = fmaxf(m, part[i][0]);
+        if (m == -INFINITY)
+            m = 0.f;
+#pragma unroll
+        for (int i = 0; i < kJoinWarps; ++i) {
+            f[i] = exp2f(part[i][0] - m);
+            l += part[i][1] * f[i];
+        }
+        if (threadIdx.x >= kHeadDim)
+            return;
+        float o = 0.f;
+#pragma unroll
+        for (int i = 0; i < kJoinWarps; ++i)
+            o = fmaf(f[i], part[i][2 + threadIdx.x], o);
+#pragma unroll
+        for (int e = 0; e < DD; ++e) {
+            float d = 0.f;
+#pragma unroll
+            for (int i = 0; i < kJoinWarps; ++i)
+                d = fmaf(f[i], part[i][2 + kHeadDim + e], d);
+            if constexpr (DD < 32)
+                o = fmaf(d, uv[e], o);
+            else
+                o = fmaf(d, __ldg(a.Uv + ((size_t)g * DD + e) * kHeadDim + threadIdx.x), o);
+        }
+        static_cast<T *>(a.out)[(size_t)row * kHeadDim + threadIdx.x] = from_f32<T>(s.L == 0 ? 0.f : o / l);
+        return;
+    }
+    if constexpr (SCORED) {
+        const int bg = ((int)blockIdx.x - rows) / chunks, chunk = ((int)blockIdx.x - rows) % chunks;
+        const int b = bg / a.Hkv, g = bg % a.Hkv;
+        grid_dep_wait();
+        const PlanSeq s = a.plan[b];
+        if ((long long)chunk * kJoinTokens >= s.L)
+            return;
+        const PlanHead hd = *a.head;
+        for (int j = warp; j < a.G; j += kJoinWarps) {  // the row's maximum and sum
+            const Parts r = private_parts<T, DD>(a, hd, s, b, g, j);
+            float m = -INFINITY, l = 0.f;
+            for (int i = lane; i < r.n; i += 32) {
+                const float2 v = *reinterpret_cast<const float2 *>(r.at(i));
+                const float mn = fmaxf(m, v.x), base = mn == -INFINITY ? 0.f : mn;
+                l = l * exp2f(m - base) + v.y * exp2f(v.x - base);
+                m = mn;
+            }
+            float top = m;
+#pragma unroll
+            for (int off = 16; off; off >>= 1)
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            const float base = top == -INFINITY ? 0.f : top;
+            l *= exp2f(m - base);
+#pragma unroll
+            for (int off = 16; off; off >>= 1)
+                l += __shfl_xor_sync(0xffffffffu, l, off);
             if (lane == 0) {
                 stat[2 * j] = base;
                 stat[2 * j + 1] = 1.f / l;
             }
         }
-        if (chunk > 0)
-            continue;
-        float o0 = 0.f, o1 = 0.f, d0 = 0.f, d1 = 0.f;  // entries lane, lane + 32 of both sums
-        for (int i = 0; i < pr.n; ++i) {
-            const float *r = pr.base + (size_t)i * pr.stride;
-            const float f = exp2f(r[0] - base);
-            o0 = fmaf(f, r[4 + lane], o0);
-            o1 = fmaf(f, r[36 + lane], o1);
-            if (lane < DD)
-                d0 = fmaf(f, r[4 + kHeadDim + lane], d0);
-            if (DD > 32)
-                d1 = fmaf(f, r[4 + kHeadDim + 32 + lane], d1);
-        }
-        for (int i = 0; i < xn * kws; ++i) {
-            const float *r = xb + (size_t)(i / kws) * kR * rec_x_floats<DD>() + (size_t)(i % kws) * xrow;
-            const float f = exp2f(r[0] - base);
-            if (lane < DD)
-                d0 = fmaf(f, r[4 + lane], d0);
-            if (DD > 32)
-                d1 = fmaf(f, r[4 + 32 + lane], d1);
-        }
-        const float *Uv = a.Uv + (size_t)g * DD * kHeadDim;
-#pragma unroll
-        for (int e = 0; e < DD; ++e) {
-            const float x = __shfl_sync(0xffffffffu, e < 32 ? d0 : d1, e & 31);
-            o0 = fmaf(x, __ldg(Uv + e * kHeadDim + lane), o0);
-            o1 = fmaf(x, __ldg(Uv + e * kHeadDim + lane + 32), o1);
-        }
-        o[lane] = from_f32<T>(o0 / l);
-        o[lane + 32] = from_f32<T>(o1 / l);
-    }
-    if constexpr (SCORED) {
         __syncthreads();
         float *w = a.weights + (size_t)bg * a.slots;
         const float *x = a.scores + ((size_t)b * a.Hq + (size_t)g * a.G) * a.score_stride;
-        const int t1 = (int)min((long long)s.L, (long long)(chunk + 1) * kJoinTokens);
-        for (int t = chunk * kJoinTokens + threadIdx.x; t < t1; t += kJoinThreads) {
-            float p = 0.f;
-            for (int j = 0; j < a.G; ++j)
-                p += ex2_approx(fmaf(x[(size_t)j * a.score_stride + t], a.c2, -stat[2 * j])) * stat[2 * j + 1];
-            w[t] = a.decay != 0.f ? fmaf(a.decay, w[t], p) : p;
+        const int t0 = chunk * kJoinTokens + threadIdx.x;
+        float old[kJoinPer], p[kJoinPer];
+#pragma unroll
+        for (int i = 0; i < kJoinPer; ++i) {
+            const int t = t0 + i * kJoinThreads;
+            old[i] = a.decay != 0.f && t < s.L ? w[t] : 0.f;
+            p[i] = 0.f;
+        }
+        for (int j = 0; j < a.G; ++j) {
+            const float m = stat[2 * j], il = stat[2 * j + 1];
+            float y[kJoinPer];
+#pragma unroll
+            for (int i = 0; i < kJoinPer; ++i)
+                y[i] = t0 + i * kJoinThreads < s.L ? x[(size_t)j * a.score_stride + t0 + i * kJoinThreads] : 0.f;
+#pragma unroll
+            for (int i = 0; i < kJoinPer; ++i)
+                p[i] = fmaf(ex2_approx(fmaf(y[i], a.c2, -m)), il, p[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < kJoinPer; ++i) {
+            const int t = t0 + i * kJoinThreads;
+            if (t < s.L)
+                w[t] = a.decay != 0.f ? fmaf(a.decay, old[i], p[i]) : p[i];
         }
     }
 }
@@ -1736,10 +1837,11 @@ static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t 
     cfg.stream = st;
     cfg.attrs = pdl;
     cfg.numAttrs = 1;
-    cfg.gridDim = dim3(s.B * s.Hkv, SCORED ? (unsigned)((a.slots + kJoinTokens - 1) / kJoinTokens) : 1u);
+    const int chunks = SCORED ? (int)((a.slots + kJoinTokens - 1) / kJoinTokens) : 0;
+    cfg.gridDim = dim3((unsigned)(s.B * s.Hq + s.B * s.Hkv * chunks));
     cfg.blockDim = dim3(kJoinThreads);
     cfg.dynamicSmemBytes = SCORED ? a.G * 2 * sizeof(float) : 0;
-    return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, SCORED>, a);
+    return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, SCORED>, a, chunks);
 }
 
 template <typename T, int DD, bool SCORED>
