@@ -482,10 +482,11 @@ dar_status dar_cache_evict(const dar_cache *cache, float *weights, const int32_t
         return fail(DAR_ERR_INVALID_ARG, "NULL pointer");
     if (!aligned16(weights) || !aligned16(workspace))
         return fail(DAR_ERR_INVALID_ARG, "weights and workspace must be 16-byte aligned");
-    if ((double)cache->B * cache->Hkv * 8 >= 2147483647.0 ||
-        (double)cache->max_pages_per_seq * DAR_PAGE_SIZE + cache->w >= 2147483647.0)
-        return fail(DAR_ERR_UNSUPPORTED, "B * Hkv=%lld heads or %lld positions are beyond int32",
-                    (long long)cache->B * cache->Hkv, (long long)cache->max_pages_per_seq * DAR_PAGE_SIZE + cache->w);
+    if ((double)cache->B * cache->Hkv * 16 >= 2147483647.0 ||
+        (double)cache->max_pages_per_seq * DAR_PAGE_SIZE + cache->w >= 2147483647.0 / 2)
+        return fail(DAR_ERR_UNSUPPORTED, "%lld heads or %lld positions are beyond 32-bit indices",
+                    (long long)cache->B * cache->Hkv,
+                    (long long)cache->max_pages_per_seq * DAR_PAGE_SIZE + cache->w);
     const size_t need = dar::evict_workspace_bytes(cache->B, cache->Hkv, cache->w, cache->max_pages_per_seq);
     if (workspace_bytes < need)
         return fail(DAR_ERR_CAPACITY, "workspace %zu bytes < %zu needed", workspace_bytes, need);

@@ -1410,6 +1410,8 @@ __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constan
 
     if (warp == kWarps) {
         // ---- one warp fills the slots
+        // a sequence's own bytes are read once: they leave L2 first, not the scores, records and prefixes
+        const uint64_t once = l2_evict_first_policy();
         int n = 0;
         bool alive = true;
         for (int p = lo, next; alive && p < hi; p = next) {
@@ -1430,8 +1432,8 @@ __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constan
                     if (lane == 0) {
                         mbar_expect_tx(&full[s], kSlot);
                         const int y = (ring0 + st * TW) * WL;
-                        tma_load_2d(dst, &m_wk, 0, y, &full[s]);
-                        tma_load_2d(dst + kHalf, &m_wv, 0, y, &full[s]);
+                        tma_load_2d_hint(smem_u32(dst), &m_wk, 0, y, &full[s], once);
+                        tma_load_2d_hint(smem_u32(dst + kHalf), &m_wv, 0, y, &full[s], once);
                     }
                     continue;
                 }
@@ -1459,8 +1461,13 @@ __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constan
                     }
                     const int y = (id * a.Hkv + c.g) * PL + (tok % kPage) * PL / kPage;
                     const int off = (pg - pg0) * BOX * 128;
-                    tma_load_2d(dst + off, &m_pk, 0, y, &full[s]);
-                    tma_load_2d(dst + kHalf + off, &m_pv, 0, y, &full[s]);
+                    if (c.grp < 0) {
+                        tma_load_2d_hint(smem_u32(dst + off), &m_pk, 0, y, &full[s], once);
+                        tma_load_2d_hint(smem_u32(dst + kHalf + off), &m_pv, 0, y, &full[s], once);
+                    } else {  // the group's other row tiles read them too
+                        tma_load_2d(dst + off, &m_pk, 0, y, &full[s]);
+                        tma_load_2d(dst + kHalf + off, &m_pv, 0, y, &full[s]);
+                    }
                 }
             }
         }

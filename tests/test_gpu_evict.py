@@ -58,6 +58,9 @@ CASES = [
     ("bf16", 16, 16, 20, [400 + 11 * i for i in range(16)], [100] * 16, [3] * 16, "few"),      # of 2
     ("bf16", 16, 8, 7, [300 + i for i in range(45)], [250] * 45, None, "spread"),              # of 1
     ("bf16", 1, 16, 16, [40000], [17000], [1000], "few"),
+    ("bf16", 1, 16, 16, [70000], [17001], [13], "equal"),      # slices longer than their bits in shared memory
+    ("bf16", 2, 16, 300, [2000, 2300], [999, 1000], [10, 1000], "spread"),  # rings that turn in shared memory
+    ("f32", 2, 8, 700, [2000, 2300], [999, 1000], [10, 1000], "spread"),    # and by reflections
 ]
 
 
