@@ -22,8 +22,10 @@
 //              private unit  (sequence, KV head, up to R rows): the ring, then the
 //                            pages behind the prefix.
 //            A CTA's cut of a unit leaves one partial result (m, l, acc) per row and
-//            key warp.  Units are laid end to end, so unit u's cut by CTA k has the
-//            slot u + k, and the joining kernel finds a unit's cuts by arithmetic.
+//            key warp.  Units are laid end to end with lengths by their cost, so unit u's
+//            cut by CTA k has the slot u + k, and the joining kernel finds a unit's cuts by
+//            arithmetic.  (A line for each kind, of which every CTA has a share, takes two
+//            set-ups per CTA: 4 to 11 us more in all three batches of 32 and 64 sequences.)
 //            Every CTA builds the same tables from the lengths and groups.  One warp
 //            fills a ring of shared-memory slots by TMA; four warps consume them,
 //            RW of them on different rows and 4 / RW on different keys of a stage.
@@ -53,6 +55,7 @@ constexpr int kThreads = (kWarps + 1) * 32;
 constexpr int kSmemPerSm = 228 * 1024;  // of which a CTA's share is its own and 1 KB
 constexpr int kMaxCtas = 480;            // the workspace holds partial results of this many CTAs
 constexpr int kCostPrivate = 4;          // cost of a private stage
+constexpr int kCostUnit = 2;             // cost of a unit's set-up (its place on the line is before the stages)
 
 // Rows a warp takes (a tensor-core tile; registers in fp32), and rows of a unit at most.
 template <typename T>
@@ -63,10 +66,17 @@ __host__ __device__ constexpr int unit_rows() { return kWarps * rpw<T>(); }
 // Rows of a tile of nr rows go to RW warps; the other warps split the keys.
 template <typename T>
 __host__ __device__ inline int row_warps(int nr) { return nr <= rpw<T>() ? 1 : nr <= 2 * rpw<T>() ? 2 : 4; }
-// Cost of a prefix stage for nr rows, in quarters of a private stage.
+
+// Cost of a prefix stage for nr rows, in quarters of a private stage.  (bf16, three CTAs on an SM: about 2000
+// cycles a private stage where HBM feeds it and 1400 where other CTAs are busy with a prefix, 4450 a prefix
+// stage of 64 rows.  fp32: by the rows of a warp.)
 template <typename T>
-__host__ __device__ inline int prefix_cost(int nr) { return 3 + (nr + rpw<T>() - 1) / rpw<T>(); }
-constexpr int kCostMax = 8;
+__host__ __device__ inline int prefix_cost(int nr)
+{
+    const int c = sizeof(T) == 2 ? (nr + 7) / 8 : (nr + rpw<T>() - 1) / rpw<T>() * 4;
+    return c < kCostPrivate ? kCostPrivate : c;
+}
+constexpr int kCostMax = 16;  // the largest
 
 template <typename T>
 __host__ __device__ constexpr int ring_tokens() { return kHalf / (kHeadDim * (int)sizeof(T)); }
@@ -75,7 +85,7 @@ __host__ __device__ constexpr int page_tokens() { return kHalf / (DD * (int)size
 
 // What the joining kernel has to know about the line of units.
 struct PlanHead {
-    int total, ctas;  // cost units on the line, CTAs that share it
+    int total, ctas;  // length of the line, CTAs that share it
 };
 struct PlanSeq {
     int L;             // tokens
@@ -110,6 +120,13 @@ __host__ __device__ constexpr int rec_p_floats() { return 4 + kHeadDim + DD; }
 template <int DD>
 __host__ __device__ constexpr int rec_x_floats() { return 4 + DD; }
 
+// Length of a unit of n stages on the line, and the place of its stage i.
+__host__ __device__ inline int unit_length(int n, int cost) { return n ? kCostUnit + n * cost : 0; }
+__host__ __device__ inline long long stage_place(long long start, int i, int cost)
+{
+    return start + kCostUnit + (long long)i * cost;
+}
+
 // The CTA that owns the stage at place p of the line: the last k with total * k / ctas <= p.
 __device__ __forceinline__ int owner(long long p, int total, int ctas)
 {
@@ -121,7 +138,7 @@ __device__ __forceinline__ int owner(long long p, int total, int ctas)
 struct Tables {  // in shared memory; B or ngroups entries each
     int *L, *grp, *rank, *start, *members;
     int *gP, *gcnt, *gmoff, *gxst, *gxu;
-    int *tot;  // [0] cost of the prefix units, [1] of all
+    int *tot;  // lengths of the prefix and of the private units, the largest cost of a stage
 };
 
 __host__ __device__ inline int table_ints(int B, int ngroups) { return 5 * B + 5 * ngroups + 4; }
@@ -159,25 +176,17 @@ __device__ __forceinline__ int prefix_stages(int P)
     return (P * kPage + TP - 1) / TP;
 }
 
-// Exclusive sums of a[0..n) in place by one warp; returns the total.
-__device__ __forceinline__ int warp_scan(int *a, int n, int lane)
+// The sum of v over the lanes before this one.
+__device__ __forceinline__ int warp_before(int v, int lane)
 {
-    int run = 0;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        const int v = i0 + lane < n ? a[i0 + lane] : 0;
-        int x = v;
+    int x = v;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o)
-                x += y;
-        }
-        if (i0 + lane < n)
-            a[i0 + lane] = run + x - v;
-        run += __shfl_sync(0xffffffffu, x, 31);
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o)
+            x += y;
     }
-    __syncwarp();
-    return run;
+    return x - v;
 }
 
 // The tables of the line of units, the same in every CTA.  A sequence belongs to its group if all
@@ -215,16 +224,12 @@ __device__ void build_tables(const Args &a, const Tables &t, bool first_cta)
     }
     __syncthreads();
     if (ng) {
-        for (int b = tid; b < a.B; b += kThreads) {
-            const int g = t.grp[b];
-            if (g >= 0 && (t.gP[g] == 0 || distant(t.L[b], a.w) < t.gP[g] * kPage))
-                t.grp[b] = -1;
-        }
-        __syncthreads();
         if (warp == 0) {  // members are numbered in the order of their sequences
             for (int b0 = 0; b0 < a.B; b0 += 32) {
                 const int b = b0 + lane;
-                const int g = b < a.B ? t.grp[b] : -1;
+                int g = b < a.B ? t.grp[b] : -1;
+                if (g >= 0 && (t.gP[g] == 0 || distant(t.L[b], a.w) < t.gP[g] * kPage))
+                    t.grp[b] = g = -1;
                 const unsigned same = __match_any_sync(0xffffffffu, g);
                 const int before = __popc(same & ((1u << lane) - 1u));
                 const int base = g >= 0 ? t.gcnt[g] : 0;
@@ -239,36 +244,61 @@ __device__ void build_tables(const Args &a, const Tables &t, bool first_cta)
         }
         __syncthreads();
     }
-    for (int b = tid; b < a.B; b += kThreads) {
-        int g = t.grp[b];
-        if (g >= 0 && t.gcnt[g] < 2)
-            t.grp[b] = g = -1;
-        t.start[b] = a.Hkv * a.RTP * kCostPrivate * private_stages<T, DD>(t.L[b], a.w, g >= 0 ? t.gP[g] : 0);
-    }
-    for (int i = tid; i < ng; i += kThreads) {
-        const int cnt = t.gcnt[i] < 2 ? 0 : t.gcnt[i];
-        const int rows = cnt * a.G, rt = (rows + kR - 1) / kR;
-        t.gmoff[i] = cnt;
-        t.gxu[i] = a.Hkv * rt;
-        t.gxst[i] = cnt ? a.Hkv * rt * prefix_cost<T>(min(rows, kR)) * prefix_stages<T, DD>(t.gP[i]) : 0;
-    }
-    __syncthreads();
+    // exclusive sums: one warp over the sequences' private units, one over the groups' prefix units
     if (warp == 0) {
-        const int s = warp_scan(t.start, a.B, lane);
+        int run = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 32) {
+            const int b = b0 + lane;
+            int v = 0;
+            if (b < a.B) {
+                const int g = t.grp[b], P = g >= 0 && t.gcnt[g] >= 2 ? t.gP[g] : 0;
+                v = a.Hkv * a.RTP * unit_length(private_stages<T, DD>(t.L[b], a.w, P), kCostPrivate);
+            }
+            const int x = run + warp_before(v, lane);
+            if (b < a.B)
+                t.start[b] = x;
+            run = __shfl_sync(0xffffffffu, x + v, 31);
+        }
         if (lane == 0)
-            t.tot[1] = s;
+            t.tot[1] = run;
     } else if (warp == 1) {
-        warp_scan(t.gmoff, ng, lane);
-        warp_scan(t.gxu, ng, lane);
-        const int s = warp_scan(t.gxst, ng, lane);
-        if (lane == 0)
-            t.tot[0] = s;
+        int members = 0, units = 0, cost = 0, most = kCostPrivate;
+        for (int i0 = 0; i0 < ng; i0 += 32) {
+            const int i = i0 + lane;
+            int cnt = 0, u = 0, v = 0;
+            if (i < ng && t.gcnt[i] >= 2) {
+                cnt = t.gcnt[i];
+                const int rows = cnt * a.G;
+                u = a.Hkv * ((rows + kR - 1) / kR);
+                const int c = prefix_cost<T>(min(rows, kR));
+                most = max(most, c);
+                v = u * unit_length(prefix_stages<T, DD>(t.gP[i]), c);
+            }
+            const int m0 = warp_before(cnt, lane), u0 = warp_before(u, lane), v0 = warp_before(v, lane);
+            if (i < ng) {
+                t.gmoff[i] = members + m0;
+                t.gxu[i] = units + u0;
+                t.gxst[i] = cost + v0;
+            }
+            members += __shfl_sync(0xffffffffu, m0 + cnt, 31);
+            units += __shfl_sync(0xffffffffu, u0 + u, 31);
+            cost += __shfl_sync(0xffffffffu, v0 + v, 31);
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) {
+            t.tot[0] = cost;
+            t.tot[2] = most;
+        }
     }
     __syncthreads();
     for (int b = tid; b < a.B; b += kThreads) {
         const int g = t.grp[b];
-        if (g >= 0)
-            t.members[t.gmoff[g] + t.rank[b]] = b;
+        if (g >= 0) {
+            if (t.gcnt[g] < 2)
+                t.grp[b] = -1;
+            else
+                t.members[t.gmoff[g] + t.rank[b]] = b;
+        }
         t.start[b] += t.tot[0];
     }
     __syncthreads();
@@ -308,8 +338,8 @@ __device__ bool find_cut(const Args &a, const Tables &t, int p, int hi, int cta,
         const int i = lo, rows = t.gcnt[i] * a.G, rts = (rows + kR - 1) / kR;
         cost = prefix_cost<T>(min(rows, kR));
         nst = prefix_stages<T, DD>(t.gP[i]);
-        const int u = (p - t.gxst[i]) / (nst * cost);
-        start = t.gxst[i] + u * nst * cost;
+        const int len = unit_length(nst, cost), u = (p - t.gxst[i]) / len;
+        start = t.gxst[i] + u * len;
         unit = t.gxu[i] + u;
         c.grp = i;
         c.g = u / rts;
@@ -332,8 +362,8 @@ __device__ bool find_cut(const Args &a, const Tables &t, int p, int hi, int cta,
         const int b = lo, P = t.grp[b] >= 0 ? t.gP[t.grp[b]] : 0;
         cost = kCostPrivate;
         nst = private_stages<T, DD>(t.L[b], a.w, P);
-        const int u = (p - t.start[b]) / (nst * cost);
-        start = t.start[b] + u * nst * cost;
+        const int len = unit_length(nst, cost), u = (p - t.start[b]) / len;
+        start = t.start[b] + u * len;
         unit = b * a.Hkv * a.RTP + u;
         c.grp = -1;
         c.b = b;
@@ -347,11 +377,41 @@ __device__ bool find_cut(const Args &a, const Tables &t, int p, int hi, int cta,
         c.tok1 = t.L[b] - c.nwin;
     }
     c.slot = unit + cta;
-    next = start + nst * cost;
-    c.st0 = (p - start + cost - 1) / cost;
-    c.st1 = min(nst, (hi - start + cost - 1) / cost);
+    next = start + unit_length(nst, cost);
+    const int first = start + kCostUnit;  // place of stage 0
+    c.st0 = p <= first ? 0 : (p - first + cost - 1) / cost;
+    c.st1 = hi <= first ? 0 : min(nst, (hi - first + cost - 1) / cost);
     return c.st0 < c.st1;
 }
+
+// The cuts of this CTA.
+struct Walk {
+    int p, hi;
+    // CTAs that share the line: a share holds a whole stage at least, so every CTA between a unit's first and
+    // last has one of it.
+    static __device__ __forceinline__ int ctas(const Tables &t)
+    {
+        return max(1, min((int)gridDim.x, (t.tot[0] + t.tot[1]) / t.tot[2]));
+    }
+    __device__ __forceinline__ Walk(const Tables &t)
+    {
+        const int total = t.tot[0] + t.tot[1], n = ctas(t), k = blockIdx.x;
+        p = k < n ? (int)((long long)total * k / n) : 0;
+        hi = k < n ? (int)((long long)total * (k + 1) / n) : 0;
+    }
+    template <typename T, int DD>
+    __device__ __forceinline__ bool next(const Args &a, const Tables &t, Cut &c)
+    {
+        while (p < hi) {
+            int after;
+            const bool some = find_cut<T, DD>(a, t, p, hi, blockIdx.x, c, after);
+            p = after;
+            if (some)
+                return true;
+        }
+        return false;
+    }
+};
 
 // Query row `row` of a cut: its (sequence, head).
 template <int kR>
@@ -366,6 +426,8 @@ __device__ __forceinline__ void row_of(const Args &a, const Tables &t, const Cut
         h = c.g * a.G + i % a.G;
     }
 }
+
+__device__ __forceinline__ void prefetch_l1(const void *p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
 
 // Byte of a tile whose 128-byte lines are swizzled in 16-byte chunks.
 __device__ __forceinline__ int swz(int byte)
@@ -475,7 +537,7 @@ __device__ __forceinline__ void lane_stage(const unsigned char *tile, int ntok, 
 // ------------------------------------------------------------------ segments
 
 __host__ __device__ constexpr int align1k(int x) { return (x + 1023) & ~1023; }
-// Shared memory: the slots (1024-byte aligned, as the swizzle wants), query rows, tables, barriers.
+// Shared memory: the slots (1024-byte aligned, as the swizzle wants), fp32 query rows, barriers, tables.
 constexpr int kQBytes = 2 * unit_rows<float>() * kHeadDim * 4;  // fp32
 template <typename T>
 inline size_t segments_smem(int B, int ngroups)
@@ -486,19 +548,16 @@ inline size_t segments_smem(int B, int ngroups)
 // ---- the four warps that consume the stages, fp32: CUDA cores
 template <typename T, int DD, bool SCORED>
 __device__ __forceinline__ void consume_lanes(const Args &a, const Tables &t, const unsigned char *slots, float *qs,
-                                              uint64_t *full, uint64_t *empty, volatile int *gave_up, int cta, int lo,
-                                              int hi)
+                                              uint64_t *full,
+                                              uint64_t *empty, volatile int *gave_up)
 {
     constexpr int TW = ring_tokens<T>(), TP = page_tokens<T, DD>(), kR = unit_rows<T>();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    float *qt = qs + kR * kHeadDim;  // [kR][64] query rows, then [kR][DD] absorbed rows
     int n = 0;
     bool alive = true;
-    for (int p = lo, next; p < hi; p = next) {
-        Cut c;
-        if (!find_cut<T, DD>(a, t, p, hi, cta, c, next))
-            continue;
-        // query rows of the cut, and q~ = q Uk^T
+    Walk walk(t);
+    float *qt = qs + kR * kHeadDim;  // [kR][64] query rows, then [kR][DD] absorbed rows
+    for (Cut c; walk.next<T, DD>(a, t, c);) {
         asm volatile("bar.sync 1, 128;" ::: "memory");  // the rows of the cut before are read
         for (int i = tid; i < kR * kHeadDim; i += kWarps * 32) {
             const int row = i / kHeadDim;
@@ -639,11 +698,27 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t (&t)[NT])
     }
 }
 
+__device__ __forceinline__ void ldsm_x2_t(uint32_t saddr, uint32_t (&r)[2])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(saddr));
+}
+
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
     uint32_t y;
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
+}
+
+// d = a * b where `first`, else d += a * b.
+__device__ __forceinline__ void mma_first(bool first, float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    if (first) {
+        const float z[4] = {0.f, 0.f, 0.f, 0.f};
+        mma_bf16_c(d, a, b0, b1, z);
+    } else {
+        mma_bf16_acc(d, a, b0, b1);
+    }
 }
 
 // 0xffff in the halves whose key (key, key + 1) is below ntok.
@@ -663,25 +738,29 @@ __device__ __forceinline__ uint32_t frag(uint32_t base, uint32_t lane0, int i, i
 }
 
 struct Soft {
-    float ms[2], l[2][2];  // running maximum of the lane's two rows, and its share of their sums
+    float ms[2];     // running maximum of the lane's two rows
+    float l[2][2];   // its share of their sums: of either row twice (cut16), or of both rows twice (cut8)
+    float bias[2];         // minus the maxima, 0 before the first
     __device__ void clear()
     {
         ms[0] = ms[1] = -INFINITY;
+        bias[0] = bias[1] = 0.f;
         l[0][0] = l[0][1] = l[1][0] = l[1][1] = 0.f;
     }
 };
 
 // Turns the scores of a step into weights relative to the running maximum of their row.  BYKEY: the layout of
 // cut8, s[i] = (key, row 0), (key, row 1), (key + 8, row 0), (key + 8, row 1); else that of cut16, rows 0 0 1 1.
+// rescale(f0, f1): what was summed against the old maxima.
 template <int TILES, bool BYKEY, typename Rescale>
 __device__ __forceinline__ void soft_step(float (&s)[TILES][4], float c2, Soft &f, const Rescale &rescale)
 {
-    constexpr int P0 = 0, P1 = BYKEY ? 2 : 1, Q0 = BYKEY ? 1 : 2, Q1 = 3;
-    float m0 = s[0][P0], m1 = s[0][Q0];
+    constexpr int P1 = BYKEY ? 2 : 1, Q0 = BYKEY ? 1 : 2;  // the first row's second score, the second row's first
+    float m0 = s[0][0], m1 = s[0][Q0];
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
-        m0 = max3(m0, s[i][P0], s[i][P1]);
-        m1 = max3(m1, s[i][Q0], s[i][Q1]);
+        m0 = max3(m0, s[i][0], s[i][P1]);
+        m1 = max3(m1, s[i][Q0], s[i][3]);
     }
     m0 *= c2;
     m1 *= c2;
@@ -696,25 +775,28 @@ __device__ __forceinline__ void soft_step(float (&s)[TILES][4], float c2, Soft &
         const float r0 = m0 == -INFINITY ? 1.f : ex2_approx(f.ms[0] - m0);
         const float r1 = m1 == -INFINITY ? 1.f : ex2_approx(f.ms[1] - m1);
         f.l[0][0] *= r0;
-        f.l[0][1] *= r0;
-        f.l[1][0] *= r1;
+        f.l[0][1] *= BYKEY ? r1 : r0;
+        f.l[1][0] *= BYKEY ? r0 : r1;
         f.l[1][1] *= r1;
         rescale(r0, r1);
         f.ms[0] = m0;
         f.ms[1] = m1;
+        f.bias[0] = m0 == -INFINITY ? 0.f : -m0;
+        f.bias[1] = m1 == -INFINITY ? 0.f : -m1;
     }
-    const float b0 = f.ms[0] == -INFINITY ? 0.f : -f.ms[0], b1 = f.ms[1] == -INFINITY ? 0.f : -f.ms[1];
+    // pairs of scores that lie in consecutive registers: two rows of a key, or two keys of a row
+    const float b0 = f.bias[0], b1 = f.bias[1];
 #pragma unroll
     for (int i = 0; i < TILES; ++i) {
         float x0, x1, y0, y1;
-        ffma2(x0, x1, s[i][P0], s[i][P1], c2, c2, b0, b0);
-        ffma2(y0, y1, s[i][Q0], s[i][Q1], c2, c2, b1, b1);
-        s[i][P0] = ex2_approx(x0);
-        s[i][P1] = ex2_approx(x1);
-        s[i][Q0] = ex2_approx(y0);
-        s[i][Q1] = ex2_approx(y1);
-        add2(f.l[0][0], f.l[0][1], f.l[0][0], f.l[0][1], s[i][P0], s[i][P1]);
-        add2(f.l[1][0], f.l[1][1], f.l[1][0], f.l[1][1], s[i][Q0], s[i][Q1]);
+        ffma2(x0, x1, s[i][0], s[i][1], c2, c2, b0, BYKEY ? b1 : b0);
+        ffma2(y0, y1, s[i][2], s[i][3], c2, c2, BYKEY ? b0 : b1, b1);
+        s[i][0] = ex2_approx(x0);
+        s[i][1] = ex2_approx(x1);
+        s[i][2] = ex2_approx(y0);
+        s[i][3] = ex2_approx(y1);
+        add2(f.l[0][0], f.l[0][1], f.l[0][0], f.l[0][1], s[i][0], s[i][1]);
+        add2(f.l[1][0], f.l[1][1], f.l[1][0], f.l[1][1], s[i][2], s[i][3]);
     }
 }
 
@@ -734,14 +816,12 @@ __device__ __forceinline__ uint32_t lane_place(int lane)
 // step) do not count.  qa: KS products of 16 entries each; a key's entries repeat every ROW.
 template <int ROW, int KS, int NB, bool MASK, typename Keep, typename Rescale>
 __device__ __forceinline__ void step16(uint32_t base, int ntok, const uint32_t (&qa)[KS][4], float c2,
-                                       float (&acc)[ROW / 8][4], Soft &f, int lane, const Keep &keep, const Rescale &rescale)
+                                       float (&acc)[ROW / 8][4], Soft &f, int lane, const Keep &keep,
+                                       const Rescale &rescale)
 {
     const uint32_t lk = lane_place<ROW, false>(lane), lv = lane_place<ROW, true>(lane);
     const int c0 = lane & 3;
     float s[2 * NB][4];
-#pragma unroll
-    for (int i = 0; i < 2 * NB; ++i)
-        s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
         if constexpr (ROW == 8) {  // both halves of the product's 16 entries are the key's 8
@@ -752,7 +832,7 @@ __device__ __forceinline__ void step16(uint32_t base, int ntok, const uint32_t (
                 for (int x = 0; x < KS; ++x)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        mma_bf16_acc(s[2 * i + j], qa[x], k[j], k[j]);
+                        mma_first(x == 0, s[2 * i + j], qa[x], k[j], k[j]);
             }
         } else {
 #pragma unroll
@@ -761,8 +841,8 @@ __device__ __forceinline__ void step16(uint32_t base, int ntok, const uint32_t (
                 ldsm_x4(frag<ROW>(base, lk, i, e), k);
 #pragma unroll
                 for (int x = e; x < KS; x += ROW / 16) {
-                    mma_bf16_acc(s[2 * i], qa[x], k[0], k[1]);
-                    mma_bf16_acc(s[2 * i + 1], qa[x], k[2], k[3]);
+                    mma_first(x == 0, s[2 * i], qa[x], k[0], k[1]);
+                    mma_first(x == 0, s[2 * i + 1], qa[x], k[2], k[3]);
                 }
             }
         }
@@ -826,9 +906,6 @@ __device__ __forceinline__ void step8(uint32_t base, int ntok, const uint32_t (&
     const int i0 = lane >> 2, c0 = lane & 3;
     float s[NB][4];
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
-        s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
-#pragma unroll
     for (int i = 0; i < NB; ++i) {
         if constexpr (ROW == 8) {
             if (i % 2 == 0) {
@@ -837,8 +914,8 @@ __device__ __forceinline__ void step8(uint32_t base, int ntok, const uint32_t (&
                 const uint32_t ka[4] = {k[0], k[1], k[0], k[1]}, kb[4] = {k[2], k[3], k[2], k[3]};
 #pragma unroll
                 for (int x = 0; x < KS; ++x) {
-                    mma_bf16_acc(s[i], ka, qb[x][0], qb[x][1]);
-                    mma_bf16_acc(s[i + 1], kb, qb[x][0], qb[x][1]);
+                    mma_first(x == 0, s[i], ka, qb[x][0], qb[x][1]);
+                    mma_first(x == 0, s[i + 1], kb, qb[x][0], qb[x][1]);
                 }
             }
         } else {
@@ -848,7 +925,7 @@ __device__ __forceinline__ void step8(uint32_t base, int ntok, const uint32_t (&
                 ldsm_x4(frag<ROW>(base, lk, i, e), k);
 #pragma unroll
                 for (int x = e; x < KS; x += ROW / 16)
-                    mma_bf16_acc(s[i], k, qb[x][0], qb[x][1]);
+                    mma_first(x == 0, s[i], k, qb[x][0], qb[x][1]);
             }
         }
     }
@@ -903,27 +980,29 @@ struct Consumer {
     const unsigned char *slots;
     uint64_t *full, *empty;
     volatile int *gave_up;
-    int n;       // stages taken
-    bool alive;  // false once a wait gave up: nothing more is computed
+    int taken, given;  // stages
+    bool alive;        // false once a wait gave up: nothing more is computed
     // The next stage's slot, or nullptr.
     __device__ __forceinline__ const unsigned char *take(int lane)
     {
-        const int s = n % kStages;
-        if (!alive || !mbar_wait(&full[s], (unsigned)((n / kStages) & 1), gave_up)) {
+        const int s = taken % kStages;
+        if (!alive || !mbar_wait(&full[s], (unsigned)((taken / kStages) & 1), gave_up)) {
             if (alive && lane == 0)
                 report(a.status, DAR_ERR_DEVICE);
             alive = false;
-            ++n;
+            ++taken;
+            ++given;
             return nullptr;
         }
+        ++taken;
         return slots + s * kSlot;
     }
     __device__ __forceinline__ void give(int lane)
     {
         __syncwarp();
         if (lane == 0)
-            mbar_arrive(&empty[n % kStages]);
-        ++n;
+            mbar_arrive(&empty[given % kStages]);
+        ++given;
     }
 };
 
@@ -937,88 +1016,97 @@ struct Shape {
     static constexpr int NBP = TP / kWarps >= 64 ? 4 : TP / kWarps / 16, NBW = TW / kWarps / 16;
 };
 
-// The query rows r0, r1 of a cut (nullptr: none), as pairs of entries from 2 c0 on.
+// A row of a cut, as an index into [B][Hq] (-1: none).
 template <int kR>
-__device__ __forceinline__ const uint32_t *query_row(const Args &a, const Tables &t, const Cut &c, int row, int c0)
+__device__ __forceinline__ long long row_index(const Args &a, const Tables &t, const Cut &c, int row)
 {
     if (row >= c.rows)
-        return nullptr;
+        return -1;
     int b, h;
     row_of<kR>(a, t, c, row, b, h);
-    return static_cast<const uint32_t *>(a.q) + ((size_t)b * a.Hq + h) * (kHeadDim / 2) + c0;
+    return (long long)b * a.Hq + h;
 }
 
-// RING: the cut may hold ring stages (private units).
-template <int DD, bool SCORED, bool RING>
+// The queries of rows r0 and r1 (indices into [B][Hq], -1: none) as A operands.
+__device__ __forceinline__ void queries16(const Args &a, long long r0, long long r1, int c0, uint32_t (&qa)[4][4])
+{
+    const uint32_t *q = static_cast<const uint32_t *>(a.q) + c0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {  // entries 8 e + 2 c, + 1 of either row
+        qa[e / 2][e % 2 * 2] = r0 >= 0 ? __ldg(q + r0 * (kHeadDim / 2) + 4 * e) : 0u;
+        qa[e / 2][e % 2 * 2 + 1] = r1 >= 0 ? __ldg(q + r1 * (kHeadDim / 2) + 4 * e) : 0u;
+    }
+}
+
+// q~ = q Uk^T of the same rows as A operands, its NT terms one after the other.  Uk is taken in three bf16
+// terms, so that the products are fp32 ones but for 2^-24.
+template <int DD, int NT, int KS>
+__device__ __forceinline__ void absorbed16(const Args &a, int g, const uint32_t (&qa)[4][4], int lane,
+                                           uint32_t (&qt)[KS][4])
+{
+    const float *u = a.Uk + ((size_t)g * DD + (lane >> 2)) * kHeadDim + 2 * (lane & 3);
+    uint32_t prev[NT][2];  // terms of the tile of 8 entries before
+#pragma unroll
+    for (int j = 0; j < DD / 8; ++j) {
+        float x[3][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 u0 = __ldg(reinterpret_cast<const float2 *>(u + j * 8 * kHeadDim + 16 * e));
+            const float2 u1 = __ldg(reinterpret_cast<const float2 *>(u + j * 8 * kHeadDim + 16 * e + 8));
+            uint32_t t0[3], t1[3];
+            split2<3>(u0.x, u0.y, t0);
+            split2<3>(u1.x, u1.y, t1);
+#pragma unroll
+            for (int y = 0; y < 3; ++y)
+                mma_first(e == 0, x[y], qa[e], t0[y], t1[y]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            x[0][i] += x[1][i] + x[2][i];
+        uint32_t lo8[NT], hi8[NT];  // terms of rows i and i + 8
+        split2<NT>(x[0][0], x[0][1], lo8);
+        split2<NT>(x[0][2], x[0][3], hi8);
+        if constexpr (DD == 8) {  // two terms are the two halves of a product's 16 entries
+#pragma unroll
+            for (int y = 0; y < KS; ++y) {
+                qt[y][0] = lo8[2 * y];
+                qt[y][1] = hi8[2 * y];
+                qt[y][2] = 2 * y + 1 < NT ? lo8[2 * y + 1 < NT ? 2 * y + 1 : 0] : 0u;
+                qt[y][3] = 2 * y + 1 < NT ? hi8[2 * y + 1 < NT ? 2 * y + 1 : 0] : 0u;
+            }
+        } else if (j % 2 == 0) {
+#pragma unroll
+            for (int y = 0; y < NT; ++y) {
+                prev[y][0] = lo8[y];
+                prev[y][1] = hi8[y];
+            }
+        } else {
+#pragma unroll
+            for (int y = 0; y < NT; ++y) {  // term y of entries 16 (j / 2) ..: product y * DD / 16 + j / 2
+                uint32_t *o = qt[y * (DD / 16) + j / 2];
+                o[0] = prev[y][0];
+                o[1] = prev[y][1];
+                o[2] = lo8[y];
+                o[3] = hi8[y];
+            }
+        }
+    }
+}
+
+// A cut of a private unit.
+template <int DD, bool SCORED>
 __device__ __forceinline__ void cut16(Consumer &w, const Cut &c)
 {
     using S = Shape<DD, SCORED>;
     constexpr int TW = S::TW, TP = S::TP, NT = S::NT, KS = S::KS, NBP = S::NBP, NBW = S::NBW, kR = unit_rows<bf16>();
-    constexpr int NL = RING ? kHeadDim / 8 : 1;
+    constexpr int NL = kHeadDim / 8;
     const Args &a = w.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i0 = lane >> 2, c0 = lane & 3;
     const int RW = c.RW, KW = kWarps / RW, rw = warp % RW, kw = warp / RW;
     const int r0 = rw * 16 + i0, r1 = r0 + 8;  // this lane's rows
-    // queries: entries 16 e + 2 c, + 1 and 16 e + 8 + 2 c, + 1 of either row
-    uint32_t qa[4][4];
-    {
-        const uint32_t *q0 = query_row<kR>(a, w.t, c, r0, c0), *q1 = query_row<kR>(a, w.t, c, r1, c0);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            qa[e][0] = q0 ? __ldg(q0 + 8 * e) : 0u;
-            qa[e][1] = q1 ? __ldg(q1 + 8 * e) : 0u;
-            qa[e][2] = q0 ? __ldg(q0 + 8 * e + 4) : 0u;
-            qa[e][3] = q1 ? __ldg(q1 + 8 * e + 4) : 0u;
-        }
-    }
-    // q~ = q Uk^T: Uk in three bf16 terms, so that the products are fp32 ones but for 2^-24
-    uint32_t qt[KS][4];
-    {
-        const float *u = a.Uk + ((size_t)c.g * DD + i0) * kHeadDim + 2 * c0;
-        uint32_t prev[NT][2];  // terms of the tile of 8 entries before
-#pragma unroll
-        for (int j = 0; j < DD / 8; ++j) {
-            float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 u0 = __ldg(reinterpret_cast<const float2 *>(u + j * 8 * kHeadDim + 16 * e));
-                const float2 u1 = __ldg(reinterpret_cast<const float2 *>(u + j * 8 * kHeadDim + 16 * e + 8));
-                uint32_t t0[3], t1[3];
-                split2<3>(u0.x, u0.y, t0);
-                split2<3>(u1.x, u1.y, t1);
-#pragma unroll
-                for (int y = 2; y >= 0; --y)
-                    mma_bf16_acc(x, qa[e], t0[y], t1[y]);
-            }
-            uint32_t lo8[NT], hi8[NT];  // terms of rows i and i + 8
-            split2<NT>(x[0], x[1], lo8);
-            split2<NT>(x[2], x[3], hi8);
-            if constexpr (DD == 8) {
-#pragma unroll
-                for (int y = 0; y < KS; ++y) {
-                    qt[y][0] = lo8[2 * y];
-                    qt[y][1] = hi8[2 * y];
-                    qt[y][2] = 2 * y + 1 < NT ? lo8[2 * y + 1 < NT ? 2 * y + 1 : 0] : 0u;
-                    qt[y][3] = 2 * y + 1 < NT ? hi8[2 * y + 1 < NT ? 2 * y + 1 : 0] : 0u;
-                }
-            } else if (j % 2 == 0) {
-#pragma unroll
-                for (int y = 0; y < NT; ++y) {
-                    prev[y][0] = lo8[y];
-                    prev[y][1] = hi8[y];
-                }
-            } else {
-#pragma unroll
-                for (int y = 0; y < NT; ++y) {  // term y of entries 16 (j / 2) ..: product y * DD / 16 + j / 2
-                    uint32_t *o = qt[y * (DD / 16) + j / 2];
-                    o[0] = prev[y][0];
-                    o[1] = prev[y][1];
-                    o[2] = lo8[y];
-                    o[3] = hi8[y];
-                }
-            }
-        }
-    }
+    uint32_t qa[4][4], qt[KS][4];
+    queries16(a, row_index<kR>(a, w.t, c, r0), row_index<kR>(a, w.t, c, r1), c0, qa);
+    absorbed16<DD, NT>(a, c.g, qa, lane, qt);
     float ol[NL][4], od[DD / 8][4];
     Soft f;
     f.clear();
@@ -1028,7 +1116,7 @@ __device__ __forceinline__ void cut16(Consumer &w, const Cut &c)
 #pragma unroll
     for (int j = 0; j < DD / 8; ++j)
         od[j][0] = od[j][1] = od[j][2] = od[j][3] = 0.f;
-    const bool ring = RING && c.st0 < c.nsw;  // the cut holds ring stages
+    const bool ring = c.st0 < c.nsw;  // the cut holds ring stages
     auto rescale = [&](float f0, float f1) {
         if (ring)
 #pragma unroll
@@ -1054,39 +1142,37 @@ __device__ __forceinline__ void cut16(Consumer &w, const Cut &c)
     }
     const int L = c.tok1 + c.nwin;
     int st = c.st0;
-    if constexpr (RING) {
-        for (; st < min(c.st1, c.nsw); ++st) {
-            const unsigned char *slot = w.take(lane);
-            if (!slot)
-                continue;
-            const uint32_t tile = smem_u32(slot);
-            const int t0 = st * TW, ntok = min(TW, c.nwin - t0);
-            for (int k = kw * (TW / KW); k < min(ntok, (kw + 1) * (TW / KW)); k += 16 * NBW) {
-                auto keep = [&](const float (&x)[2 * NBW][4], bool) {
-                    if constexpr (SCORED) {
+    for (; st < min(c.st1, c.nsw); ++st) {
+        const unsigned char *slot = w.take(lane);
+        if (!slot)
+            continue;
+        const uint32_t tile = smem_u32(slot);
+        const int t0 = st * TW, ntok = min(TW, c.nwin - t0);
+        for (int k = kw * (TW / KW); k < min(ntok, (kw + 1) * (TW / KW)); k += 16 * NBW) {
+            auto keep = [&](const float (&x)[2 * NBW][4], bool) {
+                if constexpr (SCORED) {
 #pragma unroll
-                        for (int i = 0; i < 2 * NBW; ++i)
+                    for (int i = 0; i < 2 * NBW; ++i)
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int kk = k + 8 * i + 2 * c0 + e;
-                                if (kk >= ntok)
-                                    continue;
-                                const int pos = (L - 1) - ((L - 1 - (t0 + kk)) % a.w);  // held by ring slot t0 + kk
-                                if (s0)
-                                    s0[pos] = x[i][e];
-                                if (s1)
-                                    s1[pos] = x[i][2 + e];
-                            }
-                    }
-                };
-                const uint32_t base = tile + k * kHeadDim * 2;
-                if (k + 16 * NBW <= ntok)
-                    step16<kHeadDim, 4, NBW, false>(base, ntok - k, qa, a.c2, ol, f, lane, keep, rescale);
-                else
-                    step16<kHeadDim, 4, NBW, true>(base, ntok - k, qa, a.c2, ol, f, lane, keep, rescale);
-            }
-            w.give(lane);
+                        for (int e = 0; e < 2; ++e) {
+                            const int kk = k + 8 * i + 2 * c0 + e;
+                            if (kk >= ntok)
+                                continue;
+                            const int pos = (L - 1) - ((L - 1 - (t0 + kk)) % a.w);  // held by ring slot t0 + kk
+                            if (s0)
+                                s0[pos] = x[i][e];
+                            if (s1)
+                                s1[pos] = x[i][2 + e];
+                        }
+                }
+            };
+            const uint32_t base = tile + k * kHeadDim * 2;
+            if (k + 16 * NBW <= ntok)
+                step16<kHeadDim, 4, NBW, false>(base, ntok - k, qa, a.c2, ol, f, lane, keep, rescale);
+            else
+                step16<kHeadDim, 4, NBW, true>(base, ntok - k, qa, a.c2, ol, f, lane, keep, rescale);
         }
+        w.give(lane);
     }
     for (; st < c.st1; ++st) {
         const unsigned char *slot = w.take(lane);
@@ -1129,22 +1215,74 @@ __device__ __forceinline__ void cut16(Consumer &w, const Cut &c)
         const int row = y ? r1 : r0;
         if (row >= c.rows)
             continue;
-        float *rec;
-        if (RING && c.grp < 0) {
-            rec = a.rec_p + ((size_t)c.slot * (KW * a.RP) + kw * a.RP + row) * rec_p_floats<DD>();
+        float *rec = a.rec_p + ((size_t)c.slot * (KW * a.RP) + kw * a.RP + row) * rec_p_floats<DD>();
 #pragma unroll
-            for (int j = 0; j < NL; ++j)
-                *reinterpret_cast<float2 *>(rec + 4 + 8 * j + 2 * c0) = make_float2(ol[j][2 * y], ol[j][2 * y + 1]);
+        for (int j = 0; j < NL; ++j)
+            *reinterpret_cast<float2 *>(rec + 4 + 8 * j + 2 * c0) = make_float2(ol[j][2 * y], ol[j][2 * y + 1]);
 #pragma unroll
-            for (int j = 0; j < DD / 8; ++j)
-                *reinterpret_cast<float2 *>(rec + 4 + kHeadDim + 8 * j + 2 * c0) =
-                    make_float2(od[j][2 * y], od[j][2 * y + 1]);
-        } else {
-            rec = a.rec_x + ((size_t)c.slot * kR + kw * (RW * 16) + row) * rec_x_floats<DD>();
+        for (int j = 0; j < DD / 8; ++j)
+            *reinterpret_cast<float2 *>(rec + 4 + kHeadDim + 8 * j + 2 * c0) =
+                make_float2(od[j][2 * y], od[j][2 * y + 1]);
+        if (c0 == 0)
+            *reinterpret_cast<float2 *>(rec) = make_float2(f.ms[y], l);
+    }
+}
+
+// A cut of a prefix unit.  (Two tiles of 16 rows a warp, which share what is loaded of a key: as many cycles a
+// score, and units twice as large to deal out.  The scores of the next step started before this one's are
+// exponentiated: 5850 cycles a stage instead of 4450.)
+template <int DD>
+__device__ __forceinline__ void cut_prefix(Consumer &w, const Cut &c)
+{
+    using S = Shape<DD, false>;
+    constexpr int TP = S::TP, KS = S::KS, NB = S::NBP, kR = unit_rows<bf16>();
+    const Args &a = w.a;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = lane & 3;
+    const int RW = c.RW, KW = kWarps / RW, rw = warp % RW, kw = warp / RW, r0 = rw * 16 + (lane >> 2);
+    uint32_t qt[KS][4];
+    {
+        uint32_t qa[4][4];
+        queries16(a, row_index<kR>(a, w.t, c, r0), row_index<kR>(a, w.t, c, r0 + 8), c0, qa);
+        absorbed16<DD, S::NT>(a, c.g, qa, lane, qt);
+    }
+    float od[DD / 8][4];
+    Soft f;
+    f.clear();
 #pragma unroll
-            for (int j = 0; j < DD / 8; ++j)
-                *reinterpret_cast<float2 *>(rec + 4 + 8 * j + 2 * c0) = make_float2(od[j][2 * y], od[j][2 * y + 1]);
+    for (int j = 0; j < DD / 8; ++j)
+        od[j][0] = od[j][1] = od[j][2] = od[j][3] = 0.f;
+    auto rescale = [&](float f0, float f1) {
+#pragma unroll
+        for (int j = 0; j < DD / 8; ++j) {
+            od[j][0] *= f0;
+            od[j][1] *= f0;
+            od[j][2] *= f1;
+            od[j][3] *= f1;
         }
+    };
+    for (int st = c.st0; st < c.st1; ++st) {
+        const unsigned char *slot = w.take(lane);
+        if (!slot)
+            continue;
+        const int k0 = kw * (TP / KW), k1 = min(c.tok1 - (c.tok0 + st * TP), k0 + TP / KW);
+        uint32_t base = smem_u32(slot) + k0 * DD * 2;
+        for (int k = k0; k < k1; k += 16 * NB, base += 16 * NB * DD * 2)  // whole pages, and so whole steps
+            step16<DD, KS, NB, false>(base, 16 * NB, qt, a.c2, od, f, lane, [](const float (&)[2 * NB][4], bool) {},
+                                      rescale);
+        w.give(lane);
+    }
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+        float l = f.l[y][0] + f.l[y][1];
+        l += __shfl_xor_sync(0xffffffffu, l, 1);
+        l += __shfl_xor_sync(0xffffffffu, l, 2);
+        const int row = r0 + 8 * y;
+        if (row >= c.rows)
+            continue;
+        float *rec = a.rec_x + ((size_t)c.slot * kR + kw * (RW * 16) + row) * rec_x_floats<DD>();
+#pragma unroll
+        for (int j = 0; j < DD / 8; ++j)
+            *reinterpret_cast<float2 *>(rec + 4 + 8 * j + 2 * c0) = make_float2(od[j][2 * y], od[j][2 * y + 1]);
         if (c0 == 0)
             *reinterpret_cast<float2 *>(rec) = make_float2(f.ms[y], l);
     }
@@ -1159,22 +1297,20 @@ __device__ __forceinline__ void cut8(Consumer &w, const Cut &c)
     constexpr int ND = (DD + 15) / 16;
     const Args &a = w.a;
     const int lane = threadIdx.x & 31, kw = threadIdx.x >> 5, i0 = lane >> 2, c0 = lane & 3;
-    // queries as B operands: row i0, entries 16 e + 2 c, + 1 and 16 e + 8 + 2 c, + 1
-    uint32_t qb[4][2];
+    // B operands: row i0, entries 8 e + 2 c, + 1
+    uint32_t qb[4][2], qt[KS][2];
     {
-        const uint32_t *q0 = query_row<kR>(a, w.t, c, i0, c0);
+        const long long row = row_index<kR>(a, w.t, c, i0);
+        const uint32_t *q = static_cast<const uint32_t *>(a.q) + row * (kHeadDim / 2) + c0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            qb[e][0] = q0 ? __ldg(q0 + 8 * e) : 0u;
-            qb[e][1] = q0 ? __ldg(q0 + 8 * e + 4) : 0u;
-        }
+        for (int e = 0; e < 8; ++e)
+            qb[e / 2][e % 2] = row >= 0 ? __ldg(q + 4 * e) : 0u;
     }
-    // q~^T = Uk q^T, 16 entries at a time, as in cut16; its terms turned into B operands
-    uint32_t qt[KS][2];
+    // q~^T = Uk q^T, 16 entries at a time, as in absorbed16; its terms turned into B operands
 #pragma unroll
     for (int j = 0; j < ND; ++j) {
         const float *u = a.Uk + ((size_t)c.g * DD + 16 * j + i0) * kHeadDim + 2 * c0;
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
+        float z[3][4], x[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             uint32_t t[4][3];
@@ -1186,11 +1322,14 @@ __device__ __forceinline__ void cut8(Consumer &w, const Cut &c)
                 split2<3>(v.x, v.y, t[y]);
             }
 #pragma unroll
-            for (int y = 2; y >= 0; --y) {
+            for (int y = 0; y < 3; ++y) {
                 const uint32_t ua[4] = {t[0][y], t[1][y], t[2][y], t[3][y]};
-                mma_bf16_acc(x, ua, qb[e][0], qb[e][1]);
+                mma_first(e == 0, z[y], ua, qb[e][0], qb[e][1]);
             }
         }
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+            x[y] = z[0][y] + (z[1][y] + z[2][y]);
         uint32_t lo8[NT], hi8[NT];  // terms of entries i0 and i0 + 8, rows 2 c, 2 c + 1
         split2<NT>(x[0], x[1], lo8);
         split2<NT>(x[2], x[3], hi8);
@@ -1304,7 +1443,7 @@ __device__ __forceinline__ void cut8(Consumer &w, const Cut &c)
     }
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-        float l = f.l[y][0] + f.l[y][1];
+        float l = f.l[0][y] + f.l[1][y];
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1)
             l += __shfl_xor_sync(0xffffffffu, l, o);
@@ -1331,26 +1470,23 @@ __device__ __forceinline__ void cut8(Consumer &w, const Cut &c)
 // SMALL: private units have at most 8 rows.
 template <int DD, bool SCORED, bool SMALL>
 __device__ __forceinline__ void consume_mma(const Args &a, const Tables &t, const unsigned char *slots, uint64_t *full,
-                                            uint64_t *empty, volatile int *gave_up, int cta, int lo, int hi)
+                                            uint64_t *empty, volatile int *gave_up)
 {
-    Consumer w{a, t, slots, full, empty, gave_up, 0, true};
-    for (int p = lo, next; p < hi; p = next) {
-        Cut c;
-        if (!find_cut<bf16, DD>(a, t, p, hi, cta, c, next))
-            continue;
-        if constexpr (!SMALL)
-            cut16<DD, SCORED, true>(w, c);
-        else if constexpr (SCORED)
+    Consumer w{a, t, slots, full, empty, gave_up, 0, 0, true};
+    Walk walk(t);
+    for (Cut c; walk.next<bf16, DD>(a, t, c);) {
+        if (!SCORED && c.grp >= 0) {
+            cut_prefix<DD>(w, c);
+        } else if constexpr (SMALL) {
             cut8<DD, SCORED>(w, c);
-        else if (c.grp < 0)
-            cut8<DD, SCORED>(w, c);
-        else
-            cut16<DD, SCORED, false>(w, c);
+        } else {
+            cut16<DD, SCORED>(w, c);
+        }
     }
 }
 
 template <typename T, int DD, bool SCORED, bool SMALL>
-__global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constant__ CUtensorMap m_wk,
+__global__ void __launch_bounds__(kThreads, SMALL ? 3 : 1) segments_kernel(const __grid_constant__ CUtensorMap m_wk,
                                                             const __grid_constant__ CUtensorMap m_wv,
                                                             const __grid_constant__ CUtensorMap m_pk,
                                                             const __grid_constant__ CUtensorMap m_pv, Args a)
@@ -1378,12 +1514,9 @@ __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constan
         mbar_init_fence();
     }
     build_tables<T, DD>(a, t, blockIdx.x == 0);  // its barriers also publish the mbarriers
-    const int total = t.tot[0] + t.tot[1];
-    // a CTA's share holds a whole stage at least, so every CTA between a unit's first and last has one of it
-    const int ctas = max(1, min((int)gridDim.x, total / (t.tot[0] ? kCostMax : kCostPrivate)));
     if (blockIdx.x == 0) {
         if (tid == 0)
-            *a.head = PlanHead{total, ctas};
+            *a.head = PlanHead{t.tot[0] + t.tot[1], Walk::ctas(t)};
         for (int b = tid; b < a.B; b += kThreads) {
             PlanSeq s;
             const int g = t.grp[b];
@@ -1404,20 +1537,22 @@ __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constan
             a.plan[b] = s;
         }
     }
-    const int cta = blockIdx.x;
-    const int lo = cta < ctas ? (int)((long long)total * cta / ctas) : total;
-    const int hi = cta < ctas ? (int)((long long)total * (cta + 1) / ctas) : total;
-
     if (warp == kWarps) {
         // ---- one warp fills the slots
         // a sequence's own bytes are read once: they leave L2 first, not the scores, records and prefixes
         const uint64_t once = l2_evict_first_policy();
         int n = 0;
         bool alive = true;
-        for (int p = lo, next; alive && p < hi; p = next) {
-            Cut c;
-            if (!find_cut<T, DD>(a, t, p, hi, cta, c, next))
-                continue;
+        Walk walk(t);
+        for (Cut c; alive && walk.next<T, DD>(a, t, c);) {
+            // what the consumers will want first, while they are at the cut before
+            for (int i = lane; i < DD * 2; i += 32)
+                prefetch_l1(a.Uk + ((size_t)c.g * DD * 2 + i) * (kHeadDim / 2));
+            for (int i = lane; i < c.rows; i += 32) {
+                int b, h;
+                row_of<unit_rows<T>()>(a, t, c, i, b, h);
+                prefetch_l1(static_cast<const T *>(a.q) + ((size_t)b * a.Hq + h) * kHeadDim);
+            }
             const int32_t *table = a.block_table + (size_t)c.b * a.maxp;
             const int ring0 = (c.b * a.Hkv + c.g) * a.w;
             int ids0 = -1, ids = -1;  // block-table entries ids0 .. ids0 + 31, one per lane
@@ -1483,9 +1618,9 @@ __global__ void __launch_bounds__(kThreads) segments_kernel(const __grid_constan
 
     // ---- four warps consume them
     if constexpr (sizeof(T) == 2)
-        consume_mma<DD, SCORED, SMALL>(a, t, slots, full, empty, gave_up, cta, lo, hi);
+        consume_mma<DD, SCORED, SMALL>(a, t, slots, full, empty, gave_up);
     else
-        consume_lanes<T, DD, SCORED>(a, t, slots, reinterpret_cast<float *>(rows_at), full, empty, gave_up, cta, lo, hi);
+        consume_lanes<T, DD, SCORED>(a, t, slots, reinterpret_cast<float *>(rows_at), full, empty, gave_up);
 }
 
 // ------------------------------------------------------------------ join
@@ -1506,8 +1641,9 @@ __device__ __forceinline__ Parts private_parts(const Args &a, const PlanHead &hd
     if (s.stages == 0)
         return r;
     const int rt = j / kR, row = j % kR, KW = kWarps / row_warps<T>(a.RP), u = g * a.RTP + rt;
-    const long long p0 = s.start + (long long)u * s.stages * kCostPrivate;
-    const int k0 = owner(p0, hd.total, hd.ctas), k1 = owner(p0 + (s.stages - 1) * kCostPrivate, hd.total, hd.ctas);
+    const long long p0 = s.start + (long long)u * unit_length(s.stages, kCostPrivate);
+    const int k0 = owner(stage_place(p0, 0, kCostPrivate), hd.total, hd.ctas);
+    const int k1 = owner(stage_place(p0, s.stages - 1, kCostPrivate), hd.total, hd.ctas);
     const size_t slot = (size_t)b * a.Hkv * a.RTP + u + k0;
     r.near = (size_t)a.RP * rec_p_floats<DD>();
     r.far = KW * r.near;
@@ -1526,8 +1662,9 @@ __device__ __forceinline__ Parts prefix_parts(const Args &a, const PlanHead &hd,
         return r;
     const int i = s.row0 + j, rt = i / kR, row = i % kR, rows = min(kR, s.xrows - rt * kR);
     const int RW = row_warps<T>(rows), u = g * s.xrt + rt;
-    const long long p0 = s.xstart + (long long)u * s.xstages * s.xcost;
-    const int k0 = owner(p0, hd.total, hd.ctas), k1 = owner(p0 + (s.xstages - 1) * s.xcost, hd.total, hd.ctas);
+    const long long p0 = s.xstart + (long long)u * unit_length(s.xstages, s.xcost);
+    const int k0 = owner(stage_place(p0, 0, s.xcost), hd.total, hd.ctas);
+    const int k1 = owner(stage_place(p0, s.xstages - 1, s.xcost), hd.total, hd.ctas);
     r.per = kWarps / RW;
     r.near = (size_t)(RW * rpw<T>()) * rec_x_floats<DD>();
     r.far = (size_t)kR * rec_x_floats<DD>();
@@ -1673,7 +1810,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
         return;
     }
     if constexpr (SCORED) {
-        const int bg = ((int)blockIdx.x - rows) / chunks, chunk = ((int)blockIdx.x - rows) % chunks;
+        // the last chunks first: their scores were kept last and are the likeliest to be in L2 still
+        const int heads = a.B * a.Hkv, i = (int)blockIdx.x - rows, bg = i % heads, chunk = chunks - 1 - i / heads;
         const int b = bg / a.Hkv, g = bg % a.Hkv;
         grid_dep_wait();
         const PlanSeq s = a.plan[b];
@@ -1886,7 +2024,7 @@ double segments_line_bound(dar_dtype dt, int B, int Hq, int Hkv, int dd, int w, 
     const int es = dt == DAR_F32 ? 4 : 2, G = Hq / Hkv;
     const double stages = (double)w * kHeadDim * es / seg::kHalf + (double)maxp * kPage * dd * es / seg::kHalf + 2;
     const int R = dt == DAR_F32 ? seg::unit_rows<float>() : seg::unit_rows<bf16>();
-    return (double)B * Hkv * ((G + R - 1) / R) * stages * (seg::kCostPrivate + seg::kCostMax);
+    return (double)B * Hkv * ((G + R - 1) / R) * (stages * (seg::kCostPrivate + seg::kCostMax) + 2 * seg::kCostUnit);
 }
 
 cudaError_t launch_segments(dar_dtype dt, int dd, const SegmentArgs &s, void *workspace, cudaStream_t st)

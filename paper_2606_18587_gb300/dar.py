@@ -300,11 +300,14 @@ def dar_attn_decode_noalloc(cache: DarCache, q, Uk, Uv, scale=0.0, out=None, str
 
 def _operand(t, name, dtype, shape, cache):
     """A contiguous tensor on the cache's device, of this dtype and shape (None: any)."""
+    device = cache.win_k.device
+    if isinstance(t, torch.Tensor) and t.device == device and (dtype is None or t.dtype is dtype) \
+            and (shape is None or t.shape == shape) and t.is_contiguous():
+        return
     _dev(t, name, dtype)
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.device != cache.win_k.device:
-        raise ValueError(f"{name} is on {t.device}, the cache on {cache.win_k.device}")
+    raise ValueError(f"{name} is on {t.device}, the cache on {device}")
 
 
 def _on_current_device(cache):

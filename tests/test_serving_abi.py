@@ -107,30 +107,35 @@ def owner(p, total, ctas):
     return ((p + 1) * ctas - 1) // total
 
 
+UNIT = 2  # length of a unit's set-up, before its stages
+
+
 @pytest.mark.parametrize("seed", range(60))
 def test_every_stage_has_one_cta_and_every_cut_one_slot(seed):
     """The line of units: stages are dealt to CTAs by their place, a unit's cut by CTA k has the slot unit + k, and the
     joining kernel's first and last CTA of a unit, and all between them, have a cut of it."""
     rng = random.Random(seed)
-    costs = rng.choice(((4,), (4, 5, 7, 8)))
+    costs = rng.choice(((4,), (4, 5, 7, 8, 16)))
     units = [(rng.choice((0, 1, 1, 2, 3, 17, 200)), rng.choice(costs)) for _ in range(rng.randint(1, 400))]
     if rng.random() < 0.2:
         units = [(rng.randint(1, 3000), 4)]
-    total = sum(n * c for n, c in units)
+    length = [UNIT + n * c if n else 0 for n, c in units]
+    total = sum(length)
     grid = rng.choice((1, 2, 152, 304, 456, 480))
     ctas = max(1, min(grid, total // max(costs)))
     starts, at = [], 0
-    for n, c in units:
+    for n in length:
         starts.append(at)
-        at += n * c
+        at += n
     slots, seen = set(), {}
     for k in range(ctas):
         lo, hi = total * k // ctas, total * (k + 1) // ctas
         for u, (n, c) in enumerate(units):
-            if n == 0 or starts[u] + n * c <= lo or starts[u] >= hi:
+            if n == 0 or starts[u] + length[u] <= lo or starts[u] >= hi:
                 continue
-            p = max(lo, starts[u])
-            st0, st1 = -(-(p - starts[u]) // c), min(n, -(-(hi - starts[u]) // c))
+            p, first = max(lo, starts[u]), starts[u] + UNIT
+            st0 = 0 if p <= first else -(-(p - first) // c)
+            st1 = 0 if hi <= first else min(n, -(-(hi - first) // c))
             if st0 >= st1:
                 continue
             assert u + k not in slots and u + k < len(units) + grid
@@ -139,10 +144,11 @@ def test_every_stage_has_one_cta_and_every_cut_one_slot(seed):
                 assert (u, st) not in seen
                 seen[u, st] = k
     for u, (n, c) in enumerate(units):
+        place = [starts[u] + UNIT + st * c for st in range(n)]
         for st in range(n):
-            assert seen[u, st] == owner(starts[u] + st * c, total, ctas)
+            assert seen[u, st] == owner(place[st], total, ctas)
         if n:
-            k0, k1 = owner(starts[u], total, ctas), owner(starts[u] + (n - 1) * c, total, ctas)
+            k0, k1 = owner(place[0], total, ctas), owner(place[-1], total, ctas)
             assert {seen[u, st] for st in range(n)} == set(range(k0, k1 + 1))
 
 
