@@ -536,20 +536,19 @@ __device__ __forceinline__ void lane_stage(const unsigned char *tile, int ntok, 
 
 // ------------------------------------------------------------------ segments
 
-__host__ __device__ constexpr int align1k(int x) { return (x + 1023) & ~1023; }
 // Shared memory: the slots (1024-byte aligned, as the swizzle wants), fp32 query rows, barriers, tables.
 constexpr int kQBytes = 2 * unit_rows<float>() * kHeadDim * 4;  // fp32
 template <typename T>
 inline size_t segments_smem(int B, int ngroups)
 {
-    return 1024 + (size_t)kStages * kSlot + (sizeof(T) == 4 ? kQBytes : 0) + (size_t)table_ints(B, ngroups) * 4 + 2 * kStages * 8 + 16;
+    return 1024 + (size_t)kStages * kSlot + (sizeof(T) == 4 ? kQBytes : 0) + (size_t)table_ints(B, ngroups) * 4 +
+           2 * kStages * 8 + 16;
 }
 
 // ---- the four warps that consume the stages, fp32: CUDA cores
 template <typename T, int DD, bool SCORED>
 __device__ __forceinline__ void consume_lanes(const Args &a, const Tables &t, const unsigned char *slots, float *qs,
-                                              uint64_t *full,
-                                              uint64_t *empty, volatile int *gave_up)
+                                              uint64_t *full, uint64_t *empty, volatile int *gave_up)
 {
     constexpr int TW = ring_tokens<T>(), TP = page_tokens<T, DD>(), kR = unit_rows<T>();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;

@@ -49,6 +49,11 @@ SHARED = [
     ("bf16", 32, 8, 16, 256, [4500 + 13 * i for i in range(5)], [0, 0, 0, 0, 0], [66]),
     ("bf16", 8, 2, 16, 20, [420 + (i * 37) % 300 for i in range(70)], [i % 3 - (i % 11 == 0) * (i % 3 + 1) for i in
                                                                         range(70)], [6, 3, 1]),  # many rows, many tiles
+    ("bf16", 80, 1, 16, 17, [300, 310, 320, 50], [0, 0, 0, -1], [2]),          # two row tiles a sequence
+    ("bf16", 16, 1, 64, 30, [300, 310, 320, 50], [0, 0, 0, -1], [2]),          # sixteen rows a private unit
+    ("bf16", 9, 1, 8, 30, [300, 310, 320, 50], [0, 0, 0, -1], [2]),
+    ("bf16", 2, 2, 16, 500, [100, 400, 500, 501, 564, 565], [0] * 6, [1]),     # windows that hold almost all
+    ("bf16", 1, 1, 16, 16, [40000, 40010], [0, 0], [600]),                     # one head over all CTAs
     ("f32", 4, 4, 16, 32, [230, 270], [0, 0], [3]),
     ("f32", 8, 2, 8, 21, [500, 510, 90, 600], [0, 0, 0, 0], [7]),
     ("f32", 6, 2, 32, 21, [500, 510, 90, 600], [0, 0, -1, 0], [7]),
@@ -140,6 +145,10 @@ SCORED = [
     ("bf16", 6, 2, 32, 40, [1111, 1200]),
     ("bf16", 4, 4, 64, 1000, [1111, 1200, 30]),
     ("bf16", 2, 2, 16, 1, [1, 2, 65, 66]),
+    ("bf16", 70, 1, 16, 17, [300, 2100]),
+    ("bf16", 16, 1, 8, 17, [300, 2100]),
+    ("bf16", 12, 1, 32, 17, [300, 2100]),
+    ("bf16", 1, 1, 16, 16, [40003]),
     ("f32", 8, 4, 16, 37, [20, 1501, 700]),
     ("f32", 4, 4, 8, 21, [500, 0, 90]),
     ("f32", 6, 2, 32, 21, [500, 510]),
@@ -278,3 +287,58 @@ def test_operands_are_checked():
         with pytest.raises(dar.DarError):
             call()
     assert c.device_status() == 0
+
+
+def test_the_largest_batch():
+    """1024 sequences, some empty, in 40 groups in no order; f32 so that the comparison is sharp."""
+    g = torch.Generator().manual_seed(4)
+    B, pages = 1024, [int(x) for x in torch.randint(0, 3, (40,), generator=g)]
+    group = [int(x) for x in torch.randint(-1, 40, (B,), generator=g)]
+    lens = [0 if i % 97 == 5 else 5 + 64 * (pages[k] if k >= 0 else 1) + int(x)
+            for i, (k, x) in enumerate(zip(group, torch.randint(0, 90, (B,), generator=g)))]
+    c, full = R.filled_cache(dar, 6, "f32", 1, 8, 5, lens, group, pages)
+    q, Uk, Uv = R.operands(7, "f32", B, 2, 1, 8)
+    got = dar.dar_attn_decode_shared(c, q, Uk, Uv, ints(group), ints(pages), dar.shared_decode_workspace(c, 2))
+    torch.cuda.synchronize()
+    assert c.device_status() == 0
+    check_outputs("f32", c, full, q, Uk, Uv, got)
+
+
+def test_infinite_and_nan_inputs_stay_in_their_sequence():
+    """A NaN query, an infinite key and an infinite value of one member reach nobody else's output."""
+    lens, group, pages = [500, 520, 540, 45], [0, 0, 0, -1], [5]
+    c, full = R.filled_cache(dar, 8, "bf16", 2, 16, 40, lens, group, pages)
+    q, Uk, Uv = R.operands(9, "bf16", 4, 4, 2, 16)
+    ws = dar.shared_decode_workspace(c, 4)
+    want = dar.dar_attn_decode_shared(c, q, Uk, Uv, ints(group), ints(pages), ws)
+    q[1, 0] = float("nan")
+    c.win_v[1] = float("inf")
+    c.pool_kd[full[1][6]] = float("inf")
+    got = dar.dar_attn_decode_shared(c, q, Uk, Uv, ints(group), ints(pages), ws)
+    assert torch.equal(got[[0, 2, 3]], want[[0, 2, 3]])
+    assert torch.isnan(got[1]).all()
+
+
+def test_calls_of_two_streams_with_workspaces_of_their_own():
+    lens, group, pages = [2000 + i for i in range(16)], [0] * 16, [25]
+    c, _ = R.filled_cache(dar, 8, "bf16", 2, 16, 40, lens, group, pages)
+    q, Uk, Uv = R.operands(9, "bf16", 16, 4, 2, 16)
+    for b in range(1, 16):
+        c.block_table[b, :25] = c.block_table[0, :25]
+    g, p = ints(group), ints(pages)
+    want = dar.dar_attn_decode_shared(c, q, Uk, Uv, g, p, dar.shared_decode_workspace(c, 4))
+    weights = [dar.attention_weights(c) for _ in range(3)]
+    dar.dar_attn_decode_scored(c, q, Uk, Uv, weights[2], dar.scored_decode_workspace(c, 4))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ws = [dar.shared_decode_workspace(c, 4) for _ in streams]
+    wsc = [dar.scored_decode_workspace(c, 4) for _ in streams]
+    outs = [torch.empty_like(q) for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            dar.dar_attn_decode_shared(c, q, Uk, Uv, g, p, ws[i], out=outs[i], stream=s)
+    for i, s in enumerate(streams):
+        dar.dar_attn_decode_scored(c, q, Uk, Uv, weights[i], wsc[i], stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    assert all(torch.equal(x, weights[2]) for x in weights[:2])
