@@ -234,7 +234,7 @@ dar_status dar_attn_decode_shared(const dar_cache *cache, int32_t Hq, const void
  * later finds a zero: dar_cache_evict leaves zeros behind the new end).
  * 0 <= decay <= 1; decay = 1 accumulates over all steps, and decay = 0 keeps this
  * step's weights alone, whatever was there.  out is that of dar_attn_decode.
- * Scores, maxima and sums are fp32.
+ * Scores, maxima and sums are fp32 (bf16: q~ as three bf16 terms, 2^-24 of it).
  * Arguments, sizes, alignment (weights too) and errors otherwise as
  * dar_attn_decode; Hq / Hkv <= 1024.  For a sequence with a bad length or page,
  * out and its weights are undefined.  Two kernels in order on `stream`, the first

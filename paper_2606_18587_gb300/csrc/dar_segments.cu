@@ -83,18 +83,14 @@ __host__ __device__ constexpr int ring_tokens() { return kHalf / (kHeadDim * (in
 template <typename T, int DD>
 __host__ __device__ constexpr int page_tokens() { return kHalf / (DD * (int)sizeof(T)); }
 
-// What the joining kernel has to know about the line of units.
-struct PlanHead {
-    int total, ctas;  // length of the line, CTAs that share it
-};
+// What the joining kernel has to know: of a sequence, and which CTAs have the first and the last cut of a unit.
 struct PlanSeq {
-    int L;             // tokens
-    int start, stages; // its first private unit's place on the line; stages of each private unit
-    int xstart, xstages, xcost, xunit;  // its group's first prefix unit: place, stages, cost of one, index
-    int xrt;           // row tiles of the group (0: not in a group)
-    int row0;          // the sequence's first row among the group's rows of a KV head
-    int xrows;         // rows of the group per KV head
-    int pad[2];
+    int L;      // tokens
+    int xunit;  // index of its group's first prefix unit
+    int xrt;    // row tiles of the group (0: not in a group)
+    int row0;   // the sequence's first row among the group's rows of a KV head
+    int xrows;  // rows of the group per KV head
+    int pad[3];
 };
 
 struct Args {
@@ -103,8 +99,8 @@ struct Args {
     const int32_t *block_table, *seq_lens, *group, *prefix_pages;
     int32_t *status;
     const float *Uk, *Uv;
-    PlanHead *head;
-    PlanSeq *plan;
+    PlanSeq *plan;         // [B]
+    int2 *span_p, *span_x; // of every private and every prefix unit
     float *rec_p, *rec_x;  // partial results of private and prefix units
     float *scores;         // [B][Hq][score_stride] scores, unscaled, or nullptr
     float *weights;        // [B][Hkv][slots], or nullptr
@@ -120,18 +116,8 @@ __host__ __device__ constexpr int rec_p_floats() { return 4 + kHeadDim + DD; }
 template <int DD>
 __host__ __device__ constexpr int rec_x_floats() { return 4 + DD; }
 
-// Length of a unit of n stages on the line, and the place of its stage i.
+// Length of a unit of n stages on the line: its set-up, then the stages.
 __host__ __device__ inline int unit_length(int n, int cost) { return n ? kCostUnit + n * cost : 0; }
-__host__ __device__ inline long long stage_place(long long start, int i, int cost)
-{
-    return start + kCostUnit + (long long)i * cost;
-}
-
-// The CTA that owns the stage at place p of the line: the last k with total * k / ctas <= p.
-__device__ __forceinline__ int owner(long long p, int total, int ctas)
-{
-    return (int)(((p + 1) * ctas - 1) / total);
-}
 
 // ------------------------------------------------------------------ tables
 
@@ -312,7 +298,9 @@ struct Cut {
     int rt;           // row tile
     int rows;         // rows of this tile
     int RW;           // warps on different rows (the others split the keys)
+    int unit;         // index among the units of its kind
     int slot;         // slot of the partial results
+    bool first, last; // the unit's first, last stage is in the cut
     int st0, st1;     // stages [st0, st1) of the unit
     int nwin;         // ring tokens (0 in a prefix unit)
     int tok0, tok1;   // distant tokens [tok0, tok1) of the whole unit
@@ -376,11 +364,14 @@ __device__ bool find_cut(const Args &a, const Tables &t, int p, int hi, int cta,
         c.tok0 = P * kPage;
         c.tok1 = t.L[b] - c.nwin;
     }
+    c.unit = unit;
     c.slot = unit + cta;
     next = start + unit_length(nst, cost);
     const int first = start + kCostUnit;  // place of stage 0
     c.st0 = p <= first ? 0 : (p - first + cost - 1) / cost;
     c.st1 = hi <= first ? 0 : min(nst, (hi - first + cost - 1) / cost);
+    c.first = c.st0 == 0;
+    c.last = c.st1 == nst;
     return c.st0 < c.st1;
 }
 
@@ -1514,22 +1505,13 @@ __global__ void __launch_bounds__(kThreads, SMALL ? 3 : 1) segments_kernel(const
     }
     build_tables<T, DD>(a, t, blockIdx.x == 0);  // its barriers also publish the mbarriers
     if (blockIdx.x == 0) {
-        if (tid == 0)
-            *a.head = PlanHead{t.tot[0] + t.tot[1], Walk::ctas(t)};
         for (int b = tid; b < a.B; b += kThreads) {
-            PlanSeq s;
+            PlanSeq s{};
             const int g = t.grp[b];
             s.L = t.L[b];
-            s.start = t.start[b];
-            s.stages = private_stages<T, DD>(s.L, a.w, g >= 0 ? t.gP[g] : 0);
-            s.xrt = 0;
-            s.xstart = s.xstages = s.xcost = s.xunit = s.row0 = s.xrows = 0;
             if (g >= 0) {
                 s.xrows = t.gcnt[g] * a.G;
                 s.xrt = (s.xrows + unit_rows<T>() - 1) / unit_rows<T>();
-                s.xstart = t.gxst[g];
-                s.xstages = prefix_stages<T, DD>(t.gP[g]);
-                s.xcost = prefix_cost<T>(min(s.xrows, unit_rows<T>()));
                 s.xunit = t.gxu[g];
                 s.row0 = t.rank[b] * a.G;
             }
@@ -1544,6 +1526,13 @@ __global__ void __launch_bounds__(kThreads, SMALL ? 3 : 1) segments_kernel(const
         bool alive = true;
         Walk walk(t);
         for (Cut c; alive && walk.next<T, DD>(a, t, c);) {
+            if (lane == 0) {
+                int2 *span = (c.grp < 0 ? a.span_p : a.span_x) + c.unit;
+                if (c.first)
+                    span->x = blockIdx.x;
+                if (c.last)
+                    span->y = blockIdx.x;
+            }
             // what the consumers will want first, while they are at the cut before
             for (int i = lane; i < DD * 2; i += 32)
                 prefetch_l1(a.Uk + ((size_t)c.g * DD * 2 + i) * (kHeadDim / 2));
@@ -1624,82 +1613,82 @@ __global__ void __launch_bounds__(kThreads, SMALL ? 3 : 1) segments_kernel(const
 
 // ------------------------------------------------------------------ join
 
-// Where the partial results of a row are: result i of n at base + (i / per) * far + (i % per) * near floats.
+// Where the partial results of a row are: result i of n, those of a CTA's 2^lg key warps one after the other.
 struct Parts {
     const float *base;
-    int n, per;
-    size_t far, near;
-    __device__ __forceinline__ const float *at(int i) const { return base + (i / per) * far + (i % per) * near; }
+    int n, lg;
+    size_t far, near;  // from one CTA's to the next one's, from one key warp's to the next one's
+    __device__ __forceinline__ const float *at(int i) const
+    {
+        return base + (size_t)(i >> lg) * far + (size_t)(i & ((1 << lg) - 1)) * near;
+    }
 };
 
+// The CTAs of a unit (in range whatever a kernel that gave up has left).
+__device__ __forceinline__ void span_of(const int2 *span, int &k0, int &k1)
+{
+    const int2 s = *span;
+    k0 = min(max(s.x, 0), kMaxCtas - 1);
+    k1 = min(max(s.y, k0), kMaxCtas - 1);
+}
+
+// log2 of the key warps beside RW row warps
+__device__ __forceinline__ int key_warps_lg(int RW) { return RW == 1 ? 2 : RW == 2 ? 1 : 0; }
+
 template <typename T, int DD>
-__device__ __forceinline__ Parts private_parts(const Args &a, const PlanHead &hd, const PlanSeq &s, int b, int g, int j)
+__device__ __forceinline__ Parts private_parts(const Args &a, int b, int g, int j)
 {
     constexpr int kR = unit_rows<T>();
-    Parts r{nullptr, 0, 1, 0, 0};
-    if (s.stages == 0)
-        return r;
-    const int rt = j / kR, row = j % kR, KW = kWarps / row_warps<T>(a.RP), u = g * a.RTP + rt;
-    const long long p0 = s.start + (long long)u * unit_length(s.stages, kCostPrivate);
-    const int k0 = owner(stage_place(p0, 0, kCostPrivate), hd.total, hd.ctas);
-    const int k1 = owner(stage_place(p0, s.stages - 1, kCostPrivate), hd.total, hd.ctas);
-    const size_t slot = (size_t)b * a.Hkv * a.RTP + u + k0;
+    Parts r;
+    const int rt = j / kR, row = j % kR;
+    const size_t u = ((size_t)b * a.Hkv + g) * a.RTP + rt;
+    int k0, k1;
+    span_of(a.span_p + u, k0, k1);
+    r.lg = key_warps_lg(row_warps<T>(a.RP));
     r.near = (size_t)a.RP * rec_p_floats<DD>();
-    r.far = KW * r.near;
-    r.per = KW;
-    r.n = (k1 - k0 + 1) * KW;
-    r.base = a.rec_p + slot * r.far + (size_t)row * rec_p_floats<DD>();
+    r.far = r.near << r.lg;
+    r.n = (k1 - k0 + 1) << r.lg;
+    r.base = a.rec_p + (u + k0) * r.far + (size_t)row * rec_p_floats<DD>();
     return r;
 }
 
 template <typename T, int DD>
-__device__ __forceinline__ Parts prefix_parts(const Args &a, const PlanHead &hd, const PlanSeq &s, int g, int j)
+__device__ __forceinline__ Parts prefix_parts(const Args &a, const PlanSeq &s, int g, int j)
 {
     constexpr int kR = unit_rows<T>();
-    Parts r{nullptr, 0, 1, 0, 0};
+    Parts r{nullptr, 0, 0, 0, 0};
     if (s.xrt == 0)
         return r;
-    const int i = s.row0 + j, rt = i / kR, row = i % kR, rows = min(kR, s.xrows - rt * kR);
-    const int RW = row_warps<T>(rows), u = g * s.xrt + rt;
-    const long long p0 = s.xstart + (long long)u * unit_length(s.xstages, s.xcost);
-    const int k0 = owner(stage_place(p0, 0, s.xcost), hd.total, hd.ctas);
-    const int k1 = owner(stage_place(p0, s.xstages - 1, s.xcost), hd.total, hd.ctas);
-    r.per = kWarps / RW;
+    const int i = s.row0 + j, rt = i / kR, row = i % kR, RW = row_warps<T>(min(kR, s.xrows - rt * kR));
+    const size_t u = s.xunit + g * s.xrt + rt;
+    int k0, k1;
+    span_of(a.span_x + u, k0, k1);
+    r.lg = key_warps_lg(RW);
     r.near = (size_t)(RW * rpw<T>()) * rec_x_floats<DD>();
     r.far = (size_t)kR * rec_x_floats<DD>();
-    r.n = (k1 - k0 + 1) * r.per;
-    r.base = a.rec_x + (size_t)(s.xunit + u + k0) * r.far + (size_t)row * rec_x_floats<DD>();
+    r.n = (k1 - k0 + 1) << r.lg;
+    r.base = a.rec_x + (u + k0) * r.far + (size_t)row * rec_x_floats<DD>();
     return r;
 }
 
 constexpr int kJoinWarps = 4;
 constexpr int kJoinThreads = kJoinWarps * 32;
-constexpr int kJoinPer = 8;                            // tokens of a thread
-constexpr int kJoinTokens = kJoinThreads * kJoinPer;   // tokens whose weights a block updates
+constexpr int kJoinPer = 8;                               // tokens of a thread at a time
+constexpr int kJoinTokens = 2 * kJoinThreads * kJoinPer;  // tokens whose weights a block updates
 
-// The entries lane, lane + 32 (and so on) of a run of partial results, joined on the way: NLOC and NDOWN
+// The entries lane, lane + 32 (and so on) of a run of partial results, joined on the way: NLOC and ND
 // registers of the full-width and of the bottleneck sum.
 template <int NLOC, int DD>
 struct Joined {
-    static constexpr int ND = (DD + 31) / 32;
-    float m, l, x[NLOC + ND];
+    static constexpr int ND = (DD + 31) / 32, N = NLOC + ND;
+    float m, l, x[N];
     __device__ void clear()
     {
         m = -INFINITY;
         l = 0.f;
 #pragma unroll
-        for (int i = 0; i < NLOC + ND; ++i)
+        for (int i = 0; i < N; ++i)
             x[i] = 0.f;
-    }
-    __device__ void fold(float mo, float lo, const float (&o)[NLOC + ND])
-    {
-        const float mn = fmaxf(m, mo), base = mn == -INFINITY ? 0.f : mn;
-        const float f = exp2f(m - base), fo = exp2f(mo - base);
-        m = mn;
-        l = l * f + lo * fo;
-#pragma unroll
-        for (int i = 0; i < NLOC + ND; ++i)
-            x[i] = x[i] * f + o[i] * fo;
     }
     // parts first, first + step, ..; LOC: they hold full-width sums before the others
     template <bool LOC>
@@ -1707,20 +1696,21 @@ struct Joined {
     {
         constexpr int U = 4;  // in flight together
         for (int i0 = first; i0 < r.n; i0 += U * step) {
-            float mo[U], lo[U], o[U][NLOC + ND];
+            float mo[U], lo[U], o[U][N];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = i0 + u * step;
                 mo[u] = -INFINITY;
                 lo[u] = 0.f;
 #pragma unroll
-                for (int e = 0; e < NLOC + ND; ++e)
+                for (int e = 0; e < N; ++e)
                     o[u][e] = 0.f;
                 if (i >= r.n)
                     continue;
                 const float *p = r.at(i);
-                mo[u] = p[0];
-                lo[u] = p[1];
+                const float2 ml = *reinterpret_cast<const float2 *>(p);
+                mo[u] = ml.x;
+                lo[u] = ml.y;
                 if (LOC)
 #pragma unroll
                     for (int e = 0; e < NLOC; ++e)
@@ -1731,22 +1721,37 @@ struct Joined {
                     if (32 * e + lane < DD)
                         o[u][NLOC + e] = d[32 * e + lane];
             }
+            float top = m;
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                fold(mo[u], lo[u], o[u]);
+                top = fmaxf(top, mo[u]);
+            const float base = top == -INFINITY ? 0.f : top, f = ex2_approx(m - base);
+            m = top;
+            l *= f;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                x[e] *= f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float fo = ex2_approx(mo[u] - base);
+                l = fmaf(lo[u], fo, l);
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    x[e] = fmaf(o[u][e], fo, x[e]);
+            }
         }
     }
 };
 
-// Blocks 0 .. B * Hq - 1 write one output row each: the warps take the row's partial results in turn, the
-// first warp joins the four and lifts the bottleneck sum.  Scored: the other blocks update the weights of
-// kJoinTokens tokens of a (sequence, KV head) each.
+// Blocks 0 .. B * Hq - 1 write one output row each: the warps take the row's partial results in turn, are
+// joined, and the bottleneck sum is lifted.  Scored: the other blocks update the weights of kJoinTokens
+// tokens of a (sequence, KV head) each.
 template <typename T, int DD, bool SCORED>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
 {
     constexpr int NLOC = kHeadDim / 32;
     using J = Joined<NLOC, DD>;
-    __shared__ float part[kJoinWarps][2 + 32 * (NLOC + J::ND)];
+    __shared__ float part[kJoinWarps][2 + 32 * J::N], sum[kHeadDim + DD];
     extern __shared__ float stat[];  // SCORED: [G][2] m and 1 / l
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rows = a.B * a.Hq;
@@ -1762,19 +1767,20 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
         }
         grid_dep_wait();
         const PlanSeq s = a.plan[b];
-        const PlanHead hd = *a.head;
         J x;
         x.clear();
-        x.template add<true>(private_parts<T, DD>(a, hd, s, b, g, j), warp, kJoinWarps, lane);
-        if constexpr (!SCORED)
-            x.template add<false>(prefix_parts<T, DD>(a, hd, s, g, j), warp, kJoinWarps, lane);
+        if (s.L > 0) {
+            x.template add<true>(private_parts<T, DD>(a, b, g, j), warp, kJoinWarps, lane);
+            if constexpr (!SCORED)
+                x.template add<false>(prefix_parts<T, DD>(a, s, g, j), warp, kJoinWarps, lane);
+        }
         float *p = part[warp];
         if (lane == 0) {
             p[0] = x.m;
             p[1] = x.l;
         }
 #pragma unroll
-        for (int e = 0; e < NLOC + J::ND; ++e)
+        for (int e = 0; e < J::N; ++e)
             p[2 + 32 * e + lane] = x.x[e];
         __syncthreads();
         float m = -INFINITY, f[kJoinWarps], l = 0.f;
@@ -1785,25 +1791,26 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
             m = 0.f;
 #pragma unroll
         for (int i = 0; i < kJoinWarps; ++i) {
-            f[i] = exp2f(part[i][0] - m);
-            l += part[i][1] * f[i];
+            f[i] = ex2_approx(part[i][0] - m);
+            l = fmaf(part[i][1], f[i], l);
         }
-        if (threadIdx.x >= kHeadDim)
-            return;
-        float o = 0.f;
-#pragma unroll
-        for (int i = 0; i < kJoinWarps; ++i)
-            o = fmaf(f[i], part[i][2 + threadIdx.x], o);
-#pragma unroll
-        for (int e = 0; e < DD; ++e) {
-            float d = 0.f;
+        if (threadIdx.x < kHeadDim + DD) {
+            float y = 0.f;
 #pragma unroll
             for (int i = 0; i < kJoinWarps; ++i)
-                d = fmaf(f[i], part[i][2 + kHeadDim + e], d);
+                y = fmaf(f[i], part[i][2 + threadIdx.x], y);
+            sum[threadIdx.x] = y;
+        }
+        __syncthreads();
+        if (threadIdx.x >= kHeadDim)
+            return;
+        float o = sum[threadIdx.x];
+#pragma unroll
+        for (int e = 0; e < DD; ++e) {
             if constexpr (DD < 32)
-                o = fmaf(d, uv[e], o);
+                o = fmaf(sum[kHeadDim + e], uv[e], o);
             else
-                o = fmaf(d, __ldg(a.Uv + ((size_t)g * DD + e) * kHeadDim + threadIdx.x), o);
+                o = fmaf(sum[kHeadDim + e], __ldg(a.Uv + ((size_t)g * DD + e) * kHeadDim + threadIdx.x), o);
         }
         static_cast<T *>(a.out)[(size_t)row * kHeadDim + threadIdx.x] = from_f32<T>(s.L == 0 ? 0.f : o / l);
         return;
@@ -1813,17 +1820,16 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
         const int heads = a.B * a.Hkv, i = (int)blockIdx.x - rows, bg = i % heads, chunk = chunks - 1 - i / heads;
         const int b = bg / a.Hkv, g = bg % a.Hkv;
         grid_dep_wait();
-        const PlanSeq s = a.plan[b];
-        if ((long long)chunk * kJoinTokens >= s.L)
+        const int L = a.plan[b].L;
+        if ((long long)chunk * kJoinTokens >= L)
             return;
-        const PlanHead hd = *a.head;
         for (int j = warp; j < a.G; j += kJoinWarps) {  // the row's maximum and sum
-            const Parts r = private_parts<T, DD>(a, hd, s, b, g, j);
+            const Parts r = private_parts<T, DD>(a, b, g, j);
             float m = -INFINITY, l = 0.f;
             for (int i = lane; i < r.n; i += 32) {
                 const float2 v = *reinterpret_cast<const float2 *>(r.at(i));
                 const float mn = fmaxf(m, v.x), base = mn == -INFINITY ? 0.f : mn;
-                l = l * exp2f(m - base) + v.y * exp2f(v.x - base);
+                l = l * ex2_approx(m - base) + v.y * ex2_approx(v.x - base);
                 m = mn;
             }
             float top = m;
@@ -1831,7 +1837,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
             for (int off = 16; off; off >>= 1)
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
             const float base = top == -INFINITY ? 0.f : top;
-            l *= exp2f(m - base);
+            l *= ex2_approx(m - base);
 #pragma unroll
             for (int off = 16; off; off >>= 1)
                 l += __shfl_xor_sync(0xffffffffu, l, off);
@@ -1843,29 +1849,32 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
         __syncthreads();
         float *w = a.weights + (size_t)bg * a.slots;
         const float *x = a.scores + ((size_t)b * a.Hq + (size_t)g * a.G) * a.score_stride;
-        const int t0 = chunk * kJoinTokens + threadIdx.x;
-        float old[kJoinPer], p[kJoinPer];
+        const int end = (int)min((long long)L, (long long)(chunk + 1) * kJoinTokens);
+        for (int t0 = chunk * kJoinTokens + threadIdx.x; t0 < end; t0 += kJoinThreads * kJoinPer) {
+            float old[kJoinPer], p[kJoinPer];
 #pragma unroll
-        for (int i = 0; i < kJoinPer; ++i) {
-            const int t = t0 + i * kJoinThreads;
-            old[i] = a.decay != 0.f && t < s.L ? w[t] : 0.f;
-            p[i] = 0.f;
-        }
-        for (int j = 0; j < a.G; ++j) {
-            const float m = stat[2 * j], il = stat[2 * j + 1];
-            float y[kJoinPer];
+            for (int i = 0; i < kJoinPer; ++i) {
+                const int t = t0 + i * kJoinThreads;
+                old[i] = a.decay != 0.f && t < end ? w[t] : 0.f;
+                p[i] = 0.f;
+            }
+            for (int j = 0; j < a.G; ++j) {
+                const float m = stat[2 * j], il = stat[2 * j + 1];
+                const float *xj = x + (size_t)j * a.score_stride;
+                float y[kJoinPer];
 #pragma unroll
-            for (int i = 0; i < kJoinPer; ++i)
-                y[i] = t0 + i * kJoinThreads < s.L ? x[(size_t)j * a.score_stride + t0 + i * kJoinThreads] : 0.f;
+                for (int i = 0; i < kJoinPer; ++i)
+                    y[i] = t0 + i * kJoinThreads < end ? xj[t0 + i * kJoinThreads] : 0.f;
 #pragma unroll
-            for (int i = 0; i < kJoinPer; ++i)
-                p[i] = fmaf(ex2_approx(fmaf(y[i], a.c2, -m)), il, p[i]);
-        }
+                for (int i = 0; i < kJoinPer; ++i)
+                    p[i] = fmaf(ex2_approx(fmaf(y[i], a.c2, -m)), il, p[i]);
+            }
 #pragma unroll
-        for (int i = 0; i < kJoinPer; ++i) {
-            const int t = t0 + i * kJoinThreads;
-            if (t < s.L)
-                w[t] = a.decay != 0.f ? fmaf(a.decay, old[i], p[i]) : p[i];
+            for (int i = 0; i < kJoinPer; ++i) {
+                const int t = t0 + i * kJoinThreads;
+                if (t < end)
+                    w[t] = a.decay != 0.f ? fmaf(a.decay, old[i], p[i]) : p[i];
+            }
         }
     }
 }
@@ -1873,7 +1882,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
 // ------------------------------------------------------------------ launch
 
 struct Layout {
-    size_t head, plan, rec_p, rec_x, scores, total;
+    size_t plan, span_p, span_x, rec_p, rec_x, scores, total;
     int RP, RTP;
 };
 
@@ -1892,9 +1901,10 @@ static Layout layout(int B, int Hq, int Hkv, int dd, int w, int maxp, bool score
     // a group of n rows has ceil(n / R) tiles, and there are at most B / 2 groups of two or more
     const size_t units_x = (size_t)Hkv * ((size_t)B * G / kR + B / 2 + 1) + kMaxCtas;
     const size_t slots = ((size_t)maxp * kPage + w + 3) / 4 * 4;
-    y.head = 0;
-    y.plan = 256;
-    y.rec_p = y.plan + up256((size_t)B * sizeof(PlanSeq));
+    y.plan = 0;
+    y.span_p = y.plan + up256((size_t)B * sizeof(PlanSeq));
+    y.span_x = y.span_p + up256(units * sizeof(int2));
+    y.rec_p = y.span_x + up256(units_x * sizeof(int2));
     y.rec_x = y.rec_p + up256(units * rows_p * (4 + kHeadDim + dd) * sizeof(float));
     y.scores = y.rec_x + (scored ? 0 : up256(units_x * kR * (4 + dd) * sizeof(float)));
     y.total = y.scores + (scored ? up256((size_t)B * Hq * slots * sizeof(float)) : 0);
@@ -1916,8 +1926,9 @@ static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t 
     a.status = s.status;
     a.Uk = s.Uk;
     a.Uv = s.Uv;
-    a.head = reinterpret_cast<PlanHead *>(ws + y.head);
     a.plan = reinterpret_cast<PlanSeq *>(ws + y.plan);
+    a.span_p = reinterpret_cast<int2 *>(ws + y.span_p);
+    a.span_x = reinterpret_cast<int2 *>(ws + y.span_x);
     a.rec_p = reinterpret_cast<float *>(ws + y.rec_p);
     a.rec_x = reinterpret_cast<float *>(ws + y.rec_x);
     a.scores = SCORED ? reinterpret_cast<float *>(ws + y.scores) : nullptr;
