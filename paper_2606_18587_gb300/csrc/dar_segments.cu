@@ -1671,10 +1671,8 @@ __device__ __forceinline__ Parts prefix_parts(const Args &a, const PlanSeq &s, i
     return r;
 }
 
-constexpr int kJoinWarps = 4;
-constexpr int kJoinThreads = kJoinWarps * 32;
-constexpr int kJoinPer = 8;                               // tokens of a thread at a time
-constexpr int kJoinTokens = 2 * kJoinThreads * kJoinPer;  // tokens whose weights a block updates
+constexpr int kJoinPer = 8;        // tokens of a thread at a time
+constexpr int kJoinTokens = 2048;  // tokens whose weights a block updates
 
 // The entries lane, lane + 32 (and so on) of a run of partial results, joined on the way: NLOC and ND
 // registers of the full-width and of the bottleneck sum.
@@ -1690,11 +1688,10 @@ struct Joined {
         for (int i = 0; i < N; ++i)
             x[i] = 0.f;
     }
-    // parts first, first + step, ..; LOC: they hold full-width sums before the others
-    template <bool LOC>
+    // parts first, first + step, .., U of them in flight together; LOC: they hold full-width sums before the others
+    template <bool LOC, int U>
     __device__ void add(const Parts &r, int first, int step, int lane)
     {
-        constexpr int U = 4;  // in flight together
         for (int i0 = first; i0 < r.n; i0 += U * step) {
             float mo[U], lo[U], o[U][N];
 #pragma unroll
@@ -1746,12 +1743,13 @@ struct Joined {
 // Blocks 0 .. B * Hq - 1 write one output row each: the warps take the row's partial results in turn, are
 // joined, and the bottleneck sum is lifted.  Scored: the other blocks update the weights of kJoinTokens
 // tokens of a (sequence, KV head) each.
-template <typename T, int DD, bool SCORED>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
+template <typename T, int DD, bool SCORED, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32) join_kernel(Args a, int chunks)
 {
+    constexpr int kJoinThreads = WARPS * 32, U = WARPS > 4 ? 8 : 4;
     constexpr int NLOC = kHeadDim / 32;
     using J = Joined<NLOC, DD>;
-    __shared__ float part[kJoinWarps][2 + 32 * J::N], sum[kHeadDim + DD];
+    __shared__ float part[WARPS][2 + 32 * J::N], sum[kHeadDim + DD];
     extern __shared__ float stat[];  // SCORED: [G][2] m and 1 / l
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rows = a.B * a.Hq;
@@ -1770,9 +1768,9 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
         J x;
         x.clear();
         if (s.L > 0) {
-            x.template add<true>(private_parts<T, DD>(a, b, g, j), warp, kJoinWarps, lane);
+            x.template add<true, U>(private_parts<T, DD>(a, b, g, j), warp, WARPS, lane);
             if constexpr (!SCORED)
-                x.template add<false>(prefix_parts<T, DD>(a, s, g, j), warp, kJoinWarps, lane);
+                x.template add<false, U>(prefix_parts<T, DD>(a, s, g, j), warp, WARPS, lane);
         }
         float *p = part[warp];
         if (lane == 0) {
@@ -1783,23 +1781,23 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
         for (int e = 0; e < J::N; ++e)
             p[2 + 32 * e + lane] = x.x[e];
         __syncthreads();
-        float m = -INFINITY, f[kJoinWarps], l = 0.f;
+        float m = -INFINITY, f[WARPS], l = 0.f;
 #pragma unroll
-        for (int i = 0; i < kJoinWarps; ++i)
+        for (int i = 0; i < WARPS; ++i)
             m = fmaxf(m, part[i][0]);
         if (m == -INFINITY)
             m = 0.f;
 #pragma unroll
-        for (int i = 0; i < kJoinWarps; ++i) {
+        for (int i = 0; i < WARPS; ++i) {
             f[i] = ex2_approx(part[i][0] - m);
             l = fmaf(part[i][1], f[i], l);
         }
-        if (threadIdx.x < kHeadDim + DD) {
+        for (int t = threadIdx.x; t < kHeadDim + DD; t += kJoinThreads) {
             float y = 0.f;
 #pragma unroll
-            for (int i = 0; i < kJoinWarps; ++i)
-                y = fmaf(f[i], part[i][2 + threadIdx.x], y);
-            sum[threadIdx.x] = y;
+            for (int i = 0; i < WARPS; ++i)
+                y = fmaf(f[i], part[i][2 + t], y);
+            sum[t] = y;
         }
         __syncthreads();
         if (threadIdx.x >= kHeadDim)
@@ -1823,7 +1821,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
         const int L = a.plan[b].L;
         if ((long long)chunk * kJoinTokens >= L)
             return;
-        for (int j = warp; j < a.G; j += kJoinWarps) {  // the row's maximum and sum
+        for (int j = warp; j < a.G; j += WARPS) {  // the row's maximum and sum
             const Parts r = private_parts<T, DD>(a, b, g, j);
             float m = -INFINITY, l = 0.f;
             for (int i = lane; i < r.n; i += 32) {
@@ -1858,6 +1856,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(Args a, int chunks)
                 old[i] = a.decay != 0.f && t < end ? w[t] : 0.f;
                 p[i] = 0.f;
             }
+#pragma unroll 2
             for (int j = 0; j < a.G; ++j) {
                 const float m = stat[2 * j], il = stat[2 * j + 1];
                 const float *xj = x + (size_t)j * a.score_stride;
@@ -1992,11 +1991,20 @@ static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t 
     cfg.stream = st;
     cfg.attrs = pdl;
     cfg.numAttrs = 1;
-    const int chunks = SCORED ? (int)((a.slots + kJoinTokens - 1) / kJoinTokens) : 0;
-    cfg.gridDim = dim3((unsigned)(s.B * s.Hq + s.B * s.Hkv * chunks));
-    cfg.blockDim = dim3(kJoinThreads);
+    const int chunks = SCORED ? (int)((a.slots + kJoinTokens - 1) / kJoinTokens) : 0, rows = s.B * s.Hq;
+    cfg.gridDim = dim3((unsigned)(rows + s.B * s.Hkv * chunks));
     cfg.dynamicSmemBytes = SCORED ? a.G * 2 * sizeof(float) : 0;
-    return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, SCORED>, a, chunks);
+    // Few rows may have a partial result of every CTA's four warps each, and many rows few, of which two warps
+    // are soon done.  Calls with 4 / 16 warps, us: one row over 32768 tokens 21 / 13, 128 shared rows 14.3 / 11.8,
+    // 512 shared rows 12.6 / 19.7; with 4 / 2: 2048 shared rows 36.2 / 34.1.  Scored blocks also update weights:
+    // 96 rows 14.9 / 16.6, and 2 warps are no faster.
+    const int warps = rows < (SCORED ? 64 : 192) ? 16 : rows < 1024 || SCORED ? 4 : 2;
+    cfg.blockDim = dim3(warps * 32);
+    if (warps == 16)
+        return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, SCORED, 16>, a, chunks);
+    if (warps == 4)
+        return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, SCORED, 4>, a, chunks);
+    return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, SCORED, SCORED ? 4 : 2>, a, chunks);
 }
 
 template <typename T, int DD, bool SCORED>
