@@ -151,6 +151,15 @@ __device__ __forceinline__ int rank4(unsigned nibble, int &all)
     return __popc(b0 & below) + 2 * __popc(b1 & below) + 4 * __popc(b2 & below);
 }
 
+// A cluster of one block needs no cluster barrier.
+__device__ __forceinline__ void sync_cluster(cg::cluster_group &cl, int C)
+{
+    if (C > 1)
+        cl.sync();
+    else
+        __syncthreads();
+}
+
 // Slot s of head id's rings goes to slot s - turn (mod w).
 __device__ __forceinline__ void turn_ring(const EvictArgs &a, uint4 *stage, cg::cluster_group &cl, int id, int turn)
 {
@@ -166,7 +175,7 @@ __device__ __forceinline__ void turn_ring(const EvictArgs &a, uint4 *stage, cg::
             sm100::cp_async16(sm100::smem_u32(&stage[pieces + x]), v + (size_t)s0 * rp + x);
         }
         sm100::cp_async_wait_all();
-        cl.sync();  // every slot is read
+        sync_cluster(cl, C);  // every slot is read
         for (int x = threadIdx.x; x < pieces; x += kThreads) {
             const int s = s0 + x / rp, to = s >= turn ? s - turn : s - turn + a.w;
             k[(size_t)to * rp + x % rp] = stage[x];
@@ -189,14 +198,14 @@ __device__ __forceinline__ void turn_ring(const EvictArgs &a, uint4 *stage, cg::
         }
     };
     reflect(0);
-    cl.sync();
+    sync_cluster(cl, C);
     reflect(a.w - turn);
 }
 
 __global__ void __launch_bounds__(kThreads, 5) evict_kernel(EvictArgs a, Work wk)
 {
     __shared__ __align__(16) Shared sh;
-    __shared__ int pick[2];           // digit, and how many keys lie above it
+    __shared__ int pick[3];           // digit, how many keys lie above it, how many have it
     __shared__ Counts parts[kWarps];  // of the warps' parts
     __shared__ Counts mine;           // of the block's slice
     cg::cluster_group cl = cg::this_cluster();
@@ -281,10 +290,10 @@ __global__ void __launch_bounds__(kThreads, 5) evict_kernel(EvictArgs a, Work wk
                 if (lane == 0)
                     co[c] = v;
             }
-            cl.sync();
+            sync_cluster(cl, C);
             if (warp == 0) {
                 // lane 0 has the largest digits: first two sums of 32 bins per lane, then the bins of one
-                auto descend = [&](const int *hist, int base, int n, int &above) {  // n: 1 or 2 per lane
+                auto descend = [&](const int *hist, int base, int n, int &above, int &count) {  // n: 1 or 2 per lane
                     int own[2] = {0, 0};
 #pragma unroll
                     for (int q = 0; q < kMaxCluster; ++q)
@@ -308,19 +317,26 @@ __global__ void __launch_bounds__(kThreads, 5) evict_kernel(EvictArgs a, Work wk
                     const bool second = n == 2 && before + own[0] < left;
                     const int digit = n * (31 - lane) + (n == 2 && !second ? 1 : 0);
                     above = __shfl_sync(0xffffffffu, before + (second ? own[0] : 0), src);
+                    count = __shfl_sync(0xffffffffu, second ? own[1] : own[0], src);
                     return __shfl_sync(0xffffffffu, digit, src);
                 };
-                int above = 0;
-                const int c = descend(co, 0, 2, above);
-                const int d = 32 * c + descend(h, 32 * c, 1, above);
+                int above = 0, count;
+                const int c = descend(co, 0, 2, above, count);
+                const int d = 32 * c + descend(h, 32 * c, 1, above, count);
                 if (lane == 0) {
                     pick[0] = d;
                     pick[1] = above;
+                    pick[2] = count;
                 }
             }
             __syncthreads();
             prefix |= (uint32_t)pick[0] << shift;
             left -= pick[1];
+            if (left == pick[2]) {  // all of them stay (most often the only one): what lies above the key below them
+                --prefix;           // (not 0: fewer stay than there are, so smaller keys exist)
+                left = 0;
+                break;
+            }
         }
         Counts k{0, 0, 0, 0};  // of this warp's part
         runs_each(cand, origin, i0, i1, c0, c1, [&](int c, unsigned valid, const float (&x)[4]) {
@@ -362,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, 5) evict_kernel(EvictArgs a, Work wk
         }
         mine = s;
     }
-    cl.sync();
+    sync_cluster(cl, C);
 
     // ---- 2. holes and movers of this slice, in order.  Equal keys are in the order of their positions, so
     // of the first `left` that stay those below the budget's position come first.
@@ -431,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 5) evict_kernel(EvictArgs a, Work wk
             list(nibble_in(i, edge, i1) & up, movers, nm);
         }
     }
-    cl.sync();
+    sync_cluster(cl, C);
 
     // ---- 3. hole i is filled from mover i
     // a thread's pieces of rows are all the same one of the 2 * gk 16-byte pieces of a vector's keys and
@@ -474,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 5) evict_kernel(EvictArgs a, Work wk
     float *win = wk.window + (size_t)id * a.w;
     for (int i = all; i < a.w; i += step)
         win[i] = w[n + i];
-    cl.sync();
+    sync_cluster(cl, C);
     for (int i = all; i < a.w; i += step)
         w[keep + i] = win[i];
     for (int i = keep + a.w + all; i < L; i += step)
