@@ -298,39 +298,41 @@ def dar_attn_decode_noalloc(cache: DarCache, q, Uk, Uv, scale=0.0, out=None, str
 
 # --------------------------------------------------------------------------- shared prefixes, weights, eviction
 
-def _operand(t, name, dtype, shape, cache):
-    """A contiguous tensor on the cache's device, of this dtype and shape (None: any)."""
-    device = cache.win_k.device
-    if isinstance(t, torch.Tensor) and t.device == device and (dtype is None or t.dtype is dtype) \
+def _operand(t, name, dtype, shape, dev):
+    """A contiguous tensor on CUDA device ``dev``, of this dtype and shape (None: any)."""
+    if isinstance(t, torch.Tensor) and t.get_device() == dev and (dtype is None or t.dtype is dtype) \
             and (shape is None or t.shape == shape) and t.is_contiguous():
         return
     _dev(t, name, dtype)
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    raise ValueError(f"{name} is on {t.device}, the cache on {device}")
+    raise ValueError(f"{name} is on {t.device}, the cache on cuda:{dev}")
 
 
-def _on_current_device(cache):
-    """Kernels are launched on the current device's stream: the cache has to be there."""
-    if cache.win_k.device.index != torch.cuda.current_device():
+def _cache_device(cache):
+    """The device of the cache, which has to be the current one: kernels are launched on its stream."""
+    dev = cache.win_k.get_device()
+    if dev != torch.cuda.current_device():
         raise ValueError(f"the cache is on {cache.win_k.device}, the current device is "
                          f"cuda:{torch.cuda.current_device()}")
+    return dev
 
 
 def _step_operands(cache, q, Uk, Uv, workspace, out):
-    """Checks of a decode step's operands; returns (Hq, out)."""
+    """Checks of a decode step's operands; returns (Hq, out, device)."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a tensor [B, Hq, d]")
+    dev = _cache_device(cache)
     Hq = q.shape[1]
-    _on_current_device(cache)
-    _operand(q, "q", cache.dtype, (cache.B, Hq, cache.d), cache)
-    for name, t in (("Uk", Uk), ("Uv", Uv)):
-        _operand(t, name, torch.float32, (cache.Hkv, cache.d_down, cache.d), cache)
-    _operand(workspace, "workspace", None, None, cache)
+    rows, maps = (cache.B, Hq, cache.d), (cache.Hkv, cache.d_down, cache.d)
+    _operand(q, "q", cache.dtype, rows, dev)
+    _operand(Uk, "Uk", torch.float32, maps, dev)
+    _operand(Uv, "Uv", torch.float32, maps, dev)
+    _operand(workspace, "workspace", None, None, dev)
     if out is None:
         out = torch.empty_like(q)
-    _operand(out, "out", cache.dtype, q.shape, cache)
-    return Hq, out
+    _operand(out, "out", cache.dtype, rows, dev)
+    return Hq, out, dev
 
 
 def _new_workspace(cache, nbytes):
@@ -349,12 +351,15 @@ def dar_attn_decode_shared(cache: DarCache, q, Uk, Uv, group, prefix_pages, work
     """One decode step for sequences that share their first pages in groups: sequence b belongs to
     ``group[b]`` (int32 ``[B]``, -1 = none), whose members share their first ``prefix_pages[group[b]]`` pages
     (int32 ``[n_groups]``).  Results as :func:`dar_attn_decode`; the shared pages are read once per group."""
-    Hq, out = _step_operands(cache, q, Uk, Uv, workspace, out)
-    _operand(group, "group", torch.int32, (cache.B,), cache)
-    _operand(prefix_pages, "prefix_pages", torch.int32, (prefix_pages.numel(),), cache)
+    Hq, out, dev = _step_operands(cache, q, Uk, Uv, workspace, out)
+    _operand(group, "group", torch.int32, (cache.B,), dev)
+    if not isinstance(prefix_pages, torch.Tensor) or prefix_pages.dim() != 1:
+        raise ValueError("prefix_pages must be a tensor [n_groups]")
+    _operand(prefix_pages, "prefix_pages", torch.int32, None, dev)
     _check(load_library().dar_attn_decode_shared(
-        cache.struct, Hq, _ptr(q), _ptr(Uk), _ptr(Uv), _ptr(group), prefix_pages.numel(), _ptr(prefix_pages),
-        float(scale), _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+        cache.struct, Hq, q.data_ptr(), Uk.data_ptr(), Uv.data_ptr(), group.data_ptr(), prefix_pages.shape[0],
+        prefix_pages.data_ptr(), float(scale), out.data_ptr(), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
     return out
 
 
@@ -369,20 +374,19 @@ def scored_decode_workspace(cache: DarCache, Hq: int):
     return _new_workspace(cache, int(load_library().dar_decode_scored_workspace_bytes(cache.struct, Hq)))
 
 
-def _totals(cache, weights):
-    _operand(weights, "weights", torch.float32, (cache.B, cache.Hkv, cache.max_pages_per_seq * PAGE_SIZE + cache.w),
-             cache)
+def _totals(cache, weights, dev):
+    _operand(weights, "weights", torch.float32, (cache.B, cache.Hkv, cache.max_pages_per_seq * PAGE_SIZE + cache.w), dev)
 
 
 def dar_attn_decode_scored(cache: DarCache, q, Uk, Uv, weights, workspace, decay=1.0, scale=0.0, out=None,
                            stream=None):
     """One decode step that also sets ``weights`` (see :func:`attention_weights`) to ``decay * weights`` plus each
     token's attention weight, summed over the query heads of its KV head."""
-    Hq, out = _step_operands(cache, q, Uk, Uv, workspace, out)
-    _totals(cache, weights)
+    Hq, out, dev = _step_operands(cache, q, Uk, Uv, workspace, out)
+    _totals(cache, weights, dev)
     _check(load_library().dar_attn_decode_scored(
-        cache.struct, Hq, _ptr(q), _ptr(Uk), _ptr(Uv), float(scale), _ptr(weights), float(decay), _ptr(out),
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
+        cache.struct, Hq, q.data_ptr(), Uk.data_ptr(), Uv.data_ptr(), float(scale), weights.data_ptr(), float(decay),
+        out.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
     return out
 
 
@@ -394,12 +398,12 @@ def evict_workspace(cache: DarCache):
 def dar_cache_evict(cache: DarCache, weights, keep, workspace, protect=None, stream=None):
     """Eviction in place: every sequence b with more than ``keep[b]`` distant tokens (int32 ``[B]``) keeps, per KV
     head, its first ``protect[b]`` (int32 ``[B]``; none: 0) and those with the largest ``weights``."""
-    _on_current_device(cache)
-    _totals(cache, weights)
-    _operand(keep, "keep", torch.int32, (cache.B,), cache)
+    dev = _cache_device(cache)
+    _totals(cache, weights, dev)
+    _operand(keep, "keep", torch.int32, (cache.B,), dev)
     if protect is not None:
-        _operand(protect, "protect", torch.int32, (cache.B,), cache)
-    _operand(workspace, "workspace", None, None, cache)
+        _operand(protect, "protect", torch.int32, (cache.B,), dev)
+    _operand(workspace, "workspace", None, None, dev)
     _check(load_library().dar_cache_evict(cache.struct, _ptr(weights), _ptr(keep), _ptr(protect), _ptr(workspace),
                                           workspace.numel() * workspace.element_size(), _stream(stream)))
 

@@ -257,6 +257,36 @@ def test_same_bits_eager_captured_and_on_another_stream(dtype):
         assert all(torch.equal(a, b) for a, b in zip((out1, out2, weights), want))
 
 
+def test_a_cache_without_pages_and_an_empty_batch():
+    c = dar.DarCache(3, 2, 16, 30, 0)
+    k, v = (torch.randn((3, 2, 30, 64), device="cuda").bfloat16() for _ in range(2))
+    D = torch.zeros((2, 64, 16), device="cuda")
+    dar.dar_cache_append(c, k, v, D, D, n_per_seq=ints([30, 0, 7]))
+    q, Uk, Uv = R.operands(4, "bf16", 3, 4, 2, 16)
+    # (rows that were never written are zero here, not NaN: the cache is the library's own)
+    got = dar.dar_attn_decode_shared(c, q, Uk, Uv, ints([0, 0, 0]), ints([0]), dar.shared_decode_workspace(c, 4))
+
+    def empty_contents(b):
+        L = int(c.seq_lens[b])
+        none = torch.zeros((2, 0, 16), dtype=torch.float64)
+        return none, none, c.win_k[b, :, :L].cpu().double(), c.win_v[b, :, :L].cpu().double()
+    weights = dar.attention_weights(c)
+    assert weights.shape == (3, 2, 30)
+    same = dar.dar_attn_decode_scored(c, q, Uk, Uv, weights, dar.scored_decode_workspace(c, 4))
+    for b in (0, 2):
+        out, p, mag, top = R.attend(q[b].cpu().double(), *empty_contents(b), Uk.cpu().double(), Uv.cpu().double())
+        tol = R.tolerances("bf16", out, mag, top)
+        assert ((got[b].cpu().double() - out).abs() <= tol).all() and ((same[b].cpu().double() - out).abs() <= tol).all()
+    assert not got[1].any() and not weights[1].any()
+    dar.dar_cache_evict(c, weights, ints([0, 0, 0]), dar.evict_workspace(c))
+    assert c.seq_lens.tolist() == [30, 0, 7] and c.device_status() == 0
+    e = dar.DarCache(0, 2, 16, 30, 4)
+    q0 = torch.zeros((0, 4, 64), dtype=torch.bfloat16, device="cuda")
+    assert dar.dar_attn_decode_shared(e, q0, Uk, Uv, ints([]), ints([]), dar.shared_decode_workspace(e, 4)).shape == q0.shape
+    dar.dar_attn_decode_scored(e, q0, Uk, Uv, dar.attention_weights(e), dar.scored_decode_workspace(e, 4))
+    dar.dar_cache_evict(e, dar.attention_weights(e), ints([]), dar.evict_workspace(e))
+
+
 def test_operands_are_checked():
     c, _ = R.filled_cache(dar, 3, "bf16", 2, 16, 40, [100, 200])
     q, Uk, Uv = R.operands(4, "bf16", 2, 4, 2, 16)
