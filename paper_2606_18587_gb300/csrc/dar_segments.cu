@@ -68,7 +68,7 @@ template <typename T>
 __host__ __device__ inline int row_warps(int nr) { return nr <= rpw<T>() ? 1 : nr <= 2 * rpw<T>() ? 2 : 4; }
 
 // Cost of a prefix stage for nr rows, in quarters of a private stage.  (bf16, three CTAs on an SM: about 2000
-// cycles a private stage where HBM feeds it and 1400 where other CTAs are busy with a prefix, 4450 a prefix
+// cycles a private stage where HBM feeds it and 1400 where other CTAs are busy with a prefix, 4030 a prefix
 // stage of 64 rows.  fp32: by the rows of a warp.)
 template <typename T>
 __host__ __device__ inline int prefix_cost(int nr)
@@ -739,8 +739,28 @@ struct Soft {
     }
 };
 
-// Turns the scores of a step into weights relative to the running maximum of their row.  BYKEY: the layout of
-// cut8, s[i] = (key, row 0), (key, row 1), (key + 8, row 0), (key + 8, row 1); else that of cut16, rows 0 0 1 1.
+// Scores into weights relative to the reference of their row, and their sums.  BYKEY: the layout of cut8, s[i] =
+// (key, row 0), (key, row 1), (key + 8, row 0), (key + 8, row 1); else that of cut16, rows 0 0 1 1.
+template <int TILES, bool BYKEY>
+__device__ __forceinline__ void weigh(float (&s)[TILES][4], float c2, Soft &f)
+{
+    // pairs of scores that lie in consecutive registers: two rows of a key, or two keys of a row
+    const float b0 = f.bias[0], b1 = f.bias[1];
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+        float x0, x1, y0, y1;
+        ffma2(x0, x1, s[i][0], s[i][1], c2, c2, b0, BYKEY ? b1 : b0);
+        ffma2(y0, y1, s[i][2], s[i][3], c2, c2, BYKEY ? b0 : b1, b1);
+        s[i][0] = ex2_approx(x0);
+        s[i][1] = ex2_approx(x1);
+        s[i][2] = ex2_approx(y0);
+        s[i][3] = ex2_approx(y1);
+        add2(f.l[0][0], f.l[0][1], f.l[0][0], f.l[0][1], s[i][0], s[i][1]);
+        add2(f.l[1][0], f.l[1][1], f.l[1][0], f.l[1][1], s[i][2], s[i][3]);
+    }
+}
+
+// The same relative to the running maximum of the row, which the step may raise.
 // rescale(f0, f1): what was summed against the old maxima.
 template <int TILES, bool BYKEY, typename Rescale>
 __device__ __forceinline__ void soft_step(float (&s)[TILES][4], float c2, Soft &f, const Rescale &rescale)
@@ -774,20 +794,7 @@ __device__ __forceinline__ void soft_step(float (&s)[TILES][4], float c2, Soft &
         f.bias[0] = m0 == -INFINITY ? 0.f : -m0;
         f.bias[1] = m1 == -INFINITY ? 0.f : -m1;
     }
-    // pairs of scores that lie in consecutive registers: two rows of a key, or two keys of a row
-    const float b0 = f.bias[0], b1 = f.bias[1];
-#pragma unroll
-    for (int i = 0; i < TILES; ++i) {
-        float x0, x1, y0, y1;
-        ffma2(x0, x1, s[i][0], s[i][1], c2, c2, b0, BYKEY ? b1 : b0);
-        ffma2(y0, y1, s[i][2], s[i][3], c2, c2, BYKEY ? b0 : b1, b1);
-        s[i][0] = ex2_approx(x0);
-        s[i][1] = ex2_approx(x1);
-        s[i][2] = ex2_approx(y0);
-        s[i][3] = ex2_approx(y1);
-        add2(f.l[0][0], f.l[0][1], f.l[0][0], f.l[0][1], s[i][0], s[i][1]);
-        add2(f.l[1][0], f.l[1][1], f.l[1][0], f.l[1][1], s[i][2], s[i][3]);
-    }
+    weigh<TILES, BYKEY>(s, c2, f);
 }
 
 // Lane's place of an ldmatrix.x4 whose matrices are ordered keys first (0-7 and 8-15, then the next 8
@@ -802,16 +809,12 @@ __device__ __forceinline__ uint32_t lane_place(int lane)
     return (uint32_t)swz(key * ROW * 2 + 16 * half);
 }
 
-// Scores and value sums of NB blocks of 16 keys, rows on the M side.  Keys from ntok on (counted from the
-// step) do not count.  qa: KS products of 16 entries each; a key's entries repeat every ROW.
-template <int ROW, int KS, int NB, bool MASK, typename Keep, typename Rescale>
-__device__ __forceinline__ void step16(uint32_t base, int ntok, const uint32_t (&qa)[KS][4], float c2,
-                                       float (&acc)[ROW / 8][4], Soft &f, int lane, const Keep &keep,
-                                       const Rescale &rescale)
+// Scores of NB blocks of 16 keys, rows on the M side.  qa: KS products of 16 entries each; a key's entries
+// repeat every ROW.
+template <int ROW, int KS, int NB>
+__device__ __forceinline__ void scores16(uint32_t base, const uint32_t (&qa)[KS][4], float (&s)[2 * NB][4], int lane)
 {
-    const uint32_t lk = lane_place<ROW, false>(lane), lv = lane_place<ROW, true>(lane);
-    const int c0 = lane & 3;
-    float s[2 * NB][4];
+    const uint32_t lk = lane_place<ROW, false>(lane);
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
         if constexpr (ROW == 8) {  // both halves of the product's 16 entries are the key's 8
@@ -837,16 +840,15 @@ __device__ __forceinline__ void step16(uint32_t base, int ntok, const uint32_t (
             }
         }
     }
-    if constexpr (MASK) {
-#pragma unroll
-        for (int i = 0; i < 2 * NB; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (8 * i + 2 * c0 + (e & 1) >= ntok)
-                    s[i][e] = -INFINITY;
-    }
-    keep(s, !MASK);
-    soft_step<2 * NB, false>(s, c2, f, rescale);
+}
+
+// Value sums of the same keys with weights s.  Keys from ntok on (counted from the step) do not count.
+template <int ROW, int NB, bool MASK>
+__device__ __forceinline__ void sums16(uint32_t base, int ntok, const float (&s)[2 * NB][4], float (&acc)[ROW / 8][4],
+                                       int lane)
+{
+    const uint32_t lv = lane_place<ROW, true>(lane);
+    const int c0 = lane & 3;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
         // the weights as bf16 operands: 2^-8 of each at most, beside an output that is rounded as much
@@ -884,6 +886,28 @@ __device__ __forceinline__ void step16(uint32_t base, int ntok, const uint32_t (
             }
         }
     }
+}
+
+// Both, with the softmax between them.
+template <int ROW, int KS, int NB, bool MASK, typename Keep, typename Rescale>
+__device__ __forceinline__ void step16(uint32_t base, int ntok, const uint32_t (&qa)[KS][4], float c2,
+                                       float (&acc)[ROW / 8][4], Soft &f, int lane, const Keep &keep,
+                                       const Rescale &rescale)
+{
+    const int c0 = lane & 3;
+    float s[2 * NB][4];
+    scores16<ROW, KS, NB>(base, qa, s, lane);
+    if constexpr (MASK) {
+#pragma unroll
+        for (int i = 0; i < 2 * NB; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (8 * i + 2 * c0 + (e & 1) >= ntok)
+                    s[i][e] = -INFINITY;
+    }
+    keep(s, !MASK);
+    soft_step<2 * NB, false>(s, c2, f, rescale);
+    sums16<ROW, NB, MASK>(base, ntok, s, acc, lane);
 }
 
 // The same with up to 8 rows on the N side.  qb: B operands; acc: [16 entries][8 rows] tiles.
@@ -1218,9 +1242,12 @@ __device__ __forceinline__ void cut16(Consumer &w, const Cut &c)
     }
 }
 
-// A cut of a prefix unit.  (Two tiles of 16 rows a warp, which share what is loaded of a key: as many cycles a
-// score, and units twice as large to deal out.  The scores of the next step started before this one's are
-// exponentiated: 5850 cycles a stage instead of 4450.)
+// A cut of a prefix unit.  Bound: of a block of 16 x 16 scores the products take 48 cycles of an SM's quarter and
+// the rest of its instructions (8 exponentials, 4 conversions, 8 paired sums and products, 4 maxima) some 37,
+// which do not overlap: a loop of nothing else takes 85, without the maxima 71 (this kernel 84; 90 with them).
+// (Two tiles of 16 rows a warp, which share what is loaded of a key: as many cycles a score, and units twice as
+// large to deal out.  The scores of the next step started before this one's are exponentiated: 5850 cycles a
+// stage instead of 4450.  Four CTAs an SM: as many cycles a score.)
 template <int DD>
 __device__ __forceinline__ void cut_prefix(Consumer &w, const Cut &c)
 {
@@ -1250,15 +1277,36 @@ __device__ __forceinline__ void cut_prefix(Consumer &w, const Cut &c)
             od[j][3] *= f1;
         }
     };
+    // Once every row has seen a finite score, weights are taken relative to the maximum so far without looking
+    // for a new one: they and their sums stay exact far above 1, and only sums beyond kFar (an overflow's too)
+    // have the step done again with its maximum.
+    constexpr float kFar = 1.8446744e19f;  // 2^64
+    bool settled = false;
     for (int st = c.st0; st < c.st1; ++st) {
         const unsigned char *slot = w.take(lane);
         if (!slot)
             continue;
         const int k0 = kw * (TP / KW), k1 = min(c.tok1 - (c.tok0 + st * TP), k0 + TP / KW);
         uint32_t base = smem_u32(slot) + k0 * DD * 2;
-        for (int k = k0; k < k1; k += 16 * NB, base += 16 * NB * DD * 2)  // whole pages, and so whole steps
-            step16<DD, KS, NB, false>(base, 16 * NB, qt, a.c2, od, f, lane, [](const float (&)[2 * NB][4], bool) {},
-                                      rescale);
+        for (int k = k0; k < k1; k += 16 * NB, base += 16 * NB * DD * 2) {  // whole pages, and so whole steps
+            float s[2 * NB][4];
+            scores16<DD, KS, NB>(base, qt, s, lane);
+            const float l00 = f.l[0][0], l01 = f.l[0][1], l10 = f.l[1][0], l11 = f.l[1][1];
+            bool far = !settled;
+            if (settled) {
+                weigh<2 * NB, false>(s, a.c2, f);
+                far = fmaxf(fmaxf(f.l[0][0], f.l[0][1]), fmaxf(f.l[1][0], f.l[1][1])) > kFar;
+            }
+            if (__any_sync(0xffffffffu, far)) {
+                if (settled) {
+                    f.l[0][0] = l00, f.l[0][1] = l01, f.l[1][0] = l10, f.l[1][1] = l11;
+                    scores16<DD, KS, NB>(base, qt, s, lane);
+                }
+                soft_step<2 * NB, false>(s, a.c2, f, rescale);
+                settled = __all_sync(0xffffffffu, f.ms[0] > -INFINITY && f.ms[1] > -INFINITY);
+            }
+            sums16<DD, NB, false>(base, 16 * NB, s, od, lane);
+        }
         w.give(lane);
     }
 #pragma unroll

@@ -89,6 +89,25 @@ def test_shared_peaked_scores():
     check_outputs("bf16", c, full, q, Uk, Uv, got)
 
 
+@pytest.mark.parametrize("dd,growth", [(16, 3.0), (16, 40.0), (8, 10.0), (64, 10.0), (32, -1.0)])
+def test_shared_scores_that_rise_along_the_prefix(dd, growth):
+    """Weights are taken relative to a maximum that is raised only when sums get far: keys that grow by page raise
+    it again and again; growth -1: the first pages score the lowest numbers there are, the last ordinary ones."""
+    lens, group, pages = [900, 950, 1000, 980, 990], [0] * 5, [13]
+    c, full = R.filled_cache(dar, 3, "bf16", 2, dd, 40, lens, group, pages)
+    q, Uk, Uv = R.operands(4, "bf16", 5, 8, 2, dd)
+    for i, pg in enumerate(full[0][:13]):
+        if growth > 0:
+            c.pool_kd[pg] *= 1.0 + growth * i
+        elif i < 11:
+            # k^D = -M sum over the heads' and rows' q~: a large negative score for every row
+            qt = torch.einsum("bhd,hed->bhe", q.float().view(5, 2, 4, 64).sum(2), Uk).mean(0)
+            c.pool_kd[pg] = (-1e3 * qt / qt.norm(dim=-1, keepdim=True)).bfloat16()[:, None]
+    got = dar.dar_attn_decode_shared(c, q, Uk, Uv, ints(group), ints(pages), dar.shared_decode_workspace(c, 8))
+    torch.cuda.synchronize()
+    check_outputs("bf16", c, full, q, Uk, Uv, got)
+
+
 def test_shared_reads_only_the_first_members_entries_of_the_prefix():
     """filled_cache leaves -1 in the others' tables; entries that name other pages change nothing either."""
     lens, group, pages = [500, 520, 540], [0, 0, 0], [5]
