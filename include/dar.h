@@ -200,7 +200,11 @@ dar_status dar_attn_decode_noalloc(const dar_cache *cache, int32_t Hq, const voi
  * 0 .. 64 prefix_pages[i] - 1.  Results are those of dar_attn_decode; the shared
  * pages are read once per group and KV head instead of once per member, with the
  * members' queries as the rows of one product, and joined with each sequence's
- * own part by log-sum-exp (one softmax, Eq. 4).
+ * own part by log-sum-exp (one softmax, Eq. 4).  Scores, maxima and sums are fp32.
+ *  - bf16: operands of the products are bf16 terms.  Where dar_attn_decode keeps q~
+ *    and the weights of distant tokens in fp32 (Hq / Hkv odd at d_down 16, any at
+ *    d_down 8), three of q~ (2^-24 of it) and two of a weight (2^-15); elsewhere two
+ *    of q~ (2^-16) and one of a weight (2^-8), where dar_attn_decode has one of each.
  *  - The shared pages' ids are taken from the block table of a group's first
  *    member; the others' entries for them are not read.
  *  - A member for which some of them are not distant yet
@@ -234,7 +238,8 @@ dar_status dar_attn_decode_shared(const dar_cache *cache, int32_t Hq, const void
  * later finds a zero: dar_cache_evict leaves zeros behind the new end).
  * 0 <= decay <= 1; decay = 1 accumulates over all steps, and decay = 0 keeps this
  * step's weights alone, whatever was there.  out is that of dar_attn_decode.
- * Scores, maxima and sums are fp32 (bf16: q~ as three bf16 terms, 2^-24 of it).
+ * Scores, maxima and sums are fp32 (bf16: q~ as three bf16 terms, 2^-24 of it, and
+ * weights as two, 2^-15, in the value sums).
  * Arguments, sizes, alignment (weights too) and errors otherwise as
  * dar_attn_decode; Hq / Hkv <= 1024.  For a sequence with a bad length or page,
  * out and its weights are undefined.  Two kernels in order on `stream`, the first

@@ -871,8 +871,42 @@ __device__ __forceinline__ void scores16(uint32_t base, const uint32_t (&qa)[KS]
     }
 }
 
-// Value sums of the same keys with weights s.  Keys from ntok on (counted from the step) do not count.
-template <int ROW, int NB, bool MASK>
+// Two weights as WT bf16 terms.  One: rounded, 2^-8.  Two: x = t0 + t1 but for 2^-15, t0 cut off so that both have
+// x's sign, and 2^-22 of x added so that t1 is never 0: an infinite value keeps its sign (t0 inf + t1 inf), where a
+// zero or a negative remainder would make it NaN.
+template <int WT>
+__device__ __forceinline__ void weight_terms(float x, float y, uint32_t (&t)[WT])
+{
+    if constexpr (WT == 1) {
+        t[0] = cvt_bf16x2(x, y);
+    } else {
+        constexpr float kUp = 1.f + 0x1p-22f;
+        const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+        t[0] = __byte_perm(a, b, 0x7632);
+        t[1] = cvt_bf16x2(fmaf(x, kUp, -__uint_as_float(a & 0xffff0000u)), fmaf(y, kUp, -__uint_as_float(b & 0xffff0000u)));
+    }
+}
+
+// The weights of 16 keys as WT A operands (see Shape).
+template <int WT>
+__device__ __forceinline__ void weights16(const float (&s0)[4], const float (&s1)[4], uint32_t (&p)[WT][4])
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t t0[WT], t1[WT];
+        weight_terms<WT>(s0[2 * h], s0[2 * h + 1], t0);
+        weight_terms<WT>(s1[2 * h], s1[2 * h + 1], t1);
+#pragma unroll
+        for (int y = 0; y < WT; ++y) {
+            p[y][h] = t0[y];
+            p[y][2 + h] = t1[y];
+        }
+    }
+}
+
+// Value sums of the same keys with weights s, of which WT bf16 terms are operands.  Keys from ntok on (counted from
+// the step) do not count.
+template <int ROW, int NB, bool MASK, int WT>
 __device__ __forceinline__ void sums16(uint32_t base, int ntok, const float (&s)[2 * NB][4], float (&acc)[ROW / 8][4],
                                        int lane)
 {
@@ -880,10 +914,8 @@ __device__ __forceinline__ void sums16(uint32_t base, int ntok, const float (&s)
     const int c0 = lane & 3;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-        // the weights as bf16 operands: 2^-8 of each at most, beside an output that is rounded as much
-        const uint32_t p[4] = {cvt_bf16x2(s[2 * i][0], s[2 * i][1]), cvt_bf16x2(s[2 * i][2], s[2 * i][3]),
-                               cvt_bf16x2(s[2 * i + 1][0], s[2 * i + 1][1]),
-                               cvt_bf16x2(s[2 * i + 1][2], s[2 * i + 1][3])};
+        uint32_t p[WT][4];
+        weights16<WT>(s[2 * i], s[2 * i + 1], p);
         uint32_t mk0 = ~0u, mk1 = ~0u;  // bytes behind the last key must not reach a sum: 0 * NaN is NaN
         if constexpr (MASK) {
             mk0 = key_mask(16 * i + 2 * c0, ntok);
@@ -893,32 +925,36 @@ __device__ __forceinline__ void sums16(uint32_t base, int ntok, const float (&s)
             if (i % 2 == 0) {
                 uint32_t v[4];
                 ldsm_x4_t(frag<ROW>(base + kHalf, lv, i, 0), v);
-                const uint32_t p2[4] = {cvt_bf16x2(s[2 * i + 2][0], s[2 * i + 2][1]),
-                                        cvt_bf16x2(s[2 * i + 2][2], s[2 * i + 2][3]),
-                                        cvt_bf16x2(s[2 * i + 3][0], s[2 * i + 3][1]),
-                                        cvt_bf16x2(s[2 * i + 3][2], s[2 * i + 3][3])};
+                uint32_t p2[WT][4];
+                weights16<WT>(s[2 * i + 2], s[2 * i + 3], p2);
                 uint32_t mk2 = ~0u, mk3 = ~0u;
                 if constexpr (MASK) {
                     mk2 = key_mask(16 * i + 16 + 2 * c0, ntok);
                     mk3 = key_mask(16 * i + 24 + 2 * c0, ntok);
                 }
-                mma_bf16_acc(acc[0], p, v[0] & mk0, v[1] & mk1);
-                mma_bf16_acc(acc[0], p2, v[2] & mk2, v[3] & mk3);
+#pragma unroll
+                for (int y = 0; y < WT; ++y) {
+                    mma_bf16_acc(acc[0], p[y], v[0] & mk0, v[1] & mk1);
+                    mma_bf16_acc(acc[0], p2[y], v[2] & mk2, v[3] & mk3);
+                }
             }
         } else {
 #pragma unroll
             for (int e = 0; e < ROW / 16; ++e) {
                 uint32_t v[4];
                 ldsm_x4_t(frag<ROW>(base + kHalf, lv, i, e), v);
-                mma_bf16_acc(acc[2 * e], p, v[0] & mk0, v[1] & mk1);
-                mma_bf16_acc(acc[2 * e + 1], p, v[2] & mk0, v[3] & mk1);
+#pragma unroll
+                for (int y = 0; y < WT; ++y) {
+                    mma_bf16_acc(acc[2 * e], p[y], v[0] & mk0, v[1] & mk1);
+                    mma_bf16_acc(acc[2 * e + 1], p[y], v[2] & mk0, v[3] & mk1);
+                }
             }
         }
     }
 }
 
 // Both, with the softmax between them.
-template <int ROW, int KS, int NB, bool MASK, typename Keep, typename Rescale>
+template <int ROW, int KS, int NB, bool MASK, int WT, typename Keep, typename Rescale>
 __device__ __forceinline__ void step16(uint32_t base, int ntok, const uint32_t (&qa)[KS][4], float c2,
                                        float (&acc)[ROW / 8][4], Soft &f, int lane, const Keep &keep,
                                        const Rescale &rescale)
@@ -936,11 +972,25 @@ __device__ __forceinline__ void step16(uint32_t base, int ntok, const uint32_t (
     }
     keep(s, !MASK);
     soft_step<2 * NB, false>(s, c2, f, rescale);
-    sums16<ROW, NB, MASK>(base, ntok, s, acc, lane);
+    sums16<ROW, NB, MASK, WT>(base, ntok, s, acc, lane);
+}
+
+// The weights of 16 keys as WT B operands.
+template <int WT>
+__device__ __forceinline__ void weights8(const float (&s)[4], uint32_t (&p)[WT][2])
+{
+    uint32_t t0[WT], t1[WT];
+    weight_terms<WT>(s[0], s[1], t0);
+    weight_terms<WT>(s[2], s[3], t1);
+#pragma unroll
+    for (int y = 0; y < WT; ++y) {
+        p[y][0] = transpose8(t0[y]);
+        p[y][1] = transpose8(t1[y]);
+    }
 }
 
 // The same with up to 8 rows on the N side.  qb: B operands; acc: [16 entries][8 rows] tiles.
-template <int ROW, int KS, int NB, bool MASK, typename Keep, typename Rescale>
+template <int ROW, int KS, int NB, bool MASK, int WT, typename Keep, typename Rescale>
 __device__ __forceinline__ void step8(uint32_t base, int ntok, const uint32_t (&qb)[KS][2], float c2,
                                       float (&acc)[(ROW + 15) / 16][4], Soft &f, int lane, const Keep &keep,
                                       const Rescale &rescale)
@@ -984,8 +1034,8 @@ __device__ __forceinline__ void step8(uint32_t base, int ntok, const uint32_t (&
     soft_step<NB, true>(s, c2, f, rescale);
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-        // weights rounded as in step16
-        const uint32_t p0 = transpose8(cvt_bf16x2(s[i][0], s[i][1])), p1 = transpose8(cvt_bf16x2(s[i][2], s[i][3]));
+        uint32_t p[WT][2];
+        weights8<WT>(s[i], p);
         uint32_t mk0 = ~0u, mk1 = ~0u;
         if constexpr (MASK) {
             mk0 = key_mask(16 * i + 2 * c0, ntok);
@@ -1000,9 +1050,13 @@ __device__ __forceinline__ void step8(uint32_t base, int ntok, const uint32_t (&
                     mk3 = key_mask(16 * i + 24 + 2 * c0, ntok);
                 }
                 const uint32_t va[4] = {v[0] & mk0, 0u, v[1] & mk1, 0u}, vb[4] = {v[2] & mk2, 0u, v[3] & mk3, 0u};
-                mma_bf16_acc(acc[0], va, p0, p1);
-                mma_bf16_acc(acc[0], vb, transpose8(cvt_bf16x2(s[i + 1][0], s[i + 1][1])),
-                             transpose8(cvt_bf16x2(s[i + 1][2], s[i + 1][3])));
+                uint32_t p2[WT][2];
+                weights8<WT>(s[i + 1], p2);
+#pragma unroll
+                for (int y = 0; y < WT; ++y) {
+                    mma_bf16_acc(acc[0], va, p[y][0], p[y][1]);
+                    mma_bf16_acc(acc[0], vb, p2[y][0], p2[y][1]);
+                }
             }
         } else {
 #pragma unroll
@@ -1010,7 +1064,9 @@ __device__ __forceinline__ void step8(uint32_t base, int ntok, const uint32_t (&
                 uint32_t v[4];
                 ldsm_x4_t(frag<ROW>(base + kHalf, lv, i, e), v);
                 const uint32_t vm[4] = {v[0] & mk0, v[1] & mk0, v[2] & mk1, v[3] & mk1};
-                mma_bf16_acc(acc[e], vm, p0, p1);
+#pragma unroll
+                for (int y = 0; y < WT; ++y)
+                    mma_bf16_acc(acc[e], vm, p[y][0], p[y][1]);
             }
         }
     }
@@ -1049,12 +1105,18 @@ struct Consumer {
     }
 };
 
-// Steps of a page stage (of 16 * NBP keys) and of a ring stage, and products of a global score.  q~ in bf16
-// terms: two leave 2^-16 of it, beside weights rounded to 2^-8; weights that are results take three.
-template <int DD, bool SCORED>
+// Steps of a page stage (of 16 * NBP keys) and of a ring stage, products of a global score, and the bf16 terms of q~
+// (NT) and of the weights in the value sums (WT).  FINE: three leave 2^-24 of q~ and two 2^-15 of a weight, so that
+// nothing shows beside the output's own rounding; where dar_attn_decode has fp32 weights and q~ (one query head a
+// slice at d_down 16, and d_down 8), and in scored steps, whose weights are results.  Elsewhere dar_attn_decode rounds
+// q~ and the weights to one term; here q~ has two and the weights one (2^-8), which a second one would make exact at
+// 39 -> 50 us for 64 sequences behind 32512 shared tokens and 33.7 -> 40 behind four prompts (four heads per KV head).
+// FINE costs 16.0 -> 17.3 us for 32 samples of a prompt of 4000 tokens, 12 heads, and 29.8 -> 34.7 us for 64 sequences
+// behind 16256 shared tokens, 16 heads; scored steps, bound by HBM, 28.6 -> 29.2 us and 155.6 -> 154.
+template <int DD, bool FINE>
 struct Shape {
     static constexpr int TW = ring_tokens<bf16>(), TP = page_tokens<bf16, DD>();
-    static constexpr int NT = SCORED ? 3 : 2;
+    static constexpr int NT = FINE ? 3 : 2, WT = FINE ? 2 : 1;
     static constexpr int KS = DD == 8 ? (NT + 1) / 2 : NT * DD / 16;
     static constexpr int NBP = TP / kWarps >= 64 ? 4 : TP / kWarps / 16, NBW = TW / kWarps / 16;
 };
@@ -1137,10 +1199,10 @@ __device__ __forceinline__ void absorbed16(const Args &a, int g, const uint32_t 
 }
 
 // A cut of a private unit.
-template <int DD, bool SCORED>
+template <int DD, bool SCORED, bool FINE>
 __device__ __forceinline__ void cut16(Consumer &w, const Cut &c)
 {
-    using S = Shape<DD, SCORED>;
+    using S = Shape<DD, FINE>;
     constexpr int TW = S::TW, TP = S::TP, NT = S::NT, KS = S::KS, NBP = S::NBP, NBW = S::NBW, kR = unit_rows<bf16>();
     constexpr int NL = kHeadDim / 8;
     const Args &a = w.a;
@@ -1212,9 +1274,9 @@ __device__ __forceinline__ void cut16(Consumer &w, const Cut &c)
             };
             const uint32_t base = tile + k * kHeadDim * 2;
             if (k + 16 * NBW <= ntok)
-                step16<kHeadDim, 4, NBW, false>(base, ntok - k, qa, a.c2, ol, f, lane, keep, rescale);
+                step16<kHeadDim, 4, NBW, false, S::WT>(base, ntok - k, qa, a.c2, ol, f, lane, keep, rescale);
             else
-                step16<kHeadDim, 4, NBW, true>(base, ntok - k, qa, a.c2, ol, f, lane, keep, rescale);
+                step16<kHeadDim, 4, NBW, true, S::WT>(base, ntok - k, qa, a.c2, ol, f, lane, keep, rescale);
         }
         w.give(lane);
     }
@@ -1245,9 +1307,9 @@ __device__ __forceinline__ void cut16(Consumer &w, const Cut &c)
             };
             const uint32_t base = tile + k * DD * 2;
             if (k + 16 * NBP <= ntok)
-                step16<DD, KS, NBP, false>(base, ntok - k, qt, a.c2, od, f, lane, keep, rescale);
+                step16<DD, KS, NBP, false, S::WT>(base, ntok - k, qt, a.c2, od, f, lane, keep, rescale);
             else
-                step16<DD, KS, NBP, true>(base, ntok - k, qt, a.c2, od, f, lane, keep, rescale);
+                step16<DD, KS, NBP, true, S::WT>(base, ntok - k, qt, a.c2, od, f, lane, keep, rescale);
         }
         w.give(lane);
     }
@@ -1278,10 +1340,10 @@ __device__ __forceinline__ void cut16(Consumer &w, const Cut &c)
 // (Two tiles of 16 rows a warp, which share what is loaded of a key: as many cycles a score, and units twice as
 // large to deal out.  The scores of the next step started before this one's are exponentiated: 5850 cycles a
 // stage instead of 4450.  Four CTAs an SM: as many cycles a score.)
-template <int DD>
+template <int DD, bool FINE>
 __device__ __forceinline__ void cut_prefix(Consumer &w, const Cut &c)
 {
-    using S = Shape<DD, false>;
+    using S = Shape<DD, FINE>;
     constexpr int TP = S::TP, KS = S::KS, NB = S::NBP, kR = unit_rows<bf16>();
     const Args &a = w.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = lane & 3;
@@ -1335,7 +1397,7 @@ __device__ __forceinline__ void cut_prefix(Consumer &w, const Cut &c)
                 soft_step<2 * NB, false>(s, a.c2, f, rescale);
                 settled = __all_sync(0xffffffffu, f.ms[0] > -INFINITY && f.ms[1] > -INFINITY);
             }
-            sums16<DD, NB, false>(base, 16 * NB, s, od, lane);
+            sums16<DD, NB, false, S::WT>(base, 16 * NB, s, od, lane);
         }
         w.give(lane);
     }
@@ -1357,10 +1419,10 @@ __device__ __forceinline__ void cut_prefix(Consumer &w, const Cut &c)
 }
 
 // A private unit's cut of up to 8 rows; the four warps share its keys.
-template <int DD, bool SCORED>
+template <int DD, bool SCORED, bool FINE>
 __device__ __forceinline__ void cut8(Consumer &w, const Cut &c)
 {
-    using S = Shape<DD, SCORED>;
+    using S = Shape<DD, FINE>;
     constexpr int TW = S::TW, TP = S::TP, NT = S::NT, KS = S::KS, NBP = S::NBP, NBW = S::NBW, kR = unit_rows<bf16>();
     constexpr int ND = (DD + 15) / 16;
     const Args &a = w.a;
@@ -1473,9 +1535,9 @@ __device__ __forceinline__ void cut8(Consumer &w, const Cut &c)
         };
         const uint32_t base = smem_u32(slot) + k * kHeadDim * 2;
         if (16 * NBW <= ntok)
-            step8<kHeadDim, 4, NBW, false>(base, ntok, qb, a.c2, ol, f, lane, keep, rescale);
+            step8<kHeadDim, 4, NBW, false, S::WT>(base, ntok, qb, a.c2, ol, f, lane, keep, rescale);
         else if (ntok > 0)
-            step8<kHeadDim, 4, NBW, true>(base, ntok, qb, a.c2, ol, f, lane, keep, rescale);
+            step8<kHeadDim, 4, NBW, true, S::WT>(base, ntok, qb, a.c2, ol, f, lane, keep, rescale);
         w.give(lane);
     }
     for (; st < c.st1; ++st) {
@@ -1504,9 +1566,9 @@ __device__ __forceinline__ void cut8(Consumer &w, const Cut &c)
             };
             const uint32_t base = smem_u32(slot) + k * DD * 2;
             if (16 * NBP <= ntok)
-                step8<DD, KS, NBP, false>(base, ntok, qt, a.c2, od, f, lane, keep, rescale);
+                step8<DD, KS, NBP, false, S::WT>(base, ntok, qt, a.c2, od, f, lane, keep, rescale);
             else if (ntok > 0)
-                step8<DD, KS, NBP, true>(base, ntok, qt, a.c2, od, f, lane, keep, rescale);
+                step8<DD, KS, NBP, true, S::WT>(base, ntok, qt, a.c2, od, f, lane, keep, rescale);
         }
         w.give(lane);
     }
@@ -1536,8 +1598,8 @@ __device__ __forceinline__ void cut8(Consumer &w, const Cut &c)
     }
 }
 
-// SMALL: private units have at most 8 rows.
-template <int DD, bool SCORED, bool SMALL>
+// SMALL: private units have at most 8 rows.  FINE: see Shape.
+template <int DD, bool SCORED, bool SMALL, bool FINE>
 __device__ __forceinline__ void consume_mma(const Args &a, const Tables &t, const unsigned char *slots, uint64_t *full,
                                             uint64_t *empty, volatile int *gave_up)
 {
@@ -1545,16 +1607,16 @@ __device__ __forceinline__ void consume_mma(const Args &a, const Tables &t, cons
     Walk walk(t);
     for (Cut c; walk.next<bf16, DD>(a, t, c);) {
         if (!SCORED && c.grp >= 0) {
-            cut_prefix<DD>(w, c);
+            cut_prefix<DD, FINE>(w, c);
         } else if constexpr (SMALL) {
-            cut8<DD, SCORED>(w, c);
+            cut8<DD, SCORED, FINE>(w, c);
         } else {
-            cut16<DD, SCORED>(w, c);
+            cut16<DD, SCORED, FINE>(w, c);
         }
     }
 }
 
-template <typename T, int DD, bool SCORED, bool SMALL>
+template <typename T, int DD, bool SCORED, bool SMALL, bool FINE>
 __global__ void __launch_bounds__(kThreads, SMALL ? 3 : 1) segments_kernel(const __grid_constant__ CUtensorMap m_wk,
                                                             const __grid_constant__ CUtensorMap m_wv,
                                                             const __grid_constant__ CUtensorMap m_pk,
@@ -1685,7 +1747,7 @@ __global__ void __launch_bounds__(kThreads, SMALL ? 3 : 1) segments_kernel(const
 
     // ---- four warps consume them
     if constexpr (sizeof(T) == 2)
-        consume_mma<DD, SCORED, SMALL>(a, t, slots, full, empty, gave_up);
+        consume_mma<DD, SCORED, SMALL, FINE>(a, t, slots, full, empty, gave_up);
     else
         consume_lanes<T, DD, SCORED>(a, t, slots, reinterpret_cast<float *>(rows_at), full, empty, gave_up);
 }
@@ -1990,7 +2052,7 @@ static Layout layout(int B, int Hq, int Hkv, int dd, int w, int maxp, bool score
     return y;
 }
 
-template <typename T, int DD, bool SCORED, bool SMALL>
+template <typename T, int DD, bool SCORED, bool SMALL, bool FINE>
 static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t st)
 {
     const Layout y = layout<T>(s.B, s.Hq, s.Hkv, DD, s.w, s.maxp, SCORED);
@@ -2037,7 +2099,7 @@ static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t 
     if (s.maxp > 0 && (!make_tma_2d_bf16(&pk, s.pool_kd, pool_lines, 64, box) ||
                        !make_tma_2d_bf16(&pv, s.pool_vd, pool_lines, 64, box)))
         return cudaErrorInvalidValue;
-    auto kern = segments_kernel<T, DD, SCORED, SMALL>;
+    auto kern = segments_kernel<T, DD, SCORED, SMALL, FINE>;
     // CTAs per SM by registers (once per device); by shared memory below
     static PerDeviceOnce once;
     int fit = 0, sms = 0, dev = 0;
@@ -2090,9 +2152,16 @@ static cudaError_t launch_t(const SegmentArgs &s, void *workspace, cudaStream_t 
 template <typename T, int DD, bool SCORED>
 static cudaError_t launch_rows(const SegmentArgs &s, void *ws, cudaStream_t st)
 {
-    if (sizeof(T) == 2 && s.Hq / s.Hkv <= 8)
-        return launch_t<T, DD, SCORED, sizeof(T) == 2>(s, ws, st);
-    return launch_t<T, DD, SCORED, false>(s, ws, st);
+    constexpr bool kMma = sizeof(T) == 2;
+    const int G = s.Hq / s.Hkv;
+    if constexpr (kMma && !SCORED && DD == 16) {  // dar_attn_decode takes an odd number of heads one by one
+        if (G % 2)
+            return G <= 8 ? launch_t<T, DD, SCORED, true, true>(s, ws, st)
+                          : launch_t<T, DD, SCORED, false, true>(s, ws, st);
+    }
+    constexpr bool kFine = kMma && (SCORED || DD == 8);
+    return kMma && G <= 8 ? launch_t<T, DD, SCORED, kMma, kFine>(s, ws, st)
+                          : launch_t<T, DD, SCORED, false, kFine>(s, ws, st);
 }
 
 template <typename T, bool SCORED>
