@@ -314,7 +314,9 @@ dar_status dar_attn_prefill(dar_dtype dtype, int32_t B, int32_t Hq, int32_t Hkv,
  * When the limit runs out it does what any kernel of this library does when a
  * wait gives up: writes DAR_ERR_DEVICE to *status (a device int32, first error
  * wins), waits for its own copy to land, releases its tensor memory and exits.
- * The device stays usable.  limit_us must lie in [1, 2000000].
+ * The device stays usable.  A second warp checks that its lanes agree on a wait that
+ * half of them give up (where they do not, *status stays as it is), which takes the
+ * limit once more.  limit_us must lie in [1, 2000000].
  */
 dar_status dar_check_bounded_wait(int32_t *status, uint32_t limit_us, void *stream);
 

@@ -628,7 +628,7 @@ __device__ __forceinline__ void consume_lanes(const Args &a, const Tables &t, co
         for (int st = c.st0; st < c.st1; ++st, ++n) {
             const int s = n % kStages;
             // a warp that gave up computes nothing more, but still meets the others at the barriers
-            if (!alive || !mbar_wait(&full[s], (unsigned)((n / kStages) & 1), gave_up)) {
+            if (!alive || !mbar_wait_warp(&full[s], (unsigned)((n / kStages) & 1), gave_up)) {
                 if (alive && lane == 0)
                     report(a.status, DAR_ERR_DEVICE);
                 alive = false;
@@ -1085,7 +1085,7 @@ struct Consumer {
     __device__ __forceinline__ const unsigned char *take(int lane)
     {
         const int s = taken % kStages;
-        if (!alive || !mbar_wait(&full[s], (unsigned)((taken / kStages) & 1), gave_up)) {
+        if (!alive || !mbar_wait_warp(&full[s], (unsigned)((taken / kStages) & 1), gave_up)) {
             if (alive && lane == 0)
                 report(a.status, DAR_ERR_DEVICE);
             alive = false;
@@ -1687,7 +1687,7 @@ __global__ void __launch_bounds__(kThreads, SMALL ? 3 : 1) segments_kernel(const
             int ids0 = -1, ids = -1;  // block-table entries ids0 .. ids0 + 31, one per lane
             for (int st = c.st0; st < c.st1; ++st, ++n) {
                 const int s = n % kStages;
-                if (n >= kStages && !mbar_wait(&empty[s], (unsigned)((n / kStages - 1) & 1), gave_up)) {
+                if (n >= kStages && !mbar_wait_warp(&empty[s], (unsigned)((n / kStages - 1) & 1), gave_up)) {
                     alive = false;
                     break;
                 }

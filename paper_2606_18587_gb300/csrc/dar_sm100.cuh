@@ -104,6 +104,14 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, unsigned parity, volati
     return false;
 }
 
+// The same by all lanes of a warp together, with one verdict: lanes time their waits alone, so near the limit some
+// can give up and others not, and a warp that parted there would not meet again at its next warp-wide instruction.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, unsigned parity, volatile int *abort,
+                                               unsigned long long limit_ns = kWaitLimitNs)
+{
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort, limit_ns)) != 0;
+}
+
 // ------------------------------------------------------------------ cp.async
 
 // One asynchronous 16-byte copy to shared memory (both addresses 16-byte aligned).

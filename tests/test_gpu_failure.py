@@ -42,3 +42,13 @@ def test_starved_wait_reports_device_error_and_context_survives():
     want = oracle.decode(wl.q_host, k, v, wl.lens, Dk, Uk, Dv, Uv, cfg.w, "bf16")
     assert np.abs(W.to_f64(W.download(out), "bf16") - want).max() <= 2e-2
     assert wl.cache.device_status() == 0
+
+
+def test_a_warp_has_one_verdict_on_a_wait():
+    """Half of a warp's lanes give up, then the barrier completes for the others: no lane may go on as if the wait had
+    succeeded.  The check leaves the status word alone where lanes part."""
+    for limit_us in (1, 300, 4000):
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        dar.dar_check_bounded_wait(status, limit_us)
+        torch.cuda.synchronize()
+        assert int(status.item()) == dar.DAR_ERR_DEVICE, limit_us
