@@ -205,6 +205,8 @@ dar_status dar_attn_decode_noalloc(const dar_cache *cache, int32_t Hq, const voi
  *    and the weights of distant tokens in fp32 (Hq / Hkv odd at d_down 16, any at
  *    d_down 8), three of q~ (2^-24 of it) and two of a weight (2^-15); elsewhere two
  *    of q~ (2^-16) and one of a weight (2^-8), where dar_attn_decode has one of each.
+ *    Weights of a prefix are summed relative to one that may be 2^20 below them, so
+ *    pool_vd entries beyond 2^104 there can make out infinite or NaN.
  *  - The shared pages' ids are taken from the block table of a group's first
  *    member; the others' entries for them are not read.
  *  - A member for which some of them are not distant yet

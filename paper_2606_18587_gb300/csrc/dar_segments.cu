@@ -1370,9 +1370,11 @@ __device__ __forceinline__ void cut_prefix(Consumer &w, const Cut &c)
         }
     };
     // Once every row has seen a finite score, weights are taken relative to the maximum so far without looking
-    // for a new one: they and their sums stay exact far above 1, and only sums beyond kFar (an overflow's too)
-    // have the step done again with its maximum.
-    constexpr float kFar = 1.8446744e19f;  // 2^64
+    // for a new one: they and their sums are as exact far above 1, and only sums beyond kFar (an overflow's too)
+    // have the step done again with its maximum.  A row's weights sum to 8 kFar at most (four lanes' two sums), so
+    // value sums are finite for values up to 2^104.  (64 sequences behind 32512 shared tokens: 39.3 us at scores of
+    // standard deviation 1 to 4, 41.9 at 12, where a tenth of the steps is done again.)
+    constexpr float kFar = 1048576.f;
     bool settled = false;
     for (int st = c.st0; st < c.st1; ++st) {
         const unsigned char *slot = w.take(lane);
