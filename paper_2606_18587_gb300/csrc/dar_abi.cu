@@ -231,6 +231,9 @@ dar_status prepare_segments(const dar_cache *cache, int32_t Hq, const void *q, c
         dar::segments_line_bound(cache->dtype, cache->B, Hq, cache->Hkv, cache->d_down, cache->w,
                                  cache->max_pages_per_seq) >= most)
         return fail(DAR_ERR_UNSUPPORTED, "cache too large for int32 line indices");
+    if (dar::segments_join_blocks(cache->B, Hq, cache->Hkv, cache->w, cache->max_pages_per_seq, scored) >= 2147483647.0)
+        return fail(DAR_ERR_UNSUPPORTED, "B=%d sequences of %d query and %d KV heads of this capacity are too many blocks",
+                    cache->B, Hq, cache->Hkv);
     const size_t need = dar::segments_workspace_bytes(cache->dtype, cache->B, Hq, cache->Hkv, cache->d_down, cache->w,
                                                       cache->max_pages_per_seq, scored);
     if (workspace_bytes < need)
@@ -445,10 +448,6 @@ dar_status dar_attn_decode_scored(const dar_cache *cache, int32_t Hq, const void
         return s;
     if (Hq / cache->Hkv > 1024)
         return fail(DAR_ERR_UNSUPPORTED, "%d query heads per KV head > 1024", Hq / cache->Hkv);
-    if ((double)cache->B * cache->Hkv * (((double)cache->max_pages_per_seq * DAR_PAGE_SIZE + cache->w) / 512.0 + 1.0) +
-            (double)cache->B * Hq >= 2147483647.0)
-        return fail(DAR_ERR_UNSUPPORTED, "B * Hkv=%d * %d heads of this capacity are too many blocks", cache->B,
-                    cache->Hkv);
     if (!(decay >= 0.f && decay <= 1.f))
         return fail(DAR_ERR_INVALID_ARG, "decay=%g (0 to 1)", (double)decay);
     if (empty)

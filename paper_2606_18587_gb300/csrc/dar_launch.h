@@ -177,6 +177,7 @@ struct SegmentArgs {
     float decay = 0.f;  // what the weights are multiplied by first
 };
 size_t segments_workspace_bytes(dar_dtype dt, int B, int Hq, int Hkv, int dd, int w, int maxp, bool scored);
+double segments_join_blocks(int B, int Hq, int Hkv, int w, int maxp, bool scored);
 double segments_line_bound(dar_dtype dt, int B, int Hq, int Hkv, int dd, int w, int maxp);
 cudaError_t launch_segments(dar_dtype dt, int dd, const SegmentArgs &s, void *workspace, cudaStream_t st);
 

@@ -2186,6 +2186,13 @@ size_t segments_workspace_bytes(dar_dtype dt, int B, int Hq, int Hkv, int dd, in
                          : seg::layout<bf16>(B, Hq, Hkv, dd, w, maxp, scored).total;
 }
 
+// Blocks of the joining kernel: one per output row and, scored, one per kJoinTokens tokens of a (sequence, KV head).
+double segments_join_blocks(int B, int Hq, int Hkv, int w, int maxp, bool scored)
+{
+    const long long chunks = scored ? ((long long)maxp * kPage + w + seg::kJoinTokens - 1) / seg::kJoinTokens : 0;
+    return (double)B * Hq + (double)B * Hkv * chunks;
+}
+
 // Upper bound of the line's length: every sequence at capacity, as private units and once more as
 // prefix units.
 double segments_line_bound(dar_dtype dt, int B, int Hq, int Hkv, int dd, int w, int maxp)

@@ -82,6 +82,27 @@ def test_scored_refuses(lib):
     assert b - a == 2 * 4 * 1024 * 64 * 4
 
 
+def test_the_joining_kernels_blocks_are_counted_as_they_are_launched(lib):
+    """One per output row, and of a scored step one per 2048 positions of a head: 2^31 of them are too many.  (None of
+    these calls gets as far as a launch: what comes after the count is refused.)"""
+    L = lib.load_library()
+
+    def scored(c, Hq):
+        return L.dar_attn_decode_scored(ctypes.byref(c), Hq, P, P, P, 0.0, P, 2.0, P, P, 1 << 42, None)
+
+    def shared(c, Hq):
+        return L.dar_attn_decode_shared(ctypes.byref(c), Hq, P, P, P, P, -1, P, 0.0, P, P, 1 << 42, None)
+    small = dict(d_down=8, w=1, max_pages_per_seq=1)  # capacity: 65 positions
+    # 2095000 heads, of 1024 rows and a block of weights each: 2^31 - 108648
+    assert scored(cache(lib, B=1000, Hkv=2095, **small), 2095 * 1024) == 1
+    assert "decay" in L.dar_last_error().decode()
+    assert scored(cache(lib, B=1024, Hkv=2046, **small), 2046 * 1024) == 1   # 2^31 - 2048
+    assert scored(cache(lib, B=1024, Hkv=2047, **small), 2047 * 1024) == 2   # 2^31 + 2^20 - 1024
+    assert "blocks" in L.dar_last_error().decode()
+    assert shared(cache(lib, B=1024, Hkv=2046, **small), 2046 * 1024) == 1   # rows alone: 2^31 - 2^21
+    assert shared(cache(lib, B=1024, Hkv=2048, **small), 2048 * 1024) == 2   # 2^31
+
+
 def test_evict_refuses(lib):
     L = lib.load_library()
 
