@@ -27,7 +27,8 @@
 // whose swaps are disjoint, one after the other.
 // A second kernel sets the lengths, which the clusters of other heads read before.
 // Bound: HBM for the rows that move and the weights, read once from there and then from
-// L2; short calls by the cluster's barriers.
+// L2; short calls, which a cluster of one block takes, by the selection's chain of scans and
+// barriers.
 #include <cooperative_groups.h>
 
 #include "dar_common.cuh"
@@ -539,7 +540,17 @@ cudaError_t launch_evict(const EvictArgs &a, void *workspace, cudaStream_t st)
     wk.window = reinterpret_cast<float *>(ws + y.window);
     wk.new_lens = reinterpret_cast<int32_t *>(ws + y.lens);
     const int heads = a.B * a.Hkv;
-    // blocks per head: enough of them to fill the GPU, each with a slice worth the cluster's barriers
+    // Blocks per head: enough of them to fill the GPU, each with a slice worth the cluster's barriers, by capacity (the
+    // lengths are on the device).  us a call that keeps half (w 128, rows of 32 bytes) with 1 / 2 / 4 / 8 blocks:
+    //   heads  tokens                                 heads  tokens
+    //       8    1024    9.5 / 13.0 / 13.4 / 14.5        96    8192   26.8 / 26.2 / 24.0 / 34.1
+    //       8    4096   16.6 / 16.8 / 15.0 / 14.6       152    8192   29.1 / 30.0 / 30.5 / 44.2
+    //       8    8192   23.6 / 21.6 / 18.3 / 15.5       152   32768    113 /   93 /   90 /   98
+    //       8   32768   82.0 / 53.4 / 37.3 / 29.5       304   32768    160 /  152 /  160 /  180
+    //      64    2048   13.5 / 15.2 / 16.5 / 18.5       512    2048   22.4 / 34.0 / 52.0 / 99.7
+    //      64    8192   26.0 / 24.0 / 22.2 / 21.8       512    8192   69.2 / 80.1 / 94.7 /  133
+    // The rule is within 1.5 us or 1 % of the best of the four, but for 2048 tokens, where one block is 1 to 4 us faster
+    // than two, and 4096 tokens of 152 and 304 heads, 6.5 and 3.3 us.
     int C = evict::kMaxCluster;
     while (C > 1 && (heads * C > 4 * kSms || a.maxp * kPage < 1024 * C))
         C /= 2;
