@@ -222,7 +222,8 @@ dar_status dar_attn_decode_noalloc(const dar_cache *cache, int32_t Hq, const voi
  * Arguments, sizes and alignment otherwise as dar_attn_decode; two kernels in
  * order on `stream`, the first after all earlier work on it.  Workspace of
  * dar_decode_shared_workspace_bytes(cache, Hq) bytes, no initialisation; calls
- * that share one must not overlap on the device.  Deterministic.
+ * that share one must not overlap on the device.  Deterministic.  It is made for bf16
+ * caches; on fp32 ones dar_attn_decode on the same tables is the faster call.
  */
 size_t dar_decode_shared_workspace_bytes(const dar_cache *cache, int32_t Hq);
 dar_status dar_attn_decode_shared(const dar_cache *cache, int32_t Hq, const void *q, const float *Uk,
