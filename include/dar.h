@@ -208,7 +208,7 @@ dar_status dar_attn_decode_noalloc(const dar_cache *cache, int32_t Hq, const voi
  *    Weights of a prefix are summed relative to one that may be 2^20 below them, so
  *    pool_vd entries beyond 2^104 there can make out infinite or NaN.
  *  - The shared pages' ids are taken from the block table of a group's first
- *    member; the others' entries for them are not read.
+ *    member that is not attended alone; the others' entries for them are not read.
  *  - A member for which some of them are not distant yet
  *    (seq_lens[b] - w < 64 prefix_pages[i]) is attended alone, by its own table.
  *  - group and prefix_pages are device arrays; both may be NULL when n_groups is 0.
