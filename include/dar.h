@@ -286,6 +286,88 @@ size_t dar_cache_evict_workspace_bytes(const dar_cache *cache);
 dar_status dar_cache_evict(const dar_cache *cache, float *weights, const int32_t *keep,
                            const int32_t *protect, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * A cache whose distant tokens are held in 4 bits: as dar_cache, but for the pages.
+ *
+ *  pool  [num_pages][Hkv][dar_q4_page_bytes(d_down)] bytes: the bottleneck vectors
+ *        k^D, v^D of 64 tokens.  16 consecutive entries of a vector (the 8 of a
+ *        d_down of 8) share a scale: with a the largest magnitude among them,
+ *          s = a / 7 rounded to 5 significant bits (nearest even; at most 1.125 * 2^125),
+ *          code = x / s rounded to the nearest whole number (even), within [-7, 7],
+ *        and 0 where s is 0; a group with an infinite or NaN entry is NaN as a whole.
+ *        What is stored is code * s, which is a bf16 number: it reads back exactly, and
+ *        is held by the same codes when it is written again (scales below 2^-126 aside).  x is the vector as a
+ *        dar_cache of this dtype holds it: Eq. 1 rounded once to T.  Where codes and
+ *        scales lie within a page is the library's own choice, and no part of the
+ *        interface.  20 bytes a token and KV head at d_down 16, keys and values
+ *        together, where bf16 takes 64.
+ *  win_k, win_v, block_table, seq_lens, status: as dar_cache.  A dar_cache_q4 and a
+ *        dar_cache of the same sizes may share them.
+ */
+typedef struct dar_cache_q4 {
+    dar_dtype dtype;
+    int32_t B, Hkv, d, d_down, w;
+    int32_t max_pages_per_seq;
+    int32_t num_pages;
+    void *win_k, *win_v;
+    void *pool;
+    int32_t *block_table;
+    int32_t *seq_lens;
+    int32_t *status;
+} dar_cache_q4;
+
+/* Bytes of a page of one KV head (a multiple of 256); 0 for a d_down that is not built. */
+size_t dar_q4_page_bytes(int32_t d_down);
+
+/*
+ * As dar_cache_append, with the vectors of the tokens that leave the window held in 4
+ * bits.  Tokens of a page that were there before keep their codes.
+ */
+dar_status dar_cache_append_q4(const dar_cache_q4 *cache, const void *k_new, const void *v_new,
+                               int32_t n, const int32_t *n_per_seq, const float *Dk,
+                               const float *Dv, void *stream);
+
+/*
+ * Pages of the storage type to 4 bits and back, for the distant tokens at positions
+ * [max(0, first[b]), seq_lens[b] - w) of every sequence (first: device int32[B], NULL = 0;
+ * a first[b] below 0 sets dst->status to DAR_ERR_INVALID_ARG and skips the sequence):
+ * contexts that dar_prefill_chunk has written, or that rest between two turns.
+ * pack reads src's pages and lengths and writes dst's pages, unpack the other way round;
+ * each by its own block table.  Nothing else is read or written: rings and lengths are
+ * shared or copied by the caller, and other tokens of the pages stay as they are.  Both
+ * caches have the same dtype, B, Hkv, d, d_down and w.  A length beyond either capacity,
+ * or a needed table entry of either that is no page, sets dst->status to
+ * DAR_ERR_CAPACITY and skips the sequence or the page.  A page of dst that several
+ * sequences list is written by all of them: the same bytes where src's tables share it too.
+ */
+dar_status dar_cache_pack_q4(const dar_cache *src, const int32_t *first, const dar_cache_q4 *dst,
+                             void *stream);
+dar_status dar_cache_unpack_q4(const dar_cache_q4 *src, const int32_t *first, const dar_cache *dst,
+                               void *stream);
+
+/*
+ * dar_attn_decode over such a cache: the same step on the values that the pages stand
+ * for.  Scales, scores, maxima and sums are fp32; codes are exact.  Arguments, alignment
+ * (pool too), limits and errors as dar_attn_decode; workspace of
+ * dar_decode_q4_workspace_bytes(cache, Hq) bytes, no initialisation; calls that share one
+ * must not overlap on the device.  Two kernels in order on `stream`, the first after all
+ * earlier work on it.  Deterministic.
+ */
+size_t dar_decode_q4_workspace_bytes(const dar_cache_q4 *cache, int32_t Hq);
+dar_status dar_attn_decode_q4(const dar_cache_q4 *cache, int32_t Hq, const void *q, const float *Uk,
+                              const float *Uv, float scale, void *out, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/*
+ * One serving step: dar_cache_append_q4 and then dar_attn_decode_q4, with the arguments,
+ * requirements and results of the two calls in turn; all arguments of both are checked
+ * before anything is launched.
+ */
+dar_status dar_decode_step_q4(const dar_cache_q4 *cache, const void *k_new, const void *v_new, int32_t n,
+                              const int32_t *n_per_seq, const float *Dk, const float *Dv, int32_t Hq,
+                              const void *q, const float *Uk, const float *Uv, float scale, void *out,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
 /* Bytes of workspace dar_attn_prefill needs (the Eq. 1 vectors of all tokens). */
 size_t dar_prefill_workspace_bytes(dar_dtype dtype, int32_t B, int32_t Hkv, int32_t N,
                                    int32_t d_down);

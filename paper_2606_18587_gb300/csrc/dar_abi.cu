@@ -259,6 +259,116 @@ dar_status prepare_segments(const dar_cache *cache, int32_t Hq, const void *q, c
     return ok();
 }
 
+// A 4-bit cache, checked as the ordinary one with the same rings, tables and sizes.
+dar_status check_cache_q4(const dar_cache_q4 *c)
+{
+    if (!c)
+        return fail(DAR_ERR_INVALID_ARG, "cache is NULL");
+    const dar_cache plain = {c->dtype, c->B, c->Hkv, c->d, c->d_down, c->w, c->max_pages_per_seq, c->num_pages,
+                             c->win_k, c->win_v, c->pool, c->pool, c->block_table, c->seq_lens, c->status};
+    return check_cache(&plain);
+}
+
+// Checks the arguments of dar_cache_append_q4 and fills *a; *empty = nothing to launch.
+dar_status prepare_append_q4(const dar_cache_q4 *c, const void *k_new, const void *v_new, int32_t n,
+                             const int32_t *n_per_seq, const float *Dk, const float *Dv, dar::AppendArgs *a,
+                             bool *empty)
+{
+    if (!c)
+        return fail(DAR_ERR_INVALID_ARG, "cache is NULL");
+    const dar_cache plain = {c->dtype, c->B, c->Hkv, c->d, c->d_down, c->w, c->max_pages_per_seq, c->num_pages,
+                             c->win_k, c->win_v, c->pool, c->pool, c->block_table, c->seq_lens, c->status};
+    const dar_status s = prepare_append(&plain, k_new, v_new, n, n_per_seq, Dk, Dv, a, empty);
+    // blocks of 64 tokens, which start where a page does
+    if (s == DAR_OK && !*empty && ((double)n + 126) / 64 * c->B * c->Hkv >= 2147483647.0)
+        return fail(DAR_ERR_UNSUPPORTED, "n=%d tokens of %lld heads are too many blocks", n, (long long)c->B * c->Hkv);
+    return s;
+}
+
+// Checks the arguments of dar_attn_decode_q4 and fills *a; *empty = nothing to launch.
+dar_status prepare_decode_q4(const dar_cache_q4 *c, int32_t Hq, const void *q, const float *Uk, const float *Uv,
+                             float scale, void *out, const void *workspace, size_t workspace_bytes,
+                             dar::Q4DecodeArgs *a, bool *empty)
+{
+    dar_status s = check_cache_q4(c);
+    if (s != DAR_OK)
+        return s;
+    if (Hq < c->Hkv || Hq % c->Hkv)
+        return fail(DAR_ERR_INVALID_ARG, "Hq=%d is not a multiple of Hkv=%d", Hq, c->Hkv);
+    if (c->B > DAR_DECODE_MAX_BATCH)
+        return fail(DAR_ERR_UNSUPPORTED, "decode batch %d > %d", c->B, DAR_DECODE_MAX_BATCH);
+    *empty = c->B == 0;
+    if (*empty)
+        return ok();
+    if (!q || !Uk || !Uv || !out || !workspace)
+        return fail(DAR_ERR_INVALID_ARG, "NULL pointer");
+    if (!aligned16(q) || !aligned16(out) || !aligned16(Uk) || !aligned16(Uv) || !aligned16(workspace))
+        return fail(DAR_ERR_INVALID_ARG, "q, out, Uk, Uv and workspace must be 16-byte aligned");
+    // the line of work, the rows of the ring and the output's are counted in int32
+    const double most = 2147483647.0 - 128.0;
+    if (dar::q4_decode_line_bound(c->B, Hq, c->Hkv, c->d_down, c->w, c->max_pages_per_seq) >= most ||
+        (double)c->B * c->Hkv * c->w * c->d * esize(c->dtype) / 128.0 >= most || (double)c->B * Hq >= most ||
+        (double)c->max_pages_per_seq * DAR_PAGE_SIZE + c->w >= most)
+        return fail(DAR_ERR_UNSUPPORTED, "cache too large for int32 indices");
+    const size_t need = dar::q4_decode_workspace_bytes(c->B, Hq, c->Hkv, c->d_down);
+    if (workspace_bytes < need)
+        return fail(DAR_ERR_CAPACITY, "workspace %zu bytes < %zu needed", workspace_bytes, need);
+    a->q = q;
+    a->out = out;
+    a->win_k = c->win_k;
+    a->win_v = c->win_v;
+    a->pool = c->pool;
+    a->block_table = c->block_table;
+    a->seq_lens = c->seq_lens;
+    a->status = c->status;
+    a->Uk = Uk;
+    a->Uv = Uv;
+    a->B = c->B;
+    a->Hq = Hq;
+    a->Hkv = c->Hkv;
+    a->w = c->w;
+    a->maxp = c->max_pages_per_seq;
+    a->num_pages = c->num_pages;
+    a->c2 = default_scale(scale, c->d) * kLog2e;
+    return ok();
+}
+
+// dar_cache_pack_q4 (pack) and dar_cache_unpack_q4.
+dar_status convert_q4(const dar_cache *t, const dar_cache_q4 *c, bool pack, const int32_t *first, void *stream)
+{
+    dar_status s = check_cache(t);
+    if (s == DAR_OK)
+        s = check_cache_q4(c);
+    if (s != DAR_OK)
+        return s;
+    if (t->dtype != c->dtype || t->B != c->B || t->Hkv != c->Hkv || t->d_down != c->d_down || t->w != c->w)
+        return fail(DAR_ERR_INVALID_ARG, "the caches differ: dtype %d/%d B=%d/%d Hkv=%d/%d d_down=%d/%d w=%d/%d",
+                    t->dtype, c->dtype, t->B, c->B, t->Hkv, c->Hkv, t->d_down, c->d_down, t->w, c->w);
+    const int pages = t->max_pages_per_seq < c->max_pages_per_seq ? t->max_pages_per_seq : c->max_pages_per_seq;
+    if ((double)pages * t->Hkv >= 2147483647.0)
+        return fail(DAR_ERR_UNSUPPORTED, "%d pages of %d heads a sequence are too many blocks", pages, t->Hkv);
+    if (t->B == 0)
+        return ok();
+    dar::Q4ConvertArgs a;
+    a.pool_kd = t->pool_kd;
+    a.pool_vd = t->pool_vd;
+    a.pool = c->pool;
+    a.table = t->block_table;
+    a.table4 = c->block_table;
+    a.seq_lens = pack ? t->seq_lens : c->seq_lens;
+    a.first = first;
+    a.status = pack ? c->status : t->status;
+    a.B = t->B;
+    a.Hkv = t->Hkv;
+    a.w = t->w;
+    a.maxp = t->max_pages_per_seq;
+    a.maxp4 = c->max_pages_per_seq;
+    a.num_pages = t->num_pages;
+    a.num_pages4 = c->num_pages;
+    return from_cuda(dar::launch_convert_q4(t->dtype, t->d_down, pack, a, static_cast<cudaStream_t>(stream)),
+                     pack ? "dar_cache_pack_q4 launch" : "dar_cache_unpack_q4 launch");
+}
+
 struct ChunkLayout {
     size_t pos0, kw, vw, kdt, vdt, total;
 };
@@ -508,6 +618,75 @@ dar_status dar_cache_evict(const dar_cache *cache, float *weights, const int32_t
     a.row_bytes = (int)(cache->d_down * esize(cache->dtype));
     a.ring_bytes = (int)(cache->d * esize(cache->dtype));
     return from_cuda(dar::launch_evict(a, workspace, static_cast<cudaStream_t>(stream)), "dar_cache_evict launch");
+}
+
+size_t dar_q4_page_bytes(int32_t d_down) { return dd_supported(d_down) ? dar::q4_page_bytes(d_down) : 0; }
+
+dar_status dar_cache_append_q4(const dar_cache_q4 *cache, const void *k_new, const void *v_new,
+                               int32_t n, const int32_t *n_per_seq, const float *Dk,
+                               const float *Dv, void *stream)
+{
+    dar::AppendArgs a;
+    bool empty = false;
+    const dar_status s = prepare_append_q4(cache, k_new, v_new, n, n_per_seq, Dk, Dv, &a, &empty);
+    if (s != DAR_OK || empty)
+        return s;
+    return from_cuda(dar::launch_append_q4(cache->dtype, cache->d_down, a, static_cast<cudaStream_t>(stream)),
+                     "dar_cache_append_q4 launch");
+}
+
+dar_status dar_cache_pack_q4(const dar_cache *src, const int32_t *first, const dar_cache_q4 *dst, void *stream)
+{
+    return convert_q4(src, dst, true, first, stream);
+}
+
+dar_status dar_cache_unpack_q4(const dar_cache_q4 *src, const int32_t *first, const dar_cache *dst, void *stream)
+{
+    return convert_q4(dst, src, false, first, stream);
+}
+
+size_t dar_decode_q4_workspace_bytes(const dar_cache_q4 *cache, int32_t Hq)
+{
+    if (check_cache_q4(cache) != DAR_OK || Hq < cache->Hkv || Hq % cache->Hkv)
+        return 0;
+    return dar::q4_decode_workspace_bytes(cache->B, Hq, cache->Hkv, cache->d_down);
+}
+
+dar_status dar_attn_decode_q4(const dar_cache_q4 *cache, int32_t Hq, const void *q, const float *Uk,
+                              const float *Uv, float scale, void *out, void *workspace,
+                              size_t workspace_bytes, void *stream)
+{
+    dar::Q4DecodeArgs a;
+    bool empty = false;
+    const dar_status s = prepare_decode_q4(cache, Hq, q, Uk, Uv, scale, out, workspace, workspace_bytes, &a, &empty);
+    if (s != DAR_OK || empty)
+        return s;
+    return from_cuda(dar::launch_decode_q4(cache->dtype, cache->d_down, a, workspace, static_cast<cudaStream_t>(stream)),
+                     "dar_attn_decode_q4 launch");
+}
+
+dar_status dar_decode_step_q4(const dar_cache_q4 *cache, const void *k_new, const void *v_new, int32_t n,
+                              const int32_t *n_per_seq, const float *Dk, const float *Dv, int32_t Hq,
+                              const void *q, const float *Uk, const float *Uv, float scale, void *out,
+                              void *workspace, size_t workspace_bytes, void *stream)
+{
+    // every argument of both operations is checked before anything is launched
+    dar::AppendArgs ap;
+    dar::Q4DecodeArgs dc;
+    bool app_empty = false, dec_empty = false;
+    dar_status s = prepare_append_q4(cache, k_new, v_new, n, n_per_seq, Dk, Dv, &ap, &app_empty);
+    if (s == DAR_OK)
+        s = prepare_decode_q4(cache, Hq, q, Uk, Uv, scale, out, workspace, workspace_bytes, &dc, &dec_empty);
+    if (s != DAR_OK || dec_empty)  // B = 0: nothing to append either
+        return s;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!app_empty) {
+        s = from_cuda(dar::launch_append_q4(cache->dtype, cache->d_down, ap, st), "dar_decode_step_q4 append launch");
+        if (s != DAR_OK)
+            return s;
+    }
+    return from_cuda(dar::launch_decode_q4(cache->dtype, cache->d_down, dc, workspace, st),
+                     "dar_decode_step_q4 decode launch");
 }
 
 size_t dar_prefill_chunk_workspace_bytes(const dar_cache *cache, int32_t n)

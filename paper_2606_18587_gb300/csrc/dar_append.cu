@@ -98,17 +98,6 @@ __host__ __device__ inline int app_rows(int Hkv)
     return r < 1 ? 1 : r > kAppRows ? kAppRows : r;
 }
 
-// Whether sequence lengths L and L + nb are ones an append can take (DAR_OK, or the status to report).
-__device__ __forceinline__ int append_error(int L, int nb, const AppendArgs &a)
-{
-    const long long Lnew = (long long)L + nb;
-    if (L < 0 || nb < 0 || nb > a.n)
-        return DAR_ERR_INVALID_ARG;
-    if (Lnew - a.w > (long long)a.maxp * kPage || Lnew > 0x7fffffffLL)
-        return DAR_ERR_CAPACITY;
-    return DAR_OK;
-}
-
 template <typename T, int DD>
 __device__ __forceinline__ void append_sequence(const AppendArgs &a)
 {

@@ -195,6 +195,33 @@ struct EvictArgs {
 size_t evict_workspace_bytes(int B, int Hkv, int w, int maxp);
 cudaError_t launch_evict(const EvictArgs &a, void *workspace, cudaStream_t st);
 
+// The cache whose pages hold 4 bits an entry (dar_q4.cuh): pages written by an append (AppendArgs::pool_kd is
+// the pool), converted from and to pages of the storage type (dar_q4_cache.cu), and attended (dar_q4_decode.cu).
+struct Q4ConvertArgs {
+    void *pool_kd, *pool_vd;        // [num_pages][Hkv][64][dd] T
+    void *pool;                     // [num_pages4][Hkv][bytes of a page]
+    const int32_t *table, *table4;  // block tables of either
+    const int32_t *seq_lens, *first;
+    int32_t *status;
+    int B, Hkv, w, maxp, maxp4, num_pages, num_pages4;
+};
+struct Q4DecodeArgs {
+    const void *q;
+    void *out;
+    const void *win_k, *win_v, *pool;
+    const int32_t *block_table, *seq_lens;
+    int32_t *status;
+    const float *Uk, *Uv;
+    int B, Hq, Hkv, w, maxp, num_pages;
+    float c2;  // scale * log2(e)
+};
+size_t q4_page_bytes(int dd);
+size_t q4_decode_workspace_bytes(int B, int Hq, int Hkv, int dd);
+double q4_decode_line_bound(int B, int Hq, int Hkv, int dd, int w, int maxp);
+cudaError_t launch_append_q4(dar_dtype dt, int dd, const AppendArgs &a, cudaStream_t s);
+cudaError_t launch_convert_q4(dar_dtype dt, int dd, bool pack, const Q4ConvertArgs &a, cudaStream_t s);
+cudaError_t launch_decode_q4(dar_dtype dt, int dd, const Q4DecodeArgs &a, void *workspace, cudaStream_t s);
+
 // Chunked prefill over a cache: gather kernel, attention (chunk mode), then
 // the cache append of the chunk.  Buffers of the workspace (see dar_abi.cu).
 struct ChunkArgs {

@@ -4,9 +4,21 @@
 #pragma once
 
 #include "dar_common.cuh"
+#include "dar_launch.h"
 #include "dar_sm100.cuh"
 
 namespace dar {
+
+// Whether sequence lengths L and L + nb are ones an append can take (DAR_OK, or the status to report).
+__device__ __forceinline__ int append_error(int L, int nb, const AppendArgs &a)
+{
+    const long long Lnew = (long long)L + nb;
+    if (L < 0 || nb < 0 || nb > a.n)
+        return DAR_ERR_INVALID_ARG;
+    if (Lnew - a.w > (long long)a.maxp * kPage || Lnew > 0x7fffffffLL)
+        return DAR_ERR_CAPACITY;
+    return DAR_OK;
+}
 
 // A CTA stages kStageBytesBulk of rows in shared memory, 16-byte chunk c of row
 // r at chunk c ^ (r & 7), so that a warp reading one chunk of 32 different rows

@@ -1,0 +1,277 @@
+// dar_q4_cache.cu -- writing the 4-bit pages of a cache (dar_q4.cuh) and reading
+// them back: the append of new tokens, and conversion of pages to and from the
+// storage type.
+#include <algorithm>
+#include <type_traits>
+
+#include "dar_common.cuh"
+#include "dar_launch.h"
+#include "dar_project.cuh"
+#include "dar_q4.cuh"
+#include "dar_sm100.cuh"
+
+namespace dar {
+namespace q4 {
+
+// ------------------------------------------------------------------ append
+//
+// As append_bulk_kernel (dar_append.cu): a CTA takes the new tokens j of one
+// (sequence, KV head, keys or values) that push positions m = L + j - w out of the
+// window, projects these (the same fp32 chains, rounded to T), and puts the tokens
+// that stay into the ring slots that they leave.  Its tile starts at a position that
+// is a multiple of a page, so that two tokens that share words of a page have the
+// same CTA; a thread then quantises and writes two tokens' group.
+template <typename T, int DD, int RPT, int NR>
+__global__ void __launch_bounds__(NR *slices<DD>()) append_kernel(AppendArgs a, int tiles)
+{
+    constexpr int R = RPT * NR, NT = NR * slices<DD>();
+    constexpr int CW = cols_per_thread<DD>();
+    constexpr int E = Granule<T>::kElems;
+    constexpr int CPR = kHeadDim / E;
+    using F = Fmt<DD>;
+    __shared__ __align__(16) unsigned char rows[R * kHeadDim * sizeof(T)];
+    __shared__ __align__(16) float Ws[kHeadDim * DD];
+    const int tid = threadIdx.x, kv = blockIdx.y;
+    const int bg = blockIdx.x / tiles;
+    const int b = bg / a.Hkv, g = bg % a.Hkv;
+    const int n = a.n, w = a.w;
+    const int L = a.seq_lens[b], nb = a.n_per_seq ? a.n_per_seq[b] : n;
+    if (append_error(L, nb, a) != DAR_OK)
+        return;
+    const int off = ((L - w) % kPage + kPage) % kPage;  // new token 0 pushes out a position this far into its page
+    const int j0 = (int)(blockIdx.x % tiles) * R - off;
+    if (j0 >= nb)
+        return;
+    const T *xnew = static_cast<const T *>(kv ? a.v_new : a.k_new) + (size_t)bg * n * kHeadDim;
+    T *ring = static_cast<T *>(kv ? a.win_v : a.win_k) + (size_t)bg * w * kHeadDim;
+    const int m0 = L + j0 - w;                     // a multiple of a page
+    const int ra = max(max(0, -j0), -m0), nr = min(R, nb - j0);  // rows [ra, nr) leave the window
+    if (ra < nr) {
+        const uint32_t rows_s = sm100::smem_u32(rows);
+        for (int i = tid; i < nr * CPR; i += NT) {
+            const int r = i / CPR, c = i % CPR, m = m0 + r;
+            if (r >= ra) {
+                const T *src = m < L ? ring + (size_t)(m % w) * kHeadDim : xnew + (size_t)(m - L) * kHeadDim;
+                sm100::cp_async16(rows_s + (r * CPR + (c ^ (r & 7))) * 16, src + c * E);
+            }
+        }
+        const float *W = (kv ? a.Dv : a.Dk) + (size_t)g * kHeadDim * DD;
+        for (int i = tid; i < kHeadDim * DD / 4; i += NT)
+            reinterpret_cast<float4 *>(Ws)[i] = __ldg(reinterpret_cast<const float4 *>(W) + i);
+        const int r0 = tid % NR, c0 = slices<DD>() > 1 ? tid / NR * CW : 0;  // this thread's rows r0 + k * NR and columns
+        sm100::cp_async_wait_all();
+        __syncthreads();  // every ring row this CTA reads is in shared memory
+        float acc[RPT][CW];
+        project_rows<T, DD, CW, RPT>(rows, Ws + c0, r0, NR, acc);  // (rows outside [ra, nr): of stale bytes, not used)
+        __syncthreads();
+        // the vectors, rounded to T, over the rows they come from
+        T *vec = reinterpret_cast<T *>(rows);
+#pragma unroll
+        for (int k = 0; k < RPT; ++k)
+            store_row<T, CW>(vec + (size_t)(r0 + k * NR) * DD + c0, acc[k]);
+        __syncthreads();
+        unsigned char *pool = static_cast<unsigned char *>(a.pool_kd);
+        for (int i = tid; i < R / 2 * F::kGroups; i += NT) {
+            const int r = 2 * (i % (R / 2)), sb = i / (R / 2);
+            const unsigned has = (r >= ra && r < nr ? 1u : 0u) | (r + 1 >= ra && r + 1 < nr ? 2u : 0u);
+            if (!has)
+                continue;
+            const int m = m0 + r, id = a.block_table[(size_t)b * a.maxp + m / kPage];
+            if (id < 0 || id >= a.num_pages) {
+                report(a.status, DAR_ERR_CAPACITY);
+                continue;
+            }
+            float x[F::kGroup];
+            int code0[F::kGroup], code1[F::kGroup];
+#pragma unroll
+            for (int e = 0; e < F::kGroup; ++e)
+                x[e] = to_f32(vec[(size_t)r * DD + sb * F::kGroup + e]);
+            const float s0 = quantise<F::kGroup>(x, code0);
+#pragma unroll
+            for (int e = 0; e < F::kGroup; ++e)
+                x[e] = to_f32(vec[(size_t)(r + 1) * DD + sb * F::kGroup + e]);
+            const float s1 = quantise<F::kGroup>(x, code1);
+            unsigned char *block = pool + ((size_t)id * a.Hkv + g) * F::kBytes + sb * F::kBlock;
+            if (kv)
+                write_pair<F::kGroup, true>(block, m % kPage, has, code0, code1, s0, s1);
+            else
+                write_pair<F::kGroup, false>(block, m % kPage, has, code0, code1, s0, s1);
+        }
+    }
+    // ring slots (L + j) % w, j < min(nb, w): the last new token of each
+    const int jr = max(0, j0), slots = min(min(nb, w), j0 + R) - jr;
+    for (int i = tid; i < slots * CPR; i += NT) {
+        const int c = i % CPR, j = jr + i / CPR, last = j + (nb - 1 - j) / w * w;
+        *reinterpret_cast<uint4 *>(ring + (size_t)((L + j) % w) * kHeadDim + c * E) =
+            *reinterpret_cast<const uint4 *>(xnew + (size_t)last * kHeadDim + c * E);
+    }
+}
+
+// Advances the lengths (and reports refused sequences) once every CTA of the append has read them.
+__global__ void append_lens(AppendArgs a)
+{
+    sm100::grid_dep_wait();
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b >= a.B)
+        return;
+    const int L = a.seq_lens[b], nb = a.n_per_seq ? a.n_per_seq[b] : a.n;
+    const int e = append_error(L, nb, a);
+    if (e != DAR_OK)
+        report(a.status, e);
+    else
+        a.seq_lens[b] = L + nb;
+}
+
+template <typename T, int DD, int RPT, int NR>
+static cudaError_t append_tiles(const AppendArgs &a, cudaStream_t s)
+{
+    const int tiles = (int)(((long long)a.n + kPage - 1 + RPT * NR - 1) / (RPT * NR));
+    append_kernel<T, DD, RPT, NR><<<dim3((unsigned)(a.B * a.Hkv * tiles), 2), NR * slices<DD>(), 0, s>>>(a, tiles);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess)
+        return e;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((a.B + 127) / 128);
+    cfg.blockDim = dim3(128);
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, append_lens, a);
+}
+
+// ------------------------------------------------------------------ conversion
+//
+// A warp takes a page of a (sequence, KV head), a lane two tokens, one group after the other.
+constexpr int kConvertWarps = 8;
+
+template <typename T, int GS>
+__device__ __forceinline__ void load_group(const T *p, float (&x)[GS])
+{
+    constexpr int E = Granule<T>::kElems;
+#pragma unroll
+    for (int i = 0; i < GS / E; ++i) {
+        float y[E];
+        unpack(reinterpret_cast<const uint4 *>(p)[i], y, T());
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            x[i * E + e] = y[e];
+    }
+}
+
+template <typename T, int DD, bool PACK>
+__global__ void __launch_bounds__(kConvertWarps * 32) convert_kernel(Q4ConvertArgs a)
+{
+    using F = Fmt<DD>;
+    constexpr int GS = F::kGroup;
+    const int lane = threadIdx.x & 31, b = blockIdx.y;
+    const long long item = (long long)blockIdx.x * kConvertWarps + (threadIdx.x >> 5);
+    const int L = a.seq_lens[b], first = a.first ? a.first[b] : 0;
+    const int most = min(a.maxp, a.maxp4);
+    if (L < 0 || (long long)L - a.w > (long long)most * kPage || first < 0) {
+        if (item == 0 && lane == 0)
+            report(a.status, first < 0 ? DAR_ERR_INVALID_ARG : DAR_ERR_CAPACITY);
+        return;
+    }
+    const int end = max(0, L - a.w), page0 = first / kPage;
+    const long long lp = page0 + item / a.Hkv;
+    if (first >= end || lp * kPage >= end)
+        return;
+    const int g = (int)(item % a.Hkv);
+    const int id = a.table[(size_t)b * a.maxp + lp], id4 = a.table4[(size_t)b * a.maxp4 + lp];
+    if (id < 0 || id >= a.num_pages || id4 < 0 || id4 >= a.num_pages4) {
+        if (lane == 0)
+            report(a.status, DAR_ERR_CAPACITY);
+        return;
+    }
+    const int r = 2 * lane;
+    const long long pos = lp * kPage + r;
+    const unsigned has = (pos >= first && pos < end ? 1u : 0u) | (pos + 1 >= first && pos + 1 < end ? 2u : 0u);
+    if (!has)
+        return;
+    unsigned char *page = static_cast<unsigned char *>(a.pool) + ((size_t)id4 * a.Hkv + g) * F::kBytes;
+    const size_t row = (((size_t)id * a.Hkv + g) * kPage + r) * DD;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+        T *vec = static_cast<T *>(kv ? a.pool_vd : a.pool_kd) + row;
+#pragma unroll
+        for (int sb = 0; sb < F::kGroups; ++sb) {
+            float x0[GS], x1[GS];
+            if constexpr (PACK) {
+                int c0[GS], c1[GS];
+                load_group<T, GS>(vec + sb * GS, x0);
+                load_group<T, GS>(vec + DD + sb * GS, x1);
+                const float s0 = quantise<GS>(x0, c0), s1 = quantise<GS>(x1, c1);
+                if (kv)
+                    write_pair<GS, true>(page + sb * F::kBlock, r, has, c0, c1, s0, s1);
+                else
+                    write_pair<GS, false>(page + sb * F::kBlock, r, has, c0, c1, s0, s1);
+            } else {
+                if (kv)
+                    read_pair<GS, true>(page + sb * F::kBlock, r, x0, x1);
+                else
+                    read_pair<GS, false>(page + sb * F::kBlock, r, x0, x1);
+                if (has & 1u)
+                    store_row<T, GS>(vec + sb * GS, x0);
+                if (has & 2u)
+                    store_row<T, GS>(vec + DD + sb * GS, x1);
+            }
+        }
+    }
+}
+
+template <typename F>
+static cudaError_t by_width(int dd, F &&f)
+{
+    switch (dd) {
+    case 8: return f(std::integral_constant<int, 8>());
+    case 16: return f(std::integral_constant<int, 16>());
+    case 32: return f(std::integral_constant<int, 32>());
+    case 64: return f(std::integral_constant<int, 64>());
+    default: return cudaErrorInvalidValue;
+    }
+}
+
+template <typename T>
+static cudaError_t append_t(int dd, const AppendArgs &a, cudaStream_t s)
+{
+    return by_width(dd, [&](auto width) { return append_tiles<T, decltype(width)::value, 1, 64>(a, s); });
+}
+
+template <typename T, bool PACK>
+static cudaError_t convert_t(int dd, const Q4ConvertArgs &a, cudaStream_t s)
+{
+    const long long items = (long long)std::min(a.maxp, a.maxp4) * a.Hkv;
+    const dim3 grid((unsigned)std::max(1ll, (items + kConvertWarps - 1) / kConvertWarps), (unsigned)a.B);
+    return by_width(dd, [&](auto width) {
+        convert_kernel<T, decltype(width)::value, PACK><<<grid, kConvertWarps * 32, 0, s>>>(a);
+        return cudaGetLastError();
+    });
+}
+
+}  // namespace q4
+
+size_t q4_page_bytes(int dd)
+{
+    return dd == 8 ? q4::Fmt<8>::kBytes : (size_t)(dd / 16) * q4::Fmt<16>::kBytes;
+}
+
+cudaError_t launch_append_q4(dar_dtype dt, int dd, const AppendArgs &a, cudaStream_t s)
+{
+    if (a.B == 0)
+        return cudaSuccess;
+    return dt == DAR_F32 ? q4::append_t<float>(dd, a, s) : q4::append_t<bf16>(dd, a, s);
+}
+
+cudaError_t launch_convert_q4(dar_dtype dt, int dd, bool pack, const Q4ConvertArgs &a, cudaStream_t s)
+{
+    if (a.B == 0)
+        return cudaSuccess;
+    if (pack)
+        return dt == DAR_F32 ? q4::convert_t<float, true>(dd, a, s) : q4::convert_t<bf16, true>(dd, a, s);
+    return dt == DAR_F32 ? q4::convert_t<float, false>(dd, a, s) : q4::convert_t<bf16, false>(dd, a, s);
+}
+
+}  // namespace dar

@@ -53,6 +53,17 @@ class dar_latent_cache(ctypes.Structure):
     ]
 
 
+class dar_cache_q4(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int),
+        ("B", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("d_down", ctypes.c_int32), ("w", ctypes.c_int32),
+        ("max_pages_per_seq", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+        ("win_k", ctypes.c_void_p), ("win_v", ctypes.c_void_p), ("pool", ctypes.c_void_p),
+        ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("status", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -68,6 +79,7 @@ def load_library(path: str = LIB_PATH):
     P, I32, SZ, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float
     LP = ctypes.POINTER(dar_latent_cache)
     CP = ctypes.POINTER(dar_cache)
+    QP = ctypes.POINTER(dar_cache_q4)
     sig = {
         "dar_down_project": ([ctypes.c_int, I32, I32, I32, I32, I32, P, P, P, P], ctypes.c_int),
         "dar_cache_append": ([CP, P, P, I32, P, P, P, P], ctypes.c_int),
@@ -81,6 +93,13 @@ def load_library(path: str = LIB_PATH):
         "dar_attn_decode_scored": ([CP, I32, P, P, P, F, P, F, P, P, SZ, P], ctypes.c_int),
         "dar_cache_evict_workspace_bytes": ([CP], SZ),
         "dar_cache_evict": ([CP, P, P, P, P, SZ, P], ctypes.c_int),
+        "dar_q4_page_bytes": ([I32], SZ),
+        "dar_cache_append_q4": ([QP, P, P, I32, P, P, P, P], ctypes.c_int),
+        "dar_cache_pack_q4": ([CP, P, QP, P], ctypes.c_int),
+        "dar_cache_unpack_q4": ([QP, P, CP, P], ctypes.c_int),
+        "dar_decode_q4_workspace_bytes": ([QP, I32], SZ),
+        "dar_attn_decode_q4": ([QP, I32, P, P, P, F, P, P, SZ, P], ctypes.c_int),
+        "dar_decode_step_q4": ([QP, P, P, I32, P, P, P, I32, P, P, P, F, P, P, SZ, P], ctypes.c_int),
         "dar_check_bounded_wait": ([P, ctypes.c_uint32, P], ctypes.c_int),
         "dar_prefill_workspace_bytes": ([ctypes.c_int, I32, I32, I32, I32], SZ),
         "dar_prefill_chunk_workspace_bytes": ([CP, I32], SZ),
@@ -406,6 +425,134 @@ def dar_cache_evict(cache: DarCache, weights, keep, workspace, protect=None, str
     _operand(workspace, "workspace", None, None, dev)
     _check(load_library().dar_cache_evict(cache.struct, _ptr(weights), _ptr(keep), _ptr(protect), _ptr(workspace),
                                           workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+# --------------------------------------------------------------------------- pages in 4 bits
+
+def dar_q4_page_bytes(d_down: int) -> int:
+    """Bytes of a page of one KV head with ``d_down`` entries a vector in 4 bits."""
+    return int(load_library().dar_q4_page_bytes(int(d_down)))
+
+
+class DarCacheQ4:
+    """Caller-owned cache whose pages hold 4 bits an entry, and its ``dar_cache_q4`` struct.  Arguments as
+    :class:`DarCache`; ``pool`` is uint8 ``[num_pages, Hkv, dar_q4_page_bytes(d_down)]``.
+
+    ``share`` (a :class:`DarCache` of the same sizes): its ring, block table, lengths and status word are this
+    cache's too (see :meth:`beside`)."""
+
+    def __init__(self, B, Hkv, d_down, w, max_pages_per_seq, num_pages=None, dtype=torch.bfloat16,
+                 block_table=None, device="cuda", d=64, share=None):
+        self.dtype = dtype
+        self.B, self.Hkv, self.d, self.d_down, self.w = B, Hkv, d, d_down, w
+        self.max_pages_per_seq = max_pages_per_seq
+        if num_pages is None:
+            num_pages = B * max_pages_per_seq
+        self.num_pages = num_pages
+        nbytes = dar_q4_page_bytes(d_down)
+        if nbytes == 0:
+            raise DarError(DAR_ERR_UNSUPPORTED, f"d_down={d_down} (built: 8, 16, 32, 64)")
+        self.pool = torch.zeros((max(num_pages, 1), Hkv, nbytes), dtype=torch.uint8, device=device)
+        if share is not None:
+            self.win_k, self.win_v = share.win_k, share.win_v
+            self.block_table, self.seq_lens, self.status = share.block_table, share.seq_lens, share.status
+        else:
+            self.win_k = torch.zeros((B, Hkv, w, d), dtype=dtype, device=device)
+            self.win_v = torch.zeros_like(self.win_k)
+            if block_table is None:
+                block_table = torch.arange(B * max_pages_per_seq, dtype=torch.int32).reshape(B, max_pages_per_seq)
+            self.block_table = torch.as_tensor(block_table, dtype=torch.int32).to(device).contiguous()
+            if self.block_table.numel() == 0:
+                self.block_table = torch.full((max(B, 1), 1), -1, dtype=torch.int32, device=device)
+            self.seq_lens = torch.zeros(B, dtype=torch.int32, device=device)
+            self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self._struct = dar_cache_q4(
+            _CODE[dtype], B, Hkv, d, d_down, w, max_pages_per_seq, num_pages, self.win_k.data_ptr(),
+            self.win_v.data_ptr(), self.pool.data_ptr(), self.block_table.data_ptr(), self.seq_lens.data_ptr(),
+            self.status.data_ptr())
+
+    @classmethod
+    def beside(cls, cache: DarCache, num_pages=None):
+        """Pages in 4 bits beside an ordinary cache, whose ring, block table, lengths and status word both use."""
+        return cls(cache.B, cache.Hkv, cache.d_down, cache.w, cache.max_pages_per_seq,
+                   cache.num_pages if num_pages is None else num_pages, dtype=cache.dtype,
+                   device=cache.win_k.device, d=cache.d, share=cache)
+
+    @property
+    def struct(self):
+        return ctypes.byref(self._struct)
+
+    def device_status(self) -> int:
+        return int(self.status.item())
+
+
+def _append_operands(cache, k_new, v_new, Dk, Dv, n_per_seq):
+    """Checks of an append's operands; returns the tokens per sequence."""
+    if not isinstance(k_new, torch.Tensor) or k_new.dim() != 4:
+        raise ValueError("k_new must be a tensor [B, Hkv, n, d]")
+    dev, n = _cache_device(cache), k_new.shape[2]
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        _operand(t, name, cache.dtype, (cache.B, cache.Hkv, n, cache.d), dev)
+    for name, t in (("Dk", Dk), ("Dv", Dv)):
+        _operand(t, name, torch.float32, (cache.Hkv, cache.d, cache.d_down), dev)
+    if n_per_seq is not None:
+        _operand(n_per_seq, "n_per_seq", torch.int32, (cache.B,), dev)
+    return n
+
+
+def dar_cache_append_q4(cache: DarCacheQ4, k_new, v_new, Dk, Dv, n_per_seq=None, stream=None):
+    """Append ``k_new, v_new [B,Hkv,n,d]`` (first ``n_per_seq[b]`` rows of sequence b); what leaves the window is
+    held in 4 bits."""
+    n = _append_operands(cache, k_new, v_new, Dk, Dv, n_per_seq)
+    _check(load_library().dar_cache_append_q4(cache.struct, k_new.data_ptr(), v_new.data_ptr(), n, _ptr(n_per_seq),
+                                              Dk.data_ptr(), Dv.data_ptr(), _stream(stream)))
+
+
+def _convert_operands(src, dst, first):
+    dev = _cache_device(src)
+    if dst.win_k.get_device() != dev:
+        raise ValueError(f"the caches are on {src.win_k.device} and {dst.win_k.device}")
+    if first is not None:
+        _operand(first, "first", torch.int32, (src.B,), dev)
+
+
+def dar_cache_pack_q4(src: DarCache, dst: DarCacheQ4, first=None, stream=None):
+    """Distant tokens of ``src`` (from position ``first[b]`` on, int32 ``[B]``; none: 0) into ``dst``'s pages, in 4 bits."""
+    _convert_operands(src, dst, first)
+    _check(load_library().dar_cache_pack_q4(src.struct, _ptr(first), dst.struct, _stream(stream)))
+
+
+def dar_cache_unpack_q4(src: DarCacheQ4, dst: DarCache, first=None, stream=None):
+    """Distant tokens of ``src`` (from position ``first[b]`` on, int32 ``[B]``; none: 0) back into pages of the
+    storage type."""
+    _convert_operands(src, dst, first)
+    _check(load_library().dar_cache_unpack_q4(src.struct, _ptr(first), dst.struct, _stream(stream)))
+
+
+def decode_q4_workspace(cache: DarCacheQ4, Hq: int):
+    """A workspace of the size dar_attn_decode_q4 needs (no initialisation needed)."""
+    return _new_workspace(cache, int(load_library().dar_decode_q4_workspace_bytes(cache.struct, Hq)))
+
+
+def dar_attn_decode_q4(cache: DarCacheQ4, q, Uk, Uv, workspace, scale=0.0, out=None, stream=None):
+    """One decode step for queries ``q [B,Hq,d]`` over a cache in 4 bits."""
+    Hq, out, _ = _step_operands(cache, q, Uk, Uv, workspace, out)
+    _check(load_library().dar_attn_decode_q4(
+        cache.struct, Hq, q.data_ptr(), Uk.data_ptr(), Uv.data_ptr(), float(scale), out.data_ptr(),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
+
+
+def dar_decode_step_q4(cache: DarCacheQ4, k_new, v_new, Dk, Dv, q, Uk, Uv, workspace, scale=0.0, out=None,
+                       n_per_seq=None, stream=None):
+    """dar_cache_append_q4 of ``k_new, v_new [B,Hkv,n,d]`` then dar_attn_decode_q4 of ``q [B,Hq,d]``, in one call."""
+    n = _append_operands(cache, k_new, v_new, Dk, Dv, n_per_seq)
+    Hq, out, _ = _step_operands(cache, q, Uk, Uv, workspace, out)
+    _check(load_library().dar_decode_step_q4(
+        cache.struct, k_new.data_ptr(), v_new.data_ptr(), n, _ptr(n_per_seq), Dk.data_ptr(), Dv.data_ptr(), Hq,
+        q.data_ptr(), Uk.data_ptr(), Uv.data_ptr(), float(scale), out.data_ptr(), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
 
 
 # --------------------------------------------------------------------------- prefill
