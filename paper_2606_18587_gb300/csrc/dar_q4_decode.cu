@@ -32,7 +32,10 @@ using namespace sm100;
 
 constexpr int kRows = 8;         // query heads of a unit at most
 constexpr int kRun = 16;         // ring tokens of a stage
-constexpr int kWarps = 8;        // of a CTA
+constexpr int kWarps = 8;        // of a CTA (CUDA cores)
+constexpr int kMmaWarps = 12;    // of a CTA (tensor cores)
+constexpr int kSlots = 3;        // stages in flight of a warp
+constexpr int kSlot = 5120;      // bytes of one
 constexpr int kMaxShares = 1920; // the workspace holds partial results of this many warps
 constexpr int kCostUnit = 8;     // cost of a unit's set-up (its place on the line is before the stages)
 constexpr int kCostRun = 8;      // of kRun ring tokens
@@ -374,6 +377,8 @@ __device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, Lan
     }
 }
 
+constexpr size_t lanes_smem(int B) { return kWarps * sizeof(LaneSmem) + (2 * (size_t)B + 1) * 4; }
+
 template <typename T, int DD>
 __global__ void __launch_bounds__(kWarps * 32) attend_kernel(Args a)
 {
@@ -382,6 +387,599 @@ __global__ void __launch_bounds__(kWarps * 32) attend_kernel(Args a)
     grid_dep_launch();
     build_tables<DD>(a, t);
     attend_lanes<T, DD>(a, t, reinterpret_cast<LaneSmem *>(smem)[threadIdx.x >> 5]);
+}
+
+// ------------------------------------------------------------------ attend, tensor cores
+//
+// Up to 8 query heads lie on the N side of mma.sync products with 16 tokens on the M side
+// (a tcgen05 tile has 128 rows: most calls have 1 to 8 heads per KV head).  Column 2 t of a
+// product belongs to head t and column 2 t + 1 to head t + 4, so lane (g, t) = 4 g + t has the
+// scores, weights, references and sums of heads t and t + 4 (CT = 2; of head t alone with CT = 1).
+//
+//  scores   m16n8k32 on e4m3 operands: the codes are e4m3 numbers as they lie in memory (three
+//           instructions for eight), and q~, brought to [128, 256) by a power of two, is four e4m3
+//           terms (2^-16 of it).  K = 32 takes the 16 entries twice: a column's terms 0 and 1, the
+//           next column's terms 2 and 3.  With a d_down of 8 one column takes all four.
+//  weights  p s_v as fp16 (2^-11) relative to a reference of the row that keeps the largest at
+//           2^8 when it is set and below 2^15 always; it is raised by a vote.  (bf16 operands need two
+//           terms for the same error, twice the conversions and transpositions.)
+//  sums     m16n8k16 on fp16: code + 8 in the low bits of 1024's significand, and 1032 subtracted.
+// Of a page of 64 tokens this is some 145 instructions of a warp for four heads.
+
+struct Soft {  // of one head of a lane
+    float bias, l;  // minus the reference; the lane's share of the sum of weights
+};
+
+__device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1)
+{
+    const float z = 0.f;
+    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%4,%5}, {%6,%7}, {%8,%8,%8,%8};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(b0), "r"(b1), "f"(z));
+}
+
+__device__ __forceinline__ void mma_f16_acc(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// Four values as NT e4m3 terms each, four bytes to a word.
+template <int NT>
+__device__ __forceinline__ void e4m3_terms(float (&x)[4], uint32_t (&t)[NT])
+{
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        uint32_t w[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            uint16_t u;
+            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(u) : "f"(x[2 * j + 1]), "f"(x[2 * j]));
+            uint32_t h;
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(u));
+            float lo, hi;
+            asm("{.reg .b16 a, b; mov.b32 {a, b}, %2; cvt.f32.f16 %0, a; cvt.f32.f16 %1, b;}" : "=f"(lo), "=f"(hi) : "r"(h));
+            x[2 * j] -= lo;
+            x[2 * j + 1] -= hi;
+            w[j] = u;
+        }
+        t[i] = w[0] | w[1] << 16;
+    }
+}
+
+// Two fp32 values as three bf16 terms each: all but 2^-24 of them.
+__device__ __forceinline__ void split3(float x, float y, uint32_t (&t)[3])
+{
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        t[i] = cvt_bf16x2(x, y);
+        x -= bf16lo(t[i]);
+        y -= bf16hi(t[i]);
+    }
+}
+
+// 0xffff in the halves whose key (key, key + 1) is below n.
+__device__ __forceinline__ uint32_t key_mask(int key, int n)
+{
+    return (key < n ? 0xffffu : 0u) | (key + 1 < n ? 0xffff0000u : 0u);
+}
+
+// What a warp fills its slots with, ahead of what it computes.
+template <int DD>
+struct Filler {
+    static constexpr int kPages = Fmt<DD>::kBytes > kSlot / 4 ? kSlot / Fmt<DD>::kBytes : 4;  // of a stage
+    Walk walk;
+    Cut c;
+    int st;          // next stage of the cut
+    int ids0, ids;   // block-table entries ids0 .. ids0 + 31 of its sequence, one per lane
+    int filled;
+    bool more;
+
+    __device__ __forceinline__ void begin(const Args &a, const Tables &t, int share)
+    {
+        walk.begin<DD>(a, t, share);
+        filled = 0;
+        next_cut(a, t);
+    }
+    __device__ __forceinline__ void next_cut(const Args &a, const Tables &t)
+    {
+        more = walk.next<DD>(a, t, c);
+        st = c.st0;
+        ids0 = -1;
+    }
+    // Starts the copies of the next stage.
+    __device__ __forceinline__ void fill(const Args &a, const Tables &t, const CUtensorMap &wk, const CUtensorMap &wv,
+                                         unsigned char *slots, uint64_t *full, uint64_t policy, int lane)
+    {
+        if (!more)
+            return;
+        unsigned char *dst = slots + filled % kSlots * kSlot;
+        uint64_t *bar = full + filled % kSlots;
+        ++filled;
+        if (st < c.nrun) {
+            if (lane == 0) {
+                mbar_expect_tx(bar, 2 * kRun * kHeadDim * 2);
+                const int y = (c.b * a.c.Hkv + c.g) * a.c.w + st * kRun;
+                tma_load_2d_hint(smem_u32(dst), &wk, 0, y, bar, policy);
+                tma_load_2d_hint(smem_u32(dst + kRun * kHeadDim * 2), &wv, 0, y, bar, policy);
+            }
+            ++st;
+        } else {
+            const int lp = st - c.nrun, n = min(kPages, c.st1 - st);
+            if (ids0 < 0 || lp + n > ids0 + 32) {
+                ids0 = lp;
+                ids = lp + lane < a.c.maxp ? __ldg(a.c.block_table + (size_t)c.b * a.c.maxp + lp + lane) : -1;
+            }
+            const int id = __shfl_sync(0xffffffffu, ids, (lp - ids0 + lane) & 31);
+            const bool mine = lane < n, good = mine && id >= 0 && id < a.c.num_pages;
+            const unsigned pages = __popc(__ballot_sync(0xffffffffu, good));
+            if (lane == 0)
+                mbar_expect_tx(bar, pages * Fmt<DD>::kBytes);
+            __syncwarp();
+            if (good)
+                bulk_g2s_hint(dst + lane * Fmt<DD>::kBytes,
+                              static_cast<const unsigned char *>(a.c.pool) + ((size_t)id * a.c.Hkv + c.g) * Fmt<DD>::kBytes,
+                              Fmt<DD>::kBytes, bar, policy);
+            else if (mine)
+                report(a.c.status, DAR_ERR_CAPACITY);
+            st += n;
+        }
+        if (st >= c.st1)
+            next_cut(a, t);
+    }
+};
+
+// What a warp has of a cut's query heads, and its sums.
+template <int DD, int CT>
+struct Heads {
+    static constexpr int GS = Fmt<DD>::kGroup, NB = Fmt<DD>::kGroups;
+    static constexpr int TB = GS == 16 ? CT : 1;  // score products of a group
+    uint32_t q[4][2];        // ring: queries as B operands
+    uint32_t qt[NB][TB][2];  // pages: q~ as B operands, four e4m3 terms
+    float cq[CT];            // scale of a score: c2, the power of two taken out of q~, and the codes' 2^9
+    Soft ring[CT], page[CT];
+    float ol[kHeadDim / 16][4], od[NB][4];
+
+    // Queries of a cut, and q~^T = Uk q^T with Uk in three bf16 terms (products exact but for 2^-24).
+    __device__ __forceinline__ void begin(const Args &a, const Cut &c, int lane)
+    {
+        const int i0 = lane >> 2, c0 = lane & 3;
+        const int head = (i0 >> 1) + 4 * (i0 & 1);  // of column i0
+        const uint32_t *qp = static_cast<const uint32_t *>(a.c.q) +
+                             ((size_t)c.b * a.c.Hq + c.g * a.G + c.rt * kRows + head) * (kHeadDim / 2) + c0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            q[e / 2][e % 2] = head < c.rows ? __ldg(qp + 4 * e) : 0u;
+        float x[NB][4];  // entries 16 j + i0 (+ 8) of heads c0, c0 + 4: [0] i0 c0, [1] i0 c0 + 4, [2], [3] i0 + 8
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const float *u = a.c.Uk + ((size_t)c.g * DD + 16 * j + i0) * kHeadDim + 2 * c0;
+            float z[3][4] = {};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t t[4][3];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {  // entries i0, i0 + 8 and inputs 2 c, 2 c + 8
+                    float2 v = make_float2(0.f, 0.f);
+                    if (GS == 16 || y % 2 == 0)
+                        v = __ldg(reinterpret_cast<const float2 *>(u + (y & 1) * 8 * kHeadDim + 16 * e + 8 * (y >> 1)));
+                    split3(v.x, v.y, t[y]);
+                }
+#pragma unroll
+                for (int y = 0; y < 3; ++y) {
+                    const uint32_t ua[4] = {t[0][y], t[1][y], t[2][y], t[3][y]};
+                    mma_bf16_acc(z[y], ua, q[e][0], q[e][1]);
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                x[j][y] = z[0][y] + (z[1][y] + z[2][y]);
+        }
+        // the largest entry of each head, and the power of two that brings it to [2^7, 2^8)
+        float up[CT];
+#pragma unroll
+        for (int k = 0; k < CT; ++k) {
+            uint32_t top = 0u;
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                top = max(top, max(magnitude(x[j][k]), magnitude(x[j][2 + k])));
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1)
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const int e = max((int)(top >> 23) - 127, -100);
+            up[k] = __uint_as_float((uint32_t)(127 + 7 - e) << 23);  // e <= 127: 2^-120 at least
+            // infinite or NaN: so are all scores
+            cq[k] = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u)
+                                       : a.c.c2 * __uint_as_float((uint32_t)(127 + e) << 23) * 4.f;
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                x[j][k] *= up[k];
+                x[j][2 + k] *= up[k];
+            }
+        }
+        // column i0 of a score product wants four consecutive entries of its head
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int k = 0; k < TB; ++k) {
+                float y[4];
+                uint32_t t[4];
+                if constexpr (GS == 16) {  // head i0 / 2 + 4 k, entries 4 c0 ..
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int from = ((4 * c0 + e) & 7) * 4 + (i0 >> 1);
+                        const float lo = __shfl_sync(0xffffffffu, x[j][k], from);
+                        const float hi = __shfl_sync(0xffffffffu, x[j][2 + k], from);
+                        y[e] = c0 < 2 ? lo : hi;
+                    }
+                    e4m3_terms<4>(y, t);
+                    qt[j][k][0] = i0 & 1 ? t[2] : t[0];
+                    qt[j][k][1] = i0 & 1 ? t[3] : t[1];
+                } else {  // head i0 / 2 + 4 (i0 mod 2), entries 4 (c0 mod 2) ..
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int from = ((4 * c0 + e) & 7) * 4 + (i0 >> 1);
+                        y[e] = __shfl_sync(0xffffffffu, x[j][0], from);
+                        if constexpr (CT == 2) {
+                            const float hi = __shfl_sync(0xffffffffu, x[j][1], from);
+                            y[e] = i0 & 1 ? hi : y[e];
+                        } else {
+                            y[e] = i0 & 1 ? 0.f : y[e];
+                        }
+                    }
+                    e4m3_terms<4>(y, t);
+                    qt[j][k][0] = c0 < 2 ? t[0] : t[1];
+                    qt[j][k][1] = c0 < 2 ? t[2] : t[3];
+                }
+            }
+#pragma unroll
+        for (int k = 0; k < CT; ++k) {
+            ring[k].bias = page[k].bias = INFINITY;
+            ring[k].l = page[k].l = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < kHeadDim / 16; ++e)
+            ol[e][0] = ol[e][1] = ol[e][2] = ol[e][3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            od[j][0] = od[j][1] = od[j][2] = od[j][3] = 0.f;
+    }
+
+    // A run of n ring tokens at `tile`: 16 rows of keys, then of values, 128-byte swizzle.
+    __device__ __forceinline__ void ring_step(uint32_t tile, int n, float c2, int lane)
+    {
+        const int i0 = lane >> 2, c0 = lane & 3, mat = lane >> 3, r = lane & 7;
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint32_t krow = tile + (r + 8 * (mat & 1)) * 128;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t k[4];
+            ldsm_x4(krow + (((2 * e + (mat >> 1)) ^ r) << 4), k);
+            mma_bf16_acc(s, k, q[e][0], q[e][1]);
+        }
+        uint32_t w0[2], w1[2];  // weights as two bf16 terms: tokens i0, and i0 + 8
+        float p[2][2] = {};
+        bool up = false;
+#pragma unroll
+        for (int k = 0; k < CT; ++k) {
+            s[k] = i0 < n ? s[k] * c2 : -INFINITY;
+            s[2 + k] = i0 + 8 < n ? s[2 + k] * c2 : -INFINITY;
+            up |= fmaxf(s[k], s[2 + k]) > -ring[k].bias;
+        }
+        if (__any_sync(0xffffffffu, up)) {
+#pragma unroll
+            for (int k = 0; k < CT; ++k) {
+                float top = fmaxf(s[k], s[2 + k]);
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1)
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float was = -ring[k].bias, now = fmaxf(top, was), f = now == -INFINITY ? 1.f : ex2_approx(was - now);
+                ring[k].bias = -now;
+                ring[k].l *= f;
+#pragma unroll
+                for (int e = 0; e < kHeadDim / 16; ++e) {
+                    ol[e][k] *= f;
+                    ol[e][2 + k] *= f;
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < CT; ++k) {
+            const float bias = ring[k].bias == INFINITY ? 0.f : ring[k].bias;
+            p[0][k] = ex2_approx(s[k] + bias);
+            p[1][k] = ex2_approx(s[2 + k] + bias);
+            ring[k].l += p[0][k] + p[1][k];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            // hi cut off, so that both terms have the weight's sign; 2^-22 of it keeps lo from 0, where an infinite
+            // value would become NaN
+            constexpr float kUp = 1.f + 0x1p-22f;
+            const uint32_t x = __float_as_uint(p[h][0]), y = __float_as_uint(p[h][1]);
+            uint32_t &hi = h ? w1[0] : w0[0], &lo = h ? w1[1] : w0[1];
+            hi = transpose8(__byte_perm(x, y, 0x7632));
+            lo = transpose8(cvt_bf16x2(fmaf(p[h][0], kUp, -__uint_as_float(x & 0xffff0000u)),
+                                       fmaf(p[h][1], kUp, -__uint_as_float(y & 0xffff0000u))));
+        }
+        const uint32_t m0 = key_mask(2 * c0, n), m1 = key_mask(2 * c0 + 8, n);  // 0 * NaN is NaN
+        const uint32_t vrow = tile + kRun * kHeadDim * 2 + (r + 8 * (mat >> 1)) * 128;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t v[4];
+            ldsm_x4_t(vrow + (((2 * e + (mat & 1)) ^ r) << 4), v);
+            const uint32_t vm[4] = {v[0] & m0, v[1] & m0, v[2] & m1, v[3] & m1};
+            mma_bf16_acc(ol[e], vm, w0[0], w1[0]);
+            mma_bf16_acc(ol[e], vm, w0[1], w1[1]);
+        }
+    }
+
+    // A page of n tokens.
+    __device__ __forceinline__ void page_step(const unsigned char *at, int n, int lane)
+    {
+        using F = Fmt<DD>;
+        const int i0 = lane >> 2, c0 = lane & 3;
+        constexpr uint32_t kCode = 0x87878787u;
+        float y[CT][4][2];  // scores of tokens 8 i0 + 2 i, + 1
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const unsigned char *block = at + j * F::kBlock;
+            const uint4 kw = *reinterpret_cast<const uint4 *>(block + (GS == 16 ? lane * 16 : i0 * 32 + (c0 & 1) * 16));
+            const uint4 sw = *reinterpret_cast<const uint4 *>(block + F::kScales + i0 * 16);
+            const uint32_t w[4] = {kw.x, kw.y, kw.z, kw.w}, sc[4] = {sw.x, sw.y, sw.z, sw.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t a0 = w[i] & kCode, a1 = __funnelshift_r(w[i], w[i], 4) & kCode;
+                float d[TB][4];
+#pragma unroll
+                for (int k = 0; k < TB; ++k)
+                    mma_e4m3(d[k], a0, a1, qt[j][k][0], qt[j][k][1]);
+#pragma unroll
+                for (int k = 0; k < CT; ++k) {
+                    const float x0 = GS == 16 ? d[k % TB][0] + d[k % TB][1] : d[0][k];
+                    const float x1 = GS == 16 ? d[k % TB][2] + d[k % TB][3] : d[0][2 + k];
+                    y[k][i][0] = j ? fmaf(x0, bf16lo(sc[i]), y[k][i][0]) : x0 * bf16lo(sc[i]);
+                    y[k][i][1] = j ? fmaf(x1, bf16hi(sc[i]), y[k][i][1]) : x1 * bf16hi(sc[i]);
+                }
+            }
+        }
+        uint32_t vs[NB][4];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(at + j * F::kBlock + F::kScales + 2 * kPage + i0 * 16);
+            vs[j][0] = v.x, vs[j][1] = v.y, vs[j][2] = v.z, vs[j][3] = v.w;
+        }
+        if (n < kPage) {  // rows behind the last token may hold anything
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int tok = 8 * i0 + 2 * i;
+                const uint32_t m = key_mask(tok, n);
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                    vs[j][i] &= m;
+#pragma unroll
+                for (int k = 0; k < CT; ++k) {
+                    y[k][i][0] = tok < n ? y[k][i][0] : -INFINITY;
+                    y[k][i][1] = tok + 1 < n ? y[k][i][1] : -INFINITY;
+                }
+            }
+        }
+        constexpr float kFar = 32768.f, kFarSum = 0x1p90f;
+        float p[CT][4][2], l[CT];
+        auto weigh = [&]() {  // returns whether something got far above the reference
+            float top = 0.f;
+            bool far = false;
+#pragma unroll
+            for (int k = 0; k < CT; ++k) {
+                l[k] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[k][i][0] = ex2_approx(fmaf(y[k][i][0], cq[k], page[k].bias));
+                    p[k][i][1] = ex2_approx(fmaf(y[k][i][1], cq[k], page[k].bias));
+                    l[k] += p[k][i][0] + p[k][i][1];
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+                        top = max3(top, p[k][i][0] * bf16lo(vs[j][i]), p[k][i][1] * bf16hi(vs[j][i]));
+                }
+                far |= l[k] > kFarSum;
+            }
+            return far || top > kFar;
+        };
+        if (__any_sync(0xffffffffu, weigh())) {
+#pragma unroll
+            for (int k = 0; k < CT; ++k) {
+                float top = -INFINITY;  // of p s_v, and of 2^-64 p
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float s = 0x1p-64f;
+#pragma unroll
+                        for (int j = 0; j < NB; ++j)
+                            s = fmaxf(s, h ? bf16hi(vs[j][i]) : bf16lo(vs[j][i]));
+                        top = fmaxf(top, fmaf(y[k][i][h], cq[k], __log2f(s)));
+                    }
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1)
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float was = -page[k].bias, now = fmaxf(was, top - 8.f);
+                const float f = now == -INFINITY ? 1.f : ex2_approx(was - now);
+                page[k].bias = -now;
+                page[k].l *= f;
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    od[j][k] *= f;
+                    od[j][2 + k] *= f;
+                }
+            }
+            weigh();
+        }
+#pragma unroll
+        for (int k = 0; k < CT; ++k)
+            page[k].l += l[k];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const unsigned char *block = at + j * F::kBlock + F::kCodes;
+            uint32_t w[4];
+            if constexpr (GS == 16) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(block + lane * 16);
+                w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+            } else {
+                const uint2 v = *reinterpret_cast<const uint2 *>(block + lane * 8);
+                w[0] = v.x, w[1] = v.x >> 8, w[2] = v.y, w[3] = v.y >> 8;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float s0 = bf16lo(vs[j][i]), s1 = bf16hi(vs[j][i]);
+                const uint32_t b0 = transpose8(cvt_f16x2(p[0][i][0] * s0, CT == 2 ? p[CT - 1][i][0] * s0 : 0.f));
+                const uint32_t b1 = transpose8(cvt_f16x2(p[0][i][1] * s1, CT == 2 ? p[CT - 1][i][1] * s1 : 0.f));
+                // 1024 + (code + 8) and 1024 + 16 (code + 8)
+                auto low = [](uint32_t x) { return add_f16x2((x & 0x000f000fu) | 0x64006400u, 0xe408e408u); };
+                auto high = [](uint32_t x) { return fma_f16x2((x & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u); };
+                uint32_t v[4];
+                v[0] = low(w[i]);
+                if constexpr (GS == 16) {
+                    v[1] = high(w[i]);
+                    v[2] = low(w[i] >> 8);
+                    v[3] = high(w[i] >> 8);
+                } else {
+                    v[1] = v[3] = 0u;
+                    v[2] = high(w[i]);
+                }
+                mma_f16_acc(od[j], v, b0, b1);
+            }
+        }
+    }
+
+    // The partial result of the cut.
+    __device__ __forceinline__ void leave(const Args &a, const Cut &c, int lane)
+    {
+        const int i0 = lane >> 2, c0 = lane & 3;
+#pragma unroll
+        for (int k = 0; k < CT; ++k) {
+            float lr = ring[k].l, lp = page[k].l;
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) {
+                lr += __shfl_xor_sync(0xffffffffu, lr, o);
+                lp += __shfl_xor_sync(0xffffffffu, lp, o);
+            }
+            const int head = c0 + 4 * k;
+            if (head >= c.rows)
+                continue;
+            const float m = fmaxf(-ring[k].bias, -page[k].bias), base = m == -INFINITY ? 0.f : m;
+            const float fr = ex2_approx(-ring[k].bias - base), fp = ex2_approx(-page[k].bias - base);
+            float *rec = a.rec + ((size_t)c.slot * a.RU + head) * rec_floats<DD>();
+            if (i0 == 0) {
+                rec[0] = m;
+                rec[1] = lr * fr + lp * fp;
+            }
+#pragma unroll
+            for (int e = 0; e < kHeadDim / 16; ++e) {
+                rec[4 + 16 * e + i0] = ol[e][k] * fr;
+                rec[4 + 16 * e + 8 + i0] = ol[e][2 + k] * fr;
+            }
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                rec[4 + kHeadDim + 16 * j + i0] = od[j][k] * fp;
+                if (GS == 16)
+                    rec[4 + kHeadDim + 16 * j + 8 + i0] = od[j][2 + k] * fp;
+            }
+        }
+    }
+};
+
+constexpr size_t mma_smem(int B) { return 1024 + (size_t)kMmaWarps * kSlots * (kSlot + 8) + 16 + (2 * (size_t)B + 1) * 4; }
+
+template <int DD, int CT>
+__global__ void __launch_bounds__(kMmaWarps * 32, 1)
+    attend_mma_kernel(const __grid_constant__ CUtensorMap wk, const __grid_constant__ CUtensorMap wv, const Args a)
+{
+    extern __shared__ unsigned char raw[];
+    unsigned char *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);  // the swizzle's atoms
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = blockIdx.x * kMmaWarps + warp;
+    unsigned char *slots = base + warp * kSlots * kSlot;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(base + kMmaWarps * kSlots * kSlot), *full = bars + warp * kSlots;
+    volatile int *gave_up = reinterpret_cast<volatile int *>(bars + kMmaWarps * kSlots);
+    const Tables t = tables_at(reinterpret_cast<int *>(bars + kMmaWarps * kSlots + 2), a.c.B);
+    grid_dep_launch();
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kMmaWarps * kSlots; ++i)
+            mbar_init(bars + i, 1);
+        *gave_up = 0;
+        mbar_init_fence();
+    }
+    build_tables<DD>(a, t);  // its barriers also publish the mbarriers
+    const uint64_t once = l2_evict_first_policy();  // the cache is read once
+    Filler<DD> fill;
+    fill.begin(a, t, share);
+#pragma unroll 1
+    for (int i = 0; i < kSlots; ++i)
+        fill.fill(a, t, wk, wv, slots, full, once, lane);
+    Walk walk;
+    walk.begin<DD>(a, t, share);
+    int n = 0;  // stages taken
+    bool alive = true;
+    for (Cut c; alive && walk.next<DD>(a, t, c);) {
+        if (lane == 0)
+            leave_span(a, c, share);
+        Heads<DD, CT> h;
+        h.begin(a, c, lane);
+        for (int st = c.st0; st < c.st1; ++n) {
+            const int s = n % kSlots;
+            if (!mbar_wait_warp(full + s, (unsigned)((n / kSlots) & 1), gave_up)) {
+                alive = false;
+                break;
+            }
+            const unsigned char *slot = slots + s * kSlot;
+            if (st < c.nrun) {
+                h.ring_step(smem_u32(slot), min(kRun, c.nwin - st * kRun), a.c.c2, lane);
+                ++st;
+            } else {
+                const int pages = min(Filler<DD>::kPages, c.st1 - st);
+                for (int i = 0; i < pages; ++i)
+                    h.page_step(slot + i * Fmt<DD>::kBytes, min(kPage, c.L - c.nwin - (st - c.nrun + i) * kPage), lane);
+                st += pages;
+            }
+            __syncwarp();  // the slot is read
+            fill.fill(a, t, wk, wv, slots, full, once, lane);
+        }
+        if (alive)
+            h.leave(a, c, lane);
+    }
+    if (!alive) {
+        // a wait gave up: the copies in flight land (again a bounded wait) before the warp leaves
+        if (lane == 0)
+            report(a.c.status, DAR_ERR_DEVICE);
+        for (int i = n; i < fill.filled; ++i)
+            mbar_wait(full + i % kSlots, (unsigned)((i / kSlots) & 1), nullptr);
+    }
 }
 
 // ------------------------------------------------------------------ join
@@ -490,23 +1088,44 @@ static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s
     a.G = c.Hq / c.Hkv;
     a.RT = y.RT;
     a.RU = y.RU;
-    auto kern = attend_kernel<T, DD>;
     static PerDeviceOnce once;
     int sms = 0;
     cudaError_t e = per_device_once(
         once,
         [&](int d) {
-            const cudaError_t e2 = cudaDeviceGetAttribute(&once.value[d], cudaDevAttrMultiProcessorCount, d);
-            return e2 != cudaSuccess ? e2
-                                     : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                            (int)(kWarps * sizeof(LaneSmem) + (2 * DAR_DECODE_MAX_BATCH + 1) * 4));
+            cudaError_t e2 = cudaDeviceGetAttribute(&once.value[d], cudaDevAttrMultiProcessorCount, d);
+            if constexpr (sizeof(T) == 2) {
+                if (e2 == cudaSuccess)
+                    e2 = cudaFuncSetAttribute(attend_mma_kernel<DD, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                              (int)mma_smem(DAR_DECODE_MAX_BATCH));
+                if (e2 == cudaSuccess)
+                    e2 = cudaFuncSetAttribute(attend_mma_kernel<DD, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                              (int)mma_smem(DAR_DECODE_MAX_BATCH));
+            } else if (e2 == cudaSuccess) {
+                e2 = cudaFuncSetAttribute(attend_kernel<T, DD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                          (int)lanes_smem(DAR_DECODE_MAX_BATCH));
+            }
+            return e2;
         },
         &sms);
     if (e != cudaSuccess)
         return e;
-    const int grid = std::min(sms, kMaxShares / kWarps);
-    a.shares = grid * kWarps;
-    kern<<<grid, kWarps * 32, kWarps * sizeof(LaneSmem) + (2 * (size_t)c.B + 1) * 4, s>>>(a);
+    if constexpr (sizeof(T) == 2) {
+        CUtensorMap wk, wv;
+        const unsigned long long rows = (unsigned long long)c.B * c.Hkv * c.w;
+        if (!make_tma_2d_bf16(&wk, c.win_k, rows, kHeadDim, kRun) || !make_tma_2d_bf16(&wv, c.win_v, rows, kHeadDim, kRun))
+            return cudaErrorInvalidValue;
+        const int grid = std::min(sms, kMaxShares / kMmaWarps);
+        a.shares = grid * kMmaWarps;
+        if (y.RU <= 4)
+            attend_mma_kernel<DD, 1><<<grid, kMmaWarps * 32, mma_smem(c.B), s>>>(wk, wv, a);
+        else
+            attend_mma_kernel<DD, 2><<<grid, kMmaWarps * 32, mma_smem(c.B), s>>>(wk, wv, a);
+    } else {
+        const int grid = std::min(sms, kMaxShares / kWarps);
+        a.shares = grid * kWarps;
+        attend_kernel<T, DD><<<grid, kWarps * 32, lanes_smem(c.B), s>>>(a);
+    }
     e = cudaGetLastError();
     if (e != cudaSuccess)
         return e;
