@@ -10,17 +10,20 @@
 //
 // A page of one KV head is kBlock bytes for every 16 entries (8): codes of the keys,
 // codes of the values, 64 scales of the keys, 64 of the values (bf16).  Codes lie
-// where the lanes of a warp want them as operands of mma.sync (dar_q4_decode.cu),
-// lane 4 g + t with one 16-byte load for all 64 tokens of a group:
-//   keys    lane (g, t) holds entries 4 t .. 4 t + 3 of tokens 8 g .. 8 g + 7, a word for
-//           two consecutive tokens: the even one's codes as sign and magnitude in bits 7
-//           and 0-2 of each byte, the odd one's in the same places of the word turned
-//           right by four bits.  As an e4m3 number such a byte is code * 2^-9.
-//   values  lane (g, t) holds entries g and g + 8 of tokens 16 t .. 16 t + 15 as code + 8:
-//           tokens 16 t + 2 i + {0, 1} and 16 t + 8 + 2 i + {0, 1} are bytes 0 to 3 of
-//           word i, entry g the low half of a byte.  (Of a d_down of 8, a byte is two
-//           tokens' entry g.)
-// Two consecutive tokens from an even row on share words, so one thread writes both.
+// where the lanes of a warp want them as operands of mma.sync (dar_q4_decode.cu), all
+// 64 tokens of a group with one load of 16 bytes (8) a lane.  A word is eight codes, in
+// slots 0 to 3 of either half: turned right by 4 r bits it has slot r's two codes as sign
+// and magnitude in bits 15, 0-2 and 31, 16-18, which are the fp16 numbers code * 2^-24:
+// an instruction to turn and one to mask make an operand register.
+//   row      r of a page is token 4 i + 2 c + o of 16 t ..: t = r / 16, i = r / 4 mod 4, c = r / 2 mod 2, o = r mod 2
+//   keys     lane (g, u) = 4 g + u has rows with 2 t + o = g: word i, slots c and 2 + c, are
+//            entries 4 u, 4 u + 1 and 4 u + 2, 4 u + 3 in the two halves
+//   values   lane (g, t): word i, slots 2 c and 2 c + 1, are entries g and g + 8 in half o
+//   scales   of row r at (2 t + o) * 8 + 2 i + c
+// With 8 entries, two rows' words are one: word i / 2, slots 2 (i mod 2) + c, are entries
+// 2 u, 2 u + 1 of a key in the two halves, or entry g of a value in half o.
+// So four consecutive tokens (eight) share eight words of keys and eight of values, and
+// one thread writes either (a unit).
 #pragma once
 
 #include "dar_common.cuh"
@@ -36,6 +39,7 @@ struct Fmt {
     static constexpr int kScales = 2 * kCodes;         // offset of the keys' scales; the values' are kPage * 2 behind
     static constexpr int kBlock = 2 * kCodes + 4 * kPage;
     static constexpr int kBytes = kGroups * kBlock;    // of a page of one KV head
+    static constexpr int kUnit = kGroup == 16 ? 4 : 8; // rows that share words
 };
 
 // The scale of a group whose largest magnitude has the bits `a` (of NaN and infinity the group is NaN).
@@ -50,125 +54,165 @@ __device__ __forceinline__ float group_scale(uint32_t a)
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// Codes of a group of GS entries; returns its scale.
-template <int GS>
-__device__ __forceinline__ float quantise(const float (&x)[GS], int (&code)[GS])
-{
-    uint32_t a = 0u;
-#pragma unroll
-    for (int i = 0; i < GS; ++i)
-        a = max(a, magnitude(x[i]));
-    const float s = group_scale(a);
-#pragma unroll
-    for (int i = 0; i < GS; ++i)
-        code[i] = s > 0.f ? (int)fminf(fmaxf(rintf(__fdiv_rn(x[i], s)), -7.f), 7.f) : 0;
-    return s;
-}
+// Slot r of half h of a word: where a code's magnitude and its sign are.
+__host__ __device__ constexpr int slot_shift(int r, int h) { return 16 * h + 4 * r; }
+__host__ __device__ constexpr int slot_sign(int r, int h) { return (15 + 16 * h + 4 * r) % 32; }
+__host__ __device__ constexpr uint32_t slot_mask(int r, int h) { return 7u << slot_shift(r, h) | 1u << slot_sign(r, h); }
 
-// Offsets within a block: the word of a token pair's four key entries from 4 t on, and the 16-bit unit (8 bits where a
-// group has 8 entries) of the pair's value entries gg (and gg + 8).  r: row of the pair's first token, even.
-template <int GS>
-__device__ __forceinline__ int key_word(int r, int t)
-{
-    return (r >> 3) * (4 * GS) + t * 16 + ((r >> 1) & 3) * 4;
-}
-template <int GS>
-__device__ __forceinline__ int value_unit(int r, int gg)
-{
-    const int t = r >> 4, h = (r >> 3) & 1, i = (r >> 1) & 3;
-    return GS == 16 ? (gg * 4 + t) * 16 + i * 4 + 2 * h : (gg * 4 + t) * 8 + (i >> 1) * 4 + 2 * h + (i & 1);
-}
-
-// Writes the keys' (VALUES: the values') codes and scales of rows r and r + 1 (r even) into a block; `has`: bit 0 for
-// row r, bit 1 for row r + 1.  The other one's codes stay.
+// Word j (of 8) of a unit: the row in the unit and the entry that slot r of half h holds.
 template <int GS, bool VALUES>
-__device__ __forceinline__ void write_pair(unsigned char *block, int r, unsigned has, const int (&c0)[GS],
-                                           const int (&c1)[GS], float s0, float s1)
+__host__ __device__ constexpr int word_row(int j, int r, int h)
 {
-    constexpr int kCodes = kPage * GS / 2;
-    unsigned char *at = block + (VALUES ? kCodes : 0);
-    if constexpr (!VALUES) {
+    return GS == 16 ? (VALUES ? 2 * (r >> 1) + h : (j >> 2) + 2 * (r & 1)) : VALUES ? 2 * r + h : (j >> 2) + 2 * r;
+}
+template <int GS, bool VALUES>
+__host__ __device__ constexpr int word_entry(int j, int r, int h)
+{
+    return VALUES ? j + (GS == 16 ? 8 * (r & 1) : 0) : GS == 16 ? 4 * (j & 3) + 2 * (r >> 1) + h : 2 * (j & 3) + h;
+}
+// Its offset in the block's keys (values); row0: the unit's first row.
+template <int GS, bool VALUES>
+__device__ __forceinline__ int word_offset(int row0, int j)
+{
+    const int t = row0 >> 4, lane = VALUES ? j * 4 + t : (2 * t + (j >> 2)) * 4 + (j & 3);
+    return GS == 16 ? lane * 16 + ((row0 >> 2) & 3) * 4 : lane * 8 + ((row0 >> 3) & 1) * 4;
+}
+__device__ __forceinline__ int scale_index(int row)
+{
+    return (2 * (row >> 4) + (row & 1)) * 8 + 2 * ((row >> 2) & 3) + ((row >> 1) & 1);
+}
+
+// A unit on its way into a block: eight words of its keys or values.
+template <int GS, bool VALUES>
+struct UnitWords {
+    static constexpr int kRows = GS == 16 ? 4 : 8;
+    uint32_t w[8];
+    __device__ __forceinline__ UnitWords()
+    {
 #pragma unroll
-        for (int t = 0; t < GS / 4; ++t) {
-            uint32_t x0 = 0u, x1 = 0u;
+        for (int j = 0; j < 8; ++j)
+            w[j] = 0u;
+    }
+    // Row k (a constant) of the unit; returns its scale.
+    __device__ __forceinline__ float add(const float (&x)[GS], int k)
+    {
+        uint32_t a = 0u;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int p = c0[4 * t + e], q = c1[4 * t + e];
-                x0 |= ((uint32_t)abs(p) | (p < 0 ? 0x80u : 0u)) << (8 * e);
-                x1 |= ((uint32_t)abs(q) | (q < 0 ? 0x80u : 0u)) << (8 * e);
+        for (int i = 0; i < GS; ++i)
+            a = max(a, magnitude(x[i]));
+        const float s = group_scale(a);
+        uint32_t code[GS];  // magnitude, sign at bit 31
+#pragma unroll
+        for (int i = 0; i < GS; ++i) {
+            const float q = s > 0.f ? fminf(rintf(__fdiv_rn(fabsf(x[i]), s)), 7.f) : 0.f;
+            code[i] = (uint32_t)q | (q > 0.f ? __float_as_uint(x[i]) & 0x80000000u : 0u);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (word_row<GS, VALUES>(j, r, h) == k) {
+                        const uint32_t c = code[word_entry<GS, VALUES>(j, r, h)];
+                        w[j] |= (c & 7u) << slot_shift(r, h) | (c >> 31) << slot_sign(r, h);
+                    }
+        return s;
+    }
+    // Rows of which `has` has no bit keep their codes.
+    __device__ __forceinline__ void store(unsigned char *block, int row0, unsigned has) const
+    {
+        unsigned char *at = block + (VALUES ? kPage * GS / 2 : 0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            uint32_t *p = reinterpret_cast<uint32_t *>(at + word_offset<GS, VALUES>(row0, j));
+            uint32_t x = w[j];
+            if (has != (1u << kRows) - 1u) {
+                uint32_t mask = 0u;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        mask |= has >> word_row<GS, VALUES>(j, r, h) & 1u ? slot_mask(r, h) : 0u;
+                x = (*p & ~mask) | (x & mask);
             }
-            uint32_t *w = reinterpret_cast<uint32_t *>(at + key_word<GS>(r, t));
-            const uint32_t x = x0 | __funnelshift_l(x1, x1, 4);
-            if (has == 3u)
-                *w = x;
-            else if (has == 1u)
-                *w = (*w & ~0x87878787u) | x0;
-            else
-                *w = (*w & 0x87878787u) | __funnelshift_l(x1, x1, 4);
-        }
-    } else if constexpr (GS == 16) {
-#pragma unroll
-        for (int gg = 0; gg < 8; ++gg) {
-            const uint32_t x0 = (c0[gg] + 8) | (c0[gg + 8] + 8) << 4, x1 = (c1[gg] + 8) | (c1[gg + 8] + 8) << 4;
-            unsigned char *u = at + value_unit<16>(r, gg);
-            if (has == 3u)
-                *reinterpret_cast<uint16_t *>(u) = (uint16_t)(x0 | x1 << 8);
-            else
-                u[has == 1u ? 0 : 1] = (unsigned char)(has == 1u ? x0 : x1);
-        }
-    } else {
-#pragma unroll
-        for (int gg = 0; gg < 8; ++gg) {
-            const uint32_t x0 = c0[gg] + 8, x1 = (c1[gg] + 8) << 4;
-            unsigned char *u = at + value_unit<8>(r, gg);
-            *u = (unsigned char)(has == 3u ? x0 | x1 : has == 1u ? (*u & 0xf0u) | x0 : (*u & 0x0fu) | x1);
+            *p = x;
         }
     }
-    uint16_t *sc = reinterpret_cast<uint16_t *>(block + 2 * kCodes + (VALUES ? 2 * kPage : 0)) + r;
-    const uint32_t b0 = __float_as_uint(s0) >> 16, b1 = __float_as_uint(s1) >> 16;  // (a scale is a bf16 number)
-    if (has == 3u)
-        *reinterpret_cast<uint32_t *>(sc) = b0 | b1 << 16;
-    else if (has == 1u)
-        sc[0] = (uint16_t)b0;
-    else
-        sc[1] = (uint16_t)b1;
+};
+
+template <int GS, bool VALUES>
+__device__ __forceinline__ uint16_t *scales_of(unsigned char *block)
+{
+    return reinterpret_cast<uint16_t *>(block + kPage * GS + (VALUES ? 2 * kPage : 0));
 }
 
-// The values that rows r and r + 1 (r even) of a block stand for.
-template <int GS, bool VALUES>
-__device__ __forceinline__ void read_pair(const unsigned char *block, int r, float (&x0)[GS], float (&x1)[GS])
+// Quantises rows row0 .. (a unit's; row(k, x) fetches row k of it) into a block.
+template <int GS, bool VALUES, typename Row>
+__device__ __forceinline__ void write_unit(unsigned char *block, int row0, unsigned has, const Row &row)
 {
-    constexpr int kCodes = kPage * GS / 2;
-    const unsigned char *at = block + (VALUES ? kCodes : 0);
-    const uint32_t sc = *reinterpret_cast<const uint32_t *>(block + 2 * kCodes + (VALUES ? 2 * kPage : 0) + 2 * r);
-    const float s0 = bf16lo(sc), s1 = bf16hi(sc);
-    if constexpr (!VALUES) {
+    UnitWords<GS, VALUES> u;
+    uint16_t *scales = scales_of<GS, VALUES>(block);
 #pragma unroll
-        for (int t = 0; t < GS / 4; ++t) {
-            const uint32_t w = *reinterpret_cast<const uint32_t *>(at + key_word<GS>(r, t));
-            const uint32_t v = __funnelshift_r(w, w, 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float y0 = (float)((w >> (8 * e)) & 7u) * s0, y1 = (float)((v >> (8 * e)) & 7u) * s1;
-                x0[4 * t + e] = (w >> (8 * e)) & 0x80u ? -y0 : y0;
-                x1[4 * t + e] = (v >> (8 * e)) & 0x80u ? -y1 : y1;
-            }
+    for (int k = 0; k < UnitWords<GS, VALUES>::kRows; ++k)
+        if (has >> k & 1u) {
+            float x[GS];
+            row(k, x);
+            scales[scale_index(row0 + k)] = (uint16_t)(__float_as_uint(u.add(x, k)) >> 16);  // (a bf16 number)
         }
-    } else {
+    u.store(block, row0, has);
+}
+
+// The values that a row of a block stands for.
+template <int GS, bool VALUES>
+__device__ __forceinline__ void read_row(const unsigned char *block, int row, float (&x)[GS])
+{
+    constexpr int U = GS == 16 ? 4 : 8;
+    const int row0 = row & ~(U - 1), k = row - row0;
+    const float s = __uint_as_float((uint32_t)scales_of<GS, VALUES>(const_cast<unsigned char *>(block))[scale_index(row)] << 16);
+    const unsigned char *at = block + (VALUES ? kPage * GS / 2 : 0);
 #pragma unroll
-        for (int gg = 0; gg < 8; ++gg) {
-            const unsigned char *p = at + value_unit<GS>(r, gg);
-            if constexpr (GS == 16) {
-                const uint32_t u = *reinterpret_cast<const uint16_t *>(p);
-                x0[gg] = (float)((int)(u & 15u) - 8) * s0;
-                x0[gg + 8] = (float)((int)(u >> 4 & 15u) - 8) * s0;
-                x1[gg] = (float)((int)(u >> 8 & 15u) - 8) * s1;
-                x1[gg + 8] = (float)((int)(u >> 12) - 8) * s1;
-            } else {
-                x0[gg] = (float)((int)(*p & 15u) - 8) * s0;
-                x1[gg] = (float)((int)(*p >> 4) - 8) * s1;
-            }
-        }
+    for (int j = 0; j < 8; ++j) {
+        if (!VALUES && (j >> 2) != (row & 1))
+            continue;
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(at + word_offset<GS, VALUES>(row0, j));
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (word_row<GS, VALUES>(j, r, h) == k) {
+                    const float y = (float)((w >> slot_shift(r, h)) & 7u) * s;
+                    x[word_entry<GS, VALUES>(j, r, h)] = w >> slot_sign(r, h) & 1u ? -y : y;
+                }
+    }
+}
+
+// All rows of a unit; put(k, x) takes row k.
+template <int GS, bool VALUES, typename Put>
+__device__ __forceinline__ void read_unit(const unsigned char *block, int row0, const Put &put)
+{
+    constexpr int U = GS == 16 ? 4 : 8;
+    const unsigned char *at = block + (VALUES ? kPage * GS / 2 : 0);
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        w[j] = *reinterpret_cast<const uint32_t *>(at + word_offset<GS, VALUES>(row0, j));
+    const uint16_t *scales = scales_of<GS, VALUES>(const_cast<unsigned char *>(block));
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const float s = __uint_as_float((uint32_t)scales[scale_index(row0 + k)] << 16);
+        float x[GS];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (word_row<GS, VALUES>(j, r, h) == k) {
+                        const float y = (float)((w[j] >> slot_shift(r, h)) & 7u) * s;
+                        x[word_entry<GS, VALUES>(j, r, h)] = w[j] >> slot_sign(r, h) & 1u ? -y : y;
+                    }
+        put(k, x);
     }
 }
 

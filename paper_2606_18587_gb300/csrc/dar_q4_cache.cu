@@ -19,8 +19,8 @@ namespace q4 {
 // (sequence, KV head, keys or values) that push positions m = L + j - w out of the
 // window, projects these (the same fp32 chains, rounded to T), and puts the tokens
 // that stay into the ring slots that they leave.  Its tile starts at a position that
-// is a multiple of a page, so that two tokens that share words of a page have the
-// same CTA; a thread then quantises and writes two tokens' group.
+// is a multiple of a page, so that tokens that share words of a page have the same CTA; a
+// thread then quantises and writes a unit of them.
 template <typename T, int DD, int RPT, int NR>
 __global__ void __launch_bounds__(NR *slices<DD>()) append_kernel(AppendArgs a, int tiles)
 {
@@ -71,9 +71,12 @@ __global__ void __launch_bounds__(NR *slices<DD>()) append_kernel(AppendArgs a, 
             store_row<T, CW>(vec + (size_t)(r0 + k * NR) * DD + c0, acc[k]);
         __syncthreads();
         unsigned char *pool = static_cast<unsigned char *>(a.pool_kd);
-        for (int i = tid; i < R / 2 * F::kGroups; i += NT) {
-            const int r = 2 * (i % (R / 2)), sb = i / (R / 2);
-            const unsigned has = (r >= ra && r < nr ? 1u : 0u) | (r + 1 >= ra && r + 1 < nr ? 2u : 0u);
+        for (int i = tid; i < R / F::kUnit * F::kGroups; i += NT) {
+            const int r = i % (R / F::kUnit) * F::kUnit, sb = i / (R / F::kUnit);
+            unsigned has = 0u;
+#pragma unroll
+            for (int k = 0; k < F::kUnit; ++k)
+                has |= r + k >= ra && r + k < nr ? 1u << k : 0u;
             if (!has)
                 continue;
             const int m = m0 + r, id = a.block_table[(size_t)b * a.maxp + m / kPage];
@@ -81,21 +84,16 @@ __global__ void __launch_bounds__(NR *slices<DD>()) append_kernel(AppendArgs a, 
                 report(a.status, DAR_ERR_CAPACITY);
                 continue;
             }
-            float x[F::kGroup];
-            int code0[F::kGroup], code1[F::kGroup];
-#pragma unroll
-            for (int e = 0; e < F::kGroup; ++e)
-                x[e] = to_f32(vec[(size_t)r * DD + sb * F::kGroup + e]);
-            const float s0 = quantise<F::kGroup>(x, code0);
-#pragma unroll
-            for (int e = 0; e < F::kGroup; ++e)
-                x[e] = to_f32(vec[(size_t)(r + 1) * DD + sb * F::kGroup + e]);
-            const float s1 = quantise<F::kGroup>(x, code1);
             unsigned char *block = pool + ((size_t)id * a.Hkv + g) * F::kBytes + sb * F::kBlock;
+            auto row = [&](int k, float (&x)[F::kGroup]) {
+#pragma unroll
+                for (int e = 0; e < F::kGroup; ++e)
+                    x[e] = to_f32(vec[(size_t)(r + k) * DD + sb * F::kGroup + e]);
+            };
             if (kv)
-                write_pair<F::kGroup, true>(block, m % kPage, has, code0, code1, s0, s1);
+                write_unit<F::kGroup, true>(block, m % kPage, has, row);
             else
-                write_pair<F::kGroup, false>(block, m % kPage, has, code0, code1, s0, s1);
+                write_unit<F::kGroup, false>(block, m % kPage, has, row);
         }
     }
     // ring slots (L + j) % w, j < min(nb, w): the last new token of each
@@ -144,7 +142,7 @@ static cudaError_t append_tiles(const AppendArgs &a, cudaStream_t s)
 
 // ------------------------------------------------------------------ conversion
 //
-// A warp takes a page of a (sequence, KV head), a lane two tokens, one group after the other.
+// A warp takes a page of a (sequence, KV head), a lane a unit of its keys or values, one group after the other.
 constexpr int kConvertWarps = 8;
 
 template <typename T, int GS>
@@ -186,38 +184,36 @@ __global__ void __launch_bounds__(kConvertWarps * 32) convert_kernel(Q4ConvertAr
             report(a.status, DAR_ERR_CAPACITY);
         return;
     }
-    const int r = 2 * lane;
+    constexpr int U = F::kUnit, UNITS = kPage / U;  // of keys, and of values
+    const int r = lane % UNITS * U;
+    const bool values = lane >= UNITS;
     const long long pos = lp * kPage + r;
-    const unsigned has = (pos >= first && pos < end ? 1u : 0u) | (pos + 1 >= first && pos + 1 < end ? 2u : 0u);
-    if (!has)
+    unsigned has = 0u;
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+        has |= pos + k >= first && pos + k < end ? 1u << k : 0u;
+    if (!has || lane >= 2 * UNITS)
         return;
     unsigned char *page = static_cast<unsigned char *>(a.pool) + ((size_t)id4 * a.Hkv + g) * F::kBytes;
-    const size_t row = (((size_t)id * a.Hkv + g) * kPage + r) * DD;
+    T *vec = static_cast<T *>(values ? a.pool_vd : a.pool_kd) + (((size_t)id * a.Hkv + g) * kPage + r) * DD;
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-        T *vec = static_cast<T *>(kv ? a.pool_vd : a.pool_kd) + row;
-#pragma unroll
-        for (int sb = 0; sb < F::kGroups; ++sb) {
-            float x0[GS], x1[GS];
-            if constexpr (PACK) {
-                int c0[GS], c1[GS];
-                load_group<T, GS>(vec + sb * GS, x0);
-                load_group<T, GS>(vec + DD + sb * GS, x1);
-                const float s0 = quantise<GS>(x0, c0), s1 = quantise<GS>(x1, c1);
-                if (kv)
-                    write_pair<GS, true>(page + sb * F::kBlock, r, has, c0, c1, s0, s1);
-                else
-                    write_pair<GS, false>(page + sb * F::kBlock, r, has, c0, c1, s0, s1);
-            } else {
-                if (kv)
-                    read_pair<GS, true>(page + sb * F::kBlock, r, x0, x1);
-                else
-                    read_pair<GS, false>(page + sb * F::kBlock, r, x0, x1);
-                if (has & 1u)
-                    store_row<T, GS>(vec + sb * GS, x0);
-                if (has & 2u)
-                    store_row<T, GS>(vec + DD + sb * GS, x1);
-            }
+    for (int sb = 0; sb < F::kGroups; ++sb) {
+        unsigned char *block = page + sb * F::kBlock;
+        if constexpr (PACK) {
+            auto row = [&](int k, float (&x)[GS]) { load_group<T, GS>(vec + k * DD + sb * GS, x); };
+            if (values)
+                write_unit<GS, true>(block, r, has, row);
+            else
+                write_unit<GS, false>(block, r, has, row);
+        } else {
+            auto put = [&](int k, const float (&x)[GS]) {
+                if (has >> k & 1u)
+                    store_row<T, GS>(vec + k * DD + sb * GS, x);
+            };
+            if (values)
+                read_unit<GS, true>(block, r, put);
+            else
+                read_unit<GS, false>(block, r, put);
         }
     }
 }

@@ -317,7 +317,8 @@ __device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, Lan
 #pragma unroll 1
             for (int i = 0; i < NB; ++i) {
                 float x0[GS], x1[GS];
-                read_pair<GS, false>(page + i * F::kBlock, 2 * lane, x0, x1);
+                read_row<GS, false>(page + i * F::kBlock, 2 * lane, x0);
+                read_row<GS, false>(page + i * F::kBlock, 2 * lane + 1, x1);
 #pragma unroll
                 for (int r = 0; r < kRows; ++r)
 #pragma unroll
@@ -333,7 +334,8 @@ __device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, Lan
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 float x0[GS], x1[GS];
-                read_pair<GS, true>(page + i * F::kBlock, 2 * lane, x0, x1);
+                read_row<GS, true>(page + i * F::kBlock, 2 * lane, x0);
+                read_row<GS, true>(page + i * F::kBlock, 2 * lane + 1, x1);
                 __syncwarp();
 #pragma unroll
                 for (int e = 0; e < GS; ++e) {  // rows behind the last token may hold anything
@@ -391,38 +393,40 @@ __global__ void __launch_bounds__(kWarps * 32) attend_kernel(Args a)
 
 // ------------------------------------------------------------------ attend, tensor cores
 //
-// Up to 8 query heads lie on the N side of mma.sync products with 16 tokens on the M side
-// (a tcgen05 tile has 128 rows: most calls have 1 to 8 heads per KV head).  Column 2 t of a
-// product belongs to head t and column 2 t + 1 to head t + 4, so lane (g, t) = 4 g + t has the
-// scores, weights, references and sums of heads t and t + 4 (CT = 2; of head t alone with CT = 1).
+// Up to 8 query heads lie on the N side of mma.sync products (m16n8k16, fp16) with 16 tokens
+// on the M side (a tcgen05 tile has 128 rows: most calls have 1 to 8 heads per KV head).
+// Column 2 t of a product belongs to head t and column 2 t + 1 to head t + 4, so lane (g, t) =
+// 4 g + t has the scores, weights, references and sums of heads t and t + 4 (CT = 2); with CT = 1
+// of head t alone, and the other column takes what is said below.
 //
-//  scores   m16n8k32 on e4m3 operands: the codes are e4m3 numbers as they lie in memory (three
-//           instructions for eight), and q~, brought to [128, 256) by a power of two, is four e4m3
-//           terms (2^-16 of it).  K = 32 takes the 16 entries twice: a column's terms 0 and 1, the
-//           next column's terms 2 and 3.  With a d_down of 8 one column takes all four.
+//  codes    fp16 subnormals code * 2^-24 as they lie: seven instructions for the eight of a word.
+//           (Their values by a conversion of offset codes take 13: an AND and an OR each, since an
+//           instruction has one immediate, and the offset subtracted; e4m3 operands are converted
+//           by twice as many: mma.sync has no products of them here.)
+//  scores   q~, brought to [2^14, 2^15) by a power of two, is two fp16 terms (2^-22 of it).  CT = 1:
+//           the second one is the other column's.  CT = 2: a product of its own.  A d_down of 8:
+//           the other half of the product's 16 entries.
 //  weights  p s_v as fp16 (2^-11) relative to a reference of the row that keeps the largest at
 //           2^8 when it is set and below 2^15 always; it is raised by a vote.  (bf16 operands need two
 //           terms for the same error, twice the conversions and transpositions.)
-//  sums     m16n8k16 on fp16: code + 8 in the low bits of 1024's significand, and 1032 subtracted.
-// Of a page of 64 tokens this is some 145 instructions of a warp for four heads.
 
 struct Soft {  // of one head of a lane
     float bias, l;  // minus the reference; the lane's share of the sum of weights
 };
-
-__device__ __forceinline__ void mma_e4m3(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1)
-{
-    const float z = 0.f;
-    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%4,%5}, {%6,%7}, {%8,%8,%8,%8};"
-        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-        : "r"(a0), "r"(a1), "r"(b0), "r"(b1), "f"(z));
-}
 
 __device__ __forceinline__ void mma_f16_acc(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ void mma_f16_c(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1,
+                                          const float (&c)[4])
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
@@ -439,40 +443,21 @@ __device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi)
     return r;
 }
 
-__device__ __forceinline__ uint32_t fma_f16x2(uint32_t a, uint32_t b, uint32_t c)
+// Two values as two fp16 terms each: all but 2^-22 of them.
+__device__ __forceinline__ void split_f16(float x, float y, uint32_t &hi, uint32_t &lo)
 {
-    uint32_t r;
-    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-    return r;
-}
-__device__ __forceinline__ uint32_t add_f16x2(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("add.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
+    hi = cvt_f16x2(x, y);
+    float a, b;
+    asm("{.reg .b16 p, q; mov.b32 {p, q}, %2; cvt.f32.f16 %0, p; cvt.f32.f16 %1, q;}" : "=f"(a), "=f"(b) : "r"(hi));
+    lo = cvt_f16x2(x - a, y - b);
 }
 
-// Four values as NT e4m3 terms each, four bytes to a word.
-template <int NT>
-__device__ __forceinline__ void e4m3_terms(float (&x)[4], uint32_t (&t)[NT])
+// Slots 0 to 3 of a word of codes as operand registers.
+__device__ __forceinline__ void codes_of(uint32_t w, uint32_t (&c)[4])
 {
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        uint32_t w[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            uint16_t u;
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(u) : "f"(x[2 * j + 1]), "f"(x[2 * j]));
-            uint32_t h;
-            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(u));
-            float lo, hi;
-            asm("{.reg .b16 a, b; mov.b32 {a, b}, %2; cvt.f32.f16 %0, a; cvt.f32.f16 %1, b;}" : "=f"(lo), "=f"(hi) : "r"(h));
-            x[2 * j] -= lo;
-            x[2 * j + 1] -= hi;
-            w[j] = u;
-        }
-        t[i] = w[0] | w[1] << 16;
-    }
+    for (int r = 0; r < 4; ++r)
+        c[r] = __funnelshift_r(w, w, 4 * r) & 0x80078007u;
 }
 
 // Two fp32 values as three bf16 terms each: all but 2^-24 of them.
@@ -561,12 +546,13 @@ struct Filler {
 template <int DD, int CT>
 struct Heads {
     static constexpr int GS = Fmt<DD>::kGroup, NB = Fmt<DD>::kGroups;
-    static constexpr int TB = GS == 16 ? CT : 1;  // score products of a group
+    static constexpr int TB = GS == 16 && CT == 2 ? 2 : 1;  // score products of a group
+    static constexpr int OD = CT == 1 ? 2 : 1;    // sums of a group (see page_step)
     uint32_t q[4][2];        // ring: queries as B operands
-    uint32_t qt[NB][TB][2];  // pages: q~ as B operands, four e4m3 terms
-    float cq[CT];            // scale of a score: c2, the power of two taken out of q~, and the codes' 2^9
+    uint32_t qt[NB][TB][2];  // pages: q~ as B operands, two fp16 terms
+    float cq[CT];            // scale of a score: c2, the power of two taken out of q~, and the codes' 2^24
     Soft ring[CT], page[CT];
-    float ol[kHeadDim / 16][4], od[NB][4];
+    float ol[kHeadDim / 16][4], od[NB][OD][4];
 
     // Queries of a cut, and q~^T = Uk q^T with Uk in three bf16 terms (products exact but for 2^-24).
     __device__ __forceinline__ void begin(const Args &a, const Cut &c, int lane)
@@ -603,7 +589,7 @@ struct Heads {
             for (int y = 0; y < 4; ++y)
                 x[j][y] = z[0][y] + (z[1][y] + z[2][y]);
         }
-        // the largest entry of each head, and the power of two that brings it to [2^7, 2^8)
+        // the largest entry of each head, and the power of two that brings it to [2^14, 2^15)
         float up[CT];
 #pragma unroll
         for (int k = 0; k < CT; ++k) {
@@ -615,51 +601,52 @@ struct Heads {
             for (int o = 4; o < 32; o <<= 1)
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
             const int e = max((int)(top >> 23) - 127, -100);
-            up[k] = __uint_as_float((uint32_t)(127 + 7 - e) << 23);  // e <= 127: 2^-120 at least
+            up[k] = __uint_as_float((uint32_t)(127 + 14 - e) << 23);  // e <= 127: 2^-113 at least
             // infinite or NaN: so are all scores
             cq[k] = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u)
-                                       : a.c.c2 * __uint_as_float((uint32_t)(127 + e) << 23) * 4.f;
+                                       : a.c.c2 * __uint_as_float((uint32_t)(127 + e) << 23) * 1024.f;
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 x[j][k] *= up[k];
                 x[j][2 + k] *= up[k];
             }
         }
-        // column i0 of a score product wants four consecutive entries of its head
+        // column i0 of a score product wants consecutive entries of its head, i0 / 2 (+ 4 in odd columns with CT = 2): four
+        // from 4 c0 on, or of a d_down of 8 two from 2 c0 on
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
+        for (int j = 0; j < NB; ++j) {
+            constexpr int NE = GS == 16 ? 4 : 2;
+            float y[NE];
 #pragma unroll
-            for (int k = 0; k < TB; ++k) {
-                float y[4];
-                uint32_t t[4];
-                if constexpr (GS == 16) {  // head i0 / 2 + 4 k, entries 4 c0 ..
+            for (int e = 0; e < NE; ++e) {
+                const int from = ((NE * c0 + e) & 7) * 4 + (i0 >> 1);
+                float z[CT];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int from = ((4 * c0 + e) & 7) * 4 + (i0 >> 1);
-                        const float lo = __shfl_sync(0xffffffffu, x[j][k], from);
+                for (int k = 0; k < CT; ++k) {
+                    z[k] = __shfl_sync(0xffffffffu, x[j][k], from);
+                    if constexpr (GS == 16) {
                         const float hi = __shfl_sync(0xffffffffu, x[j][2 + k], from);
-                        y[e] = c0 < 2 ? lo : hi;
+                        z[k] = c0 < 2 ? z[k] : hi;
                     }
-                    e4m3_terms<4>(y, t);
-                    qt[j][k][0] = i0 & 1 ? t[2] : t[0];
-                    qt[j][k][1] = i0 & 1 ? t[3] : t[1];
-                } else {  // head i0 / 2 + 4 (i0 mod 2), entries 4 (c0 mod 2) ..
+                }
+                y[e] = i0 & 1 ? z[CT - 1] : z[0];
+            }
+            uint32_t hi[NE / 2], lo[NE / 2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int from = ((4 * c0 + e) & 7) * 4 + (i0 >> 1);
-                        y[e] = __shfl_sync(0xffffffffu, x[j][0], from);
-                        if constexpr (CT == 2) {
-                            const float hi = __shfl_sync(0xffffffffu, x[j][1], from);
-                            y[e] = i0 & 1 ? hi : y[e];
-                        } else {
-                            y[e] = i0 & 1 ? 0.f : y[e];
-                        }
-                    }
-                    e4m3_terms<4>(y, t);
-                    qt[j][k][0] = c0 < 2 ? t[0] : t[1];
-                    qt[j][k][1] = c0 < 2 ? t[2] : t[3];
+            for (int e = 0; e < NE / 2; ++e)
+                split_f16(y[2 * e], y[2 * e + 1], hi[e], lo[e]);
+            if constexpr (GS == 8) {
+                qt[j][0][0] = CT == 2 || !(i0 & 1) ? hi[0] : 0u;
+                qt[j][0][1] = CT == 2 || !(i0 & 1) ? lo[0] : 0u;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    qt[j][0][e] = CT == 1 && (i0 & 1) ? lo[e % (NE / 2)] : hi[e % (NE / 2)];
+                    if constexpr (CT == 2)
+                        qt[j][TB - 1][e] = lo[e % (NE / 2)];
                 }
             }
+        }
 #pragma unroll
         for (int k = 0; k < CT; ++k) {
             ring[k].bias = page[k].bias = INFINITY;
@@ -670,7 +657,9 @@ struct Heads {
             ol[e][0] = ol[e][1] = ol[e][2] = ol[e][3] = 0.f;
 #pragma unroll
         for (int j = 0; j < NB; ++j)
-            od[j][0] = od[j][1] = od[j][2] = od[j][3] = 0.f;
+#pragma unroll
+            for (int o = 0; o < OD; ++o)
+                od[j][o][0] = od[j][o][1] = od[j][o][2] = od[j][o][3] = 0.f;
     }
 
     // A run of n ring tokens at `tile`: 16 rows of keys, then of values, 128-byte swizzle.
@@ -741,32 +730,66 @@ struct Heads {
         }
     }
 
-    // A page of n tokens.
+    // The lane's words of a page's keys or values: four, or of a d_down of 8 two, each twice.
+    static __device__ __forceinline__ void load_words(const unsigned char *at, int lane, uint32_t (&w)[4])
+    {
+        if constexpr (GS == 16) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(at + lane * 16);
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2 *>(at + lane * 8);
+            w[0] = w[1] = v.x, w[2] = w[3] = v.y;
+        }
+    }
+
+    // A page of n tokens; lane (g, t) has the scores of rows 16 (g / 2) + 4 i + 2 c + g mod 2.  Products of weights: with
+    // CT = 2 a column has 8 tokens' weights of head t or t + 4.  With CT = 1 column 2 t has those of rows with c = 0 and
+    // column 2 t + 1 those with c = 1, which one transposition brings; products with the codes of c = 0 are right in the
+    // even columns and products with those of c = 1 in the odd ones, so each has sums of its own, whose other columns are
+    // not used.
     __device__ __forceinline__ void page_step(const unsigned char *at, int n, int lane)
     {
         using F = Fmt<DD>;
         const int i0 = lane >> 2, c0 = lane & 3;
-        constexpr uint32_t kCode = 0x87878787u;
-        float y[CT][4][2];  // scores of tokens 8 i0 + 2 i, + 1
+        // pairs: two tokens (c = 0, 1) of a head, or two heads of a token; pair i, or pairs 2 i, 2 i + 1
+        constexpr int NP = 4 * CT;
+        float y[NP][2];
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const unsigned char *block = at + j * F::kBlock;
-            const uint4 kw = *reinterpret_cast<const uint4 *>(block + (GS == 16 ? lane * 16 : i0 * 32 + (c0 & 1) * 16));
             const uint4 sw = *reinterpret_cast<const uint4 *>(block + F::kScales + i0 * 16);
-            const uint32_t w[4] = {kw.x, kw.y, kw.z, kw.w}, sc[4] = {sw.x, sw.y, sw.z, sw.w};
+            const uint32_t sc[4] = {sw.x, sw.y, sw.z, sw.w};
+            uint32_t w[4];
+            load_words(block, lane, w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t a0 = w[i] & kCode, a1 = __funnelshift_r(w[i], w[i], 4) & kCode;
-                float d[TB][4];
-#pragma unroll
-                for (int k = 0; k < TB; ++k)
-                    mma_e4m3(d[k], a0, a1, qt[j][k][0], qt[j][k][1]);
-#pragma unroll
-                for (int k = 0; k < CT; ++k) {
-                    const float x0 = GS == 16 ? d[k % TB][0] + d[k % TB][1] : d[0][k];
-                    const float x1 = GS == 16 ? d[k % TB][2] + d[k % TB][3] : d[0][2 + k];
-                    y[k][i][0] = j ? fmaf(x0, bf16lo(sc[i]), y[k][i][0]) : x0 * bf16lo(sc[i]);
-                    y[k][i][1] = j ? fmaf(x1, bf16hi(sc[i]), y[k][i][1]) : x1 * bf16hi(sc[i]);
+                uint32_t c[4];
+                codes_of(w[i], c);
+                if constexpr (GS == 8) {  // both halves of the product's 16 entries are the key's 8
+                    c[0] = i % 2 ? c[2] : c[0];
+                    c[1] = i % 2 ? c[3] : c[1];
+                    c[2] = c[0];
+                    c[3] = c[1];
+                }
+                const float z[4] = {0.f, 0.f, 0.f, 0.f};
+                float d[4];
+                mma_f16_c(d, c, qt[j][0][0], qt[j][0][1], z);
+                if constexpr (TB == 2)
+                    mma_f16_acc(d, c, qt[j][TB - 1][0], qt[j][TB - 1][1]);
+                const float s0 = bf16lo(sc[i]), s1 = bf16hi(sc[i]);
+                if constexpr (CT == 1) {
+                    const float x0 = GS == 16 ? d[0] + d[1] : d[0], x1 = GS == 16 ? d[2] + d[3] : d[2];
+                    y[i][0] = j ? fmaf(x0, s0, y[i][0]) : x0 * s0;
+                    y[i][1] = j ? fmaf(x1, s1, y[i][1]) : x1 * s1;
+                } else {
+                    float(&u)[2] = y[2 * i], (&v)[2] = y[(2 * i + 1) % NP];
+                    if (j == 0) {
+                        mul2(u[0], u[1], d[0], d[1], s0, s0);
+                        mul2(v[0], v[1], d[2], d[3], s1, s1);
+                    } else {
+                        ffma2(u[0], u[1], d[0], d[1], s0, s0, u[0], u[1]);
+                        ffma2(v[0], v[1], d[2], d[3], s1, s1, v[0], v[1]);
+                    }
                 }
             }
         }
@@ -779,52 +802,67 @@ struct Heads {
         if (n < kPage) {  // rows behind the last token may hold anything
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int tok = 8 * i0 + 2 * i;
-                const uint32_t m = key_mask(tok, n);
+                const int tok = 16 * (i0 >> 1) + 4 * i + (i0 & 1);  // and tok + 2
+                const uint32_t m = (tok < n ? 0xffffu : 0u) | (tok + 2 < n ? 0xffff0000u : 0u);
 #pragma unroll
                 for (int j = 0; j < NB; ++j)
                     vs[j][i] &= m;
 #pragma unroll
-                for (int k = 0; k < CT; ++k) {
-                    y[k][i][0] = tok < n ? y[k][i][0] : -INFINITY;
-                    y[k][i][1] = tok + 1 < n ? y[k][i][1] : -INFINITY;
+                for (int e = 0; e < 2; ++e) {
+                    if constexpr (CT == 1) {
+                        y[i][e] = tok + 2 * e < n ? y[i][e] : -INFINITY;
+                    } else {
+                        y[2 * i][e] = tok < n ? y[2 * i][e] : -INFINITY;
+                        y[(2 * i + 1) % NP][e] = tok + 2 < n ? y[(2 * i + 1) % NP][e] : -INFINITY;
+                    }
                 }
             }
         }
+        // the largest scales of the tokens' groups
+        uint32_t vm[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            vm[i] = vs[0][i];
+#pragma unroll
+            for (int j = 1; j < NB; ++j)
+                asm("max.bf16x2 %0, %0, %1;" : "+r"(vm[i]) : "r"(vs[j][i]));
+        }
         constexpr float kFar = 32768.f, kFarSum = 0x1p90f;
-        float p[CT][4][2], l[CT];
+        float p[NP][2], pw[NP][2], l[2];  // weights, and times vm
+        // a pair's scales
+        auto scales = [](uint32_t s, int k, float &s0, float &s1) {
+            s0 = CT == 1 || k % 2 == 0 ? bf16lo(s) : bf16hi(s);
+            s1 = CT == 1 || k % 2 != 0 ? bf16hi(s) : bf16lo(s);
+        };
         auto weigh = [&]() {  // returns whether something got far above the reference
             float top = 0.f;
-            bool far = false;
+            l[0] = l[1] = 0.f;
 #pragma unroll
-            for (int k = 0; k < CT; ++k) {
-                l[k] = 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    p[k][i][0] = ex2_approx(fmaf(y[k][i][0], cq[k], page[k].bias));
-                    p[k][i][1] = ex2_approx(fmaf(y[k][i][1], cq[k], page[k].bias));
-                    l[k] += p[k][i][0] + p[k][i][1];
-#pragma unroll
-                    for (int j = 0; j < NB; ++j)
-                        top = max3(top, p[k][i][0] * bf16lo(vs[j][i]), p[k][i][1] * bf16hi(vs[j][i]));
-                }
-                far |= l[k] > kFarSum;
+            for (int k = 0; k < NP; ++k) {
+                float x0, x1, s0, s1;
+                ffma2(x0, x1, y[k][0], y[k][1], cq[0], cq[CT - 1], page[0].bias, page[CT - 1].bias);
+                p[k][0] = ex2_approx(x0);
+                p[k][1] = ex2_approx(x1);
+                add2(l[0], l[1], l[0], l[1], p[k][0], p[k][1]);
+                scales(vm[k / CT], k, s0, s1);
+                mul2(pw[k][0], pw[k][1], p[k][0], p[k][1], s0, s1);
+                top = max3(top, pw[k][0], pw[k][1]);
             }
-            return far || top > kFar;
+            return fmaxf(l[0], l[1]) > kFarSum || top > kFar;
         };
         if (__any_sync(0xffffffffu, weigh())) {
 #pragma unroll
             for (int k = 0; k < CT; ++k) {
                 float top = -INFINITY;  // of p s_v, and of 2^-64 p
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < NP; ++i)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float s = 0x1p-64f;
-#pragma unroll
-                        for (int j = 0; j < NB; ++j)
-                            s = fmaxf(s, h ? bf16hi(vs[j][i]) : bf16lo(vs[j][i]));
-                        top = fmaxf(top, fmaf(y[k][i][h], cq[k], __log2f(s)));
+                    for (int e = 0; e < 2; ++e) {
+                        if (CT == 2 && e != k)
+                            continue;
+                        float s[2];
+                        scales(vm[i / CT], i, s[0], s[1]);
+                        top = fmaxf(top, fmaf(y[i][e], cq[k], __log2f(fmaxf(0x1p-64f, s[e]))));
                     }
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1)
@@ -835,45 +873,60 @@ struct Heads {
                 page[k].l *= f;
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
-                    od[j][k] *= f;
-                    od[j][2 + k] *= f;
+                    od[j][0][k] *= f;
+                    od[j][0][2 + k] *= f;
+                    if constexpr (CT == 1) {
+                        od[j][OD - 1][1] *= f;
+                        od[j][OD - 1][3] *= f;
+                    }
                 }
             }
             weigh();
         }
-#pragma unroll
-        for (int k = 0; k < CT; ++k)
-            page[k].l += l[k];
+        if constexpr (CT == 1) {
+            page[0].l += l[0] + l[1];
+        } else {
+            page[0].l += l[0];
+            page[CT - 1].l += l[1];
+        }
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            const unsigned char *block = at + j * F::kBlock + F::kCodes;
             uint32_t w[4];
-            if constexpr (GS == 16) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(block + lane * 16);
-                w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-            } else {
-                const uint2 v = *reinterpret_cast<const uint2 *>(block + lane * 8);
-                w[0] = v.x, w[1] = v.x >> 8, w[2] = v.y, w[3] = v.y >> 8;
+            load_words(at + j * F::kBlock + F::kCodes, lane, w);
+            uint32_t b[NP];
+#pragma unroll
+            for (int k = 0; k < NP; ++k) {
+                float s0, s1, w0 = pw[k][0], w1 = pw[k][1];
+                if constexpr (NB > 1) {
+                    scales(vs[j][k / CT], k, s0, s1);
+                    mul2(w0, w1, p[k][0], p[k][1], s0, s1);
+                }
+                b[k] = transpose8(cvt_f16x2(w0, w1));
             }
+            uint32_t v[4][4];  // entries i0 and i0 + 8 of the rows of word i with c = 0, and with c = 1
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float s0 = bf16lo(vs[j][i]), s1 = bf16hi(vs[j][i]);
-                const uint32_t b0 = transpose8(cvt_f16x2(p[0][i][0] * s0, CT == 2 ? p[CT - 1][i][0] * s0 : 0.f));
-                const uint32_t b1 = transpose8(cvt_f16x2(p[0][i][1] * s1, CT == 2 ? p[CT - 1][i][1] * s1 : 0.f));
-                // 1024 + (code + 8) and 1024 + 16 (code + 8)
-                auto low = [](uint32_t x) { return add_f16x2((x & 0x000f000fu) | 0x64006400u, 0xe408e408u); };
-                auto high = [](uint32_t x) { return fma_f16x2((x & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u); };
-                uint32_t v[4];
-                v[0] = low(w[i]);
                 if constexpr (GS == 16) {
-                    v[1] = high(w[i]);
-                    v[2] = low(w[i] >> 8);
-                    v[3] = high(w[i] >> 8);
-                } else {
-                    v[1] = v[3] = 0u;
-                    v[2] = high(w[i]);
+                    codes_of(w[i], v[i]);
+                } else if (i % 2 == 0) {
+                    uint32_t c[4];
+                    codes_of(w[i], c);
+                    v[i][0] = c[0], v[i][2] = c[1], v[i + 1][0] = c[2], v[i + 1][2] = c[3];
+                    v[i][1] = v[i][3] = v[i + 1][1] = v[i + 1][3] = 0u;
                 }
-                mma_f16_acc(od[j], v, b0, b1);
+            }
+            if constexpr (CT == 2) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    mma_f16_acc(od[j][0], v[i], b[2 * i], b[(2 * i + 1) % NP]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    const uint32_t even[4] = {v[i][0], v[i][1], v[i + 1][0], v[i + 1][1]};
+                    const uint32_t odd[4] = {v[i][2], v[i][3], v[i + 1][2], v[i + 1][3]};
+                    mma_f16_acc(od[j][0], even, b[i], b[i + 1]);
+                    mma_f16_acc(od[j][OD - 1], odd, b[i], b[i + 1]);
+                }
             }
         }
     }
@@ -907,9 +960,14 @@ struct Heads {
             }
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
-                rec[4 + kHeadDim + 16 * j + i0] = od[j][k] * fp;
+                float x = od[j][0][k], y = od[j][0][2 + k];
+                if constexpr (CT == 1) {
+                    x += od[j][OD - 1][1];
+                    y += od[j][OD - 1][3];
+                }
+                rec[4 + kHeadDim + 16 * j + i0] = x * (fp * 0x1p24f);  // (the codes were 2^-24 of themselves)
                 if (GS == 16)
-                    rec[4 + kHeadDim + 16 * j + 8 + i0] = od[j][2 + k] * fp;
+                    rec[4 + kHeadDim + 16 * j + 8 + i0] = y * (fp * 0x1p24f);
             }
         }
     }
