@@ -22,11 +22,12 @@
 //   scales   of row r at (2 t + o) * 8 + 2 i + c
 // With 8 entries, two rows' words are one: word i / 2, slots 2 (i mod 2) + c, are entries
 // 2 u, 2 u + 1 of a key in the two halves, or entry g of a value in half o.
-// So four consecutive tokens (eight) share eight words of keys and eight of values, and
-// one thread writes either (a unit).
+// So four consecutive tokens (eight) share eight words of keys and eight of values: a unit,
+// which one thread writes where few tokens come; pages are written and read by warps.
 #pragma once
 
 #include "dar_common.cuh"
+#include "dar_sm100.cuh"
 
 namespace dar {
 namespace q4 {
@@ -42,14 +43,47 @@ struct Fmt {
     static constexpr int kUnit = kGroup == 16 ? 4 : 8; // rows that share words
 };
 
+// Bits of a quotient rounded to a scale: 5 significant bits, nearest even; 7 s is finite in bf16.
+__device__ __forceinline__ float round_scale(uint32_t u)
+{
+    u = (u + 0x3ffffu + ((u >> 19) & 1u)) & ~0x7ffffu;
+    return fminf(__uint_as_float(u), 0x1.2p125f);
+}
+
 // The scale of a group whose largest magnitude has the bits `a` (of NaN and infinity the group is NaN).
 __device__ __forceinline__ float group_scale(uint32_t a)
 {
     if (a >= 0x7f800000u)
         return __uint_as_float(0x7fc00000u);
-    uint32_t u = __float_as_uint(__fdiv_rn(__uint_as_float(a), 7.0f));
-    u = (u + 0x3ffffu + ((u >> 19) & 1u)) & ~0x7ffffu;     // nearest even at 5 significant bits
-    return fminf(__uint_as_float(u), 0x1.2p125f);          // 7 s is finite in bf16
+    return round_scale(__float_as_uint(__fdiv_rn(__uint_as_float(a), 7.0f)));
+}
+
+// The same of a bf16 number without a division.  a has 8 significant bits: where a / 7 does not lie halfway between two
+// scales, it lies 2^-12 of itself away at least, so that the product's rounding error goes with the bits below 2^-13.
+// (Subnormal quotients have fewer bits: from 2^-100 down it is a division.)
+__device__ __forceinline__ float group_scale_bf16(uint32_t a)
+{
+    if (a - 0x0d800000u >= 0x7f800000u - 0x0d800000u)
+        return group_scale(a);
+    const uint32_t u = __float_as_uint(__uint_as_float(a) * (1.0f / 7.0f));
+    return round_scale((u + 0x200u) & ~0x3ffu);
+}
+
+// Magnitudes |x| / s of two entries, rounded, in the low halves of either half.  The quotient is a product with 1 / s;
+// exact: on bf16 numbers, whose quotients lie 2^-11 away from halves at least where they are no halves, its error goes
+// with a rounding to 2^-13.  Else by division (rounded to 24 bits it is on the same side of a half as the quotient).
+__device__ __forceinline__ uint32_t magnitudes_bf16(float x, float y, float inv)
+{
+    constexpr float kGrid = 1536.f, kInt = 8388608.f;  // 1.5 * 2^10, 2^23
+    const float a = fmaf(fabsf(x), inv, kGrid) - kGrid + kInt, b = fmaf(fabsf(y), inv, kGrid) - kGrid + kInt;
+    return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410);
+}
+__device__ __forceinline__ uint32_t magnitudes(float x, float y, float s)
+{
+    if (!(s > 0.f))
+        return 0u;
+    const float a = fminf(rintf(__fdiv_rn(fabsf(x), s)), 7.f), b = fminf(rintf(__fdiv_rn(fabsf(y), s)), 7.f);
+    return (uint32_t)a | (uint32_t)b << 16;
 }
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
@@ -68,7 +102,7 @@ __host__ __device__ constexpr int word_row(int j, int r, int h)
 template <int GS, bool VALUES>
 __host__ __device__ constexpr int word_entry(int j, int r, int h)
 {
-    return VALUES ? j + (GS == 16 ? 8 * (r & 1) : 0) : GS == 16 ? 4 * (j & 3) + 2 * (r >> 1) + h : 2 * (j & 3) + h;
+    return VALUES ? (GS == 16 ? 4 * (j >> 1) + (j & 1) + 2 * (r & 1) : j) : GS == 16 ? 4 * (j & 3) + 2 * (r >> 1) + h : 2 * (j & 3) + h;
 }
 // Its offset in the block's keys (values); row0: the unit's first row.
 template <int GS, bool VALUES>
@@ -105,7 +139,7 @@ struct UnitWords {
 #pragma unroll
         for (int i = 0; i < GS; ++i) {
             const float q = s > 0.f ? fminf(rintf(__fdiv_rn(fabsf(x[i]), s)), 7.f) : 0.f;
-            code[i] = (uint32_t)q | (q > 0.f ? __float_as_uint(x[i]) & 0x80000000u : 0u);
+            code[i] = (uint32_t)q | (__float_as_uint(x[i]) & 0x80000000u);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -187,33 +221,233 @@ __device__ __forceinline__ void read_row(const unsigned char *block, int row, fl
     }
 }
 
-// All rows of a unit; put(k, x) takes row k.
-template <int GS, bool VALUES, typename Put>
-__device__ __forceinline__ void read_unit(const unsigned char *block, int row0, const Put &put)
+// ------------------------------------------------------------------ pages, by warps
+//
+// Lane (g, u) has entries 4 u .. 4 u + 3 (of 8: 2 u, 2 u + 1) of rows with 2 t + o = g.  As pairs in slot form (two
+// codes, the word's slot 0) they are the slots of its words of keys, and transposed those of its words of values.
+
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
-    constexpr int U = GS == 16 ? 4 : 8;
-    const unsigned char *at = block + (VALUES ? kPage * GS / 2 : 0);
-    uint32_t w[8];
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+__device__ __forceinline__ int lane_row(int g, int i, int c) { return 16 * (g >> 1) + 4 * i + 2 * c + (g & 1); }
+
+// Entries of a lane's rows as they come from memory: pairs of T.
+template <typename T, int GS>
+struct Raw;
+template <int GS>
+struct Raw<bf16, GS> {
+    static constexpr int N = GS / 8;  // pairs
+    uint32_t w[N];
+    __device__ __forceinline__ void zero()
+    {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        w[j] = *reinterpret_cast<const uint32_t *>(at + word_offset<GS, VALUES>(row0, j));
-    const uint16_t *scales = scales_of<GS, VALUES>(const_cast<unsigned char *>(block));
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-        const float s = __uint_as_float((uint32_t)scales[scale_index(row0 + k)] << 16);
-        float x[GS];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (word_row<GS, VALUES>(j, r, h) == k) {
-                        const float y = (float)((w[j] >> slot_shift(r, h)) & 7u) * s;
-                        x[word_entry<GS, VALUES>(j, r, h)] = w[j] >> slot_sign(r, h) & 1u ? -y : y;
-                    }
-        put(k, x);
+        for (int i = 0; i < N; ++i)
+            w[i] = 0u;
     }
+    __device__ __forceinline__ void load(const bf16 *p)
+    {
+        if constexpr (N == 2) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(p);
+            w[0] = v.x, w[1] = v.y;
+        } else {
+            w[0] = *reinterpret_cast<const uint32_t *>(p);
+        }
+    }
+    // The pairs' codes in slot form, and the group's scale in 16 bits; all lanes.
+    __device__ __forceinline__ uint32_t codes(uint32_t (&x)[N]) const
+    {
+        uint32_t m = w[0] & 0x7fff7fffu;
+        if constexpr (N == 2)
+            m = __vmaxu2(m, w[N - 1] & 0x7fff7fffu);
+        m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        const uint32_t a = max(m << 16, m & 0xffff0000u);
+        const float s = group_scale_bf16(a);
+        if (a - 0x0d800000u < 0x7f800000u - 0x0d800000u) {
+            float inv;
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                x[i] = magnitudes_bf16(bf16lo(w[i]), bf16hi(w[i]), inv) | (w[i] & 0x80008000u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                x[i] = magnitudes(bf16lo(w[i]), bf16hi(w[i]), s) | (w[i] & 0x80008000u);
+        }
+        return __float_as_uint(s) >> 16;
+    }
+    static __device__ __forceinline__ void store(bf16 *p, const uint32_t (&x)[N], float s)
+    {
+        uint32_t y[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float a, b;
+            asm("{.reg .b16 p, q; mov.b32 {p, q}, %2; cvt.f32.f16 %0, p; cvt.f32.f16 %1, q;}" : "=f"(a), "=f"(b) : "r"(x[i]));
+            y[i] = sm100::cvt_bf16x2((a * 0x1p24f) * s, (b * 0x1p24f) * s);
+        }
+        if constexpr (N == 2)
+            *reinterpret_cast<uint2 *>(p) = make_uint2(y[0], y[N - 1]);
+        else
+            *reinterpret_cast<uint32_t *>(p) = y[0];
+    }
+};
+template <int GS>
+struct Raw<float, GS> {
+    static constexpr int N = GS / 8;
+    float w[2 * N];
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < 2 * N; ++i)
+            w[i] = 0.f;
+    }
+    __device__ __forceinline__ void load(const float *p)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float2 v = reinterpret_cast<const float2 *>(p)[i];
+            w[2 * i] = v.x, w[2 * i + 1] = v.y;
+        }
+    }
+    __device__ __forceinline__ uint32_t codes(uint32_t (&x)[N]) const
+    {
+        uint32_t a = 0u;
+#pragma unroll
+        for (int i = 0; i < 2 * N; ++i)
+            a = max(a, magnitude(w[i]));
+        a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
+        a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
+        const float s = group_scale(a);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            x[i] = magnitudes(w[2 * i], w[2 * i + 1], s) | __float_as_uint(w[2 * i]) >> 31 << 15 |
+                   (__float_as_uint(w[2 * i + 1]) & 0x80000000u);
+        return __float_as_uint(s) >> 16;
+    }
+    static __device__ __forceinline__ void store(float *p, const uint32_t (&x)[N], float s)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float a, b;
+            asm("{.reg .b16 p, q; mov.b32 {p, q}, %2; cvt.f32.f16 %0, p; cvt.f32.f16 %1, q;}" : "=f"(a), "=f"(b) : "r"(x[i]));
+            reinterpret_cast<float2 *>(p)[i] = make_float2((a * 0x1p24f) * s, (b * 0x1p24f) * s);
+        }
+    }
+};
+
+// Quantises rows [first, end) of a page into a block; row r's entries are at vec + r * stride.
+template <typename T, int GS, bool VALUES>
+__device__ __forceinline__ void write_page(unsigned char *block, const T *vec, int stride, int first, int end, int lane)
+{
+    constexpr int N = GS / 8;
+    const int g = lane >> 2, u = lane & 3;
+    Raw<T, GS> raw[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int r = lane_row(g, i, c);
+            raw[i][c].zero();
+            if (r >= first && r < end)
+                raw[i][c].load(vec + (size_t)r * stride + u * 2 * N);
+        }
+    uint32_t w[4], sc[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t x[2][N];
+        const uint32_t s0 = raw[i][0].codes(x[0]), s1 = raw[i][1].codes(x[1]);
+        sc[i] = s0 | s1 << 16;
+        if constexpr (VALUES) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int k = 0; k < N; ++k)
+                    x[c][k] = transpose8(x[c][k]);
+        }
+        auto turned = [](uint32_t v, int r) { return __funnelshift_l(v, v, 4 * r); };
+        if constexpr (GS == 16) {  // slots: keys c + 2 k, values 2 c + k
+            const uint32_t y1 = VALUES ? x[0][N - 1] : x[1][0], y2 = VALUES ? x[1][0] : x[0][N - 1];
+            w[i] = x[0][0] | turned(y1, 1) | turned(y2, 2) | turned(x[1][N - 1], 3);
+        } else {
+            const uint32_t y = x[0][0] | turned(x[1][0], 1);
+            w[i] = i % 2 ? w[i - i % 2] | turned(y, 2) : y;
+        }
+    }
+    constexpr int kCodes = kPage * GS / 2;
+    unsigned char *at = block + (VALUES ? kCodes : 0) + lane * GS;
+    uint16_t *scales = scales_of<GS, VALUES>(block) + g * 8;
+    if (first <= 0 && end >= kPage) {
+        if constexpr (GS == 16)
+            *reinterpret_cast<uint4 *>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+        else
+            *reinterpret_cast<uint2 *>(at) = make_uint2(w[1], w[3]);
+        if (u == 0)
+            *reinterpret_cast<uint4 *>(scales) = make_uint4(sc[0], sc[1], sc[2], sc[3]);
+        return;
+    }
+    uint32_t *words = reinterpret_cast<uint32_t *>(at);
+#pragma unroll
+    for (int i = 0; i < (GS == 16 ? 4 : 2); ++i) {
+        const int row0 = VALUES ? 16 * u : 16 * (g >> 1);
+        uint32_t mask = 0u;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = row0 + (GS == 16 ? 4 : 8) * i + word_row<GS, VALUES>(VALUES ? 0 : 4 * (g & 1), r, h);
+                mask |= row >= first && row < end ? slot_mask(r, h) : 0u;
+            }
+        if (mask)
+            words[i] = (words[i] & ~mask) | (w[GS == 16 ? i : 2 * i + 1] & mask);
+    }
+    if (u == 0)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int r = lane_row(g, i, c);
+                if (r >= first && r < end)
+                    scales[2 * i + c] = (uint16_t)(sc[i] >> (16 * c));
+            }
+}
+
+// Reads rows [first, end) of a block back.
+template <typename T, int GS, bool VALUES>
+__device__ __forceinline__ void read_page(const unsigned char *block, T *vec, int stride, int first, int end, int lane)
+{
+    constexpr int N = GS / 8, kCodes = kPage * GS / 2;
+    const int g = lane >> 2, u = lane & 3;
+    const unsigned char *at = block + (VALUES ? kCodes : 0) + lane * GS;
+    uint32_t w[4];
+    if constexpr (GS == 16) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(at);
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else {
+        const uint2 v = *reinterpret_cast<const uint2 *>(at);
+        w[0] = v.x, w[1] = __funnelshift_r(v.x, v.x, 8), w[2] = v.y, w[3] = __funnelshift_r(v.y, v.y, 8);
+    }
+    const uint4 v = *reinterpret_cast<const uint4 *>(scales_of<GS, VALUES>(const_cast<unsigned char *>(block)) + g * 8);
+    const uint32_t sc[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            uint32_t x[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int r = GS == 16 ? (VALUES ? 2 * c + k : c + 2 * k) : c;
+                x[k] = __funnelshift_r(w[i], w[i], 4 * r) & 0x80078007u;
+                if constexpr (VALUES)
+                    x[k] = transpose8(x[k]);
+            }
+            const int row = lane_row(g, i, c);
+            if (row >= first && row < end)
+                Raw<T, GS>::store(vec + (size_t)row * stride + u * 2 * N, x, c ? bf16hi(sc[i]) : bf16lo(sc[i]));
+        }
 }
 
 }  // namespace q4

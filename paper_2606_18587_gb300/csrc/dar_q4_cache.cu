@@ -20,7 +20,7 @@ namespace q4 {
 // window, projects these (the same fp32 chains, rounded to T), and puts the tokens
 // that stay into the ring slots that they leave.  Its tile starts at a position that
 // is a multiple of a page, so that tokens that share words of a page have the same CTA; a
-// thread then quantises and writes a unit of them.
+// warp then quantises and writes a page's group.
 template <typename T, int DD, int RPT, int NR>
 __global__ void __launch_bounds__(NR *slices<DD>()) append_kernel(AppendArgs a, int tiles)
 {
@@ -71,29 +71,22 @@ __global__ void __launch_bounds__(NR *slices<DD>()) append_kernel(AppendArgs a, 
             store_row<T, CW>(vec + (size_t)(r0 + k * NR) * DD + c0, acc[k]);
         __syncthreads();
         unsigned char *pool = static_cast<unsigned char *>(a.pool_kd);
-        for (int i = tid; i < R / F::kUnit * F::kGroups; i += NT) {
-            const int r = i % (R / F::kUnit) * F::kUnit, sb = i / (R / F::kUnit);
-            unsigned has = 0u;
-#pragma unroll
-            for (int k = 0; k < F::kUnit; ++k)
-                has |= r + k >= ra && r + k < nr ? 1u << k : 0u;
-            if (!has)
+        for (int i = tid / 32; i < R / kPage * F::kGroups; i += NT / 32) {
+            const int p = i % (R / kPage), sb = i / (R / kPage), m = m0 + p * kPage;
+            const int first = max(0, ra - p * kPage), end = min(kPage, nr - p * kPage);
+            if (first >= end)
                 continue;
-            const int m = m0 + r, id = a.block_table[(size_t)b * a.maxp + m / kPage];
+            const int id = a.block_table[(size_t)b * a.maxp + m / kPage];
             if (id < 0 || id >= a.num_pages) {
                 report(a.status, DAR_ERR_CAPACITY);
                 continue;
             }
             unsigned char *block = pool + ((size_t)id * a.Hkv + g) * F::kBytes + sb * F::kBlock;
-            auto row = [&](int k, float (&x)[F::kGroup]) {
-#pragma unroll
-                for (int e = 0; e < F::kGroup; ++e)
-                    x[e] = to_f32(vec[(size_t)(r + k) * DD + sb * F::kGroup + e]);
-            };
+            const T *v = vec + (size_t)p * kPage * DD + sb * F::kGroup;
             if (kv)
-                write_unit<F::kGroup, true>(block, m % kPage, has, row);
+                write_page<T, F::kGroup, true>(block, v, DD, first, end, tid & 31);
             else
-                write_unit<F::kGroup, false>(block, m % kPage, has, row);
+                write_page<T, F::kGroup, false>(block, v, DD, first, end, tid & 31);
         }
     }
     // ring slots (L + j) % w, j < min(nb, w): the last new token of each
@@ -103,6 +96,165 @@ __global__ void __launch_bounds__(NR *slices<DD>()) append_kernel(AppendArgs a, 
         *reinterpret_cast<uint4 *>(ring + (size_t)((L + j) % w) * kHeadDim + c * E) =
             *reinterpret_cast<const uint4 *>(xnew + (size_t)last * kHeadDim + c * E);
     }
+}
+
+// Few tokens a sequence: one CTA per sequence, as cache_append_kernel (dar_append.cu), so that its length can be
+// advanced at the end and a call is one launch.  A thread runs one chain (keys or values, KV head, entry) for the
+// tokens that leave, kept in registers and then as vectors in shared memory; then a thread quantises and writes the
+// unit of a group.
+constexpr int kFewThreads = 512;
+constexpr int kFewRows = 8;               // tokens of a round
+constexpr int kFewStageBytes = 96 << 10;  // their rows of 64
+
+template <typename T>
+__host__ __device__ constexpr int few_rows(int Hkv)
+{
+    const int r = kFewStageBytes / (2 * Hkv * kHeadDim * (int)sizeof(T));
+    return r > kFewRows ? kFewRows : r;
+}
+template <typename T, int DD>
+__host__ __device__ constexpr size_t few_smem(int Hkv)
+{
+    return (size_t)few_rows<T>(Hkv) * 2 * Hkv * (kHeadDim + DD) * sizeof(T);
+}
+
+template <typename T, int DD>
+__device__ __forceinline__ void append_few(const AppendArgs &a)
+{
+    using F = Fmt<DD>;
+    constexpr int E = Granule<T>::kElems, GPR = kHeadDim / E, GS = F::kGroup;
+    extern __shared__ __align__(16) unsigned char few[];
+    __shared__ int s_L, s_nb, s_ok;
+    const int b = blockIdx.x, tid = threadIdx.x, Hkv = a.Hkv, n = a.n, w = a.w;
+    const int chains = 2 * Hkv * DD, R = few_rows<T>(Hkv);
+    T *rows = reinterpret_cast<T *>(few);           // [R][kv][Hkv][64]
+    T *vec = rows + (size_t)R * 2 * Hkv * kHeadDim;  // [R][kv][Hkv][DD]
+    const T *knew = static_cast<const T *>(a.k_new), *vnew = static_cast<const T *>(a.v_new);
+    T *wk = static_cast<T *>(a.win_k), *wv = static_cast<T *>(a.win_v);
+    unsigned char *pool = static_cast<unsigned char *>(a.pool_kd);
+    if (tid == 0) {
+        s_L = a.seq_lens[b];
+        s_nb = a.n_per_seq ? a.n_per_seq[b] : n;
+    }
+    // what does not depend on the length: the first chain's column of W, and a granule of the last new rows
+    float wc[kHeadDim];
+    auto load_w = [&](int ch) {
+        const int kv = ch / (Hkv * DD), g = (ch / DD) % Hkv, c = ch % DD;
+        const float *W = (kv ? a.Dv : a.Dk) + (size_t)g * kHeadDim * DD + c;
+#pragma unroll
+        for (int t = 0; t < kHeadDim; ++t)
+            wc[t] = __ldg(W + (size_t)t * DD);
+    };
+    if (tid < chains)
+        load_w(tid);
+    auto new_granule = [&](int i, int j0) {  // i over [row][kv][g][granule]
+        const int q = i % GPR, rest = i / GPR, g = rest % Hkv, kv = (rest / Hkv) & 1, j = j0 + rest / (2 * Hkv);
+        return (kv ? vnew : knew) + (((size_t)b * Hkv + g) * n + j) * kHeadDim + q * E;
+    };
+    const int pre_rows = min(n, w);
+    uint4 pre = make_uint4(0u, 0u, 0u, 0u);
+    if (tid < 2 * Hkv * pre_rows * GPR)
+        pre = *reinterpret_cast<const uint4 *>(new_granule(tid, n - pre_rows));
+    __syncthreads();
+    if (tid == 0) {
+        const int e = append_error(s_L, s_nb, a);
+        if (e != DAR_OK)
+            report(a.status, e);
+        s_ok = e == DAR_OK;
+    }
+    __syncthreads();
+    if (!s_ok || s_nb == 0)
+        return;
+    const int L = s_L, nb = s_nb, Lnew = L + nb;
+    const int lo = max(0, L - w), hi = max(0, Lnew - w);  // positions that leave the window
+    for (int m0 = lo; m0 < hi; m0 += R) {
+        const int nr = min(R, hi - m0);
+        for (int i = tid; i < nr * 2 * Hkv * GPR; i += kFewThreads) {
+            const int q = i % GPR, rest = i / GPR, g = rest % Hkv, kv = (rest / Hkv) & 1, p = m0 + rest / (2 * Hkv);
+            const T *src = p < L ? (kv ? wv : wk) + (((size_t)b * Hkv + g) * w + p % w) * kHeadDim
+                                 : (kv ? vnew : knew) + (((size_t)b * Hkv + g) * n + (p - L)) * kHeadDim;
+            reinterpret_cast<uint4 *>(rows)[i] = *reinterpret_cast<const uint4 *>(src + q * E);
+        }
+        __syncthreads();
+        for (int ch0 = 0; ch0 < chains; ch0 += kFewThreads) {
+            const int ch = ch0 + tid;
+            if (ch >= chains)
+                break;
+            if (ch0 > 0)
+                load_w(ch);
+            for (int r = 0; r < nr; ++r) {
+                const uint4 *x4 = reinterpret_cast<const uint4 *>(rows + ((size_t)r * 2 * Hkv + ch / DD) * kHeadDim);
+                float acc = 0.0f;  // Eq. 1: one fp32 FMA chain over t = 0..63
+#pragma unroll
+                for (int q = 0; q < GPR; ++q) {
+                    float xf[E];
+                    unpack(x4[q], xf, T());
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        acc = __fmaf_rn(xf[e], wc[q * E + e], acc);
+                }
+                vec[(size_t)r * chains + ch] = from_f32<T>(acc);
+            }
+        }
+        if (chains > kFewThreads && m0 + R < hi && tid < chains)  // the first chains' columns again
+            load_w(tid);
+        __syncthreads();
+        const int u0 = m0 / F::kUnit, units = (m0 + nr - 1) / F::kUnit - u0 + 1, heads = 2 * Hkv * F::kGroups;
+        for (int i = tid; i < units * heads; i += kFewThreads) {
+            const int p0 = (u0 + i / heads) * F::kUnit, h = i % heads, sb = h % F::kGroups, kg = h / F::kGroups;
+            const int kv = kg / Hkv, g = kg % Hkv;
+            unsigned has = 0u;
+#pragma unroll
+            for (int k = 0; k < F::kUnit; ++k)
+                has |= p0 + k >= m0 && p0 + k < m0 + nr ? 1u << k : 0u;
+            const int id = a.block_table[(size_t)b * a.maxp + p0 / kPage];
+            if (id < 0 || id >= a.num_pages) {
+                report(a.status, DAR_ERR_CAPACITY);
+                continue;
+            }
+            unsigned char *block = pool + ((size_t)id * Hkv + g) * F::kBytes + sb * F::kBlock;
+            auto row = [&](int k, float (&x)[GS]) {
+#pragma unroll
+                for (int e = 0; e < GS; ++e)
+                    x[e] = to_f32(vec[(size_t)(p0 + k - m0) * chains + kg * DD + sb * GS + e]);
+            };
+            if (kv)
+                write_unit<GS, true>(block, p0 % kPage, has, row);
+            else
+                write_unit<GS, false>(block, p0 % kPage, has, row);
+        }
+        __syncthreads();
+    }
+    // new tokens that stay in the window: every ring row above is read
+    const int j0 = max(0, nb - w), granules = 2 * Hkv * (nb - j0) * GPR;
+    for (int i = tid; i < granules; i += kFewThreads) {
+        const int q = i % GPR, rest = i / GPR, g = rest % Hkv, kv = (rest / Hkv) & 1, j = j0 + rest / (2 * Hkv);
+        const uint4 v = nb == n && i == tid ? pre : *reinterpret_cast<const uint4 *>(new_granule(i, j0));
+        *reinterpret_cast<uint4 *>((kv ? wv : wk) + (((size_t)b * Hkv + g) * w + (L + j) % w) * kHeadDim + q * E) = v;
+    }
+    __syncthreads();
+    if (tid == 0)
+        a.seq_lens[b] = Lnew;
+}
+
+template <typename T, int DD>
+__global__ void __launch_bounds__(kFewThreads) append_few_kernel(AppendArgs a)
+{
+    append_few<T, DD>(a);
+}
+
+template <typename T, int DD>
+static cudaError_t append_few_launch(const AppendArgs &a, cudaStream_t s)
+{
+    static PerDeviceOnce once;  // opt-in to more than 48 KB of shared memory, once per device
+    const cudaError_t e = per_device_once(once, [](int) {
+        return cudaFuncSetAttribute(append_few_kernel<T, DD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    2 * kFewStageBytes);
+    });
+    if (e != cudaSuccess)
+        return e;
+    append_few_kernel<T, DD><<<a.B, kFewThreads, few_smem<T, DD>(a.Hkv), s>>>(a);
+    return cudaGetLastError();
 }
 
 // Advances the lengths (and reports refused sequences) once every CTA of the append has read them.
@@ -142,22 +294,8 @@ static cudaError_t append_tiles(const AppendArgs &a, cudaStream_t s)
 
 // ------------------------------------------------------------------ conversion
 //
-// A warp takes a page of a (sequence, KV head), a lane a unit of its keys or values, one group after the other.
+// A warp takes a page of a (sequence, KV head), one group after the other.
 constexpr int kConvertWarps = 8;
-
-template <typename T, int GS>
-__device__ __forceinline__ void load_group(const T *p, float (&x)[GS])
-{
-    constexpr int E = Granule<T>::kElems;
-#pragma unroll
-    for (int i = 0; i < GS / E; ++i) {
-        float y[E];
-        unpack(reinterpret_cast<const uint4 *>(p)[i], y, T());
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            x[i * E + e] = y[e];
-    }
-}
 
 template <typename T, int DD, bool PACK>
 __global__ void __launch_bounds__(kConvertWarps * 32) convert_kernel(Q4ConvertArgs a)
@@ -184,36 +322,19 @@ __global__ void __launch_bounds__(kConvertWarps * 32) convert_kernel(Q4ConvertAr
             report(a.status, DAR_ERR_CAPACITY);
         return;
     }
-    constexpr int U = F::kUnit, UNITS = kPage / U;  // of keys, and of values
-    const int r = lane % UNITS * U;
-    const bool values = lane >= UNITS;
-    const long long pos = lp * kPage + r;
-    unsigned has = 0u;
-#pragma unroll
-    for (int k = 0; k < U; ++k)
-        has |= pos + k >= first && pos + k < end ? 1u << k : 0u;
-    if (!has || lane >= 2 * UNITS)
-        return;
     unsigned char *page = static_cast<unsigned char *>(a.pool) + ((size_t)id4 * a.Hkv + g) * F::kBytes;
-    T *vec = static_cast<T *>(values ? a.pool_vd : a.pool_kd) + (((size_t)id * a.Hkv + g) * kPage + r) * DD;
+    const size_t row = ((size_t)id * a.Hkv + g) * kPage * DD;
+    T *k = static_cast<T *>(a.pool_kd) + row, *v = static_cast<T *>(a.pool_vd) + row;
+    const int from = (int)max(0ll, first - lp * kPage), to = (int)min((long long)kPage, end - lp * kPage);
 #pragma unroll
     for (int sb = 0; sb < F::kGroups; ++sb) {
         unsigned char *block = page + sb * F::kBlock;
         if constexpr (PACK) {
-            auto row = [&](int k, float (&x)[GS]) { load_group<T, GS>(vec + k * DD + sb * GS, x); };
-            if (values)
-                write_unit<GS, true>(block, r, has, row);
-            else
-                write_unit<GS, false>(block, r, has, row);
+            write_page<T, GS, false>(block, k + sb * GS, DD, from, to, lane);
+            write_page<T, GS, true>(block, v + sb * GS, DD, from, to, lane);
         } else {
-            auto put = [&](int k, const float (&x)[GS]) {
-                if (has >> k & 1u)
-                    store_row<T, GS>(vec + k * DD + sb * GS, x);
-            };
-            if (values)
-                read_unit<GS, true>(block, r, put);
-            else
-                read_unit<GS, false>(block, r, put);
+            read_page<T, GS, false>(block, k + sb * GS, DD, from, to, lane);
+            read_page<T, GS, true>(block, v + sb * GS, DD, from, to, lane);
         }
     }
 }
@@ -233,7 +354,12 @@ static cudaError_t by_width(int dd, F &&f)
 template <typename T>
 static cudaError_t append_t(int dd, const AppendArgs &a, cudaStream_t s)
 {
-    return by_width(dd, [&](auto width) { return append_tiles<T, decltype(width)::value, 1, 64>(a, s); });
+    return by_width(dd, [&](auto width) {
+        constexpr int DD = decltype(width)::value;
+        if (a.n <= kFewRows && few_rows<T>(a.Hkv) > 0)
+            return append_few_launch<T, DD>(a, s);
+        return append_tiles<T, DD, 1, 64>(a, s);
+    });
 }
 
 template <typename T, bool PACK>

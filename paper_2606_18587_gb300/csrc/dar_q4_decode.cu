@@ -429,13 +429,6 @@ __device__ __forceinline__ void mma_f16_c(float (&d)[4], const uint32_t (&a)[4],
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 
-__device__ __forceinline__ uint32_t transpose8(uint32_t x)
-{
-    uint32_t y;
-    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-
 __device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi)
 {
     uint32_t r;
@@ -903,7 +896,7 @@ struct Heads {
                 }
                 b[k] = transpose8(cvt_f16x2(w0, w1));
             }
-            uint32_t v[4][4];  // entries i0 and i0 + 8 of the rows of word i with c = 0, and with c = 1
+            uint32_t v[4][4];  // both entries of the rows of word i with c = 0, and with c = 1
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if constexpr (GS == 16) {
@@ -965,9 +958,10 @@ struct Heads {
                     x += od[j][OD - 1][1];
                     y += od[j][OD - 1][3];
                 }
-                rec[4 + kHeadDim + 16 * j + i0] = x * (fp * 0x1p24f);  // (the codes were 2^-24 of themselves)
+                const int e = GS == 16 ? 16 * j + 4 * (i0 >> 1) + (i0 & 1) : i0;
+                rec[4 + kHeadDim + e] = x * (fp * 0x1p24f);  // (the codes were 2^-24 of themselves)
                 if (GS == 16)
-                    rec[4 + kHeadDim + 16 * j + 8 + i0] = y * (fp * 0x1p24f);
+                    rec[4 + kHeadDim + e + 2] = y * (fp * 0x1p24f);
             }
         }
     }
