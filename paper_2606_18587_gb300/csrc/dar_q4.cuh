@@ -12,9 +12,15 @@
 // codes of the values, 64 scales of the keys, 64 of the values (bf16).  Codes lie
 // where the lanes of a warp want them as operands of mma.sync (dar_q4_decode.cu), all
 // 64 tokens of a group with one load of 16 bytes (8) a lane.  A word is eight codes, in
-// slots 0 to 3 of either half: turned right by 4 r bits it has slot r's two codes as sign
-// and magnitude in bits 15, 0-2 and 31, 16-18, which are the fp16 numbers code * 2^-24:
-// an instruction to turn and one to mask make an operand register.
+// slots 0 to 3 of either half:
+//   values   turned right by 4 r bits it has slot r's two codes as sign and magnitude in bits 15,
+//            0-2 and 31, 16-18, which are the fp16 numbers code * 2^-24: an instruction to turn
+//            and one to mask make an operand register.
+//   keys     slot r is bits 4 r .. 4 r + 3 of either half, code + 8.  fp16 numbers are linear in
+//            their lowest 11 bits, so that slots 0 and 1 are (code + 8) 2^-24 and 2^-20 where they
+//            lie, and slots 2 and 3 shifted right by 8: five instructions for four operand registers,
+//            not seven; a score takes the offset back with what its sum starts from.  (The values' sums
+//            run over thousands of tokens, in which the offset's part would drown the rest.)
 //   row      r of a page is token 4 i + 2 c + o of 16 t ..: t = r / 16, i = r / 4 mod 4, c = r / 2 mod 2, o = r mod 2
 //   keys     lane (g, u) = 4 g + u has rows with 2 t + o = g: word i, slots c and 2 + c, are
 //            entries 4 u, 4 u + 1 and 4 u + 2, 4 u + 3 in the two halves
@@ -88,10 +94,14 @@ __device__ __forceinline__ uint32_t magnitudes(float x, float y, float s)
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// Slot r of half h of a word: where a code's magnitude and its sign are.
+// Slot r of half h of a word: where a value's magnitude and its sign are, or a key's code.
 __host__ __device__ constexpr int slot_shift(int r, int h) { return 16 * h + 4 * r; }
 __host__ __device__ constexpr int slot_sign(int r, int h) { return (15 + 16 * h + 4 * r) % 32; }
-__host__ __device__ constexpr uint32_t slot_mask(int r, int h) { return 7u << slot_shift(r, h) | 1u << slot_sign(r, h); }
+template <bool VALUES>
+__host__ __device__ constexpr uint32_t slot_mask(int r, int h)
+{
+    return VALUES ? 7u << slot_shift(r, h) | 1u << slot_sign(r, h) : 15u << slot_shift(r, h);
+}
 
 // Word j (of 8) of a unit: the row in the unit and the entry that slot r of half h holds.
 template <int GS, bool VALUES>
@@ -116,85 +126,10 @@ __device__ __forceinline__ int scale_index(int row)
     return (2 * (row >> 4) + (row & 1)) * 8 + 2 * ((row >> 2) & 3) + ((row >> 1) & 1);
 }
 
-// A unit on its way into a block: eight words of its keys or values.
-template <int GS, bool VALUES>
-struct UnitWords {
-    static constexpr int kRows = GS == 16 ? 4 : 8;
-    uint32_t w[8];
-    __device__ __forceinline__ UnitWords()
-    {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            w[j] = 0u;
-    }
-    // Row k (a constant) of the unit; returns its scale.
-    __device__ __forceinline__ float add(const float (&x)[GS], int k)
-    {
-        uint32_t a = 0u;
-#pragma unroll
-        for (int i = 0; i < GS; ++i)
-            a = max(a, magnitude(x[i]));
-        const float s = group_scale(a);
-        uint32_t code[GS];  // magnitude, sign at bit 31
-#pragma unroll
-        for (int i = 0; i < GS; ++i) {
-            const float q = s > 0.f ? fminf(rintf(__fdiv_rn(fabsf(x[i]), s)), 7.f) : 0.f;
-            code[i] = (uint32_t)q | (__float_as_uint(x[i]) & 0x80000000u);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (word_row<GS, VALUES>(j, r, h) == k) {
-                        const uint32_t c = code[word_entry<GS, VALUES>(j, r, h)];
-                        w[j] |= (c & 7u) << slot_shift(r, h) | (c >> 31) << slot_sign(r, h);
-                    }
-        return s;
-    }
-    // Rows of which `has` has no bit keep their codes.
-    __device__ __forceinline__ void store(unsigned char *block, int row0, unsigned has) const
-    {
-        unsigned char *at = block + (VALUES ? kPage * GS / 2 : 0);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            uint32_t *p = reinterpret_cast<uint32_t *>(at + word_offset<GS, VALUES>(row0, j));
-            uint32_t x = w[j];
-            if (has != (1u << kRows) - 1u) {
-                uint32_t mask = 0u;
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        mask |= has >> word_row<GS, VALUES>(j, r, h) & 1u ? slot_mask(r, h) : 0u;
-                x = (*p & ~mask) | (x & mask);
-            }
-            *p = x;
-        }
-    }
-};
-
 template <int GS, bool VALUES>
 __device__ __forceinline__ uint16_t *scales_of(unsigned char *block)
 {
     return reinterpret_cast<uint16_t *>(block + kPage * GS + (VALUES ? 2 * kPage : 0));
-}
-
-// Quantises rows row0 .. (a unit's; row(k, x) fetches row k of it) into a block.
-template <int GS, bool VALUES, typename Row>
-__device__ __forceinline__ void write_unit(unsigned char *block, int row0, unsigned has, const Row &row)
-{
-    UnitWords<GS, VALUES> u;
-    uint16_t *scales = scales_of<GS, VALUES>(block);
-#pragma unroll
-    for (int k = 0; k < UnitWords<GS, VALUES>::kRows; ++k)
-        if (has >> k & 1u) {
-            float x[GS];
-            row(k, x);
-            scales[scale_index(row0 + k)] = (uint16_t)(__float_as_uint(u.add(x, k)) >> 16);  // (a bf16 number)
-        }
-    u.store(block, row0, has);
 }
 
 // The values that a row of a block stands for.
@@ -215,16 +150,45 @@ __device__ __forceinline__ void read_row(const unsigned char *block, int row, fl
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 if (word_row<GS, VALUES>(j, r, h) == k) {
-                    const float y = (float)((w >> slot_shift(r, h)) & 7u) * s;
-                    x[word_entry<GS, VALUES>(j, r, h)] = w >> slot_sign(r, h) & 1u ? -y : y;
+                    float y;
+                    if constexpr (VALUES) {
+                        y = (float)((w >> slot_shift(r, h)) & 7u) * s;
+                        y = w >> slot_sign(r, h) & 1u ? -y : y;
+                    } else {
+                        y = (float)((int)((w >> slot_shift(r, h)) & 15u) - 8) * s;
+                    }
+                    x[word_entry<GS, VALUES>(j, r, h)] = y;
                 }
     }
 }
 
 // ------------------------------------------------------------------ pages, by warps
 //
-// Lane (g, u) has entries 4 u .. 4 u + 3 (of 8: 2 u, 2 u + 1) of rows with 2 t + o = g.  As pairs in slot form (two
-// codes, the word's slot 0) they are the slots of its words of keys, and transposed those of its words of values.
+// Lane (g, u) has entries 4 u .. 4 u + 3 (of 8: 2 u, 2 u + 1) of rows with 2 t + o = g.  As pairs (two codes in the
+// form of a word's slot 0) they are the slots of its words of keys, and transposed those of its words of values.
+
+// Magnitudes m and the sign bits of two entries: a pair's codes.
+template <bool VALUES>
+__device__ __forceinline__ uint32_t pair_codes(uint32_t m, uint32_t signs)
+{
+    if constexpr (VALUES)
+        return m | (signs & 0x80008000u);
+    const uint32_t neg = ((signs >> 15) & 0x00010001u) * 0xffffu;  // all ones in negative halves
+    return __vadd2(__vadd2(m ^ neg, neg & 0x00010001u), 0x00080008u);
+}
+// A pair's codes as numbers, times 2^-24 (values) or as they are (keys).
+template <bool VALUES>
+__device__ __forceinline__ void pair_numbers(uint32_t x, float &a, float &b)
+{
+    if constexpr (VALUES) {
+        asm("{.reg .b16 p, q; mov.b32 {p, q}, %2; cvt.f32.f16 %0, p; cvt.f32.f16 %1, q;}" : "=f"(a), "=f"(b) : "r"(x));
+        a *= 0x1p24f;
+        b *= 0x1p24f;
+    } else {  // 2^23 + code
+        a = __uint_as_float((x & 15u) | 0x4b000000u) - 8388616.f;
+        b = __uint_as_float((x >> 16) | 0x4b000000u) - 8388616.f;
+    }
+}
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
@@ -257,7 +221,8 @@ struct Raw<bf16, GS> {
             w[0] = *reinterpret_cast<const uint32_t *>(p);
         }
     }
-    // The pairs' codes in slot form, and the group's scale in 16 bits; all lanes.
+    // The pairs' codes, and the group's scale in 16 bits; all lanes.
+    template <bool VALUES>
     __device__ __forceinline__ uint32_t codes(uint32_t (&x)[N]) const
     {
         uint32_t m = w[0] & 0x7fff7fffu;
@@ -272,22 +237,23 @@ struct Raw<bf16, GS> {
             asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                x[i] = magnitudes_bf16(bf16lo(w[i]), bf16hi(w[i]), inv) | (w[i] & 0x80008000u);
+                x[i] = pair_codes<VALUES>(magnitudes_bf16(bf16lo(w[i]), bf16hi(w[i]), inv), w[i]);
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                x[i] = magnitudes(bf16lo(w[i]), bf16hi(w[i]), s) | (w[i] & 0x80008000u);
+                x[i] = pair_codes<VALUES>(magnitudes(bf16lo(w[i]), bf16hi(w[i]), s), w[i]);
         }
         return __float_as_uint(s) >> 16;
     }
+    template <bool VALUES>
     static __device__ __forceinline__ void store(bf16 *p, const uint32_t (&x)[N], float s)
     {
         uint32_t y[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float a, b;
-            asm("{.reg .b16 p, q; mov.b32 {p, q}, %2; cvt.f32.f16 %0, p; cvt.f32.f16 %1, q;}" : "=f"(a), "=f"(b) : "r"(x[i]));
-            y[i] = sm100::cvt_bf16x2((a * 0x1p24f) * s, (b * 0x1p24f) * s);
+            pair_numbers<VALUES>(x[i], a, b);
+            y[i] = sm100::cvt_bf16x2(a * s, b * s);
         }
         if constexpr (N == 2)
             *reinterpret_cast<uint2 *>(p) = make_uint2(y[0], y[N - 1]);
@@ -313,6 +279,7 @@ struct Raw<float, GS> {
             w[2 * i] = v.x, w[2 * i + 1] = v.y;
         }
     }
+    template <bool VALUES>
     __device__ __forceinline__ uint32_t codes(uint32_t (&x)[N]) const
     {
         uint32_t a = 0u;
@@ -324,17 +291,18 @@ struct Raw<float, GS> {
         const float s = group_scale(a);
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            x[i] = magnitudes(w[2 * i], w[2 * i + 1], s) | __float_as_uint(w[2 * i]) >> 31 << 15 |
-                   (__float_as_uint(w[2 * i + 1]) & 0x80000000u);
+            x[i] = pair_codes<VALUES>(magnitudes(w[2 * i], w[2 * i + 1], s),
+                                      __byte_perm(__float_as_uint(w[2 * i]), __float_as_uint(w[2 * i + 1]), 0x7632));
         return __float_as_uint(s) >> 16;
     }
+    template <bool VALUES>
     static __device__ __forceinline__ void store(float *p, const uint32_t (&x)[N], float s)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float a, b;
-            asm("{.reg .b16 p, q; mov.b32 {p, q}, %2; cvt.f32.f16 %0, p; cvt.f32.f16 %1, q;}" : "=f"(a), "=f"(b) : "r"(x[i]));
-            reinterpret_cast<float2 *>(p)[i] = make_float2((a * 0x1p24f) * s, (b * 0x1p24f) * s);
+            pair_numbers<VALUES>(x[i], a, b);
+            reinterpret_cast<float2 *>(p)[i] = make_float2(a * s, b * s);
         }
     }
 };
@@ -359,7 +327,7 @@ __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, i
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t x[2][N];
-        const uint32_t s0 = raw[i][0].codes(x[0]), s1 = raw[i][1].codes(x[1]);
+        const uint32_t s0 = raw[i][0].template codes<VALUES>(x[0]), s1 = raw[i][1].template codes<VALUES>(x[1]);
         sc[i] = s0 | s1 << 16;
         if constexpr (VALUES) {
 #pragma unroll
@@ -368,7 +336,7 @@ __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, i
                 for (int k = 0; k < N; ++k)
                     x[c][k] = transpose8(x[c][k]);
         }
-        auto turned = [](uint32_t v, int r) { return __funnelshift_l(v, v, 4 * r); };
+        auto turned = [](uint32_t v, int r) { return VALUES ? __funnelshift_l(v, v, 4 * r) : v << (4 * r); };
         if constexpr (GS == 16) {  // slots: keys c + 2 k, values 2 c + k
             const uint32_t y1 = VALUES ? x[0][N - 1] : x[1][0], y2 = VALUES ? x[1][0] : x[0][N - 1];
             w[i] = x[0][0] | turned(y1, 1) | turned(y2, 2) | turned(x[1][N - 1], 3);
@@ -399,7 +367,7 @@ __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, i
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int row = row0 + (GS == 16 ? 4 : 8) * i + word_row<GS, VALUES>(VALUES ? 0 : 4 * (g & 1), r, h);
-                mask |= row >= first && row < end ? slot_mask(r, h) : 0u;
+                mask |= row >= first && row < end ? slot_mask<VALUES>(r, h) : 0u;
             }
         if (mask)
             words[i] = (words[i] & ~mask) | (w[GS == 16 ? i : 2 * i + 1] & mask);
@@ -428,7 +396,8 @@ __device__ __forceinline__ void read_page(const unsigned char *block, T *vec, in
         w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
     } else {
         const uint2 v = *reinterpret_cast<const uint2 *>(at);
-        w[0] = v.x, w[1] = __funnelshift_r(v.x, v.x, 8), w[2] = v.y, w[3] = __funnelshift_r(v.y, v.y, 8);
+        w[0] = v.x, w[1] = VALUES ? __funnelshift_r(v.x, v.x, 8) : v.x >> 8;
+        w[2] = v.y, w[3] = VALUES ? __funnelshift_r(v.y, v.y, 8) : v.y >> 8;
     }
     const uint4 v = *reinterpret_cast<const uint4 *>(scales_of<GS, VALUES>(const_cast<unsigned char *>(block)) + g * 8);
     const uint32_t sc[4] = {v.x, v.y, v.z, v.w};
@@ -440,13 +409,14 @@ __device__ __forceinline__ void read_page(const unsigned char *block, T *vec, in
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 const int r = GS == 16 ? (VALUES ? 2 * c + k : c + 2 * k) : c;
-                x[k] = __funnelshift_r(w[i], w[i], 4 * r) & 0x80078007u;
                 if constexpr (VALUES)
-                    x[k] = transpose8(x[k]);
+                    x[k] = transpose8(__funnelshift_r(w[i], w[i], 4 * r) & 0x80078007u);
+                else
+                    x[k] = (w[i] >> (4 * r)) & 0x000f000fu;
             }
             const int row = lane_row(g, i, c);
             if (row >= first && row < end)
-                Raw<T, GS>::store(vec + (size_t)row * stride + u * 2 * N, x, c ? bf16hi(sc[i]) : bf16lo(sc[i]));
+                Raw<T, GS>::template store<VALUES>(vec + (size_t)row * stride + u * 2 * N, x, c ? bf16hi(sc[i]) : bf16lo(sc[i]));
         }
 }
 

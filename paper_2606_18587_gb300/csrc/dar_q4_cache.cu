@@ -100,8 +100,7 @@ __global__ void __launch_bounds__(NR *slices<DD>()) append_kernel(AppendArgs a, 
 
 // Few tokens a sequence: one CTA per sequence, as cache_append_kernel (dar_append.cu), so that its length can be
 // advanced at the end and a call is one launch.  A thread runs one chain (keys or values, KV head, entry) for the
-// tokens that leave, kept in registers and then as vectors in shared memory; then a thread quantises and writes the
-// unit of a group.
+// tokens that leave; the lanes that have a group quantise it together.
 constexpr int kFewThreads = 512;
 constexpr int kFewRows = 8;               // tokens of a round
 constexpr int kFewStageBytes = 96 << 10;  // their rows of 64
@@ -112,11 +111,69 @@ __host__ __device__ constexpr int few_rows(int Hkv)
     const int r = kFewStageBytes / (2 * Hkv * kHeadDim * (int)sizeof(T));
     return r > kFewRows ? kFewRows : r;
 }
-template <typename T, int DD>
-__host__ __device__ constexpr size_t few_smem(int Hkv)
-{
-    return (size_t)few_rows<T>(Hkv) * 2 * Hkv * (kHeadDim + DD) * sizeof(T);
-}
+
+// Rows on their way into a block, an entry a thread: GS consecutive lanes have a group.  Words that several of the
+// unit's rows share are written once.
+template <int GS>
+struct FewWords {
+    uint32_t x0 = 0u, x1 = 0u, m0 = 0u, m1 = 0u;  // of the rows so far: words and masks (keys: of even and of odd rows)
+    // Entry e of a row of a page, in this lane; all lanes.  last: the last row of its unit, or of all.
+    __device__ __forceinline__ void add(float x, int e, bool values, int row, unsigned char *block, bool last)
+    {
+        uint32_t a = magnitude(x);
+#pragma unroll
+        for (int o = 1; o < GS; o <<= 1)
+            a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
+        const float s = group_scale(a);
+        const uint32_t code = s > 0.f ? (uint32_t)fminf(rintf(__fdiv_rn(fabsf(x), s)), 7.f) : 0u;
+        // where the entry is: keys, slot c + 2 (e / 2 mod 2) of half e mod 2; values, slot 2 c + (e / 2 mod 2) of half o
+        const int o = row & 1, c = (row >> 1) & 1, i = (row >> 2) & 1, k = (e >> 1) & 1;
+        const int slot = GS == 16 ? (values ? 2 * c + k : c + 2 * k) : 2 * i + c, half = values ? o : e & 1;
+        const uint32_t neg = __float_as_uint(x) >> 31;
+        uint32_t y = values ? code << slot_shift(slot, half) | neg << slot_sign(slot, half)
+                            : (neg ? 8u - code : 8u + code) << slot_shift(slot, half);
+        // the other entries of the word: keys, of four (two) consecutive ones; values, of e and e + 2
+        uint32_t m = values ? slot_mask<true>(slot, half) : slot_mask<false>(slot, half);
+#pragma unroll
+        for (int q = 1; q < 4; q <<= 1) {
+            const uint32_t yo = __shfl_xor_sync(0xffffffffu, y, q), mo = __shfl_xor_sync(0xffffffffu, m, q);
+            if (GS == 16 ? !values || q == 2 : !values && q == 1) {
+                y |= yo;
+                m |= mo;
+            }
+        }
+        if (values || o == 0)
+            x0 |= y, m0 |= m;
+        else
+            x1 |= y, m1 |= m;
+        if (block && e == 0)
+            reinterpret_cast<uint16_t *>(block + kPage * GS + (values ? 2 * kPage : 0))[scale_index(row)] =
+                (uint16_t)(__float_as_uint(s) >> 16);
+        if (!last)
+            return;
+        const int row0 = row & ~(GS == 16 ? 3 : 7);
+        auto put = [&](int j, uint32_t x, uint32_t mask) {
+            uint32_t *p = reinterpret_cast<uint32_t *>(
+                block + (values ? kPage * GS / 2 + word_offset<GS, true>(row0, j) : word_offset<GS, false>(row0, j)));
+            *p = (*p & ~mask) | x;
+        };
+        if (block) {
+            if (values) {
+                if (GS == 8)
+                    put(e, x0, m0);
+                else if ((e & 2) == 0)
+                    put(2 * (e >> 2) + (e & 1), x0, m0);
+            } else {  // words 4 o + u, u = e / 4 (e / 2): one lane writes the even rows', the next one the odd rows'
+                const int u = GS == 16 ? e >> 2 : e >> 1, l = GS == 16 ? e & 3 : e & 1;
+                if (l == 0 && m0)
+                    put(u, x0, m0);
+                else if (l == 1 && m1)
+                    put(4 + u, x1, m1);
+            }
+        }
+        x0 = x1 = m0 = m1 = 0u;
+    }
+};
 
 template <typename T, int DD>
 __device__ __forceinline__ void append_few(const AppendArgs &a)
@@ -125,10 +182,10 @@ __device__ __forceinline__ void append_few(const AppendArgs &a)
     constexpr int E = Granule<T>::kElems, GPR = kHeadDim / E, GS = F::kGroup;
     extern __shared__ __align__(16) unsigned char few[];
     __shared__ int s_L, s_nb, s_ok;
+    __shared__ int s_pid[kFewRows];  // page of each staged row (-1: invalid)
     const int b = blockIdx.x, tid = threadIdx.x, Hkv = a.Hkv, n = a.n, w = a.w;
     const int chains = 2 * Hkv * DD, R = few_rows<T>(Hkv);
     T *rows = reinterpret_cast<T *>(few);           // [R][kv][Hkv][64]
-    T *vec = rows + (size_t)R * 2 * Hkv * kHeadDim;  // [R][kv][Hkv][DD]
     const T *knew = static_cast<const T *>(a.k_new), *vnew = static_cast<const T *>(a.v_new);
     T *wk = static_cast<T *>(a.win_k), *wv = static_cast<T *>(a.win_v);
     unsigned char *pool = static_cast<unsigned char *>(a.pool_kd);
@@ -175,54 +232,43 @@ __device__ __forceinline__ void append_few(const AppendArgs &a)
                                  : (kv ? vnew : knew) + (((size_t)b * Hkv + g) * n + (p - L)) * kHeadDim;
             reinterpret_cast<uint4 *>(rows)[i] = *reinterpret_cast<const uint4 *>(src + q * E);
         }
+        if (tid < nr) {
+            const int lp = (m0 + tid) / kPage, id = lp < a.maxp ? a.block_table[(size_t)b * a.maxp + lp] : -1;
+            const bool valid = id >= 0 && id < a.num_pages;
+            if (!valid)
+                report(a.status, DAR_ERR_CAPACITY);
+            s_pid[tid] = valid ? id : -1;
+        }
         __syncthreads();
-        for (int ch0 = 0; ch0 < chains; ch0 += kFewThreads) {
-            const int ch = ch0 + tid;
-            if (ch >= chains)
-                break;
-            if (ch0 > 0)
+        for (int ch0 = 0; ch0 < chains; ch0 += kFewThreads) {  // (whole warps take part: chains is a multiple of 16)
+            const int ch = ch0 + tid, kg = ch / DD, c = ch % DD;
+            if (ch0 > 0 && ch < chains)
                 load_w(ch);
+            if (ch0 + (tid & ~31) >= chains)
+                break;
+            FewWords<GS> out;
+            const bool mine = ch < chains;
+            unsigned char *heads = pool + (size_t)(kg % Hkv) * F::kBytes + c / GS * F::kBlock;
             for (int r = 0; r < nr; ++r) {
-                const uint4 *x4 = reinterpret_cast<const uint4 *>(rows + ((size_t)r * 2 * Hkv + ch / DD) * kHeadDim);
                 float acc = 0.0f;  // Eq. 1: one fp32 FMA chain over t = 0..63
+                if (mine) {
+                    const uint4 *x4 = reinterpret_cast<const uint4 *>(rows + ((size_t)r * 2 * Hkv + kg) * kHeadDim);
 #pragma unroll
-                for (int q = 0; q < GPR; ++q) {
-                    float xf[E];
-                    unpack(x4[q], xf, T());
+                    for (int q = 0; q < GPR; ++q) {
+                        float xf[E];
+                        unpack(x4[q], xf, T());
 #pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        acc = __fmaf_rn(xf[e], wc[q * E + e], acc);
+                        for (int e = 0; e < E; ++e)
+                            acc = __fmaf_rn(xf[e], wc[q * E + e], acc);
+                    }
                 }
-                vec[(size_t)r * chains + ch] = from_f32<T>(acc);
+                const int m = m0 + r, id = s_pid[r];
+                out.add(to_f32(from_f32<T>(acc)), c % GS, kg >= Hkv, m % kPage,
+                        mine && id >= 0 ? heads + (size_t)id * Hkv * F::kBytes : nullptr, r + 1 == nr || (m + 1) % F::kUnit == 0);
             }
         }
         if (chains > kFewThreads && m0 + R < hi && tid < chains)  // the first chains' columns again
             load_w(tid);
-        __syncthreads();
-        const int u0 = m0 / F::kUnit, units = (m0 + nr - 1) / F::kUnit - u0 + 1, heads = 2 * Hkv * F::kGroups;
-        for (int i = tid; i < units * heads; i += kFewThreads) {
-            const int p0 = (u0 + i / heads) * F::kUnit, h = i % heads, sb = h % F::kGroups, kg = h / F::kGroups;
-            const int kv = kg / Hkv, g = kg % Hkv;
-            unsigned has = 0u;
-#pragma unroll
-            for (int k = 0; k < F::kUnit; ++k)
-                has |= p0 + k >= m0 && p0 + k < m0 + nr ? 1u << k : 0u;
-            const int id = a.block_table[(size_t)b * a.maxp + p0 / kPage];
-            if (id < 0 || id >= a.num_pages) {
-                report(a.status, DAR_ERR_CAPACITY);
-                continue;
-            }
-            unsigned char *block = pool + ((size_t)id * Hkv + g) * F::kBytes + sb * F::kBlock;
-            auto row = [&](int k, float (&x)[GS]) {
-#pragma unroll
-                for (int e = 0; e < GS; ++e)
-                    x[e] = to_f32(vec[(size_t)(p0 + k - m0) * chains + kg * DD + sb * GS + e]);
-            };
-            if (kv)
-                write_unit<GS, true>(block, p0 % kPage, has, row);
-            else
-                write_unit<GS, false>(block, p0 % kPage, has, row);
-        }
         __syncthreads();
     }
     // new tokens that stay in the window: every ring row above is read
@@ -249,11 +295,11 @@ static cudaError_t append_few_launch(const AppendArgs &a, cudaStream_t s)
     static PerDeviceOnce once;  // opt-in to more than 48 KB of shared memory, once per device
     const cudaError_t e = per_device_once(once, [](int) {
         return cudaFuncSetAttribute(append_few_kernel<T, DD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    2 * kFewStageBytes);
+                                    kFewStageBytes);
     });
     if (e != cudaSuccess)
         return e;
-    append_few_kernel<T, DD><<<a.B, kFewThreads, few_smem<T, DD>(a.Hkv), s>>>(a);
+    append_few_kernel<T, DD><<<a.B, kFewThreads, (size_t)few_rows<T>(a.Hkv) * 2 * a.Hkv * kHeadDim * sizeof(T), s>>>(a);
     return cudaGetLastError();
 }
 
@@ -351,6 +397,8 @@ static cudaError_t by_width(int dd, F &&f)
     }
 }
 
+constexpr long long kBigTiles = kSms * 6 * 2;
+
 template <typename T>
 static cudaError_t append_t(int dd, const AppendArgs &a, cudaStream_t s)
 {
@@ -358,7 +406,13 @@ static cudaError_t append_t(int dd, const AppendArgs &a, cudaStream_t s)
         constexpr int DD = decltype(width)::value;
         if (a.n <= kFewRows && few_rows<T>(a.Hkv) > 0)
             return append_few_launch<T, DD>(a, s);
-        return append_tiles<T, DD, 1, 64>(a, s);
+        // Large tiles, whose threads have several rows for a read of W, once they fill the chip a few times over and are
+        // not mostly empty (the rule of dar_append.cu, whose tiles these are).
+        constexpr int R = rows_bulk<T>();
+        const long long tiles = ((long long)a.n + kPage - 1 + R - 1) / R;
+        if (tiles * a.B * a.Hkv * 2 >= kBigTiles && a.n >= 4 * R)
+            return append_tiles<T, DD, rows_per_thread<DD>(), R / rows_per_thread<DD>()>(a, s);
+        return append_tiles<T, DD, 1, kPage>(a, s);
     });
 }
 

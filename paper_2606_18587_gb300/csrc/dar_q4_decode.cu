@@ -33,10 +33,13 @@ using namespace sm100;
 constexpr int kRows = 8;         // query heads of a unit at most
 constexpr int kRun = 16;         // ring tokens of a stage
 constexpr int kWarps = 8;        // of a CTA (CUDA cores)
-constexpr int kMmaWarps = 12;    // of a CTA (tensor cores)
-constexpr int kSlots = 3;        // stages in flight of a warp
-constexpr int kSlot = 5120;      // bytes of one
-constexpr int kMaxShares = 1920; // the workspace holds partial results of this many warps
+// Of a CTA (tensor cores), and stages in flight of each: as many warps as registers allow.
+template <int DD>
+__host__ __device__ constexpr int mma_warps() { return DD <= 16 ? 16 : 12; }
+template <int DD>
+__host__ __device__ constexpr int mma_slots() { return DD <= 16 ? 2 : 3; }
+constexpr int kSlot = 5120;      // bytes of a stage at most
+constexpr int kMaxShares = 2560; // the workspace holds partial results of this many warps
 constexpr int kCostUnit = 8;     // cost of a unit's set-up (its place on the line is before the stages)
 constexpr int kCostRun = 8;      // of kRun ring tokens
 template <int DD>
@@ -399,13 +402,14 @@ __global__ void __launch_bounds__(kWarps * 32) attend_kernel(Args a)
 // 4 g + t has the scores, weights, references and sums of heads t and t + 4 (CT = 2); with CT = 1
 // of head t alone, and the other column takes what is said below.
 //
-//  codes    fp16 subnormals code * 2^-24 as they lie: seven instructions for the eight of a word.
-//           (Their values by a conversion of offset codes take 13: an AND and an OR each, since an
-//           instruction has one immediate, and the offset subtracted; e4m3 operands are converted
-//           by twice as many: mma.sync has no products of them here.)
+//  codes    fp16 subnormals as they lie (dar_q4.cuh): five instructions for the eight of a word of
+//           keys, seven for one of values.  (Conversions of offset codes take 13: an AND and an OR each,
+//           since an instruction has one immediate, and the offset subtracted; e4m3 operands are
+//           converted by twice as many: mma.sync has no products of them here.)
 //  scores   q~, brought to [2^14, 2^15) by a power of two, is two fp16 terms (2^-22 of it).  CT = 1:
 //           the second one is the other column's.  CT = 2: a product of its own.  A d_down of 8:
-//           the other half of the product's 16 entries.
+//           the two halves of a product's 16 entries.  The sum starts from
+//           minus 8 times theirs.  Rows with c = 1 are in slots 1 and 3: their scores are 16 times as large.
 //  weights  p s_v as fp16 (2^-11) relative to a reference of the row that keeps the largest at
 //           2^8 when it is set and below 2^15 always; it is raised by a vote.  (bf16 operands need two
 //           terms for the same error, twice the conversions and transpositions.)
@@ -436,17 +440,27 @@ __device__ __forceinline__ uint32_t cvt_f16x2(float lo, float hi)
     return r;
 }
 
-// Two values as two fp16 terms each: all but 2^-22 of them.
-__device__ __forceinline__ void split_f16(float x, float y, uint32_t &hi, uint32_t &lo)
+// Two values as two fp16 terms each, all but 2^-22 of them; the terms are added to their sums.
+__device__ __forceinline__ void split_f16(float x, float y, uint32_t &hi, uint32_t &lo, float (&sums)[2])
 {
     hi = cvt_f16x2(x, y);
-    float a, b;
+    float a, b, c, d;
     asm("{.reg .b16 p, q; mov.b32 {p, q}, %2; cvt.f32.f16 %0, p; cvt.f32.f16 %1, q;}" : "=f"(a), "=f"(b) : "r"(hi));
     lo = cvt_f16x2(x - a, y - b);
+    asm("{.reg .b16 p, q; mov.b32 {p, q}, %2; cvt.f32.f16 %0, p; cvt.f32.f16 %1, q;}" : "=f"(c), "=f"(d) : "r"(lo));
+    sums[0] += a + b;
+    sums[1] += c + d;
 }
 
-// Slots 0 to 3 of a word of codes as operand registers.
-__device__ __forceinline__ void codes_of(uint32_t w, uint32_t (&c)[4])
+// Slots 0 to 3 of a word of keys (slots 1 and 3 times 16) and of values as operand registers.
+__device__ __forceinline__ void keys_of(uint32_t w, uint32_t (&c)[4])
+{
+    c[0] = w & 0x000f000fu;
+    c[1] = w & 0x00f000f0u;
+    c[2] = (w >> 8) & 0x000f000fu;
+    c[3] = (w >> 8) & 0x00f000f0u;
+}
+__device__ __forceinline__ void values_of(uint32_t w, uint32_t (&c)[4])
 {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -473,6 +487,7 @@ __device__ __forceinline__ uint32_t key_mask(int key, int n)
 // What a warp fills its slots with, ahead of what it computes.
 template <int DD>
 struct Filler {
+    static constexpr int kSlots = mma_slots<DD>();
     static constexpr int kPages = Fmt<DD>::kBytes > kSlot / 4 ? kSlot / Fmt<DD>::kBytes : 4;  // of a stage
     Walk walk;
     Cut c;
@@ -543,6 +558,7 @@ struct Heads {
     static constexpr int OD = CT == 1 ? 2 : 1;    // sums of a group (see page_step)
     uint32_t q[4][2];        // ring: queries as B operands
     uint32_t qt[NB][TB][2];  // pages: q~ as B operands, two fp16 terms
+    float from[NB][4];       // what a score's sum starts from
     float cq[CT];            // scale of a score: c2, the power of two taken out of q~, and the codes' 2^24
     Soft ring[CT], page[CT];
     float ol[kHeadDim / 16][4], od[NB][OD][4];
@@ -604,7 +620,7 @@ struct Heads {
                 x[j][2 + k] *= up[k];
             }
         }
-        // column i0 of a score product wants consecutive entries of its head, i0 / 2 (+ 4 in odd columns with CT = 2): four
+        // column i0 of a score product wants consecutive entries of its head, i0 / 2 (+ 4 in odd columns): four
         // from 4 c0 on, or of a d_down of 8 two from 2 c0 on
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
@@ -622,22 +638,31 @@ struct Heads {
                         z[k] = c0 < 2 ? z[k] : hi;
                     }
                 }
-                y[e] = i0 & 1 ? z[CT - 1] : z[0];
+                y[e] = CT == 2 && (i0 & 1) ? z[CT - 1] : z[0];  // (with CT = 1 the odd columns are not used)
             }
-            uint32_t hi[NE / 2], lo[NE / 2];
+            float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < NE / 2; ++e)
-                split_f16(y[2 * e], y[2 * e + 1], hi[e], lo[e]);
-            if constexpr (GS == 8) {
-                qt[j][0][0] = CT == 2 || !(i0 & 1) ? hi[0] : 0u;
-                qt[j][0][1] = CT == 2 || !(i0 & 1) ? lo[0] : 0u;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    qt[j][0][e] = CT == 1 && (i0 & 1) ? lo[e % (NE / 2)] : hi[e % (NE / 2)];
-                    if constexpr (CT == 2)
-                        qt[j][TB - 1][e] = lo[e % (NE / 2)];
+            for (int e = 0; e < NE / 2; ++e) {
+                uint32_t hi, lo;
+                float sums[2] = {0.f, 0.f};
+                split_f16(y[2 * e], y[2 * e + 1], hi, lo, sums);
+                if constexpr (GS == 8) {
+                    qt[j][0][0] = hi;
+                    qt[j][0][1] = lo;
+                } else if constexpr (CT == 2) {
+                    qt[j][0][e] = hi;
+                    qt[j][TB - 1][e] = lo;
+                } else {
+                    qt[j][0][e] = i0 & 1 ? lo : hi;
                 }
+                sum += CT == 2 || GS == 8 ? sums[0] + sums[1] : i0 & 1 ? sums[1] : sums[0];
+            }
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                from[j][k] = -0x1p-21f * __shfl_sync(0xffffffffu, sum, (2 * c0 + k) * 4);  // 8 * 2^-24
+                from[j][2 + k] = 16.f * from[j][k];
             }
         }
 #pragma unroll
@@ -757,16 +782,15 @@ struct Heads {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t c[4];
-                codes_of(w[i], c);
+                keys_of(w[i], c);
                 if constexpr (GS == 8) {  // both halves of the product's 16 entries are the key's 8
                     c[0] = i % 2 ? c[2] : c[0];
                     c[1] = i % 2 ? c[3] : c[1];
                     c[2] = c[0];
                     c[3] = c[1];
                 }
-                const float z[4] = {0.f, 0.f, 0.f, 0.f};
                 float d[4];
-                mma_f16_c(d, c, qt[j][0][0], qt[j][0][1], z);
+                mma_f16_c(d, c, qt[j][0][0], qt[j][0][1], from[j]);
                 if constexpr (TB == 2)
                     mma_f16_acc(d, c, qt[j][TB - 1][0], qt[j][TB - 1][1]);
                 const float s0 = bf16lo(sc[i]), s1 = bf16hi(sc[i]);
@@ -827,13 +851,18 @@ struct Heads {
             s0 = CT == 1 || k % 2 == 0 ? bf16lo(s) : bf16hi(s);
             s1 = CT == 1 || k % 2 != 0 ? bf16hi(s) : bf16lo(s);
         };
+        // scale of a pair's scores: slots of c = 1 are 16 times as large
+        auto scale = [&](int k, int e) {
+            const float s = cq[CT == 2 ? e : 0];
+            return (CT == 1 ? e : k % 2) ? s * 0.0625f : s;
+        };
         auto weigh = [&]() {  // returns whether something got far above the reference
             float top = 0.f;
             l[0] = l[1] = 0.f;
 #pragma unroll
             for (int k = 0; k < NP; ++k) {
                 float x0, x1, s0, s1;
-                ffma2(x0, x1, y[k][0], y[k][1], cq[0], cq[CT - 1], page[0].bias, page[CT - 1].bias);
+                ffma2(x0, x1, y[k][0], y[k][1], scale(k, 0), scale(k, 1), page[0].bias, page[CT - 1].bias);
                 p[k][0] = ex2_approx(x0);
                 p[k][1] = ex2_approx(x1);
                 add2(l[0], l[1], l[0], l[1], p[k][0], p[k][1]);
@@ -855,7 +884,7 @@ struct Heads {
                             continue;
                         float s[2];
                         scales(vm[i / CT], i, s[0], s[1]);
-                        top = fmaxf(top, fmaf(y[i][e], cq[k], __log2f(fmaxf(0x1p-64f, s[e]))));
+                        top = fmaxf(top, fmaf(y[i][e], scale(i, e), __log2f(fmaxf(0x1p-64f, s[e]))));
                     }
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1)
@@ -900,10 +929,10 @@ struct Heads {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if constexpr (GS == 16) {
-                    codes_of(w[i], v[i]);
+                    values_of(w[i], v[i]);
                 } else if (i % 2 == 0) {
                     uint32_t c[4];
-                    codes_of(w[i], c);
+                    values_of(w[i], c);
                     v[i][0] = c[0], v[i][2] = c[1], v[i + 1][0] = c[2], v[i + 1][2] = c[3];
                     v[i][1] = v[i][3] = v[i + 1][1] = v[i + 1][3] = 0u;
                 }
@@ -967,12 +996,17 @@ struct Heads {
     }
 };
 
-constexpr size_t mma_smem(int B) { return 1024 + (size_t)kMmaWarps * kSlots * (kSlot + 8) + 16 + (2 * (size_t)B + 1) * 4; }
+template <int DD>
+constexpr size_t mma_smem(int B)
+{
+    return 1024 + (size_t)mma_warps<DD>() * mma_slots<DD>() * (kSlot + 8) + 16 + (2 * (size_t)B + 1) * 4;
+}
 
 template <int DD, int CT>
-__global__ void __launch_bounds__(kMmaWarps * 32, 1)
+__global__ void __launch_bounds__(mma_warps<DD>() * 32, 1)
     attend_mma_kernel(const __grid_constant__ CUtensorMap wk, const __grid_constant__ CUtensorMap wv, const Args a)
 {
+    constexpr int kMmaWarps = mma_warps<DD>(), kSlots = mma_slots<DD>();
     extern __shared__ unsigned char raw[];
     unsigned char *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);  // the swizzle's atoms
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = blockIdx.x * kMmaWarps + warp;
@@ -1149,10 +1183,10 @@ static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s
             if constexpr (sizeof(T) == 2) {
                 if (e2 == cudaSuccess)
                     e2 = cudaFuncSetAttribute(attend_mma_kernel<DD, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                              (int)mma_smem(DAR_DECODE_MAX_BATCH));
+                                              (int)mma_smem<DD>(DAR_DECODE_MAX_BATCH));
                 if (e2 == cudaSuccess)
                     e2 = cudaFuncSetAttribute(attend_mma_kernel<DD, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                              (int)mma_smem(DAR_DECODE_MAX_BATCH));
+                                              (int)mma_smem<DD>(DAR_DECODE_MAX_BATCH));
             } else if (e2 == cudaSuccess) {
                 e2 = cudaFuncSetAttribute(attend_kernel<T, DD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                           (int)lanes_smem(DAR_DECODE_MAX_BATCH));
@@ -1167,12 +1201,13 @@ static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s
         const unsigned long long rows = (unsigned long long)c.B * c.Hkv * c.w;
         if (!make_tma_2d_bf16(&wk, c.win_k, rows, kHeadDim, kRun) || !make_tma_2d_bf16(&wv, c.win_v, rows, kHeadDim, kRun))
             return cudaErrorInvalidValue;
-        const int grid = std::min(sms, kMaxShares / kMmaWarps);
-        a.shares = grid * kMmaWarps;
+        constexpr int warps = mma_warps<DD>();
+        const int grid = std::min(sms, kMaxShares / warps);
+        a.shares = grid * warps;
         if (y.RU <= 4)
-            attend_mma_kernel<DD, 1><<<grid, kMmaWarps * 32, mma_smem(c.B), s>>>(wk, wv, a);
+            attend_mma_kernel<DD, 1><<<grid, warps * 32, mma_smem<DD>(c.B), s>>>(wk, wv, a);
         else
-            attend_mma_kernel<DD, 2><<<grid, kMmaWarps * 32, mma_smem(c.B), s>>>(wk, wv, a);
+            attend_mma_kernel<DD, 2><<<grid, warps * 32, mma_smem<DD>(c.B), s>>>(wk, wv, a);
     } else {
         const int grid = std::min(sms, kMaxShares / kWarps);
         a.shares = grid * kWarps;
