@@ -12,15 +12,10 @@
 // codes of the values, 64 scales of the keys, 64 of the values (bf16).  Codes lie
 // where the lanes of a warp want them as operands of mma.sync (dar_q4_decode.cu), all
 // 64 tokens of a group with one load of 16 bytes (8) a lane.  A word is eight codes, in
-// slots 0 to 3 of either half:
-//   values   turned right by 4 r bits it has slot r's two codes as sign and magnitude in bits 15,
-//            0-2 and 31, 16-18, which are the fp16 numbers code * 2^-24: an instruction to turn
-//            and one to mask make an operand register.
-//   keys     slot r is bits 4 r .. 4 r + 3 of either half, code + 8.  fp16 numbers are linear in
-//            their lowest 11 bits, so that slots 0 and 1 are (code + 8) 2^-24 and 2^-20 where they
-//            lie, and slots 2 and 3 shifted right by 8: five instructions for four operand registers,
-//            not seven; a score takes the offset back with what its sum starts from.  (The values' sums
-//            run over thousands of tokens, in which the offset's part would drown the rest.)
+// slots 0 to 3 of either half: slot r is bits 4 r .. 4 r + 3, code + 8.  fp16 numbers are
+// linear in their lowest 11 bits, so that slots 0 and 1 are (code + 8) 2^-24 and 2^-20 where
+// they lie, and slots 2 and 3 shifted right by 8: an AND each and a shift make four operand
+// registers.  The products take the offset back.
 //   row      r of a page is token 4 i + 2 c + o of 16 t ..: t = r / 16, i = r / 4 mod 4, c = r / 2 mod 2, o = r mod 2
 //   keys     lane (g, u) = 4 g + u has rows with 2 t + o = g: word i, slots c and 2 + c, are
 //            entries 4 u, 4 u + 1 and 4 u + 2, 4 u + 3 in the two halves
@@ -75,33 +70,24 @@ __device__ __forceinline__ float group_scale_bf16(uint32_t a)
     return round_scale((u + 0x200u) & ~0x3ffu);
 }
 
-// Magnitudes |x| / s of two entries, rounded, in the low halves of either half.  The quotient is a product with 1 / s;
-// exact: on bf16 numbers, whose quotients lie 2^-11 away from halves at least where they are no halves, its error goes
-// with a rounding to 2^-13.  Else by division (rounded to 24 bits it is on the same side of a half as the quotient).
-__device__ __forceinline__ uint32_t magnitudes_bf16(float x, float y, float inv)
+// x / s of two entries, rounded, plus 8 in either half.  The quotient is a product with 1 / s; exact: on bf16
+// numbers, whose quotients lie 2^-11 away from halves at least where they are no halves, its error goes with a rounding
+// to 2^-13.  Else by division (rounded to 24 bits it is on the same side of a half as the quotient).
+__device__ __forceinline__ uint32_t codes_bf16(float x, float y, float inv)
 {
-    constexpr float kGrid = 1536.f, kInt = 8388608.f;  // 1.5 * 2^10, 2^23
-    const float a = fmaf(fabsf(x), inv, kGrid) - kGrid + kInt, b = fmaf(fabsf(y), inv, kGrid) - kGrid + kInt;
+    constexpr float kGrid = 1536.f, kInt = 8388616.f;  // 1.5 * 2^10, 2^23 + 8
+    const float a = fmaf(x, inv, kGrid) - kGrid + kInt, b = fmaf(y, inv, kGrid) - kGrid + kInt;
     return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410);
 }
-__device__ __forceinline__ uint32_t magnitudes(float x, float y, float s)
+__device__ __forceinline__ uint32_t code_of(float x, float s)
 {
-    if (!(s > 0.f))
-        return 0u;
-    const float a = fminf(rintf(__fdiv_rn(fabsf(x), s)), 7.f), b = fminf(rintf(__fdiv_rn(fabsf(y), s)), 7.f);
-    return (uint32_t)a | (uint32_t)b << 16;
+    return s > 0.f ? (uint32_t)((int)fminf(fmaxf(rintf(__fdiv_rn(x, s)), -7.f), 7.f) + 8) : 8u;
 }
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// Slot r of half h of a word: where a value's magnitude and its sign are, or a key's code.
+// Where slot r of half h of a word is.
 __host__ __device__ constexpr int slot_shift(int r, int h) { return 16 * h + 4 * r; }
-__host__ __device__ constexpr int slot_sign(int r, int h) { return (15 + 16 * h + 4 * r) % 32; }
-template <bool VALUES>
-__host__ __device__ constexpr uint32_t slot_mask(int r, int h)
-{
-    return VALUES ? 7u << slot_shift(r, h) | 1u << slot_sign(r, h) : 15u << slot_shift(r, h);
-}
 
 // Word j (of 8) of a unit: the row in the unit and the entry that slot r of half h holds.
 template <int GS, bool VALUES>
@@ -149,16 +135,8 @@ __device__ __forceinline__ void read_row(const unsigned char *block, int row, fl
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                if (word_row<GS, VALUES>(j, r, h) == k) {
-                    float y;
-                    if constexpr (VALUES) {
-                        y = (float)((w >> slot_shift(r, h)) & 7u) * s;
-                        y = w >> slot_sign(r, h) & 1u ? -y : y;
-                    } else {
-                        y = (float)((int)((w >> slot_shift(r, h)) & 15u) - 8) * s;
-                    }
-                    x[word_entry<GS, VALUES>(j, r, h)] = y;
-                }
+                if (word_row<GS, VALUES>(j, r, h) == k)
+                    x[word_entry<GS, VALUES>(j, r, h)] = (float)((int)((w >> slot_shift(r, h)) & 15u) - 8) * s;
     }
 }
 
@@ -167,27 +145,11 @@ __device__ __forceinline__ void read_row(const unsigned char *block, int row, fl
 // Lane (g, u) has entries 4 u .. 4 u + 3 (of 8: 2 u, 2 u + 1) of rows with 2 t + o = g.  As pairs (two codes in the
 // form of a word's slot 0) they are the slots of its words of keys, and transposed those of its words of values.
 
-// Magnitudes m and the sign bits of two entries: a pair's codes.
-template <bool VALUES>
-__device__ __forceinline__ uint32_t pair_codes(uint32_t m, uint32_t signs)
-{
-    if constexpr (VALUES)
-        return m | (signs & 0x80008000u);
-    const uint32_t neg = ((signs >> 15) & 0x00010001u) * 0xffffu;  // all ones in negative halves
-    return __vadd2(__vadd2(m ^ neg, neg & 0x00010001u), 0x00080008u);
-}
-// A pair's codes as numbers, times 2^-24 (values) or as they are (keys).
-template <bool VALUES>
+// A pair's codes as numbers (2^23 + code + 8 less 2^23 + 8).
 __device__ __forceinline__ void pair_numbers(uint32_t x, float &a, float &b)
 {
-    if constexpr (VALUES) {
-        asm("{.reg .b16 p, q; mov.b32 {p, q}, %2; cvt.f32.f16 %0, p; cvt.f32.f16 %1, q;}" : "=f"(a), "=f"(b) : "r"(x));
-        a *= 0x1p24f;
-        b *= 0x1p24f;
-    } else {  // 2^23 + code
-        a = __uint_as_float((x & 15u) | 0x4b000000u) - 8388616.f;
-        b = __uint_as_float((x >> 16) | 0x4b000000u) - 8388616.f;
-    }
+    a = __uint_as_float((x & 15u) | 0x4b000000u) - 8388616.f;
+    b = __uint_as_float((x >> 16) | 0x4b000000u) - 8388616.f;
 }
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
@@ -222,7 +184,6 @@ struct Raw<bf16, GS> {
         }
     }
     // The pairs' codes, and the group's scale in 16 bits; all lanes.
-    template <bool VALUES>
     __device__ __forceinline__ uint32_t codes(uint32_t (&x)[N]) const
     {
         uint32_t m = w[0] & 0x7fff7fffu;
@@ -237,22 +198,21 @@ struct Raw<bf16, GS> {
             asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                x[i] = pair_codes<VALUES>(magnitudes_bf16(bf16lo(w[i]), bf16hi(w[i]), inv), w[i]);
+                x[i] = codes_bf16(bf16lo(w[i]), bf16hi(w[i]), inv);
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                x[i] = pair_codes<VALUES>(magnitudes(bf16lo(w[i]), bf16hi(w[i]), s), w[i]);
+                x[i] = code_of(bf16lo(w[i]), s) | code_of(bf16hi(w[i]), s) << 16;
         }
         return __float_as_uint(s) >> 16;
     }
-    template <bool VALUES>
     static __device__ __forceinline__ void store(bf16 *p, const uint32_t (&x)[N], float s)
     {
         uint32_t y[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float a, b;
-            pair_numbers<VALUES>(x[i], a, b);
+            pair_numbers(x[i], a, b);
             y[i] = sm100::cvt_bf16x2(a * s, b * s);
         }
         if constexpr (N == 2)
@@ -279,7 +239,6 @@ struct Raw<float, GS> {
             w[2 * i] = v.x, w[2 * i + 1] = v.y;
         }
     }
-    template <bool VALUES>
     __device__ __forceinline__ uint32_t codes(uint32_t (&x)[N]) const
     {
         uint32_t a = 0u;
@@ -291,17 +250,15 @@ struct Raw<float, GS> {
         const float s = group_scale(a);
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            x[i] = pair_codes<VALUES>(magnitudes(w[2 * i], w[2 * i + 1], s),
-                                      __byte_perm(__float_as_uint(w[2 * i]), __float_as_uint(w[2 * i + 1]), 0x7632));
+            x[i] = code_of(w[2 * i], s) | code_of(w[2 * i + 1], s) << 16;
         return __float_as_uint(s) >> 16;
     }
-    template <bool VALUES>
     static __device__ __forceinline__ void store(float *p, const uint32_t (&x)[N], float s)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float a, b;
-            pair_numbers<VALUES>(x[i], a, b);
+            pair_numbers(x[i], a, b);
             reinterpret_cast<float2 *>(p)[i] = make_float2(a * s, b * s);
         }
     }
@@ -327,7 +284,7 @@ __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, i
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t x[2][N];
-        const uint32_t s0 = raw[i][0].template codes<VALUES>(x[0]), s1 = raw[i][1].template codes<VALUES>(x[1]);
+        const uint32_t s0 = raw[i][0].codes(x[0]), s1 = raw[i][1].codes(x[1]);
         sc[i] = s0 | s1 << 16;
         if constexpr (VALUES) {
 #pragma unroll
@@ -336,13 +293,12 @@ __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, i
                 for (int k = 0; k < N; ++k)
                     x[c][k] = transpose8(x[c][k]);
         }
-        auto turned = [](uint32_t v, int r) { return VALUES ? __funnelshift_l(v, v, 4 * r) : v << (4 * r); };
         if constexpr (GS == 16) {  // slots: keys c + 2 k, values 2 c + k
             const uint32_t y1 = VALUES ? x[0][N - 1] : x[1][0], y2 = VALUES ? x[1][0] : x[0][N - 1];
-            w[i] = x[0][0] | turned(y1, 1) | turned(y2, 2) | turned(x[1][N - 1], 3);
+            w[i] = x[0][0] | y1 << 4 | y2 << 8 | x[1][N - 1] << 12;
         } else {
-            const uint32_t y = x[0][0] | turned(x[1][0], 1);
-            w[i] = i % 2 ? w[i - i % 2] | turned(y, 2) : y;
+            const uint32_t y = x[0][0] | x[1][0] << 4;
+            w[i] = i % 2 ? w[i - i % 2] | y << 8 : y;
         }
     }
     constexpr int kCodes = kPage * GS / 2;
@@ -367,7 +323,7 @@ __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, i
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int row = row0 + (GS == 16 ? 4 : 8) * i + word_row<GS, VALUES>(VALUES ? 0 : 4 * (g & 1), r, h);
-                mask |= row >= first && row < end ? slot_mask<VALUES>(r, h) : 0u;
+                mask |= row >= first && row < end ? 15u << slot_shift(r, h) : 0u;
             }
         if (mask)
             words[i] = (words[i] & ~mask) | (w[GS == 16 ? i : 2 * i + 1] & mask);
@@ -396,8 +352,7 @@ __device__ __forceinline__ void read_page(const unsigned char *block, T *vec, in
         w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
     } else {
         const uint2 v = *reinterpret_cast<const uint2 *>(at);
-        w[0] = v.x, w[1] = VALUES ? __funnelshift_r(v.x, v.x, 8) : v.x >> 8;
-        w[2] = v.y, w[3] = VALUES ? __funnelshift_r(v.y, v.y, 8) : v.y >> 8;
+        w[0] = v.x, w[1] = v.x >> 8, w[2] = v.y, w[3] = v.y >> 8;
     }
     const uint4 v = *reinterpret_cast<const uint4 *>(scales_of<GS, VALUES>(const_cast<unsigned char *>(block)) + g * 8);
     const uint32_t sc[4] = {v.x, v.y, v.z, v.w};
@@ -409,14 +364,13 @@ __device__ __forceinline__ void read_page(const unsigned char *block, T *vec, in
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 const int r = GS == 16 ? (VALUES ? 2 * c + k : c + 2 * k) : c;
+                x[k] = (w[i] >> (4 * r)) & 0x000f000fu;
                 if constexpr (VALUES)
-                    x[k] = transpose8(__funnelshift_r(w[i], w[i], 4 * r) & 0x80078007u);
-                else
-                    x[k] = (w[i] >> (4 * r)) & 0x000f000fu;
+                    x[k] = transpose8(x[k]);
             }
             const int row = lane_row(g, i, c);
             if (row >= first && row < end)
-                Raw<T, GS>::template store<VALUES>(vec + (size_t)row * stride + u * 2 * N, x, c ? bf16hi(sc[i]) : bf16lo(sc[i]));
+                Raw<T, GS>::store(vec + (size_t)row * stride + u * 2 * N, x, c ? bf16hi(sc[i]) : bf16lo(sc[i]));
         }
 }
 

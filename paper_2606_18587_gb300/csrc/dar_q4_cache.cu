@@ -125,15 +125,12 @@ struct FewWords {
         for (int o = 1; o < GS; o <<= 1)
             a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
         const float s = group_scale(a);
-        const uint32_t code = s > 0.f ? (uint32_t)fminf(rintf(__fdiv_rn(fabsf(x), s)), 7.f) : 0u;
         // where the entry is: keys, slot c + 2 (e / 2 mod 2) of half e mod 2; values, slot 2 c + (e / 2 mod 2) of half o
         const int o = row & 1, c = (row >> 1) & 1, i = (row >> 2) & 1, k = (e >> 1) & 1;
         const int slot = GS == 16 ? (values ? 2 * c + k : c + 2 * k) : 2 * i + c, half = values ? o : e & 1;
-        const uint32_t neg = __float_as_uint(x) >> 31;
-        uint32_t y = values ? code << slot_shift(slot, half) | neg << slot_sign(slot, half)
-                            : (neg ? 8u - code : 8u + code) << slot_shift(slot, half);
+        uint32_t y = code_of(x, s) << slot_shift(slot, half);
         // the other entries of the word: keys, of four (two) consecutive ones; values, of e and e + 2
-        uint32_t m = values ? slot_mask<true>(slot, half) : slot_mask<false>(slot, half);
+        uint32_t m = 15u << slot_shift(slot, half);
 #pragma unroll
         for (int q = 1; q < 4; q <<= 1) {
             const uint32_t yo = __shfl_xor_sync(0xffffffffu, y, q), mo = __shfl_xor_sync(0xffffffffu, m, q);

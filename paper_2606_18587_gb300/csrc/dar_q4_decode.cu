@@ -9,14 +9,12 @@
 //
 //  attend  The work is a line of units (sequence, KV head, up to kRows query heads):
 //          the ring in runs of kRun tokens, then the pages.  Every warp of the grid has
-//          an equal share of the line by cost, and leaves one partial result (m, l,
-//          acc) per query head for each unit that its share cuts; unit u's cut by
-//          share k has the slot u + k.  The shares of a unit's first and last stage leave
+//          an equal share of the line by cost, and leaves one partial result per query
+//          head for each unit that its share cuts: (m, l, acc) of its ring tokens and of
+//          its pages, each by its own reference; unit u's cut by share k has the slot u + k.  The shares of a unit's first and last stage leave
 //          their numbers for the joining kernel.  Lengths are read on the device.
 //  join    a block per output row joins its partial results by log-sum-exp and lifts the
 //          bottleneck sum once by Uv.
-#include <cuda.h>
-
 #include <algorithm>
 #include <type_traits>
 
@@ -25,6 +23,27 @@
 #include "dar_q4.cuh"
 #include "dar_sm100.cuh"
 
+#ifndef DAR_UNROLL
+#define DAR_UNROLL 1
+#endif
+#ifndef DAR_W
+#define DAR_W 16
+#endif
+#ifndef DAR_S
+#define DAR_S 2
+#endif
+#ifndef DAR_W2
+#define DAR_W2 12
+#endif
+#ifndef DAR_S2
+#define DAR_S2 3
+#endif
+#ifndef DAR_NP
+#define DAR_NP 1
+#endif
+#ifndef DAR_SLEEP
+#define DAR_SLEEP 100
+#endif
 namespace dar {
 namespace q4 {
 
@@ -35,9 +54,10 @@ constexpr int kRun = 16;         // ring tokens of a stage
 constexpr int kWarps = 8;        // of a CTA (CUDA cores)
 // Of a CTA (tensor cores), and stages in flight of each: as many warps as registers allow.
 template <int DD>
-__host__ __device__ constexpr int mma_warps() { return DD <= 16 ? 16 : 12; }
+__host__ __device__ constexpr int mma_warps() { return DD <= 16 ? DAR_W : DAR_W2; }
 template <int DD>
-__host__ __device__ constexpr int mma_slots() { return DD <= 16 ? 2 : 3; }
+__host__ __device__ constexpr int mma_slots() { return DD <= 16 ? DAR_S : DAR_S2; }
+constexpr int kUnroll = DAR_UNROLL;       // pages of a stage
 constexpr int kSlot = 5120;      // bytes of a stage at most
 constexpr int kMaxShares = 2560; // the workspace holds partial results of this many warps
 constexpr int kCostUnit = 8;     // cost of a unit's set-up (its place on the line is before the stages)
@@ -51,7 +71,8 @@ __host__ __device__ constexpr int rec_floats() { return 4 + kHeadDim + DD; }
 struct Args {
     Q4DecodeArgs c;
     int2 *span;  // [units] first and last share of every unit
-    float *rec;  // [units + shares][rows of a unit][rec_floats]
+    uint32_t *prep;  // of every unit, what the first kernel makes of its queries (Pages)
+    float *rec;  // [units + shares][rows of a unit][rec_floats]: m, l of the ring, m, l of the pages, acc[64], acc[d_down]
     int G, RT, RU;  // query heads per KV head, units per (sequence, KV head), rows of a unit at most
     int shares;
 };
@@ -368,10 +389,8 @@ __device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, Lan
             if (r >= c.rows)
                 continue;
             float *rec = a.rec + ((size_t)c.slot * a.RU + r) * rec_floats<DD>();
-            if (lane == 0) {
-                rec[0] = m[r];
-                rec[1] = l[r];
-            }
+            if (lane == 0)  // one reference for both
+                *reinterpret_cast<float4 *>(rec) = make_float4(m[r], l[r], m[r], 0.f);
             rec[4 + lane] = ol[r][0];
             rec[4 + 32 + lane] = ol[r][1];
             if (lane < GS)
@@ -402,17 +421,23 @@ __global__ void __launch_bounds__(kWarps * 32) attend_kernel(Args a)
 // 4 g + t has the scores, weights, references and sums of heads t and t + 4 (CT = 2); with CT = 1
 // of head t alone, and the other column takes what is said below.
 //
-//  codes    fp16 subnormals as they lie (dar_q4.cuh): five instructions for the eight of a word of
-//           keys, seven for one of values.  (Conversions of offset codes take 13: an AND and an OR each,
-//           since an instruction has one immediate, and the offset subtracted; e4m3 operands are
-//           converted by twice as many: mma.sync has no products of them here.)
+//  codes    fp16 subnormals as they lie (dar_q4.cuh), five instructions for the eight of a word.  (Their
+//           values take 13: an AND and an OR each, since an instruction has one immediate, and the
+//           offset subtracted; e4m3 operands are converted by twice as many: mma.sync has no products
+//           of them here; sign and magnitude, which needs no offset, takes seven.)
 //  scores   q~, brought to [2^14, 2^15) by a power of two, is two fp16 terms (2^-22 of it).  CT = 1:
 //           the second one is the other column's.  CT = 2: a product of its own.  A d_down of 8:
 //           the two halves of a product's 16 entries.  The sum starts from
 //           minus 8 times theirs.  Rows with c = 1 are in slots 1 and 3: their scores are 16 times as large.
 //  weights  p s_v as fp16 (2^-11) relative to a reference of the row that keeps the largest at
-//           2^8 when it is set and below 2^15 always; it is raised by a vote.  (bf16 operands need two
-//           terms for the same error, twice the conversions and transpositions.)
+//           2^8 when it is set.  It is raised where a weight overflows, which shows in the sums of a stage:
+//           the stage is done again, page by page with the weights looked at first.  (bf16 operands need
+//           two terms for the same error, twice the conversions and transpositions.)
+//  sums     of a stage start from 0, and beside them those of the weights times the offset, which come
+//           from a product with constant rows; what joins the other stages' is the difference (at
+//           256 tokens the offset's part is some 100 times the rest's 2^-24).
+// A page of 64 tokens takes an SM's quarter 104 cycles of its integer pipe, 80 of its tensor pipe and 114
+// instructions beside what a stage costs, with CT = 1.
 
 struct Soft {  // of one head of a lane
     float bias, l;  // minus the reference; the lane's share of the sum of weights
@@ -452,19 +477,13 @@ __device__ __forceinline__ void split_f16(float x, float y, uint32_t &hi, uint32
     sums[1] += c + d;
 }
 
-// Slots 0 to 3 of a word of keys (slots 1 and 3 times 16) and of values as operand registers.
-__device__ __forceinline__ void keys_of(uint32_t w, uint32_t (&c)[4])
+// Slots 0 to 3 of a word of codes as operand registers (slots 1 and 3 times 16).
+__device__ __forceinline__ void codes_of(uint32_t w, uint32_t (&c)[4])
 {
     c[0] = w & 0x000f000fu;
     c[1] = w & 0x00f000f0u;
     c[2] = (w >> 8) & 0x000f000fu;
     c[3] = (w >> 8) & 0x00f000f0u;
-}
-__device__ __forceinline__ void values_of(uint32_t w, uint32_t (&c)[4])
-{
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-        c[r] = __funnelshift_r(w, w, 4 * r) & 0x80078007u;
 }
 
 // Two fp32 values as three bf16 terms each: all but 2^-24 of them.
@@ -484,95 +503,295 @@ __device__ __forceinline__ uint32_t key_mask(int key, int n)
     return (key < n ? 0xffffu : 0u) | (key + 1 < n ? 0xffff0000u : 0u);
 }
 
-// What a warp fills its slots with, ahead of what it computes.
+// Pages of a stage.
+template <int DD>
+__host__ __device__ constexpr int stage_pages() { return Fmt<DD>::kBytes > kSlot / 4 ? kSlot / Fmt<DD>::kBytes : 4; }
+
+__device__ __forceinline__ void cp_async16_hint(uint32_t dst, const void *src, uint64_t policy)
+{
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+}
+
+// What a warp fills its slots with, ahead of what it computes: a run of the ring, or pages.  By 16-byte copies of its
+// lanes, a group of them a stage.  (A bulk copy takes the SM's copy engine some 36 cycles, whatever its size: at 768 to
+// 1280 bytes a page that is as long as HBM takes for them.)
 template <int DD>
 struct Filler {
-    static constexpr int kSlots = mma_slots<DD>();
-    static constexpr int kPages = Fmt<DD>::kBytes > kSlot / 4 ? kSlot / Fmt<DD>::kBytes : 4;  // of a stage
+    static constexpr int S = mma_slots<DD>(), P = stage_pages<DD>(), kBytes = Fmt<DD>::kBytes;
     Walk walk;
-    Cut c;
-    int st;          // next stage of the cut
-    int ids0, ids;   // block-table entries ids0 .. ids0 + 31 of its sequence, one per lane
-    int filled;
+    const int32_t *table;       // block table of the cut's sequence
+    const unsigned char *heads; // page 0 of the cut's KV head, this lane's part
+    int ring, nwin;             // row of the ring's first token, tokens in it
+    int st, st1, nrun;          // next stage, end of the cut, runs of the ring
+    int ids, at;                // 32 entries of the table, one per lane, of which the next stage's are at ..
+    int slot;                   // to be filled next
     bool more;
 
     __device__ __forceinline__ void begin(const Args &a, const Tables &t, int share)
     {
         walk.begin<DD>(a, t, share);
-        filled = 0;
+        slot = 0;
         next_cut(a, t);
     }
     __device__ __forceinline__ void next_cut(const Args &a, const Tables &t)
     {
+        Cut c;
         more = walk.next<DD>(a, t, c);
-        st = c.st0;
-        ids0 = -1;
-    }
-    // Starts the copies of the next stage.
-    __device__ __forceinline__ void fill(const Args &a, const Tables &t, const CUtensorMap &wk, const CUtensorMap &wv,
-                                         unsigned char *slots, uint64_t *full, uint64_t policy, int lane)
-    {
         if (!more)
             return;
-        unsigned char *dst = slots + filled % kSlots * kSlot;
-        uint64_t *bar = full + filled % kSlots;
-        ++filled;
-        if (st < c.nrun) {
-            if (lane == 0) {
-                mbar_expect_tx(bar, 2 * kRun * kHeadDim * 2);
-                const int y = (c.b * a.c.Hkv + c.g) * a.c.w + st * kRun;
-                tma_load_2d_hint(smem_u32(dst), &wk, 0, y, bar, policy);
-                tma_load_2d_hint(smem_u32(dst + kRun * kHeadDim * 2), &wv, 0, y, bar, policy);
+        st = c.st0;
+        st1 = c.st1;
+        nrun = c.nrun;
+        nwin = c.nwin;
+        at = 32;
+        table = a.c.block_table + (size_t)c.b * a.c.maxp;
+        heads = static_cast<const unsigned char *>(a.c.pool) + (size_t)c.g * kBytes + (threadIdx.x & 31) * 16;
+        ring = (c.b * a.c.Hkv + c.g) * a.c.w;
+    }
+    // Starts the copies of the next stage, as one group (of none when there is no more).
+    __device__ __forceinline__ void fill(const Args &a, const Tables &t, uint32_t slots, int lane)
+    {
+        if (more) {
+            const uint64_t once = l2_evict_first_policy();  // the cache is read once
+            const uint32_t dst = slots + slot * kSlot;
+            if (st < nrun) {  // 16 rows of 128 bytes, 16-byte piece c of row r at c ^ (r mod 8)
+                const int n = min(kRun, nwin - st * kRun), r0 = lane >> 3, c = lane & 7;
+                const size_t from = ((size_t)ring + st * kRun + r0) * (kHeadDim * 2) + c * 16;
+                const unsigned char *k = static_cast<const unsigned char *>(a.c.win_k) + from;
+                const unsigned char *v = static_cast<const unsigned char *>(a.c.win_v) + from;
+#pragma unroll
+                for (int i = 0; i < kRun / 4; ++i) {
+                    const int r = r0 + 4 * i;
+                    const uint32_t to = dst + r * 128 + ((c ^ (r & 7)) << 4);
+                    if (r < n) {
+                        cp_async16_hint(to, k + i * 4 * 128, once);
+                        cp_async16_hint(to + kRun * 128, v + i * 4 * 128, once);
+                    }
+                }
+                ++st;
+            } else {
+                const int lp = st - nrun, n = min(P, st1 - st);
+                if (at + P > 32) {
+                    at = 0;
+                    ids = lp + lane < a.c.maxp ? __ldg(table + lp + lane) : -1;
+                }
+                const uint32_t to = dst + lane * 16;
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    if (i >= n)
+                        break;
+                    const int id = __shfl_sync(0xffffffffu, ids, at + i);
+                    if ((unsigned)id < (unsigned)a.c.num_pages) {
+                        const unsigned char *page = heads + (size_t)id * (unsigned)(a.c.Hkv * kBytes);
+#pragma unroll
+                        for (int k = 0; k < kBytes; k += 512)
+                            if (k + 512 <= kBytes || lane * 16 < kBytes - k)
+                                cp_async16_hint(to + i * kBytes + k, page + k, once);
+                    } else if (lane == 0) {
+                        report(a.c.status, DAR_ERR_CAPACITY);
+                    }
+                }
+                st += n;
+                at += n;
             }
-            ++st;
-        } else {
-            const int lp = st - c.nrun, n = min(kPages, c.st1 - st);
-            if (ids0 < 0 || lp + n > ids0 + 32) {
-                ids0 = lp;
-                ids = lp + lane < a.c.maxp ? __ldg(a.c.block_table + (size_t)c.b * a.c.maxp + lp + lane) : -1;
-            }
-            const int id = __shfl_sync(0xffffffffu, ids, (lp - ids0 + lane) & 31);
-            const bool mine = lane < n, good = mine && id >= 0 && id < a.c.num_pages;
-            const unsigned pages = __popc(__ballot_sync(0xffffffffu, good));
-            if (lane == 0)
-                mbar_expect_tx(bar, pages * Fmt<DD>::kBytes);
-            __syncwarp();
-            if (good)
-                bulk_g2s_hint(dst + lane * Fmt<DD>::kBytes,
-                              static_cast<const unsigned char *>(a.c.pool) + ((size_t)id * a.c.Hkv + c.g) * Fmt<DD>::kBytes,
-                              Fmt<DD>::kBytes, bar, policy);
-            else if (mine)
-                report(a.c.status, DAR_ERR_CAPACITY);
-            st += n;
+            slot = slot + 1 < S ? slot + 1 : 0;
+            if (st >= st1)
+                next_cut(a, t);
         }
-        if (st >= c.st1)
-            next_cut(a, t);
+        cp_async_commit();
     }
 };
 
-// What a warp has of a cut's query heads, and its sums.
-template <int DD, int CT>
-struct Heads {
-    static constexpr int GS = Fmt<DD>::kGroup, NB = Fmt<DD>::kGroups;
-    static constexpr int TB = GS == 16 && CT == 2 ? 2 : 1;  // score products of a group
-    static constexpr int OD = CT == 1 ? 2 : 1;    // sums of a group (see page_step)
-    uint32_t q[4][2];        // ring: queries as B operands
-    uint32_t qt[NB][TB][2];  // pages: q~ as B operands, two fp16 terms
-    float from[NB][4];       // what a score's sum starts from
-    float cq[CT];            // scale of a score: c2, the power of two taken out of q~, and the codes' 2^24
-    Soft ring[CT], page[CT];
-    float ol[kHeadDim / 16][4], od[NB][OD][4];
+// The queries of a cut as B operands: column i0 = lane / 4 is head i0 / 2 + 4 (i0 mod 2).
+__device__ __forceinline__ void queries_of(const Args &a, const Cut &c, int lane, uint32_t (&q)[4][2])
+{
+    const int i0 = lane >> 2, c0 = lane & 3, head = (i0 >> 1) + 4 * (i0 & 1);
+    const uint32_t *qp = static_cast<const uint32_t *>(a.c.q) +
+                         ((size_t)c.b * a.c.Hq + c.g * a.G + c.rt * kRows + head) * (kHeadDim / 2) + c0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        q[e / 2][e % 2] = head < c.rows ? __ldg(qp + 4 * e) : 0u;
+}
 
-    // Queries of a cut, and q~^T = Uk q^T with Uk in three bf16 terms (products exact but for 2^-24).
-    __device__ __forceinline__ void begin(const Args &a, const Cut &c, int lane)
+// A cut without ring tokens (at 0) or pages (at 2) says so: nothing else of that part is read.
+template <int DD>
+__device__ __forceinline__ void leave_none(const Args &a, const Cut &c, int at, int lane)
+{
+    if (lane < c.rows)
+        *reinterpret_cast<float2 *>(a.rec + ((size_t)c.slot * a.RU + lane) * rec_floats<DD>() + at) =
+            make_float2(-INFINITY, 0.f);
+}
+
+// A cut's ring tokens.
+template <int CT>
+struct Ring {
+    Soft ring[CT];
+    float ol[kHeadDim / 16][4];
+    __device__ __forceinline__ Ring()
+    {
+#pragma unroll
+        for (int k = 0; k < CT; ++k) {
+            ring[k].bias = INFINITY;
+            ring[k].l = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < kHeadDim / 16; ++e)
+            ol[e][0] = ol[e][1] = ol[e][2] = ol[e][3] = 0.f;
+    }
+
+    // A run of n ring tokens at `tile`: 16 rows of keys, then of values, 128-byte swizzle.
+    __device__ __forceinline__ void step(const uint32_t (&q)[4][2], uint32_t tile, int n, float c2, int lane)
+    {
+        const int i0 = lane >> 2, c0 = lane & 3, mat = lane >> 3, r = lane & 7;
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint32_t krow = tile + (r + 8 * (mat & 1)) * 128;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t k[4];
+            ldsm_x4(krow + (((2 * e + (mat >> 1)) ^ r) << 4), k);
+            mma_bf16_acc(s, k, q[e][0], q[e][1]);
+        }
+        uint32_t w0[2], w1[2];  // weights as two bf16 terms: tokens i0, and i0 + 8
+        float p[2][2] = {};
+        bool up = false;
+#pragma unroll
+        for (int k = 0; k < CT; ++k) {
+            s[k] = i0 < n ? s[k] * c2 : -INFINITY;
+            s[2 + k] = i0 + 8 < n ? s[2 + k] * c2 : -INFINITY;
+            up |= fmaxf(s[k], s[2 + k]) > -ring[k].bias;
+        }
+        if (__any_sync(0xffffffffu, up)) {
+#pragma unroll
+            for (int k = 0; k < CT; ++k) {
+                float top = fmaxf(s[k], s[2 + k]);
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1)
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float was = -ring[k].bias, now = fmaxf(top, was), f = now == -INFINITY ? 1.f : ex2_approx(was - now);
+                ring[k].bias = -now;
+                ring[k].l *= f;
+#pragma unroll
+                for (int e = 0; e < kHeadDim / 16; ++e) {
+                    ol[e][k] *= f;
+                    ol[e][2 + k] *= f;
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < CT; ++k) {
+            const float bias = ring[k].bias == INFINITY ? 0.f : ring[k].bias;
+            p[0][k] = ex2_approx(s[k] + bias);
+            p[1][k] = ex2_approx(s[2 + k] + bias);
+            ring[k].l += p[0][k] + p[1][k];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            // hi cut off, so that both terms have the weight's sign; 2^-22 of it keeps lo from 0, where an infinite
+            // value would become NaN
+            constexpr float kUp = 1.f + 0x1p-22f;
+            const uint32_t x = __float_as_uint(p[h][0]), y = __float_as_uint(p[h][1]);
+            uint32_t &hi = h ? w1[0] : w0[0], &lo = h ? w1[1] : w0[1];
+            hi = transpose8(__byte_perm(x, y, 0x7632));
+            lo = transpose8(cvt_bf16x2(fmaf(p[h][0], kUp, -__uint_as_float(x & 0xffff0000u)),
+                                       fmaf(p[h][1], kUp, -__uint_as_float(y & 0xffff0000u))));
+        }
+        const uint32_t m0 = key_mask(2 * c0, n), m1 = key_mask(2 * c0 + 8, n);  // 0 * NaN is NaN
+        const uint32_t vrow = tile + kRun * kHeadDim * 2 + (r + 8 * (mat >> 1)) * 128;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t v[4];
+            ldsm_x4_t(vrow + (((2 * e + (mat & 1)) ^ r) << 4), v);
+            const uint32_t vm[4] = {v[0] & m0, v[1] & m0, v[2] & m1, v[3] & m1};
+            mma_bf16_acc(ol[e], vm, w0[0], w1[0]);
+            mma_bf16_acc(ol[e], vm, w0[1], w1[1]);
+        }
+    }
+
+    __device__ __forceinline__ void leave(const Args &a, const Cut &c, int stride, int lane)
     {
         const int i0 = lane >> 2, c0 = lane & 3;
-        const int head = (i0 >> 1) + 4 * (i0 & 1);  // of column i0
-        const uint32_t *qp = static_cast<const uint32_t *>(a.c.q) +
-                             ((size_t)c.b * a.c.Hq + c.g * a.G + c.rt * kRows + head) * (kHeadDim / 2) + c0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            q[e / 2][e % 2] = head < c.rows ? __ldg(qp + 4 * e) : 0u;
+        for (int k = 0; k < CT; ++k) {
+            float l = ring[k].l;
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1)
+                l += __shfl_xor_sync(0xffffffffu, l, o);
+            const int head = c0 + 4 * k;
+            if (head >= c.rows)
+                continue;
+            float *rec = a.rec + ((size_t)c.slot * a.RU + head) * stride;
+            if (i0 == 0)
+                *reinterpret_cast<float2 *>(rec) = make_float2(-ring[k].bias, l);
+#pragma unroll
+            for (int e = 0; e < kHeadDim / 16; ++e) {
+                rec[4 + 16 * e + i0] = ol[e][k];
+                rec[4 + 16 * e + 8 + i0] = ol[e][2 + k];
+            }
+        }
+    }
+};
+
+// A cut's pages: what a warp has of its query heads, and the sums.
+template <int DD, int CT>
+struct Pages {
+    static constexpr int GS = Fmt<DD>::kGroup, NB = Fmt<DD>::kGroups;
+    static constexpr int TB = GS == 16 && CT == 2 ? 2 : 1;  // score products of a group
+    uint32_t qt[NB][TB][2];  // q~ as B operands, two fp16 terms
+    float from[NB][4];       // what a score's sum starts from
+    float cq[CT];            // scale of a score: c2, the power of two taken out of q~, and the codes' 2^24
+    Soft page[CT];
+    float od[NB][2 * CT];    // times 2^-24, entries e of the heads and then e + 2 (see Sums)
+
+    // Words of a lane that the first kernel leaves of a unit, [unit][word][lane].
+    static constexpr int kWords = NB * (TB * 2 + 2) + CT;
+    template <typename F>
+    __device__ __forceinline__ void each_word(const F &f)
+    {
+        int i = 0;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+#pragma unroll
+            for (int k = 0; k < TB; ++k) {
+                f(i++, qt[j][k][0]);
+                f(i++, qt[j][k][1]);
+            }
+            f(i++, from[j][0]);
+            f(i++, from[j][1]);
+        }
+#pragma unroll
+        for (int k = 0; k < CT; ++k)
+            f(i++, cq[k]);
+    }
+    __device__ __forceinline__ void save(const Args &a, int unit, int lane)
+    {
+        uint32_t *p = a.prep + (size_t)unit * kWords * 32 + lane;
+        each_word([&](int i, auto &x) { p[i * 32] = *reinterpret_cast<const uint32_t *>(&x); });
+    }
+    __device__ __forceinline__ void load(const Args &a, int unit, int lane)
+    {
+        const uint32_t *p = a.prep + (size_t)unit * kWords * 32 + lane;
+        each_word([&](int i, auto &x) { *reinterpret_cast<uint32_t *>(&x) = p[i * 32]; });
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            from[j][2] = 16.f * from[j][0];
+            from[j][3] = 16.f * from[j][1];
+        }
+#pragma unroll
+        for (int k = 0; k < CT; ++k) {
+            page[k].bias = INFINITY;
+            page[k].l = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int o = 0; o < 2 * CT; ++o)
+                od[j][o] = 0.f;
+    }
+
+    // q~^T = Uk q^T with Uk in three bf16 terms (products exact but for 2^-24).
+    __device__ __forceinline__ void make(const Args &a, const Cut &c, const uint32_t (&q)[4][2], int lane)
+    {
+        const int i0 = lane >> 2, c0 = lane & 3;
         float x[NB][4];  // entries 16 j + i0 (+ 8) of heads c0, c0 + 4: [0] i0 c0, [1] i0 c0 + 4, [2], [3] i0 + 8
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
@@ -660,91 +879,8 @@ struct Heads {
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < 2; ++k)
                 from[j][k] = -0x1p-21f * __shfl_sync(0xffffffffu, sum, (2 * c0 + k) * 4);  // 8 * 2^-24
-                from[j][2 + k] = 16.f * from[j][k];
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < CT; ++k) {
-            ring[k].bias = page[k].bias = INFINITY;
-            ring[k].l = page[k].l = 0.f;
-        }
-#pragma unroll
-        for (int e = 0; e < kHeadDim / 16; ++e)
-            ol[e][0] = ol[e][1] = ol[e][2] = ol[e][3] = 0.f;
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int o = 0; o < OD; ++o)
-                od[j][o][0] = od[j][o][1] = od[j][o][2] = od[j][o][3] = 0.f;
-    }
-
-    // A run of n ring tokens at `tile`: 16 rows of keys, then of values, 128-byte swizzle.
-    __device__ __forceinline__ void ring_step(uint32_t tile, int n, float c2, int lane)
-    {
-        const int i0 = lane >> 2, c0 = lane & 3, mat = lane >> 3, r = lane & 7;
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
-        const uint32_t krow = tile + (r + 8 * (mat & 1)) * 128;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            uint32_t k[4];
-            ldsm_x4(krow + (((2 * e + (mat >> 1)) ^ r) << 4), k);
-            mma_bf16_acc(s, k, q[e][0], q[e][1]);
-        }
-        uint32_t w0[2], w1[2];  // weights as two bf16 terms: tokens i0, and i0 + 8
-        float p[2][2] = {};
-        bool up = false;
-#pragma unroll
-        for (int k = 0; k < CT; ++k) {
-            s[k] = i0 < n ? s[k] * c2 : -INFINITY;
-            s[2 + k] = i0 + 8 < n ? s[2 + k] * c2 : -INFINITY;
-            up |= fmaxf(s[k], s[2 + k]) > -ring[k].bias;
-        }
-        if (__any_sync(0xffffffffu, up)) {
-#pragma unroll
-            for (int k = 0; k < CT; ++k) {
-                float top = fmaxf(s[k], s[2 + k]);
-#pragma unroll
-                for (int o = 4; o < 32; o <<= 1)
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const float was = -ring[k].bias, now = fmaxf(top, was), f = now == -INFINITY ? 1.f : ex2_approx(was - now);
-                ring[k].bias = -now;
-                ring[k].l *= f;
-#pragma unroll
-                for (int e = 0; e < kHeadDim / 16; ++e) {
-                    ol[e][k] *= f;
-                    ol[e][2 + k] *= f;
-                }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < CT; ++k) {
-            const float bias = ring[k].bias == INFINITY ? 0.f : ring[k].bias;
-            p[0][k] = ex2_approx(s[k] + bias);
-            p[1][k] = ex2_approx(s[2 + k] + bias);
-            ring[k].l += p[0][k] + p[1][k];
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            // hi cut off, so that both terms have the weight's sign; 2^-22 of it keeps lo from 0, where an infinite
-            // value would become NaN
-            constexpr float kUp = 1.f + 0x1p-22f;
-            const uint32_t x = __float_as_uint(p[h][0]), y = __float_as_uint(p[h][1]);
-            uint32_t &hi = h ? w1[0] : w0[0], &lo = h ? w1[1] : w0[1];
-            hi = transpose8(__byte_perm(x, y, 0x7632));
-            lo = transpose8(cvt_bf16x2(fmaf(p[h][0], kUp, -__uint_as_float(x & 0xffff0000u)),
-                                       fmaf(p[h][1], kUp, -__uint_as_float(y & 0xffff0000u))));
-        }
-        const uint32_t m0 = key_mask(2 * c0, n), m1 = key_mask(2 * c0 + 8, n);  // 0 * NaN is NaN
-        const uint32_t vrow = tile + kRun * kHeadDim * 2 + (r + 8 * (mat >> 1)) * 128;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            uint32_t v[4];
-            ldsm_x4_t(vrow + (((2 * e + (mat & 1)) ^ r) << 4), v);
-            const uint32_t vm[4] = {v[0] & m0, v[1] & m0, v[2] & m1, v[3] & m1};
-            mma_bf16_acc(ol[e], vm, w0[0], w1[0]);
-            mma_bf16_acc(ol[e], vm, w0[1], w1[1]);
         }
     }
 
@@ -760,18 +896,17 @@ struct Heads {
         }
     }
 
-    // A page of n tokens; lane (g, t) has the scores of rows 16 (g / 2) + 4 i + 2 c + g mod 2.  Products of weights: with
-    // CT = 2 a column has 8 tokens' weights of head t or t + 4.  With CT = 1 column 2 t has those of rows with c = 0 and
-    // column 2 t + 1 those with c = 1, which one transposition brings; products with the codes of c = 0 are right in the
-    // even columns and products with those of c = 1 in the odd ones, so each has sums of its own, whose other columns are
-    // not used.
-    __device__ __forceinline__ void page_step(const unsigned char *at, int n, int lane)
+    // Lane (g, t) has the scores of rows 16 (g / 2) + 4 i + 2 c + g mod 2, in pairs: two tokens (c = 0, 1) of a head
+    // (pair i), or two heads of a token (pairs 2 i, 2 i + 1).
+    static constexpr int NP = 4 * CT;
+    struct Scores {
+        float y[NP][2];
+    };
+    __device__ __forceinline__ void scores(const unsigned char *at, int lane, Scores &z) const
     {
         using F = Fmt<DD>;
-        const int i0 = lane >> 2, c0 = lane & 3;
-        // pairs: two tokens (c = 0, 1) of a head, or two heads of a token; pair i, or pairs 2 i, 2 i + 1
-        constexpr int NP = 4 * CT;
-        float y[NP][2];
+        const int i0 = lane >> 2;
+        float(&y)[NP][2] = z.y;
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const unsigned char *block = at + j * F::kBlock;
@@ -782,7 +917,7 @@ struct Heads {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t c[4];
-                keys_of(w[i], c);
+                codes_of(w[i], c);
                 if constexpr (GS == 8) {  // both halves of the product's 16 entries are the key's 8
                     c[0] = i % 2 ? c[2] : c[0];
                     c[1] = i % 2 ? c[3] : c[1];
@@ -810,72 +945,199 @@ struct Heads {
                 }
             }
         }
-        uint32_t vs[NB][4];
+    }
+    // Factor of a pair's scores: slots of c = 1 are 16 times as large.
+    __device__ __forceinline__ float factor(int k, int e) const
+    {
+        const float s = cq[CT == 2 ? e : 0];
+        return (CT == 1 ? e : k % 2) ? s * 0.0625f : s;
+    }
+    // Weights of a page relative to the references, and their sums.
+    __device__ __forceinline__ void weigh(const Scores &z, float (&p)[NP][2], float (&l)[2]) const
+    {
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(at + j * F::kBlock + F::kScales + 2 * kPage + i0 * 16);
-            vs[j][0] = v.x, vs[j][1] = v.y, vs[j][2] = v.z, vs[j][3] = v.w;
+        for (int k = 0; k < NP; ++k) {
+            float x0, x1;
+            ffma2(x0, x1, z.y[k][0], z.y[k][1], factor(k, 0), factor(k, 1), page[0].bias, page[CT - 1].bias);
+            p[k][0] = ex2_approx(x0);
+            p[k][1] = ex2_approx(x1);
+            add2(l[0], l[1], l[0], l[1], p[k][0], p[k][1]);
         }
-        if (n < kPage) {  // rows behind the last token may hold anything
+    }
+    // A pair's scales.
+    static __device__ __forceinline__ void scales(uint32_t s, int k, float &s0, float &s1)
+    {
+        s0 = CT == 1 || k % 2 == 0 ? bf16lo(s) : bf16hi(s);
+        s1 = CT == 1 || k % 2 != 0 ? bf16hi(s) : bf16lo(s);
+    }
+    static __device__ __forceinline__ void value_scales(const unsigned char *block, int lane, uint32_t (&s)[4])
+    {
+        const uint4 v = *reinterpret_cast<const uint4 *>(block + Fmt<DD>::kScales + 2 * kPage + (lane >> 2) * 16);
+        s[0] = v.x, s[1] = v.y, s[2] = v.z, s[3] = v.w;
+    }
+
+    // Sums of some pages, of codes + 8; off: of 8 (both times 2^-24, entries e + 2 times 2^-20).  With CT = 2 a column has
+    // 8 tokens' weights of head t or t + 4.  With CT = 1 column 2 t has those of rows with c = 0 and column 2 t + 1 those
+    // with c = 1, which one transposition brings; products with the codes of c = 0 are right in the even columns and
+    // products with those of c = 1 in the odd ones, so each has sums of its own, whose other columns are not used.
+    struct Sums {
+        static constexpr int OD = CT == 1 ? 2 : 1;
+        float x[NB][OD][4], off[NB][4];
+        __device__ __forceinline__ Sums()
+        {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int tok = 16 * (i0 >> 1) + 4 * i + (i0 & 1);  // and tok + 2
-                const uint32_t m = (tok < n ? 0xffffu : 0u) | (tok + 2 < n ? 0xffff0000u : 0u);
+            for (int j = 0; j < NB; ++j)
 #pragma unroll
-                for (int j = 0; j < NB; ++j)
-                    vs[j][i] &= m;
+                for (int e = 0; e < 4; ++e) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    if constexpr (CT == 1) {
-                        y[i][e] = tok + 2 * e < n ? y[i][e] : -INFINITY;
+                    for (int o = 0; o < OD; ++o)
+                        x[j][o][e] = 0.f;
+                    off[j][e] = 0.f;
+                }
+        }
+        // keep: rows that count (bits as in a word of scales)
+        template <bool MASK>
+        __device__ __forceinline__ void add(const unsigned char *at, int lane, const float (&p)[NP][2],
+                                            const uint32_t (&keep)[4])
+        {
+            using F = Fmt<DD>;
+            constexpr uint32_t kOff0 = 0x80088008u, kOff1 = 0x80808080u;  // -8 in slots 0 and 1
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                uint32_t w[4], s[4], b[NP];
+                load_words(at + j * F::kBlock + F::kCodes, lane, w);
+                value_scales(at + j * F::kBlock, lane, s);
+#pragma unroll
+                for (int k = 0; k < NP; ++k) {
+                    float s0, s1, w0, w1;
+                    scales(MASK ? s[k / CT] & keep[k / CT] : s[k / CT], k, s0, s1);
+                    mul2(w0, w1, p[k][0], p[k][1], s0, s1);
+                    b[k] = transpose8(cvt_f16x2(w0, w1));
+                }
+                uint32_t v[4][4];  // both entries of the rows of word i with c = 0, and with c = 1
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (GS == 16) {
+                        codes_of(w[i], v[i]);
                     } else {
-                        y[2 * i][e] = tok < n ? y[2 * i][e] : -INFINITY;
-                        y[(2 * i + 1) % NP][e] = tok + 2 < n ? y[(2 * i + 1) % NP][e] : -INFINITY;
+                        v[i][0] = (i % 2 ? w[i] >> 8 : w[i]) & 0x000f000fu;
+                        v[i][2] = (i % 2 ? w[i] >> 12 : w[i] >> 4) & 0x000f000fu;
+                        v[i][1] = v[i][3] = 0u;
+                    }
+                }
+                const uint32_t off8[4] = {kOff0, GS == 16 ? kOff1 : 0u, kOff0, GS == 16 ? kOff1 : 0u};
+#pragma unroll
+                for (int i = 0; i < 4; i += CT == 1 ? 2 : 1) {
+                    const uint32_t b0 = CT == 1 ? b[i % NP] : b[2 * i % NP], b1 = CT == 1 ? b[(i + 1) % NP] : b[(2 * i + 1) % NP];
+                    mma_f16_acc(off[j], off8, b0, b1);
+                    if constexpr (CT == 2) {
+                        mma_f16_acc(x[j][0], v[i], b0, b1);
+                    } else {
+                        const uint32_t even[4] = {v[i][0], v[i][1], v[(i + 1) % 4][0], v[(i + 1) % 4][1]};
+                        const uint32_t odd[4] = {v[i][2], v[i][3], v[(i + 1) % 4][2], v[(i + 1) % 4][3]};
+                        mma_f16_acc(x[j][0], even, b0, b1);
+                        mma_f16_acc(x[j][OD - 1], odd, b0, b1);
                     }
                 }
             }
         }
-        // the largest scales of the tokens' groups
-        uint32_t vm[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            vm[i] = vs[0][i];
-#pragma unroll
-            for (int j = 1; j < NB; ++j)
-                asm("max.bf16x2 %0, %0, %1;" : "+r"(vm[i]) : "r"(vs[j][i]));
+        // Entry e (k = 0) or e + 2 (k = 1) of head h of the lane.
+        __device__ __forceinline__ float value(int j, int k, int h) const
+        {
+            if constexpr (CT == 2)
+                return x[j][0][2 * k + h] + off[j][2 * k + h];
+            else
+                return (x[j][0][2 * k] + off[j][2 * k]) + (x[j][OD - 1][2 * k + 1] + off[j][2 * k + 1]);
         }
-        constexpr float kFar = 32768.f, kFarSum = 0x1p90f;
-        float p[NP][2], pw[NP][2], l[2];  // weights, and times vm
-        // a pair's scales
-        auto scales = [](uint32_t s, int k, float &s0, float &s1) {
-            s0 = CT == 1 || k % 2 == 0 ? bf16lo(s) : bf16hi(s);
-            s1 = CT == 1 || k % 2 != 0 ? bf16hi(s) : bf16lo(s);
-        };
-        // scale of a pair's scores: slots of c = 1 are 16 times as large
-        auto scale = [&](int k, int e) {
-            const float s = cq[CT == 2 ? e : 0];
-            return (CT == 1 ? e : k % 2) ? s * 0.0625f : s;
-        };
-        auto weigh = [&]() {  // returns whether something got far above the reference
-            float top = 0.f;
-            l[0] = l[1] = 0.f;
+    };
+    __device__ __forceinline__ void join(const Sums &s, const float (&l)[2])
+    {
 #pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                float x0, x1, s0, s1;
-                ffma2(x0, x1, y[k][0], y[k][1], scale(k, 0), scale(k, 1), page[0].bias, page[CT - 1].bias);
-                p[k][0] = ex2_approx(x0);
-                p[k][1] = ex2_approx(x1);
-                add2(l[0], l[1], l[0], l[1], p[k][0], p[k][1]);
-                scales(vm[k / CT], k, s0, s1);
-                mul2(pw[k][0], pw[k][1], p[k][0], p[k][1], s0, s1);
-                top = max3(top, pw[k][0], pw[k][1]);
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int h = 0; h < CT; ++h) {
+                od[j][h] += s.value(j, 0, h);
+                if constexpr (GS == 16)
+                    od[j][CT + h] = fmaf(0.0625f, s.value(j, 1, h), od[j][CT + h]);
             }
-            return fmaxf(l[0], l[1]) > kFarSum || top > kFar;
-        };
-        if (__any_sync(0xffffffffu, weigh())) {
+        page[0].l += CT == 1 ? l[0] + l[1] : l[0];
+        if constexpr (CT == 2)
+            page[CT - 1].l += l[1];
+    }
+
+    // n whole pages.  False if a weight was too large for its operand (or a sum for what comes of it): nothing is added then.
+    __device__ __forceinline__ bool pages_step(const unsigned char *at, int n, int lane)
+    {
+        Sums s;
+        float l[2] = {0.f, 0.f};
+        const uint32_t all[4] = {~0u, ~0u, ~0u, ~0u};
+#pragma unroll kUnroll
+        for (int i = 0; i < n; ++i, at += Fmt<DD>::kBytes) {
+            Scores z;
+            float p[NP][2];
+            scores(at, lane, z);
+            weigh(z, p, l);
+            s.template add<false>(at, lane, p, all);
+        }
+        // an infinite weight makes its column infinite or NaN
+        bool fine = fmaxf(l[0], l[1]) < 0x1p90f;
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int h = 0; h < CT; ++h)
+                fine &= fabsf(s.off[j][h]) < INFINITY && (CT == 2 || fabsf(s.off[j][1]) < INFINITY);
+        if (!__all_sync(0xffffffffu, fine))
+            return false;
+        join(s, l);
+        return true;
+    }
+
+    // A page of n tokens, whose weights are looked at first.
+    __device__ __forceinline__ void page_step(const unsigned char *at, int n, int lane)
+    {
+        Scores z;
+        scores(at, lane, z);
+        const int i0 = lane >> 2;
+        uint32_t keep[4], vm[4];  // rows that count, and the largest scales of their groups
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // rows behind the last token may hold anything
+            const int tok = 16 * (i0 >> 1) + 4 * i + (i0 & 1);  // and tok + 2
+            keep[i] = (tok < n ? 0xffffu : 0u) | (tok + 2 < n ? 0xffff0000u : 0u);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                if constexpr (CT == 1) {
+                    z.y[i][e] = tok + 2 * e < n ? z.y[i][e] : -INFINITY;
+                } else {
+                    z.y[2 * i][e] = tok < n ? z.y[2 * i][e] : -INFINITY;
+                    z.y[(2 * i + 1) % NP][e] = tok + 2 < n ? z.y[(2 * i + 1) % NP][e] : -INFINITY;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            uint32_t s[4];
+            value_scales(at + j * Fmt<DD>::kBlock, lane, s);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (j == 0)
+                    vm[i] = s[i] & keep[i];
+                else
+                    asm("max.bf16x2 %0, %0, %1;" : "+r"(vm[i]) : "r"(s[i] & keep[i]));
+            }
+        }
+        constexpr float kFar = 32768.f, kFarSum = 0x1p80f;
+        float p[NP][2], l[2] = {0.f, 0.f}, top = 0.f;
+        weigh(z, p, l);
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+            float s0, s1;
+            scales(vm[k / CT], k, s0, s1);
+            top = max3(top, p[k][0] * s0, p[k][1] * s1);
+        }
+        if (__any_sync(0xffffffffu, fmaxf(l[0], l[1]) > kFarSum || top > kFar)) {
 #pragma unroll
             for (int k = 0; k < CT; ++k) {
-                float top = -INFINITY;  // of p s_v, and of 2^-64 p
+                top = -INFINITY;  // of p s_v, and of 2^-64 p
 #pragma unroll
                 for (int i = 0; i < NP; ++i)
 #pragma unroll
@@ -884,7 +1146,7 @@ struct Heads {
                             continue;
                         float s[2];
                         scales(vm[i / CT], i, s[0], s[1]);
-                        top = fmaxf(top, fmaf(y[i][e], scale(i, e), __log2f(fmaxf(0x1p-64f, s[e]))));
+                        top = fmaxf(top, fmaf(z.y[i][e], factor(i, e), __log2f(fmaxf(0x1p-64f, s[e]))));
                     }
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1)
@@ -895,191 +1157,168 @@ struct Heads {
                 page[k].l *= f;
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
-                    od[j][0][k] *= f;
-                    od[j][0][2 + k] *= f;
-                    if constexpr (CT == 1) {
-                        od[j][OD - 1][1] *= f;
-                        od[j][OD - 1][3] *= f;
-                    }
+                    od[j][k] *= f;
+                    od[j][CT + k] *= f;
                 }
             }
-            weigh();
+            l[0] = l[1] = 0.f;
+            weigh(z, p, l);
         }
-        if constexpr (CT == 1) {
-            page[0].l += l[0] + l[1];
-        } else {
-            page[0].l += l[0];
-            page[CT - 1].l += l[1];
-        }
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            uint32_t w[4];
-            load_words(at + j * F::kBlock + F::kCodes, lane, w);
-            uint32_t b[NP];
-#pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                float s0, s1, w0 = pw[k][0], w1 = pw[k][1];
-                if constexpr (NB > 1) {
-                    scales(vs[j][k / CT], k, s0, s1);
-                    mul2(w0, w1, p[k][0], p[k][1], s0, s1);
-                }
-                b[k] = transpose8(cvt_f16x2(w0, w1));
-            }
-            uint32_t v[4][4];  // both entries of the rows of word i with c = 0, and with c = 1
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (GS == 16) {
-                    values_of(w[i], v[i]);
-                } else if (i % 2 == 0) {
-                    uint32_t c[4];
-                    values_of(w[i], c);
-                    v[i][0] = c[0], v[i][2] = c[1], v[i + 1][0] = c[2], v[i + 1][2] = c[3];
-                    v[i][1] = v[i][3] = v[i + 1][1] = v[i + 1][3] = 0u;
-                }
-            }
-            if constexpr (CT == 2) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    mma_f16_acc(od[j][0], v[i], b[2 * i], b[(2 * i + 1) % NP]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                    const uint32_t even[4] = {v[i][0], v[i][1], v[i + 1][0], v[i + 1][1]};
-                    const uint32_t odd[4] = {v[i][2], v[i][3], v[i + 1][2], v[i + 1][3]};
-                    mma_f16_acc(od[j][0], even, b[i], b[i + 1]);
-                    mma_f16_acc(od[j][OD - 1], odd, b[i], b[i + 1]);
-                }
-            }
-        }
+        Sums s;
+        s.template add<true>(at, lane, p, keep);
+        join(s, l);
     }
 
-    // The partial result of the cut.
     __device__ __forceinline__ void leave(const Args &a, const Cut &c, int lane)
     {
         const int i0 = lane >> 2, c0 = lane & 3;
 #pragma unroll
         for (int k = 0; k < CT; ++k) {
-            float lr = ring[k].l, lp = page[k].l;
+            float l = page[k].l;
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) {
-                lr += __shfl_xor_sync(0xffffffffu, lr, o);
-                lp += __shfl_xor_sync(0xffffffffu, lp, o);
-            }
+            for (int o = 4; o < 32; o <<= 1)
+                l += __shfl_xor_sync(0xffffffffu, l, o);
             const int head = c0 + 4 * k;
             if (head >= c.rows)
                 continue;
-            const float m = fmaxf(-ring[k].bias, -page[k].bias), base = m == -INFINITY ? 0.f : m;
-            const float fr = ex2_approx(-ring[k].bias - base), fp = ex2_approx(-page[k].bias - base);
             float *rec = a.rec + ((size_t)c.slot * a.RU + head) * rec_floats<DD>();
-            if (i0 == 0) {
-                rec[0] = m;
-                rec[1] = lr * fr + lp * fp;
-            }
-#pragma unroll
-            for (int e = 0; e < kHeadDim / 16; ++e) {
-                rec[4 + 16 * e + i0] = ol[e][k] * fr;
-                rec[4 + 16 * e + 8 + i0] = ol[e][2 + k] * fr;
-            }
+            if (i0 == 0)
+                *reinterpret_cast<float2 *>(rec + 2) = make_float2(-page[k].bias, l);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
-                float x = od[j][0][k], y = od[j][0][2 + k];
-                if constexpr (CT == 1) {
-                    x += od[j][OD - 1][1];
-                    y += od[j][OD - 1][3];
-                }
                 const int e = GS == 16 ? 16 * j + 4 * (i0 >> 1) + (i0 & 1) : i0;
-                rec[4 + kHeadDim + e] = x * (fp * 0x1p24f);  // (the codes were 2^-24 of themselves)
+                rec[4 + kHeadDim + e] = od[j][k] * 0x1p24f;  // (the codes were 2^-24 of themselves)
                 if (GS == 16)
-                    rec[4 + kHeadDim + e + 2] = y * (fp * 0x1p24f);
+                    rec[4 + kHeadDim + e + 2] = od[j][CT + k] * 0x1p24f;
             }
         }
     }
 };
 
+// The first kernel: q~ of every unit, a warp each, as the second one's lanes want it.
+constexpr int kPrepWarps = 4;
+template <int DD, int CT>
+__global__ void __launch_bounds__(kPrepWarps * 32) prep_kernel(const Args a, int units)
+{
+    grid_dep_launch();
+    const int unit = blockIdx.x * kPrepWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (unit >= units)
+        return;
+    Cut c;
+    c.b = unit / (a.c.Hkv * a.RT);
+    c.g = unit / a.RT % a.c.Hkv;
+    c.rt = unit % a.RT;
+    c.rows = min(kRows, a.G - c.rt * kRows);
+    uint32_t q[4][2];
+    queries_of(a, c, lane, q);
+    Pages<DD, CT> h;
+    h.make(a, c, q, lane);
+    h.save(a, unit, lane);
+}
+
 template <int DD>
 constexpr size_t mma_smem(int B)
 {
-    return 1024 + (size_t)mma_warps<DD>() * mma_slots<DD>() * (kSlot + 8) + 16 + (2 * (size_t)B + 1) * 4;
+    return 128 + (size_t)mma_warps<DD>() * mma_slots<DD>() * kSlot + (2 * (size_t)B + 1) * 4;
 }
 
 template <int DD, int CT>
-__global__ void __launch_bounds__(mma_warps<DD>() * 32, 1)
-    attend_mma_kernel(const __grid_constant__ CUtensorMap wk, const __grid_constant__ CUtensorMap wv, const Args a)
+__global__ void __launch_bounds__(mma_warps<DD>() * 32, 1) attend_mma_kernel(const Args a)
 {
-    constexpr int kMmaWarps = mma_warps<DD>(), kSlots = mma_slots<DD>();
+    constexpr int W = mma_warps<DD>(), S = mma_slots<DD>();
     extern __shared__ unsigned char raw[];
-    unsigned char *base = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);  // the swizzle's atoms
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, share = blockIdx.x * kMmaWarps + warp;
-    unsigned char *slots = base + warp * kSlots * kSlot;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(base + kMmaWarps * kSlots * kSlot), *full = bars + warp * kSlots;
-    volatile int *gave_up = reinterpret_cast<volatile int *>(bars + kMmaWarps * kSlots);
-    const Tables t = tables_at(reinterpret_cast<int *>(bars + kMmaWarps * kSlots + 2), a.c.B);
+    unsigned char *slots = raw + ((128u - (smem_u32(raw) & 127u)) & 127u);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Tables t = tables_at(reinterpret_cast<int *>(slots + W * S * kSlot), a.c.B);
     grid_dep_launch();
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kMmaWarps * kSlots; ++i)
-            mbar_init(bars + i, 1);
-        *gave_up = 0;
-        mbar_init_fence();
-    }
-    build_tables<DD>(a, t);  // its barriers also publish the mbarriers
-    const uint64_t once = l2_evict_first_policy();  // the cache is read once
-    Filler<DD> fill;
-    fill.begin(a, t, share);
+    build_tables<DD>(a, t);
+    slots += warp * S * kSlot;
+    const uint32_t slots_s = smem_u32(slots);
+    const int share = blockIdx.x * W + warp;
+    Filler<DD> ahead;
+    ahead.begin(a, t, share);
 #pragma unroll 1
-    for (int i = 0; i < kSlots; ++i)
-        fill.fill(a, t, wk, wv, slots, full, once, lane);
+    for (int i = 0; i < S; ++i)
+        ahead.fill(a, t, slots_s, lane);
     Walk walk;
     walk.begin<DD>(a, t, share);
-    int n = 0;  // stages taken
-    bool alive = true;
-    for (Cut c; alive && walk.next<DD>(a, t, c);) {
+    int s = 0;  // slot of the next stage
+    auto take = [&]() {
+        cp_async_wait<S - 1>();
+        __syncwarp();  // the stage's copies by all lanes have landed
+        return s * kSlot;
+    };
+    auto give = [&]() {
+        __syncwarp();  // the slot is read
+        s = s + 1 < S ? s + 1 : 0;
+        ahead.fill(a, t, slots_s, lane);
+    };
+    bool waited = false;
+    for (Cut c; walk.next<DD>(a, t, c);) {
         if (lane == 0)
             leave_span(a, c, share);
-        Heads<DD, CT> h;
-        h.begin(a, c, lane);
-        for (int st = c.st0; st < c.st1; ++n) {
-            const int s = n % kSlots;
-            if (!mbar_wait_warp(full + s, (unsigned)((n / kSlots) & 1), gave_up)) {
-                alive = false;
-                break;
+        int st = c.st0;
+        if (st < c.nrun) {
+            uint32_t q[4][2];
+            queries_of(a, c, lane, q);
+            Ring<CT> r;
+            for (; st < min(c.st1, c.nrun); ++st) {
+                r.step(q, slots_s + take(), min(kRun, c.nwin - st * kRun), a.c.c2, lane);
+                give();
             }
-            const unsigned char *slot = slots + s * kSlot;
-            if (st < c.nrun) {
-                h.ring_step(smem_u32(slot), min(kRun, c.nwin - st * kRun), a.c.c2, lane);
-                ++st;
-            } else {
-                const int pages = min(Filler<DD>::kPages, c.st1 - st);
-                for (int i = 0; i < pages; ++i)
-                    h.page_step(slot + i * Fmt<DD>::kBytes, min(kPage, c.L - c.nwin - (st - c.nrun + i) * kPage), lane);
-                st += pages;
-            }
-            __syncwarp();  // the slot is read
-            fill.fill(a, t, wk, wv, slots, full, once, lane);
+            r.leave(a, c, rec_floats<DD>(), lane);
+        } else {
+            leave_none<DD>(a, c, 0, lane);
         }
-        if (alive)
-            h.leave(a, c, lane);
+        if (st == c.st1) {
+            leave_none<DD>(a, c, 2, lane);
+            continue;
+        }
+        if (!waited) {  // for the first kernel
+            grid_dep_wait();
+            waited = true;
+        }
+        Pages<DD, CT> h;
+        h.load(a, c.unit, lane);
+        int left = c.L - c.nwin - (st - c.nrun) * kPage;  // tokens of the unit from here on
+        for (int pages = c.st1 - st; pages > 0; pages -= stage_pages<DD>()) {
+            const unsigned char *slot = slots + take();
+            const int m = min(stage_pages<DD>(), pages), whole = min(m, left / kPage);
+            if (!h.pages_step(slot, whole, lane))
+                for (int i = 0; i < whole; ++i)
+                    h.page_step(slot + i * Fmt<DD>::kBytes, kPage, lane);
+            if (whole < m)
+                h.page_step(slot + whole * Fmt<DD>::kBytes, left - whole * kPage, lane);
+            left -= m * kPage;
+            give();
+        }
+        h.leave(a, c, lane);
     }
-    if (!alive) {
-        // a wait gave up: the copies in flight land (again a bounded wait) before the warp leaves
-        if (lane == 0)
-            report(a.c.status, DAR_ERR_DEVICE);
-        for (int i = n; i < fill.filled; ++i)
-            mbar_wait(full + i % kSlots, (unsigned)((i / kSlots) & 1), nullptr);
-    }
+    if (!waited)
+        grid_dep_wait();  // this kernel ends after the first one
 }
 
 // ------------------------------------------------------------------ join
 
-// Block i writes output row i: the warps take its partial results in turn, and are joined.
-template <typename T, int DD, int WARPS>
+// Block i writes output row i: the warps take its partial results in turn, U of them in flight together, and are
+// joined.
+template <typename T, int DD, int WARPS, int U>
 __global__ void __launch_bounds__(WARPS * 32) join_kernel(Args a)
 {
     constexpr int ND = (DD + 31) / 32, N = 2 + ND;
     __shared__ float part[WARPS][2 + 32 * N], sum[kHeadDim + DD];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int row = blockIdx.x, b = row / a.c.Hq, h = row % a.c.Hq, g = h / a.G, j = h % a.G;
-    grid_dep_wait();
+    // the lift's columns and the lengths are the caller's: the kernel before, which alone may still run, does not write them
+    float uv[DD >= 32 ? 1 : DD];
+    if constexpr (DD < 32) {
+        if (threadIdx.x < kHeadDim)
+#pragma unroll
+            for (int e = 0; e < DD; ++e)
+                uv[e] = __ldg(a.c.Uv + ((size_t)g * DD + e) * kHeadDim + threadIdx.x);
+    }
     const int L = a.c.seq_lens[b];
+    grid_dep_wait();
     if (L <= 0 || (long long)L > (long long)a.c.maxp * kPage + a.c.w) {  // empty, or refused
         for (int i = threadIdx.x; i < kHeadDim; i += WARPS * 32)
             static_cast<T *>(a.c.out)[(size_t)row * kHeadDim + i] = from_f32<T>(0.f);
@@ -1087,22 +1326,50 @@ __global__ void __launch_bounds__(WARPS * 32) join_kernel(Args a)
     }
     const int unit = (b * a.c.Hkv + g) * a.RT + j / kRows;
     const int2 span = a.span[unit];
-    const int k0 = min(max(span.x, 0), kMaxShares - 1), k1 = min(max(span.y, k0), kMaxShares - 1);
+    const int k0 = min(max(span.x, 0), kMaxShares - 1), k1 = min(max(span.y, k0), kMaxShares - 1), parts = k1 - k0 + 1;
     float m = -INFINITY, l = 0.f, x[N] = {};
     const size_t stride = (size_t)a.RU * rec_floats<DD>();
     const float *rec = a.rec + ((size_t)(unit + k0) * a.RU + j % kRows) * rec_floats<DD>();
-    for (int i = warp; i <= k1 - k0; i += WARPS) {
-        const float *p = rec + i * stride;
-        const float mo = p[0], lo = p[1], mn = fmaxf(m, mo), base = mn == -INFINITY ? 0.f : mn;
-        const float f = ex2_approx(m - base), fo = ex2_approx(mo - base);
-        m = mn;
-        l = l * f + lo * fo;
-        x[0] = x[0] * f + p[4 + lane] * fo;
-        x[1] = x[1] * f + p[36 + lane] * fo;
+    for (int i0 = warp; i0 < parts; i0 += WARPS * U) {
+        float4 ml[U];
+        float o[U][N];
 #pragma unroll
-        for (int e = 0; e < ND; ++e)
-            if (32 * e + lane < DD)
-                x[2 + e] = x[2 + e] * f + p[4 + kHeadDim + 32 * e + lane] * fo;
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * WARPS;
+            ml[u] = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+            if (i < parts)
+                ml[u] = *reinterpret_cast<const float4 *>(rec + i * stride);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float *p = rec + (i0 + u * WARPS) * stride + 4 + lane;
+            const bool ring = ml[u].x != -INFINITY, pages = ml[u].z != -INFINITY;
+            o[u][0] = ring ? p[0] : 0.f;
+            o[u][1] = ring ? p[32] : 0.f;
+#pragma unroll
+            for (int e = 0; e < ND; ++e)
+                o[u][2 + e] = pages && 32 * e + lane < DD ? p[kHeadDim + 32 * e] : 0.f;
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            top = max3(top, ml[u].x, ml[u].z);
+        const float base = top == -INFINITY ? 0.f : top, f = ex2_approx(m - base);
+        m = top;
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            x[e] *= f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float fr = ex2_approx(ml[u].x - base), fp = ex2_approx(ml[u].z - base);
+            l += ml[u].y * fr + ml[u].w * fp;
+            x[0] = fmaf(o[u][0], fr, x[0]);
+            x[1] = fmaf(o[u][1], fr, x[1]);
+#pragma unroll
+            for (int e = 0; e < ND; ++e)
+                x[2 + e] = fmaf(o[u][2 + e], fp, x[2 + e]);
+        }
     }
     if (lane == 0) {
         part[warp][0] = m;
@@ -1131,13 +1398,17 @@ __global__ void __launch_bounds__(WARPS * 32) join_kernel(Args a)
         sum[i] = y;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < kHeadDim; i += WARPS * 32) {
-        float o = sum[i];
+    if (threadIdx.x >= kHeadDim)
+        return;
+    float o = sum[threadIdx.x];
 #pragma unroll
-        for (int e = 0; e < DD; ++e)
-            o = fmaf(sum[kHeadDim + e], __ldg(a.c.Uv + ((size_t)g * DD + e) * kHeadDim + i), o);
-        static_cast<T *>(a.c.out)[(size_t)row * kHeadDim + i] = from_f32<T>(o / all);
+    for (int e = 0; e < DD; ++e) {
+        if constexpr (DD < 32)
+            o = fmaf(sum[kHeadDim + e], uv[e], o);
+        else
+            o = fmaf(sum[kHeadDim + e], __ldg(a.c.Uv + ((size_t)g * DD + e) * kHeadDim + threadIdx.x), o);
     }
+    static_cast<T *>(a.c.out)[(size_t)row * kHeadDim + threadIdx.x] = from_f32<T>(o / all);
 }
 
 // ------------------------------------------------------------------ launch
@@ -1145,7 +1416,7 @@ __global__ void __launch_bounds__(WARPS * 32) join_kernel(Args a)
 static size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
 struct Layout {
-    size_t span, rec, total;
+    size_t span, prep, rec, total;
     int RT, RU;
 };
 
@@ -1157,7 +1428,9 @@ static Layout layout(int B, int Hq, int Hkv, int dd)
     y.RT = (G + kRows - 1) / kRows;
     const size_t units = (size_t)B * Hkv * y.RT;
     y.span = 0;
-    y.rec = up256(units * sizeof(int2));
+    y.prep = up256(units * sizeof(int2));
+    // (words of a lane: two or four of q~ and two of its sum a group, and two factors at most)
+    y.rec = y.prep + up256(units * ((size_t)std::max(1, dd / 16) * (y.RU > 4 ? 6 : 4) + 2) * 32 * sizeof(uint32_t));
     y.total = y.rec + up256((units + kMaxShares) * y.RU * (4 + kHeadDim + dd) * sizeof(float));
     return y;
 }
@@ -1170,6 +1443,7 @@ static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s
     Args a;
     a.c = c;
     a.span = reinterpret_cast<int2 *>(ws + y.span);
+    a.prep = reinterpret_cast<uint32_t *>(ws + y.prep);
     a.rec = reinterpret_cast<float *>(ws + y.rec);
     a.G = c.Hq / c.Hkv;
     a.RT = y.RT;
@@ -1196,26 +1470,6 @@ static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s
         &sms);
     if (e != cudaSuccess)
         return e;
-    if constexpr (sizeof(T) == 2) {
-        CUtensorMap wk, wv;
-        const unsigned long long rows = (unsigned long long)c.B * c.Hkv * c.w;
-        if (!make_tma_2d_bf16(&wk, c.win_k, rows, kHeadDim, kRun) || !make_tma_2d_bf16(&wv, c.win_v, rows, kHeadDim, kRun))
-            return cudaErrorInvalidValue;
-        constexpr int warps = mma_warps<DD>();
-        const int grid = std::min(sms, kMaxShares / warps);
-        a.shares = grid * warps;
-        if (y.RU <= 4)
-            attend_mma_kernel<DD, 1><<<grid, warps * 32, mma_smem<DD>(c.B), s>>>(wk, wv, a);
-        else
-            attend_mma_kernel<DD, 2><<<grid, warps * 32, mma_smem<DD>(c.B), s>>>(wk, wv, a);
-    } else {
-        const int grid = std::min(sms, kMaxShares / kWarps);
-        a.shares = grid * kWarps;
-        attend_kernel<T, DD><<<grid, kWarps * 32, lanes_smem(c.B), s>>>(a);
-    }
-    e = cudaGetLastError();
-    if (e != cudaSuccess)
-        return e;
     cudaLaunchAttribute pdl[1];
     pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     pdl[0].val.programmaticStreamSerializationAllowed = 1;
@@ -1223,9 +1477,40 @@ static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s
     cfg.stream = s;
     cfg.attrs = pdl;
     cfg.numAttrs = 1;
-    cfg.gridDim = dim3((unsigned)(c.B * c.Hq));
-    cfg.blockDim = dim3(4 * 32);
-    return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, 4>, a);
+    if constexpr (sizeof(T) == 2) {
+        constexpr int warps = mma_warps<DD>();
+        const int grid = std::min(sms, kMaxShares / warps), units = c.B * c.Hkv * y.RT;
+        a.shares = grid * warps;
+        const int prep = (units + kPrepWarps - 1) / kPrepWarps;
+        if (y.RU <= 4)
+            prep_kernel<DD, 1><<<prep, kPrepWarps * 32, 0, s>>>(a, units);
+        else
+            prep_kernel<DD, 2><<<prep, kPrepWarps * 32, 0, s>>>(a, units);
+        e = cudaGetLastError();
+        if (e != cudaSuccess)
+            return e;
+        cfg.gridDim = dim3(grid);
+        cfg.blockDim = dim3(warps * 32);
+        cfg.dynamicSmemBytes = mma_smem<DD>(c.B);
+        e = y.RU <= 4 ? cudaLaunchKernelEx(&cfg, attend_mma_kernel<DD, 1>, a) : cudaLaunchKernelEx(&cfg, attend_mma_kernel<DD, 2>, a);
+    } else {
+        const int grid = std::min(sms, kMaxShares / kWarps);
+        a.shares = grid * kWarps;
+        attend_kernel<T, DD><<<grid, kWarps * 32, lanes_smem(c.B), s>>>(a);
+        e = cudaGetLastError();
+    }
+    if (e != cudaSuccess)
+        return e;
+    cfg.dynamicSmemBytes = 0;
+    // few rows may have a partial result of every share each, and many rows few
+    const int rows = c.B * c.Hq, warps = rows < 192 ? 16 : rows < 1024 ? 4 : 2;
+    cfg.gridDim = dim3((unsigned)rows);
+    cfg.blockDim = dim3(warps * 32);
+    if (warps == 16)
+        return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, 16, 4>, a);
+    if (warps == 4)
+        return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, 4, 4>, a);
+    return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, 2, 4>, a);
 }
 
 template <typename T>
