@@ -602,10 +602,11 @@ struct Filler {
     }
 };
 
-// The queries of a cut as B operands: column i0 = lane / 4 is head i0 / 2 + 4 (i0 mod 2).
+// The queries of a cut as B operands: column i0 = lane / 4 is head (i0 / 2) mod NH + 4 (i0 mod 2).
+template <int NH>
 __device__ __forceinline__ void queries_of(const Args &a, const Cut &c, int lane, uint32_t (&q)[4][2])
 {
-    const int i0 = lane >> 2, c0 = lane & 3, head = (i0 >> 1) + 4 * (i0 & 1);
+    const int i0 = lane >> 2, c0 = lane & 3, head = (i0 >> 1) % NH + 4 * (i0 & 1);
     const uint32_t *qp = static_cast<const uint32_t *>(a.c.q) +
                          ((size_t)c.b * a.c.Hq + c.g * a.G + c.rt * kRows + head) * (kHeadDim / 2) + c0;
 #pragma unroll
@@ -623,7 +624,7 @@ __device__ __forceinline__ void leave_none(const Args &a, const Cut &c, int at, 
 }
 
 // A cut's ring tokens.
-template <int CT>
+template <int CT, int NH>
 struct Ring {
     Soft ring[CT];
     float ol[kHeadDim / 16][4];
@@ -717,7 +718,7 @@ struct Ring {
             for (int o = 4; o < 32; o <<= 1)
                 l += __shfl_xor_sync(0xffffffffu, l, o);
             const int head = c0 + 4 * k;
-            if (head >= c.rows)
+            if (head >= c.rows || c0 >= NH)  // (with fewer than four heads the other columns are copies)
                 continue;
             float *rec = a.rec + ((size_t)c.slot * a.RU + head) * stride;
             if (i0 == 0)
@@ -732,11 +733,19 @@ struct Ring {
 };
 
 // A cut's pages: what a warp has of its query heads, and the sums.
-template <int DD, int CT>
+//
+// NH heads (1, 2 or 4; CT = 2: 8) share the columns of a product out: with one head, columns 2 x, 2 x + 1 belong to words
+// x of its lanes, and the products of the four words go into one result, each with an operand that is zero in the
+// others' columns.  So a lane has two scores of a page, not eight of which the lanes t have the same: 76 instructions a
+// page beside what a stage costs, instead of 114.  In general word i = x ND + d goes to columns of x in result d.
+template <int DD, int CT, int NH>
 struct Pages {
     static constexpr int GS = Fmt<DD>::kGroup, NB = Fmt<DD>::kGroups;
+    static constexpr int ND = NH, NW = 4 / NH;              // results of a page's scores, words in one
     static constexpr int TB = GS == 16 && CT == 2 ? 2 : 1;  // score products of a group
+    static_assert(CT == 1 || NH == 4, "eight heads fill the columns");
     uint32_t qt[NB][TB][2];  // q~ as B operands, two fp16 terms
+    uint32_t mine[NW];       // all ones where the lane's column belongs to words x ND ..
     float from[NB][4];       // what a score's sum starts from
     float cq[CT];            // scale of a score: c2, the power of two taken out of q~, and the codes' 2^24
     Soft page[CT];
@@ -777,6 +786,9 @@ struct Pages {
             from[j][3] = 16.f * from[j][1];
         }
 #pragma unroll
+        for (int x = 0; x < NW; ++x)
+            mine[x] = (lane >> 3) / NH == x ? ~0u : 0u;
+#pragma unroll
         for (int k = 0; k < CT; ++k) {
             page[k].bias = INFINITY;
             page[k].l = 0.f;
@@ -792,7 +804,7 @@ struct Pages {
     __device__ __forceinline__ void make(const Args &a, const Cut &c, const uint32_t (&q)[4][2], int lane)
     {
         const int i0 = lane >> 2, c0 = lane & 3;
-        float x[NB][4];  // entries 16 j + i0 (+ 8) of heads c0, c0 + 4: [0] i0 c0, [1] i0 c0 + 4, [2], [3] i0 + 8
+        float x[NB][4];  // entries 16 j + i0 (+ 8) of heads c0 mod NH, and + 4: [0] i0 c0, [1] i0 c0 + 4, [2], [3] i0 + 8
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const float *u = a.c.Uk + ((size_t)c.g * DD + 16 * j + i0) * kHeadDim + 2 * c0;
@@ -896,24 +908,37 @@ struct Pages {
         }
     }
 
-    // Lane (g, t) has the scores of rows 16 (g / 2) + 4 i + 2 c + g mod 2, in pairs: two tokens (c = 0, 1) of a head
-    // (pair i), or two heads of a token (pairs 2 i, 2 i + 1).
-    static constexpr int NP = 4 * CT;
+    // Lane (g, t) has the scores of rows 16 (g / 2) + 4 i + 2 c + g mod 2, i = (t / NH) ND + d, in pairs: two tokens (c =
+    // 0, 1) of a head (pair d), or with CT = 2 two heads of a token (pairs 2 d, 2 d + 1).
+    static constexpr int NP = ND * CT;
     struct Scores {
         float y[NP][2];
     };
+    // The lane's words of 64 scales.
+    static __device__ __forceinline__ void load_scales(const unsigned char *at, int lane, uint32_t (&s)[ND])
+    {
+        at += (lane >> 2) * 16 + (lane & 3) / NH * (4 * ND);
+        if constexpr (ND == 4) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(at);
+            s[0] = v.x, s[1] = v.y, s[2 % ND] = v.z, s[3 % ND] = v.w;
+        } else if constexpr (ND == 2) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(at);
+            s[0] = v.x, s[1 % ND] = v.y;
+        } else {
+            s[0] = *reinterpret_cast<const uint32_t *>(at);
+        }
+    }
     __device__ __forceinline__ void scores(const unsigned char *at, int lane, Scores &z) const
     {
         using F = Fmt<DD>;
-        const int i0 = lane >> 2;
         float(&y)[NP][2] = z.y;
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             const unsigned char *block = at + j * F::kBlock;
-            const uint4 sw = *reinterpret_cast<const uint4 *>(block + F::kScales + i0 * 16);
-            const uint32_t sc[4] = {sw.x, sw.y, sw.z, sw.w};
-            uint32_t w[4];
+            uint32_t w[4], sc[ND];
+            load_scales(block + F::kScales, lane, sc);
             load_words(block, lane, w);
+            float r[ND][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t c[4];
@@ -924,17 +949,25 @@ struct Pages {
                     c[2] = c[0];
                     c[3] = c[1];
                 }
-                float d[4];
-                mma_f16_c(d, c, qt[j][0][0], qt[j][0][1], from[j]);
+                float(&d)[4] = r[i % ND];
+                const uint32_t m = mine[i / ND];
+                if (i < ND)
+                    mma_f16_c(d, c, NW == 1 ? qt[j][0][0] : qt[j][0][0] & m, NW == 1 ? qt[j][0][1] : qt[j][0][1] & m, from[j]);
+                else
+                    mma_f16_acc(d, c, qt[j][0][0] & m, qt[j][0][1] & m);
                 if constexpr (TB == 2)
                     mma_f16_acc(d, c, qt[j][TB - 1][0], qt[j][TB - 1][1]);
+            }
+#pragma unroll
+            for (int i = 0; i < ND; ++i) {
                 const float s0 = bf16lo(sc[i]), s1 = bf16hi(sc[i]);
+                const float(&d)[4] = r[i];
                 if constexpr (CT == 1) {
                     const float x0 = GS == 16 ? d[0] + d[1] : d[0], x1 = GS == 16 ? d[2] + d[3] : d[2];
                     y[i][0] = j ? fmaf(x0, s0, y[i][0]) : x0 * s0;
                     y[i][1] = j ? fmaf(x1, s1, y[i][1]) : x1 * s1;
                 } else {
-                    float(&u)[2] = y[2 * i], (&v)[2] = y[(2 * i + 1) % NP];
+                    float(&u)[2] = y[2 * i % NP], (&v)[2] = y[(2 * i + 1) % NP];
                     if (j == 0) {
                         mul2(u[0], u[1], d[0], d[1], s0, s0);
                         mul2(v[0], v[1], d[2], d[3], s1, s1);
@@ -970,18 +1003,13 @@ struct Pages {
         s0 = CT == 1 || k % 2 == 0 ? bf16lo(s) : bf16hi(s);
         s1 = CT == 1 || k % 2 != 0 ? bf16hi(s) : bf16lo(s);
     }
-    static __device__ __forceinline__ void value_scales(const unsigned char *block, int lane, uint32_t (&s)[4])
-    {
-        const uint4 v = *reinterpret_cast<const uint4 *>(block + Fmt<DD>::kScales + 2 * kPage + (lane >> 2) * 16);
-        s[0] = v.x, s[1] = v.y, s[2] = v.z, s[3] = v.w;
-    }
-
     // Sums of some pages, of codes + 8; off: of 8 (both times 2^-24, entries e + 2 times 2^-20).  With CT = 2 a column has
     // 8 tokens' weights of head t or t + 4.  With CT = 1 column 2 t has those of rows with c = 0 and column 2 t + 1 those
     // with c = 1, which one transposition brings; products with the codes of c = 0 are right in the even columns and
-    // products with those of c = 1 in the odd ones, so each has sums of its own, whose other columns are not used.
+    // products with those of c = 1 in the odd ones, so each has sums of its own, whose other columns are not used.  With
+    // fewer than four heads a word's weights are in its columns alone, and masks leave the rest 0.
     struct Sums {
-        static constexpr int OD = CT == 1 ? 2 : 1;
+        static constexpr int OD = NH == 4 && CT == 1 ? 2 : 1;
         float x[NB][OD][4], off[NB][4];
         __device__ __forceinline__ Sums()
         {
@@ -998,15 +1026,15 @@ struct Pages {
         // keep: rows that count (bits as in a word of scales)
         template <bool MASK>
         __device__ __forceinline__ void add(const unsigned char *at, int lane, const float (&p)[NP][2],
-                                            const uint32_t (&keep)[4])
+                                            const uint32_t (&keep)[ND], const uint32_t (&mine)[NW])
         {
             using F = Fmt<DD>;
             constexpr uint32_t kOff0 = 0x80088008u, kOff1 = 0x80808080u;  // -8 in slots 0 and 1
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
-                uint32_t w[4], s[4], b[NP];
+                uint32_t w[4], s[ND], b[NP];
                 load_words(at + j * F::kBlock + F::kCodes, lane, w);
-                value_scales(at + j * F::kBlock, lane, s);
+                load_scales(at + j * F::kBlock + F::kScales + 2 * kPage, lane, s);
 #pragma unroll
                 for (int k = 0; k < NP; ++k) {
                     float s0, s1, w0, w1;
@@ -1027,16 +1055,26 @@ struct Pages {
                 }
                 const uint32_t off8[4] = {kOff0, GS == 16 ? kOff1 : 0u, kOff0, GS == 16 ? kOff1 : 0u};
 #pragma unroll
-                for (int i = 0; i < 4; i += CT == 1 ? 2 : 1) {
-                    const uint32_t b0 = CT == 1 ? b[i % NP] : b[2 * i % NP], b1 = CT == 1 ? b[(i + 1) % NP] : b[(2 * i + 1) % NP];
-                    mma_f16_acc(off[j], off8, b0, b1);
-                    if constexpr (CT == 2) {
-                        mma_f16_acc(x[j][0], v[i], b0, b1);
-                    } else {
-                        const uint32_t even[4] = {v[i][0], v[i][1], v[(i + 1) % 4][0], v[(i + 1) % 4][1]};
-                        const uint32_t odd[4] = {v[i][2], v[i][3], v[(i + 1) % 4][2], v[(i + 1) % 4][3]};
-                        mma_f16_acc(x[j][0], even, b0, b1);
-                        mma_f16_acc(x[j][OD - 1], odd, b0, b1);
+                for (int k = 0; k < NP; k += 2)
+                    mma_f16_acc(off[j], off8, b[k], k + 1 < NP ? b[(k + 1) % NP] : 0u);
+                if constexpr (CT == 2) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        mma_f16_acc(x[j][0], v[i], b[2 * i % NP], b[(2 * i + 1) % NP]);
+                } else if constexpr (NH == 4) {
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        const uint32_t even[4] = {v[i][0], v[i][1], v[i + 1][0], v[i + 1][1]};
+                        const uint32_t odd[4] = {v[i][2], v[i][3], v[i + 1][2], v[i + 1][3]};
+                        mma_f16_acc(x[j][0], even, b[i % NP], b[(i + 1) % NP]);
+                        mma_f16_acc(x[j][OD - 1], odd, b[i % NP], b[(i + 1) % NP]);
+                    }
+                } else {
+                    const uint32_t even = lane & 4 ? 0u : ~0u;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t t = b[i % ND] & mine[i / ND];
+                        mma_f16_acc(x[j][0], v[i], t & even, t & ~even);
                     }
                 }
             }
@@ -1047,7 +1085,7 @@ struct Pages {
             if constexpr (CT == 2)
                 return x[j][0][2 * k + h] + off[j][2 * k + h];
             else
-                return (x[j][0][2 * k] + off[j][2 * k]) + (x[j][OD - 1][2 * k + 1] + off[j][2 * k + 1]);
+                return (x[j][0][2 * k] + off[j][2 * k]) + (x[j][OD - 1][2 * k + 1] + off[j][2 * k + 1]);  // both columns
         }
     };
     __device__ __forceinline__ void join(const Sums &s, const float (&l)[2])
@@ -1070,14 +1108,14 @@ struct Pages {
     {
         Sums s;
         float l[2] = {0.f, 0.f};
-        const uint32_t all[4] = {~0u, ~0u, ~0u, ~0u};
+        const uint32_t all[ND] = {};
 #pragma unroll kUnroll
         for (int i = 0; i < n; ++i, at += Fmt<DD>::kBytes) {
             Scores z;
             float p[NP][2];
             scores(at, lane, z);
             weigh(z, p, l);
-            s.template add<false>(at, lane, p, all);
+            s.template add<false>(at, lane, p, all, mine);
         }
         // an infinite weight makes its column infinite or NaN
         bool fine = fmaxf(l[0], l[1]) < 0x1p90f;
@@ -1097,28 +1135,27 @@ struct Pages {
     {
         Scores z;
         scores(at, lane, z);
-        const int i0 = lane >> 2;
-        uint32_t keep[4], vm[4];  // rows that count, and the largest scales of their groups
+        uint32_t keep[ND], vm[ND];  // rows that count, and the largest scales of their groups
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {  // rows behind the last token may hold anything
-            const int tok = 16 * (i0 >> 1) + 4 * i + (i0 & 1);  // and tok + 2
+        for (int i = 0; i < ND; ++i) {  // rows behind the last token may hold anything
+            const int tok = 16 * (lane >> 3) + 4 * ((lane & 3) / NH * ND + i) + ((lane >> 2) & 1);  // and tok + 2
             keep[i] = (tok < n ? 0xffffu : 0u) | (tok + 2 < n ? 0xffff0000u : 0u);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 if constexpr (CT == 1) {
                     z.y[i][e] = tok + 2 * e < n ? z.y[i][e] : -INFINITY;
                 } else {
-                    z.y[2 * i][e] = tok < n ? z.y[2 * i][e] : -INFINITY;
+                    z.y[2 * i % NP][e] = tok < n ? z.y[2 * i % NP][e] : -INFINITY;
                     z.y[(2 * i + 1) % NP][e] = tok + 2 < n ? z.y[(2 * i + 1) % NP][e] : -INFINITY;
                 }
             }
         }
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            uint32_t s[4];
-            value_scales(at + j * Fmt<DD>::kBlock, lane, s);
+            uint32_t s[ND];
+            load_scales(at + j * Fmt<DD>::kBlock + Fmt<DD>::kScales + 2 * kPage, lane, s);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < ND; ++i) {
                 if (j == 0)
                     vm[i] = s[i] & keep[i];
                 else
@@ -1149,7 +1186,7 @@ struct Pages {
                         top = fmaxf(top, fmaf(z.y[i][e], factor(i, e), __log2f(fmaxf(0x1p-64f, s[e]))));
                     }
 #pragma unroll
-                for (int o = 4; o < 32; o <<= 1)
+                for (int o = NH; o < 32; o <<= 1)  // all lanes of the head
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                 const float was = -page[k].bias, now = fmaxf(was, top - 8.f);
                 const float f = now == -INFINITY ? 1.f : ex2_approx(was - now);
@@ -1165,21 +1202,30 @@ struct Pages {
             weigh(z, p, l);
         }
         Sums s;
-        s.template add<true>(at, lane, p, keep);
+        s.template add<true>(at, lane, p, keep, mine);
         join(s, l);
     }
 
     __device__ __forceinline__ void leave(const Args &a, const Cut &c, int lane)
     {
         const int i0 = lane >> 2, c0 = lane & 3;
+        if constexpr (NH < 4) {  // lanes t of a head have different words' columns
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int o = NH; o < 4; o <<= 1)
+                        od[j][k] += __shfl_xor_sync(0xffffffffu, od[j][k], o);
+        }
 #pragma unroll
         for (int k = 0; k < CT; ++k) {
             float l = page[k].l;
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1)
+            for (int o = NH; o < 32; o <<= 1)
                 l += __shfl_xor_sync(0xffffffffu, l, o);
             const int head = c0 + 4 * k;
-            if (head >= c.rows)
+            if (head >= c.rows || c0 >= NH)
                 continue;
             float *rec = a.rec + ((size_t)c.slot * a.RU + head) * rec_floats<DD>();
             if (i0 == 0)
@@ -1197,7 +1243,7 @@ struct Pages {
 
 // The first kernel: q~ of every unit, a warp each, as the second one's lanes want it.
 constexpr int kPrepWarps = 4;
-template <int DD, int CT>
+template <int DD, int CT, int NH>
 __global__ void __launch_bounds__(kPrepWarps * 32) prep_kernel(const Args a, int units)
 {
     grid_dep_launch();
@@ -1210,8 +1256,8 @@ __global__ void __launch_bounds__(kPrepWarps * 32) prep_kernel(const Args a, int
     c.rt = unit % a.RT;
     c.rows = min(kRows, a.G - c.rt * kRows);
     uint32_t q[4][2];
-    queries_of(a, c, lane, q);
-    Pages<DD, CT> h;
+    queries_of<NH>(a, c, lane, q);
+    Pages<DD, CT, NH> h;
     h.make(a, c, q, lane);
     h.save(a, unit, lane);
 }
@@ -1222,7 +1268,7 @@ constexpr size_t mma_smem(int B)
     return 128 + (size_t)mma_warps<DD>() * mma_slots<DD>() * kSlot + (2 * (size_t)B + 1) * 4;
 }
 
-template <int DD, int CT>
+template <int DD, int CT, int NH>
 __global__ void __launch_bounds__(mma_warps<DD>() * 32, 1) attend_mma_kernel(const Args a)
 {
     constexpr int W = mma_warps<DD>(), S = mma_slots<DD>();
@@ -1260,8 +1306,8 @@ __global__ void __launch_bounds__(mma_warps<DD>() * 32, 1) attend_mma_kernel(con
         int st = c.st0;
         if (st < c.nrun) {
             uint32_t q[4][2];
-            queries_of(a, c, lane, q);
-            Ring<CT> r;
+            queries_of<NH>(a, c, lane, q);
+            Ring<CT, NH> r;
             for (; st < min(c.st1, c.nrun); ++st) {
                 r.step(q, slots_s + take(), min(kRun, c.nwin - st * kRun), a.c.c2, lane);
                 give();
@@ -1278,7 +1324,7 @@ __global__ void __launch_bounds__(mma_warps<DD>() * 32, 1) attend_mma_kernel(con
             grid_dep_wait();
             waited = true;
         }
-        Pages<DD, CT> h;
+        Pages<DD, CT, NH> h;
         h.load(a, c.unit, lane);
         int left = c.L - c.nwin - (st - c.nrun) * kPage;  // tokens of the unit from here on
         for (int pages = c.st1 - st; pages > 0; pages -= stage_pages<DD>()) {
@@ -1455,12 +1501,11 @@ static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s
         [&](int d) {
             cudaError_t e2 = cudaDeviceGetAttribute(&once.value[d], cudaDevAttrMultiProcessorCount, d);
             if constexpr (sizeof(T) == 2) {
-                if (e2 == cudaSuccess)
-                    e2 = cudaFuncSetAttribute(attend_mma_kernel<DD, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                              (int)mma_smem<DD>(DAR_DECODE_MAX_BATCH));
-                if (e2 == cudaSuccess)
-                    e2 = cudaFuncSetAttribute(attend_mma_kernel<DD, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                              (int)mma_smem<DD>(DAR_DECODE_MAX_BATCH));
+                for (const auto k : {attend_mma_kernel<DD, 1, 1>, attend_mma_kernel<DD, 1, 2>, attend_mma_kernel<DD, 1, 4>,
+                                     attend_mma_kernel<DD, 2, 4>})
+                    if (e2 == cudaSuccess)
+                        e2 = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                  (int)mma_smem<DD>(DAR_DECODE_MAX_BATCH));
             } else if (e2 == cudaSuccess) {
                 e2 = cudaFuncSetAttribute(attend_kernel<T, DD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                           (int)lanes_smem(DAR_DECODE_MAX_BATCH));
@@ -1481,18 +1526,18 @@ static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s
         constexpr int warps = mma_warps<DD>();
         const int grid = std::min(sms, kMaxShares / warps), units = c.B * c.Hkv * y.RT;
         a.shares = grid * warps;
-        const int prep = (units + kPrepWarps - 1) / kPrepWarps;
-        if (y.RU <= 4)
-            prep_kernel<DD, 1><<<prep, kPrepWarps * 32, 0, s>>>(a, units);
-        else
-            prep_kernel<DD, 2><<<prep, kPrepWarps * 32, 0, s>>>(a, units);
+        const auto prep = y.RU == 1 ? prep_kernel<DD, 1, 1> : y.RU == 2 ? prep_kernel<DD, 1, 2>
+                          : y.RU <= 4 ? prep_kernel<DD, 1, 4> : prep_kernel<DD, 2, 4>;
+        const auto attend = y.RU == 1 ? attend_mma_kernel<DD, 1, 1> : y.RU == 2 ? attend_mma_kernel<DD, 1, 2>
+                            : y.RU <= 4 ? attend_mma_kernel<DD, 1, 4> : attend_mma_kernel<DD, 2, 4>;
+        prep<<<(units + kPrepWarps - 1) / kPrepWarps, kPrepWarps * 32, 0, s>>>(a, units);
         e = cudaGetLastError();
         if (e != cudaSuccess)
             return e;
         cfg.gridDim = dim3(grid);
         cfg.blockDim = dim3(warps * 32);
         cfg.dynamicSmemBytes = mma_smem<DD>(c.B);
-        e = y.RU <= 4 ? cudaLaunchKernelEx(&cfg, attend_mma_kernel<DD, 1>, a) : cudaLaunchKernelEx(&cfg, attend_mma_kernel<DD, 2>, a);
+        e = cudaLaunchKernelEx(&cfg, attend, a);
     } else {
         const int grid = std::min(sms, kMaxShares / kWarps);
         a.shares = grid * kWarps;
