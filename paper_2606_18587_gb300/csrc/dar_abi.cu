@@ -680,13 +680,9 @@ dar_status dar_decode_step_q4(const dar_cache_q4 *cache, const void *k_new, cons
     if (s != DAR_OK || dec_empty)  // B = 0: nothing to append either
         return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (!app_empty) {
-        s = from_cuda(dar::launch_append_q4(cache->dtype, cache->d_down, ap, st), "dar_decode_step_q4 append launch");
-        if (s != DAR_OK)
-            return s;
-    }
-    return from_cuda(dar::launch_decode_q4(cache->dtype, cache->d_down, dc, workspace, st),
-                     "dar_decode_step_q4 decode launch");
+    return from_cuda(app_empty ? dar::launch_decode_q4(cache->dtype, cache->d_down, dc, workspace, st)
+                               : dar::launch_step_q4(cache->dtype, cache->d_down, ap, dc, workspace, st),
+                     "dar_decode_step_q4 launch");
 }
 
 size_t dar_prefill_chunk_workspace_bytes(const dar_cache *cache, int32_t n)

@@ -221,6 +221,9 @@ double q4_decode_line_bound(int B, int Hq, int Hkv, int dd, int w, int maxp);
 cudaError_t launch_append_q4(dar_dtype dt, int dd, const AppendArgs &a, cudaStream_t s);
 cudaError_t launch_convert_q4(dar_dtype dt, int dd, bool pack, const Q4ConvertArgs &a, cudaStream_t s);
 cudaError_t launch_decode_q4(dar_dtype dt, int dd, const Q4DecodeArgs &a, void *workspace, cudaStream_t s);
+// The append and then the decode.
+cudaError_t launch_step_q4(dar_dtype dt, int dd, const AppendArgs &ap, const Q4DecodeArgs &a, void *workspace,
+                           cudaStream_t s);
 
 // Chunked prefill over a cache: gather kernel, attention (chunk mode), then
 // the cache append of the chunk.  Buffers of the workspace (see dar_abi.cu).

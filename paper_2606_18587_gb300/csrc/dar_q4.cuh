@@ -264,6 +264,60 @@ struct Raw<float, GS> {
     }
 };
 
+// bf16: the maxima of a page's 64 groups, whose quarter of each lane u of (g, u) reduces, end with lane u having those of
+// rows i = u: three exchanges, and two scales a lane instead of eight, each four times.  False where one of them is
+// infinite, NaN or tiny (the rows' own path then).  sc[0]: the scales of the lane's two rows, inv: 1 / them.
+template <typename T, int GS>
+__device__ __forceinline__ bool even_page(const Raw<T, GS> (&raw)[4][2], int lane, uint32_t (&sc)[4], float (&inv)[2])
+{
+    if constexpr (sizeof(T) != 2) {
+        return false;
+    } else {
+        constexpr int N = GS / 8;
+        uint32_t m[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t x[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                x[c] = raw[i][c].w[0] & 0x7fff7fffu;
+                if constexpr (N == 2)
+                    x[c] = __vmaxu2(x[c], raw[i][c].w[N - 1] & 0x7fff7fffu);
+            }
+            m[i] = __vmaxu2(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[0], x[1], 0x7632));
+        }
+        const bool u0 = lane & 1, u1 = lane & 2;
+        const uint32_t a = __vmaxu2(u0 ? m[1] : m[0], __shfl_xor_sync(0xffffffffu, u0 ? m[0] : m[1], 1));
+        const uint32_t b = __vmaxu2(u0 ? m[3] : m[2], __shfl_xor_sync(0xffffffffu, u0 ? m[2] : m[3], 1));
+        const uint32_t r = __vmaxu2(u1 ? b : a, __shfl_xor_sync(0xffffffffu, u1 ? a : b, 2));
+        const uint32_t top[2] = {r << 16, r & 0xffff0000u};
+        bool fine = true;
+        float s[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            fine &= top[c] == 0u || top[c] - 0x0d800000u < 0x7f800000u - 0x0d800000u;
+            s[c] = round_scale((__float_as_uint(__uint_as_float(top[c]) * (1.0f / 7.0f)) + 0x200u) & ~0x3ffu);
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv[c]) : "f"(s[c]));
+            inv[c] = s[c] > 0.f ? inv[c] : 0.f;
+        }
+        sc[0] = __byte_perm(__float_as_uint(s[0]), __float_as_uint(s[1]), 0x7632);
+        return __all_sync(0xffffffffu, fine);
+    }
+}
+template <typename T, int GS>
+__device__ __forceinline__ void even_codes(const Raw<T, GS> (&raw)[2], int from, const float (&inv)[2], uint32_t (&x)[2][GS / 8])
+{
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const float v = __shfl_sync(0xffffffffu, inv[c], from);
+#pragma unroll
+            for (int k = 0; k < GS / 8; ++k)
+                x[c][k] = codes_bf16(bf16lo(raw[c].w[k]), bf16hi(raw[c].w[k]), v);
+        }
+    }
+}
+
 // Quantises rows [first, end) of a page into a block; row r's entries are at vec + r * stride.
 template <typename T, int GS, bool VALUES>
 __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, int stride, int first, int end, int lane)
@@ -281,11 +335,17 @@ __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, i
                 raw[i][c].load(vec + (size_t)r * stride + u * 2 * N);
         }
     uint32_t w[4], sc[4];
+    float inv[2];
+    const bool even = even_page<T, GS>(raw, lane, sc, inv);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t x[2][N];
-        const uint32_t s0 = raw[i][0].codes(x[0]), s1 = raw[i][1].codes(x[1]);
-        sc[i] = s0 | s1 << 16;
+        if (even) {
+            even_codes<T, GS>(raw[i], (lane & ~3) + i, inv, x);
+        } else {
+            const uint32_t s0 = raw[i][0].codes(x[0]), s1 = raw[i][1].codes(x[1]);
+            sc[i] = s0 | s1 << 16;
+        }
         if constexpr (VALUES) {
 #pragma unroll
             for (int c = 0; c < 2; ++c)
@@ -309,7 +369,9 @@ __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, i
             *reinterpret_cast<uint4 *>(at) = make_uint4(w[0], w[1], w[2], w[3]);
         else
             *reinterpret_cast<uint2 *>(at) = make_uint2(w[1], w[3]);
-        if (u == 0)
+        if (even)
+            reinterpret_cast<uint32_t *>(scales)[u] = sc[0];
+        else if (u == 0)
             *reinterpret_cast<uint4 *>(scales) = make_uint4(sc[0], sc[1], sc[2], sc[3]);
         return;
     }
@@ -328,15 +390,14 @@ __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, i
         if (mask)
             words[i] = (words[i] & ~mask) | (w[GS == 16 ? i : 2 * i + 1] & mask);
     }
-    if (u == 0)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int r = lane_row(g, i, c);
-                if (r >= first && r < end)
-                    scales[2 * i + c] = (uint16_t)(sc[i] >> (16 * c));
-            }
+        for (int c = 0; c < 2; ++c) {
+            const int r = lane_row(g, i, c);
+            if (u == (even ? i : 0) && r >= first && r < end)
+                scales[2 * i + c] = (uint16_t)((even ? sc[0] : sc[i]) >> (16 * c));
+        }
 }
 
 // Reads rows [first, end) of a block back.

@@ -5,8 +5,11 @@
 // are sum_j (p_j s_v,j) code_v,j: scales multiply scores and weights, one per group,
 // and the products take the codes themselves.
 //
-// Two kernels on the caller's stream, the second launched programmatically:
+// Two or three kernels on the caller's stream, the later ones launched programmatically:
 //
+//  prep    (bf16, tensor cores) q~ of every unit as operands; in a step of few tokens further blocks
+//          of the append's kernel.  (Made by every warp for itself it is 3 us before the first page; and
+//          without this launch one sequence of 901 tokens takes 9.0 us in a graph instead of 8.3.)
 //  attend  The work is a line of units (sequence, KV head, up to kRows query heads):
 //          the ring in runs of kRun tokens, then the pages.  Every warp of the grid has
 //          an equal share of the line by cost, and leaves one partial result per query
@@ -21,29 +24,9 @@
 #include "dar_common.cuh"
 #include "dar_launch.h"
 #include "dar_q4.cuh"
+#include "dar_q4_append.cuh"
 #include "dar_sm100.cuh"
 
-#ifndef DAR_UNROLL
-#define DAR_UNROLL 1
-#endif
-#ifndef DAR_W
-#define DAR_W 16
-#endif
-#ifndef DAR_S
-#define DAR_S 2
-#endif
-#ifndef DAR_W2
-#define DAR_W2 12
-#endif
-#ifndef DAR_S2
-#define DAR_S2 3
-#endif
-#ifndef DAR_NP
-#define DAR_NP 1
-#endif
-#ifndef DAR_SLEEP
-#define DAR_SLEEP 100
-#endif
 namespace dar {
 namespace q4 {
 
@@ -54,14 +37,17 @@ constexpr int kRun = 16;         // ring tokens of a stage
 constexpr int kWarps = 8;        // of a CTA (CUDA cores)
 // Of a CTA (tensor cores), and stages in flight of each: as many warps as registers allow.
 template <int DD>
-__host__ __device__ constexpr int mma_warps() { return DD <= 16 ? DAR_W : DAR_W2; }
+__host__ __device__ constexpr int mma_warps() { return DD <= 16 ? 16 : 12; }
 template <int DD>
-__host__ __device__ constexpr int mma_slots() { return DD <= 16 ? DAR_S : DAR_S2; }
-constexpr int kUnroll = DAR_UNROLL;       // pages of a stage
+__host__ __device__ constexpr int mma_slots() { return DD <= 16 ? 2 : 3; }
+// Registers of a thread: without spills, and for one or two heads of narrow vectors such that blocks of the first kernel
+// fit beside on an SM (else half the blocks start 1 us later; with four heads the spills cost more: 46.9 and 48.7 us).
+template <int DD, int NH>
+__host__ __device__ constexpr int mma_registers() { return DD > 16 ? 168 : NH < 4 ? 112 : 128; }
 constexpr int kSlot = 5120;      // bytes of a stage at most
 constexpr int kMaxShares = 2560; // the workspace holds partial results of this many warps
-constexpr int kCostUnit = 8;     // cost of a unit's set-up (its place on the line is before the stages)
-constexpr int kCostRun = 8;      // of kRun ring tokens
+constexpr int kCostUnit = 20;    // cost of a unit's set-up (its place on the line is before the stages)
+constexpr int kCostRun = 10;     // of kRun ring tokens
 template <int DD>
 __host__ __device__ constexpr int cost_page() { return DD == 8 ? 4 : 5 * DD / 16; }
 
@@ -70,8 +56,9 @@ __host__ __device__ constexpr int rec_floats() { return 4 + kHeadDim + DD; }
 
 struct Args {
     Q4DecodeArgs c;
-    int2 *span;  // [units] first and last share of every unit
+    int2 *span;  // [units] first and last share of every unit; -1: it has no tokens
     uint32_t *prep;  // of every unit, what the first kernel makes of its queries (Pages)
+    bool front;      // the kernel before is the step's first one: it appends too
     float *rec;  // [units + shares][rows of a unit][rec_floats]: m, l of the ring, m, l of the pages, acc[64], acc[d_down]
     int G, RT, RU;  // query heads per KV head, units per (sequence, KV head), rows of a unit at most
     int shares;
@@ -107,6 +94,9 @@ __device__ void build_tables(const Args &a, const Tables &t)
             L = 0;
         }
         t.L[b] = L;
+        if (L == 0 && blockIdx.x == 0)  // empty, or refused: the output is 0
+            for (int u = 0; u < a.c.Hkv * a.RT; ++u)
+                a.span[b * a.c.Hkv * a.RT + u].x = -1;
     }
     __syncthreads();
     if (tid < 32) {
@@ -503,7 +493,7 @@ __device__ __forceinline__ uint32_t key_mask(int key, int n)
     return (key < n ? 0xffffu : 0u) | (key + 1 < n ? 0xffff0000u : 0u);
 }
 
-// Pages of a stage.
+// Pages of a stage: 1, 2 or 4.
 template <int DD>
 __host__ __device__ constexpr int stage_pages() { return Fmt<DD>::kBytes > kSlot / 4 ? kSlot / Fmt<DD>::kBytes : 4; }
 
@@ -523,7 +513,7 @@ struct Filler {
     const unsigned char *heads; // page 0 of the cut's KV head, this lane's part
     int ring, nwin;             // row of the ring's first token, tokens in it
     int st, st1, nrun;          // next stage, end of the cut, runs of the ring
-    int ids, at;                // 32 entries of the table, one per lane, of which the next stage's are at ..
+    int ids, later, at;         // 32 entries of the table, one per lane, of which the next stage's are at .., and the next 32
     int slot;                   // to be filled next
     bool more;
 
@@ -543,10 +533,18 @@ struct Filler {
         st1 = c.st1;
         nrun = c.nrun;
         nwin = c.nwin;
-        at = 32;
         table = a.c.block_table + (size_t)c.b * a.c.maxp;
+        load_ids(a, max(0, st - nrun));
         heads = static_cast<const unsigned char *>(a.c.pool) + (size_t)c.g * kBytes + (threadIdx.x & 31) * 16;
         ring = (c.b * a.c.Hkv + c.g) * a.c.w;
+    }
+    // Entries from page lp on; they are there by the time a stage wants them.
+    __device__ __forceinline__ void load_ids(const Args &a, int lp)
+    {
+        const int i = lp + (threadIdx.x & 31);
+        ids = i < a.c.maxp ? __ldg(table + i) : -1;
+        later = i + 32 < a.c.maxp ? __ldg(table + i + 32) : -1;
+        at = 0;
     }
     // Starts the copies of the next stage, as one group (of none when there is no more).
     __device__ __forceinline__ void fill(const Args &a, const Tables &t, uint32_t slots, int lane)
@@ -571,9 +569,10 @@ struct Filler {
                 ++st;
             } else {
                 const int lp = st - nrun, n = min(P, st1 - st);
-                if (at + P > 32) {
+                if (at >= 32) {
+                    ids = later;
+                    later = lp + 32 + lane < a.c.maxp ? __ldg(table + lp + 32 + lane) : -1;
                     at = 0;
-                    ids = lp + lane < a.c.maxp ? __ldg(table + lp + lane) : -1;
                 }
                 const uint32_t to = dst + lane * 16;
 #pragma unroll
@@ -1109,13 +1108,21 @@ struct Pages {
         Sums s;
         float l[2] = {0.f, 0.f};
         const uint32_t all[ND] = {};
-#pragma unroll kUnroll
-        for (int i = 0; i < n; ++i, at += Fmt<DD>::kBytes) {
+        auto one = [&](const unsigned char *page) {
             Scores z;
             float p[NP][2];
-            scores(at, lane, z);
+            scores(page, lane, z);
             weigh(z, p, l);
-            s.template add<false>(at, lane, p, all, mine);
+            s.template add<false>(page, lane, p, all, mine);
+        };
+        if (n == stage_pages<DD>()) {  // (unrolled it is 175 instructions a page instead of 187)
+#pragma unroll
+            for (int i = 0; i < stage_pages<DD>(); ++i)
+                one(at + i * Fmt<DD>::kBytes);
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < n; ++i)
+                one(at + i * Fmt<DD>::kBytes);
         }
         // an infinite weight makes its column infinite or NaN
         bool fine = fmaxf(l[0], l[1]) < 0x1p90f;
@@ -1241,15 +1248,10 @@ struct Pages {
     }
 };
 
-// The first kernel: q~ of every unit, a warp each, as the second one's lanes want it.
-constexpr int kPrepWarps = 4;
+// q~ of every unit, a warp each, as the next kernel's lanes want it.
 template <int DD, int CT, int NH>
-__global__ void __launch_bounds__(kPrepWarps * 32) prep_kernel(const Args a, int units)
+__device__ __forceinline__ void prep_unit(const Args &a, int unit, int lane)
 {
-    grid_dep_launch();
-    const int unit = blockIdx.x * kPrepWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (unit >= units)
-        return;
     Cut c;
     c.b = unit / (a.c.Hkv * a.RT);
     c.g = unit / a.RT % a.c.Hkv;
@@ -1262,6 +1264,28 @@ __global__ void __launch_bounds__(kPrepWarps * 32) prep_kernel(const Args a, int
     h.save(a, unit, lane);
 }
 
+constexpr int kPrepWarps = 4;
+template <int DD, int CT, int NH>
+__global__ void __launch_bounds__(kPrepWarps * 32) prep_kernel(const Args a, int units)
+{
+    grid_dep_launch();
+    const int unit = blockIdx.x * kPrepWarps + (threadIdx.x >> 5);
+    if (unit < units)
+        prep_unit<DD, CT, NH>(a, unit, threadIdx.x & 31);
+}
+
+// The first kernel of a step of few tokens: the append's blocks, and the same.
+template <int DD, int CT, int NH>
+__global__ void __launch_bounds__(kFewThreads) front_kernel(AppendArgs ap, const Args a, int units)
+{
+    grid_dep_launch();
+    const int unit = ((int)blockIdx.x - ap.B) * (kFewThreads / 32) + (int)(threadIdx.x >> 5);
+    if ((int)blockIdx.x < ap.B)
+        append_few<bf16, DD>(ap);
+    else if (unit < units)
+        prep_unit<DD, CT, NH>(a, unit, threadIdx.x & 31);
+}
+
 template <int DD>
 constexpr size_t mma_smem(int B)
 {
@@ -1269,7 +1293,7 @@ constexpr size_t mma_smem(int B)
 }
 
 template <int DD, int CT, int NH>
-__global__ void __launch_bounds__(mma_warps<DD>() * 32, 1) attend_mma_kernel(const Args a)
+__global__ void __maxnreg__((mma_registers<DD, NH>())) attend_mma_kernel(const Args a)
 {
     constexpr int W = mma_warps<DD>(), S = mma_slots<DD>();
     extern __shared__ unsigned char raw[];
@@ -1277,6 +1301,12 @@ __global__ void __launch_bounds__(mma_warps<DD>() * 32, 1) attend_mma_kernel(con
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const Tables t = tables_at(reinterpret_cast<int *>(slots + W * S * kSlot), a.c.B);
     grid_dep_launch();
+    // the lengths, tables and pages may be read at once, unless the kernel before appends to them
+    bool waited = false;
+    if (a.front) {
+        grid_dep_wait();
+        waited = true;
+    }
     build_tables<DD>(a, t);
     slots += warp * S * kSlot;
     const uint32_t slots_s = smem_u32(slots);
@@ -1299,7 +1329,6 @@ __global__ void __launch_bounds__(mma_warps<DD>() * 32, 1) attend_mma_kernel(con
         s = s + 1 < S ? s + 1 : 0;
         ahead.fill(a, t, slots_s, lane);
     };
-    bool waited = false;
     for (Cut c; walk.next<DD>(a, t, c);) {
         if (lane == 0)
             leave_span(a, c, share);
@@ -1327,14 +1356,18 @@ __global__ void __launch_bounds__(mma_warps<DD>() * 32, 1) attend_mma_kernel(con
         Pages<DD, CT, NH> h;
         h.load(a, c.unit, lane);
         int left = c.L - c.nwin - (st - c.nrun) * kPage;  // tokens of the unit from here on
+        bool first = true;
         for (int pages = c.st1 - st; pages > 0; pages -= stage_pages<DD>()) {
             const unsigned char *slot = slots + take();
             const int m = min(stage_pages<DD>(), pages), whole = min(m, left / kPage);
-            if (!h.pages_step(slot, whole, lane))
-                for (int i = 0; i < whole; ++i)
-                    h.page_step(slot + i * Fmt<DD>::kBytes, kPage, lane);
-            if (whole < m)
-                h.page_step(slot + whole * Fmt<DD>::kBytes, left - whole * kPage, lane);
+            // the cut's first page sets the references
+            int done = first ? 0 : h.pages_step(slot, whole, lane) ? whole : 0;
+            for (; done < m; ++done) {
+                h.page_step(slot + done * Fmt<DD>::kBytes, min(kPage, left - done * kPage), lane);
+                if (first && done + 1 < whole && h.pages_step(slot + (done + 1) * Fmt<DD>::kBytes, whole - done - 1, lane))
+                    done = whole - 1;
+                first = false;
+            }
             left -= m * kPage;
             give();
         }
@@ -1355,7 +1388,7 @@ __global__ void __launch_bounds__(WARPS * 32) join_kernel(Args a)
     __shared__ float part[WARPS][2 + 32 * N], sum[kHeadDim + DD];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int row = blockIdx.x, b = row / a.c.Hq, h = row % a.c.Hq, g = h / a.G, j = h % a.G;
-    // the lift's columns and the lengths are the caller's: the kernel before, which alone may still run, does not write them
+    // the lift's columns are the caller's: no kernel that may still run writes them
     float uv[DD >= 32 ? 1 : DD];
     if constexpr (DD < 32) {
         if (threadIdx.x < kHeadDim)
@@ -1363,15 +1396,14 @@ __global__ void __launch_bounds__(WARPS * 32) join_kernel(Args a)
             for (int e = 0; e < DD; ++e)
                 uv[e] = __ldg(a.c.Uv + ((size_t)g * DD + e) * kHeadDim + threadIdx.x);
     }
-    const int L = a.c.seq_lens[b];
     grid_dep_wait();
-    if (L <= 0 || (long long)L > (long long)a.c.maxp * kPage + a.c.w) {  // empty, or refused
+    const int unit = (b * a.c.Hkv + g) * a.RT + j / kRows;
+    const int2 span = a.span[unit];
+    if (span.x < 0) {
         for (int i = threadIdx.x; i < kHeadDim; i += WARPS * 32)
             static_cast<T *>(a.c.out)[(size_t)row * kHeadDim + i] = from_f32<T>(0.f);
         return;
     }
-    const int unit = (b * a.c.Hkv + g) * a.RT + j / kRows;
-    const int2 span = a.span[unit];
     const int k0 = min(max(span.x, 0), kMaxShares - 1), k1 = min(max(span.y, k0), kMaxShares - 1), parts = k1 - k0 + 1;
     float m = -INFINITY, l = 0.f, x[N] = {};
     const size_t stride = (size_t)a.RU * rec_floats<DD>();
@@ -1481,8 +1513,9 @@ static Layout layout(int B, int Hq, int Hkv, int dd)
     return y;
 }
 
+// ap: the append of few tokens that comes first, or nullptr.
 template <typename T, int DD>
-static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s)
+static cudaError_t launch(const Q4DecodeArgs &c, const AppendArgs *ap, void *workspace, cudaStream_t s)
 {
     const Layout y = layout(c.B, c.Hq, c.Hkv, DD);
     char *ws = static_cast<char *>(workspace);
@@ -1501,6 +1534,19 @@ static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s
         [&](int d) {
             cudaError_t e2 = cudaDeviceGetAttribute(&once.value[d], cudaDevAttrMultiProcessorCount, d);
             if constexpr (sizeof(T) == 2) {
+                for (const auto k : {front_kernel<DD, 1, 1>, front_kernel<DD, 1, 2>, front_kernel<DD, 1, 4>,
+                                     front_kernel<DD, 2, 4>})
+                    if (e2 == cudaSuccess)
+                        e2 = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewStageBytes);
+                // with another split of an SM's L1 and shared memory the attending blocks would wait for it to run empty
+                for (const auto k : {prep_kernel<DD, 1, 1>, prep_kernel<DD, 1, 2>, prep_kernel<DD, 1, 4>, prep_kernel<DD, 2, 4>})
+                    if (e2 == cudaSuccess)
+                        e2 = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout,
+                                                  cudaSharedmemCarveoutMaxShared);
+                for (const auto k : {join_kernel<T, DD, 16, 4>, join_kernel<T, DD, 4, 4>, join_kernel<T, DD, 2, 4>})
+                    if (e2 == cudaSuccess)
+                        e2 = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout,
+                                                  cudaSharedmemCarveoutMaxShared);
                 for (const auto k : {attend_mma_kernel<DD, 1, 1>, attend_mma_kernel<DD, 1, 2>, attend_mma_kernel<DD, 1, 4>,
                                      attend_mma_kernel<DD, 2, 4>})
                     if (e2 == cudaSuccess)
@@ -1530,8 +1576,17 @@ static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s
                           : y.RU <= 4 ? prep_kernel<DD, 1, 4> : prep_kernel<DD, 2, 4>;
         const auto attend = y.RU == 1 ? attend_mma_kernel<DD, 1, 1> : y.RU == 2 ? attend_mma_kernel<DD, 1, 2>
                             : y.RU <= 4 ? attend_mma_kernel<DD, 1, 4> : attend_mma_kernel<DD, 2, 4>;
-        prep<<<(units + kPrepWarps - 1) / kPrepWarps, kPrepWarps * 32, 0, s>>>(a, units);
-        e = cudaGetLastError();
+        a.front = ap != nullptr;
+        if (ap) {
+            const auto front = y.RU == 1 ? front_kernel<DD, 1, 1> : y.RU == 2 ? front_kernel<DD, 1, 2>
+                               : y.RU <= 4 ? front_kernel<DD, 1, 4> : front_kernel<DD, 2, 4>;
+            constexpr int per = kFewThreads / 32;
+            front<<<ap->B + (units + per - 1) / per, kFewThreads, few_smem<T>(ap->Hkv), s>>>(*ap, a, units);
+            e = cudaGetLastError();
+        } else {
+            prep<<<(units + kPrepWarps - 1) / kPrepWarps, kPrepWarps * 32, 0, s>>>(a, units);
+            e = cudaGetLastError();
+        }
         if (e != cudaSuccess)
             return e;
         cfg.gridDim = dim3(grid);
@@ -1559,13 +1614,13 @@ static cudaError_t launch(const Q4DecodeArgs &c, void *workspace, cudaStream_t s
 }
 
 template <typename T>
-static cudaError_t launch_t(int dd, const Q4DecodeArgs &a, void *workspace, cudaStream_t s)
+static cudaError_t launch_t(int dd, const Q4DecodeArgs &a, const AppendArgs *ap, void *workspace, cudaStream_t s)
 {
     switch (dd) {
-    case 8: return launch<T, 8>(a, workspace, s);
-    case 16: return launch<T, 16>(a, workspace, s);
-    case 32: return launch<T, 32>(a, workspace, s);
-    case 64: return launch<T, 64>(a, workspace, s);
+    case 8: return launch<T, 8>(a, ap, workspace, s);
+    case 16: return launch<T, 16>(a, ap, workspace, s);
+    case 32: return launch<T, 32>(a, ap, workspace, s);
+    case 64: return launch<T, 64>(a, ap, workspace, s);
     default: return cudaErrorInvalidValue;
     }
 }
@@ -1586,7 +1641,19 @@ cudaError_t launch_decode_q4(dar_dtype dt, int dd, const Q4DecodeArgs &a, void *
 {
     if (a.B == 0)
         return cudaSuccess;
-    return dt == DAR_F32 ? q4::launch_t<float>(dd, a, workspace, s) : q4::launch_t<bf16>(dd, a, workspace, s);
+    return dt == DAR_F32 ? q4::launch_t<float>(dd, a, nullptr, workspace, s)
+                         : q4::launch_t<bf16>(dd, a, nullptr, workspace, s);
+}
+
+cudaError_t launch_step_q4(dar_dtype dt, int dd, const AppendArgs &ap, const Q4DecodeArgs &a, void *workspace,
+                           cudaStream_t s)
+{
+    if (a.B == 0)
+        return cudaSuccess;
+    if (dt == DAR_BF16 && q4::append_is_few<bf16>(ap))
+        return q4::launch_t<bf16>(dd, a, &ap, workspace, s);
+    const cudaError_t e = launch_append_q4(dt, dd, ap, s);
+    return e != cudaSuccess ? e : launch_decode_q4(dt, dd, a, workspace, s);
 }
 
 }  // namespace dar
