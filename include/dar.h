@@ -347,11 +347,15 @@ dar_status dar_cache_unpack_q4(const dar_cache_q4 *src, const int32_t *first, co
 
 /*
  * dar_attn_decode over such a cache: the same step on the values that the pages stand
- * for.  Scales, scores, maxima and sums are fp32; codes are exact.  Arguments, alignment
- * (pool too), limits and errors as dar_attn_decode; workspace of
+ * for.  Scales, scores, maxima and sums are fp32; codes are exact.  bf16: operands of the
+ * products with codes are fp16: q~ as two terms (2^-22 of the row's largest entry) and a
+ * distant token's weight times the scale of its values as one (2^-11 of it), which holds
+ * for pages whose values lie between 2^-90 and 2^100 in magnitude (0 aside); farther off,
+ * weights lose bits.  Arguments, alignment (pool too), limits and errors as
+ * dar_attn_decode, and Hkv * dar_q4_page_bytes(d_down) < 2^31; workspace of
  * dar_decode_q4_workspace_bytes(cache, Hq) bytes, no initialisation; calls that share one
- * must not overlap on the device.  Two kernels in order on `stream`, the first after all
- * earlier work on it.  Deterministic.
+ * must not overlap on the device.  Three kernels (fp32: two) in order on `stream`, the
+ * first after all earlier work on it.  Deterministic.
  */
 size_t dar_decode_q4_workspace_bytes(const dar_cache_q4 *cache, int32_t Hq);
 dar_status dar_attn_decode_q4(const dar_cache_q4 *cache, int32_t Hq, const void *q, const float *Uk,
@@ -361,7 +365,8 @@ dar_status dar_attn_decode_q4(const dar_cache_q4 *cache, int32_t Hq, const void 
 /*
  * One serving step: dar_cache_append_q4 and then dar_attn_decode_q4, with the arguments,
  * requirements and results of the two calls in turn; all arguments of both are checked
- * before anything is launched.
+ * before anything is launched.  Of up to eight tokens a sequence (bf16) it is a launch less:
+ * the query-side set-up runs beside the append, which writes neither q nor Uk.
  */
 dar_status dar_decode_step_q4(const dar_cache_q4 *cache, const void *k_new, const void *v_new, int32_t n,
                               const int32_t *n_per_seq, const float *Dk, const float *Dv, int32_t Hq,

@@ -304,11 +304,12 @@ dar_status prepare_decode_q4(const dar_cache_q4 *c, int32_t Hq, const void *q, c
         return fail(DAR_ERR_INVALID_ARG, "NULL pointer");
     if (!aligned16(q) || !aligned16(out) || !aligned16(Uk) || !aligned16(Uv) || !aligned16(workspace))
         return fail(DAR_ERR_INVALID_ARG, "q, out, Uk, Uv and workspace must be 16-byte aligned");
-    // the line of work, the rows of the ring and the output's are counted in int32
+    // the line of work, the rows of the ring and of the output, and the bytes of a page of all heads are counted in int32
     const double most = 2147483647.0 - 128.0;
     if (dar::q4_decode_line_bound(c->B, Hq, c->Hkv, c->d_down, c->w, c->max_pages_per_seq) >= most ||
         (double)c->B * c->Hkv * c->w * c->d * esize(c->dtype) / 128.0 >= most || (double)c->B * Hq >= most ||
-        (double)c->max_pages_per_seq * DAR_PAGE_SIZE + c->w >= most)
+        (double)c->max_pages_per_seq * DAR_PAGE_SIZE + c->w >= most ||
+        (double)c->Hkv * dar::q4_page_bytes(c->d_down) >= most)
         return fail(DAR_ERR_UNSUPPORTED, "cache too large for int32 indices");
     const size_t need = dar::q4_decode_workspace_bytes(c->B, Hq, c->Hkv, c->d_down);
     if (workspace_bytes < need)

@@ -1125,7 +1125,7 @@ struct Pages {
                 one(at + i * Fmt<DD>::kBytes);
         }
         // an infinite weight makes its column infinite or NaN
-        bool fine = fmaxf(l[0], l[1]) < 0x1p90f;
+        bool fine = fmaxf(l[0], l[1]) < 0x1p100f;
 #pragma unroll
         for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -1169,7 +1169,7 @@ struct Pages {
                     asm("max.bf16x2 %0, %0, %1;" : "+r"(vm[i]) : "r"(s[i] & keep[i]));
             }
         }
-        constexpr float kFar = 32768.f, kFarSum = 0x1p80f;
+        constexpr float kFar = 32768.f, kFarSum = 0x1p96f;
         float p[NP][2], l[2] = {0.f, 0.f}, top = 0.f;
         weigh(z, p, l);
 #pragma unroll
@@ -1181,7 +1181,7 @@ struct Pages {
         if (__any_sync(0xffffffffu, fmaxf(l[0], l[1]) > kFarSum || top > kFar)) {
 #pragma unroll
             for (int k = 0; k < CT; ++k) {
-                top = -INFINITY;  // of p s_v, and of 2^-64 p
+                top = -INFINITY;  // of p s_v, and of 2^-80 p
 #pragma unroll
                 for (int i = 0; i < NP; ++i)
 #pragma unroll
@@ -1190,7 +1190,7 @@ struct Pages {
                             continue;
                         float s[2];
                         scales(vm[i / CT], i, s[0], s[1]);
-                        top = fmaxf(top, fmaf(z.y[i][e], factor(i, e), __log2f(fmaxf(0x1p-64f, s[e]))));
+                        top = fmaxf(top, fmaf(z.y[i][e], factor(i, e), __log2f(fmaxf(0x1p-80f, s[e]))));
                     }
 #pragma unroll
                 for (int o = NH; o < 32; o <<= 1)  // all lanes of the head

@@ -54,7 +54,7 @@ def tolerances(dtype, out, mag, top):
     bf = dtype == "bf16"
     d = top * (140 * 2.0 ** -24 + (2.0 ** -16 if bf else 0.0))
     return mag * (math.expm1(2 * d) + 2.0 ** -18 + (2.0 ** -11 if bf else 0.0)) \
-        + out.abs() * torch.finfo(R.DT[dtype]).eps / 2 + 1e-30
+        + out.abs() * torch.finfo(R.DT[dtype]).eps / 2 + 1e-40
 
 
 def check_outputs(dtype, cache, full, q, Uk, Uv, got, scale=R.D ** -0.5):

@@ -37,6 +37,10 @@ DECODE = [
     ("bf16", 16, 2, 64, 15, [999, 200]),
     ("bf16", 2, 2, 16, 500, [100, 400, 500, 501, 564, 565]),                   # windows that hold almost all
     ("bf16", 1, 1, 16, 16, [40000]),                                           # one head over all SMs
+    ("bf16", 4, 2, 16, 64, [64 + 64 * i for i in range(12)]),                  # whole pages: one to eleven
+    ("bf16", 2, 2, 64, 64, [64 + 64 * i + 1 for i in range(12)]),
+    ("bf16", 2, 1, 8, 16, [3000, 17]),
+    ("bf16", 1, 1, 32, 16, [3000, 17]),
     ("bf16", 8, 8, 16, 20, [20 + (i * 37) % 300 for i in range(70)]),          # many sequences
     ("f32", 4, 4, 16, 32, [230, 270, 0, 5]),
     ("f32", 8, 2, 8, 21, [500, 510, 90]),
@@ -62,6 +66,40 @@ def test_decode(dtype, Hq, Hkv, dd, w, lens):
     assert c4.device_status() == 0
     assert torch.equal(got, again)
     Q.check_outputs(dtype, Q.read_back(dar, c4), full, q, Uk, Uv, got)
+
+
+def test_far_pages():
+    """A pool of more than 4 GB whose last pages a sequence lists."""
+    B, Hkv, dd, w, lens = 2, 8, 16, 16, [300, 77]
+    c, full = R.filled_cache(dar, 6, "bf16", Hkv, dd, w, lens)
+    n = (1 << 32) // (Hkv * dar.dar_q4_page_bytes(dd)) + 100
+    table = torch.where(c.block_table >= 0, n - 1 - c.block_table, -1).cpu()
+    c4 = dar.DarCacheQ4(B, Hkv, dd, w, c.max_pages_per_seq, n, block_table=table)
+    for t, s in ((c4.win_k, c.win_k), (c4.win_v, c.win_v), (c4.seq_lens, c.seq_lens)):
+        t.copy_(s)
+    dar.dar_cache_pack_q4(c, c4)
+    back = dar.DarCache(B, Hkv, dd, w, c.max_pages_per_seq, c.num_pages, block_table=c.block_table.cpu())
+    dar.dar_cache_unpack_q4(c4, back)
+    for t, s in ((back.win_k, c.win_k), (back.win_v, c.win_v), (back.seq_lens, c.seq_lens)):
+        t.copy_(s)
+    q, Uk, Uv = R.operands(6, "bf16", B, 16, Hkv, dd)
+    Q.check_outputs("bf16", back, full, q, Uk, Uv, decode(c4, q, Uk, Uv))
+    k, v = (torch.randn((B, Hkv, 3, 64), device="cuda").bfloat16() for _ in range(2))
+    Dk, Dv = (torch.randn((Hkv, 64, dd), device="cuda") / 8 for _ in range(2))
+    c4.seq_lens.sub_(3)
+    plain = dar.DarCacheQ4.beside(back)
+    plain.seq_lens.sub_(3)
+    dar.dar_cache_append_q4(c4, k, v, Dk, Dv)
+    dar.dar_cache_append_q4(plain, k, v, Dk, Dv)
+    for b in range(B):
+        for i, pg in enumerate(full[b]):
+            if i == (lens[b] - w - 1) // 64:
+                rows = dar.DarCache(B, Hkv, dd, w, c.max_pages_per_seq, c.num_pages, block_table=c.block_table.cpu())
+                dar.dar_cache_unpack_q4(c4, rows, first=ints([max(0, L - w - 3) for L in lens]))
+                other = dar.DarCache(B, Hkv, dd, w, c.max_pages_per_seq, c.num_pages, block_table=c.block_table.cpu())
+                dar.dar_cache_unpack_q4(plain, other, first=ints([max(0, L - w - 3) for L in lens]))
+                assert torch.equal(rows.pool_kd[pg], other.pool_kd[pg]) and rows.pool_kd[pg].any()
+    assert c4.device_status() == 0
 
 
 def test_scale_and_output():
@@ -107,16 +145,18 @@ def test_scores_and_scales_that_rise(dd, growth, values):
     Q.check_outputs("bf16", Q.read_back(dar, c4), full, q, Uk, Uv, decode(c4, q, Uk, Uv))
 
 
-@pytest.mark.parametrize("size", [1e-30, 1e-12, 1e12, 1e30])
-def test_values_of_every_size(size):
-    """Values far from 1, in the ring too: sums stay finite and exact, relative to what they are made of."""
+@pytest.mark.parametrize("size", [1e-26, 1e-12, 1e12, 1e30])
+@pytest.mark.parametrize("Hq", [2, 8, 16])
+def test_values_of_every_size(size, Hq):
+    """Values far from 1 (2^-90 to 2^100), in the ring too: sums stay finite and exact, relative to what they are made
+    of."""
     lens = [300, 40, 700]
     c, full = R.filled_cache(dar, 3, "bf16", 2, 16, 40, lens)
     c.pool_vd *= size
     c.win_v *= size
     c4 = Q.beside(dar, c)
     dar.dar_cache_pack_q4(c, c4)
-    q, Uk, Uv = R.operands(4, "bf16", 3, 8, 2, 16)
+    q, Uk, Uv = R.operands(4, "bf16", 3, Hq, 2, 16)
     Q.check_outputs("bf16", Q.read_back(dar, c4), full, q, Uk, Uv, decode(c4, q, Uk, Uv))
 
 

@@ -114,6 +114,7 @@ def test_decode_refuses(lib):
         assert f(cache(lib, w=2 ** 31 - 1)) == 2
         assert f(cache(lib, B=1024, Hkv=32, max_pages_per_seq=1 << 20), Hq=32) == 2
         assert f(cache(lib, B=0)) == 0
+        assert f(cache(lib, B=1, Hkv=1 << 21, w=1, max_pages_per_seq=0), Hq=1 << 21) == 2   # 2.7 GB a page
     assert call(Uk=0) == 1
     assert call(Uk=P + 4) == 1
     assert call(out=P + 2) == 1
