@@ -744,7 +744,7 @@ struct Pages {
     static constexpr int TB = GS == 16 && CT == 2 ? 2 : 1;  // score products of a group
     static_assert(CT == 1 || NH == 4, "eight heads fill the columns");
     uint32_t qt[NB][TB][2];  // q~ as B operands, two fp16 terms
-    uint32_t mine[NW];       // all ones where the lane's column belongs to words x ND ..
+    uint32_t mine[NW][2];    // all ones where the lane's column belongs to words x ND .., and is even (0) or odd (1)
     float from[NB][4];       // what a score's sum starts from
     float cq[CT];            // scale of a score: c2, the power of two taken out of q~, and the codes' 2^24
     Soft page[CT];
@@ -786,7 +786,9 @@ struct Pages {
         }
 #pragma unroll
         for (int x = 0; x < NW; ++x)
-            mine[x] = (lane >> 3) / NH == x ? ~0u : 0u;
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                mine[x][c] = (lane >> 3) / NH == x && ((lane >> 2) & 1) == c ? ~0u : 0u;
 #pragma unroll
         for (int k = 0; k < CT; ++k) {
             page[k].bias = INFINITY;
@@ -949,7 +951,7 @@ struct Pages {
                     c[3] = c[1];
                 }
                 float(&d)[4] = r[i % ND];
-                const uint32_t m = mine[i / ND];
+                const uint32_t m = mine[i / ND][0] | mine[i / ND][1];
                 if (i < ND)
                     mma_f16_c(d, c, NW == 1 ? qt[j][0][0] : qt[j][0][0] & m, NW == 1 ? qt[j][0][1] : qt[j][0][1] & m, from[j]);
                 else
@@ -1025,7 +1027,7 @@ struct Pages {
         // keep: rows that count (bits as in a word of scales)
         template <bool MASK>
         __device__ __forceinline__ void add(const unsigned char *at, int lane, const float (&p)[NP][2],
-                                            const uint32_t (&keep)[ND], const uint32_t (&mine)[NW])
+                                            const uint32_t (&keep)[ND], const uint32_t (&mine)[NW][2])
         {
             using F = Fmt<DD>;
             constexpr uint32_t kOff0 = 0x80088008u, kOff1 = 0x80808080u;  // -8 in slots 0 and 1
@@ -1069,12 +1071,9 @@ struct Pages {
                         mma_f16_acc(x[j][OD - 1], odd, b[i % NP], b[(i + 1) % NP]);
                     }
                 } else {
-                    const uint32_t even = lane & 4 ? 0u : ~0u;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t t = b[i % ND] & mine[i / ND];
-                        mma_f16_acc(x[j][0], v[i], t & even, t & ~even);
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        mma_f16_acc(x[j][0], v[i], b[i % ND] & mine[i / ND][0], b[i % ND] & mine[i / ND][1]);
                 }
             }
         }
