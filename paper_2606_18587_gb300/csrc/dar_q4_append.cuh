@@ -28,11 +28,16 @@ inline size_t few_smem(int Hkv)
 {
     return (size_t)few_rows<T>(Hkv) * 2 * Hkv * kHeadDim * sizeof(T);
 }
-// Whether a call is one of this kernel's.
+// Whether a call is one of this kernel's.  A sequence takes it some 4 us and 1 us for every token and round of chains, as
+// many sequences as SMs no longer; the tiles of dar_q4_cache.cu take 6.4 us up to 8 tokens and more with every CTA.
+// Here and there, d_down 16, us (B, Hkv, n): 1, 12, 1: 5.0 and 6.4; 1, 12, 4: 8.6 and 6.6; 32, 1, 4: 7.4 and 7.0; 32, 12, 8:
+// 13.0 and 13.6; 32, 32, 4: 15.6 and 18.3; 32, 32, 8: 25 and 19; 128, 12, 8: 13.2 and 25.4; of 64 entries 32, 8, 4: 13.3 and
+// 17.3; 32, 8, 8: 20.8 and 18.0.
 template <typename T>
-inline bool append_is_few(const AppendArgs &a)
+inline bool append_is_few(const AppendArgs &a, int dd)
 {
-    return a.n <= kFewRows && few_rows<T>(a.Hkv) > 0;
+    const long long chains = 2ll * a.Hkv * dd, rounds = (chains + kFewThreads - 1) / kFewThreads;
+    return a.n <= kFewRows && few_rows<T>(a.Hkv) > 0 && a.n * rounds <= 2 + a.B * chains / (8 * kFewThreads);
 }
 
 // Rows on their way into a block, an entry a thread: GS consecutive lanes have a group.  Words that several of the

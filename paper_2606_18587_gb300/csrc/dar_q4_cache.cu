@@ -226,22 +226,31 @@ static cudaError_t by_width(int dd, F &&f)
     }
 }
 
-constexpr long long kBigTiles = kSms * 6 * 2;
+constexpr long long kPairTiles = 4 * kSms;
 
 template <typename T>
 static cudaError_t append_t(int dd, const AppendArgs &a, cudaStream_t s)
 {
     return by_width(dd, [&](auto width) {
         constexpr int DD = decltype(width)::value;
-        if (append_is_few<T>(a))
+        if (append_is_few<T>(a, DD))
             return append_few_launch<T, DD>(a, s);
-        // Large tiles, whose threads have several rows for a read of W, once they fill the chip a few times over and are
-        // not mostly empty (the rule of dar_append.cu, whose tiles these are).
-        constexpr int R = rows_bulk<T>();
-        const long long tiles = ((long long)a.n + kPage - 1 + R - 1) / R;
-        if (tiles * a.B * a.Hkv * 2 >= kBigTiles && a.n >= 4 * R)
-            return append_tiles<T, DD, rows_per_thread<DD>(), R / rows_per_thread<DD>()>(a, s);
-        return append_tiles<T, DD, 1, kPage>(a, s);
+        // A tile is a page, a row to a thread; two rows for every read of W where that leaves work for all SMs: of 64
+        // entries, whose tiles have four threads a row (bf16, 8 KV heads, 32 x 2048 tokens: 246 us, 316 with one; 1 x
+        // 2048: 15.3 and 16.8), and from bf16 in tiles of two pages once these fill the chip a few times over (12 KV
+        // heads, d_down 16, 32 x 2048: 111 and 128; 32 x 64, 768 tiles: 13.9 and 15.5; 4 x 512, 480 tiles: 13.5 and
+        // 11.3).  fp32 rows are twice as long: 212 and 210 at 32 x 2048.  d_down 8: 62 and 63, but 14.7 and 13.1 at 4 x
+        // 2048.  Four rows, or tiles of four pages: between 2 % less and 40 % more.
+        if constexpr (DD == 64) {
+            return append_tiles<T, DD, 2, kPage / 2>(a, s);
+        } else {
+            if constexpr (DD >= 16 && sizeof(T) == 2) {
+                const long long tiles = ((long long)a.n + kPage - 1 + 2 * kPage - 1) / (2 * kPage);
+                if (tiles * a.B * a.Hkv * 2 >= kPairTiles)
+                    return append_tiles<T, DD, 2, kPage>(a, s);
+            }
+            return append_tiles<T, DD, 1, kPage>(a, s);
+        }
     });
 }
 

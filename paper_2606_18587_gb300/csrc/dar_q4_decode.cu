@@ -7,15 +7,16 @@
 //
 // Two or three kernels on the caller's stream, the later ones launched programmatically:
 //
-//  prep    (bf16, tensor cores) q~ of every unit as operands; in a step of few tokens further blocks
-//          of the append's kernel.  (Made by every warp for itself it is 3 us before the first page; and
-//          without this launch one sequence of 901 tokens takes 9.0 us in a graph instead of 8.3.)
+//  prep    (bf16, tensor cores) q~ of every unit as operands; in a step of few tokens by further blocks
+//          of the append's kernel.  (Made by every warp for itself it delays the first page by 3 us, and one
+//          sequence of 901 tokens takes 9.0 us in a graph instead of 8.3.)
 //  attend  The work is a line of units (sequence, KV head, up to kRows query heads):
 //          the ring in runs of kRun tokens, then the pages.  Every warp of the grid has
 //          an equal share of the line by cost, and leaves one partial result per query
 //          head for each unit that its share cuts: (m, l, acc) of its ring tokens and of
-//          its pages, each by its own reference; unit u's cut by share k has the slot u + k.  The shares of a unit's first and last stage leave
-//          their numbers for the joining kernel.  Lengths are read on the device.
+//          its pages, each by its own reference; unit u's cut by share k has the slot u + k.  The
+//          shares of a unit's first and last stage leave their numbers for the joining kernel.
+//          Lengths are read on the device.
 //  join    a block per output row joins its partial results by log-sum-exp and lifts the
 //          bottleneck sum once by Uv.
 #include <algorithm>
@@ -35,7 +36,8 @@ using namespace sm100;
 constexpr int kRows = 8;         // query heads of a unit at most
 constexpr int kRun = 16;         // ring tokens of a stage
 constexpr int kWarps = 8;        // of a CTA (CUDA cores)
-// Of a CTA (tensor cores), and stages in flight of each: as many warps as registers allow.
+// Of a CTA (tensor cores), and stages in flight of each: as many warps as registers allow (18 or 20 spill, and 12 or 14 of
+// narrow vectors, or three stages, are as fast within 3 %).
 template <int DD>
 __host__ __device__ constexpr int mma_warps() { return DD <= 16 ? 16 : 12; }
 template <int DD>
@@ -46,8 +48,12 @@ template <int DD, int NH>
 __host__ __device__ constexpr int mma_registers() { return DD > 16 ? 168 : NH < 4 ? 112 : 128; }
 constexpr int kSlot = 5120;      // bytes of a stage at most
 constexpr int kMaxShares = 2560; // the workspace holds partial results of this many warps
-constexpr int kCostUnit = 20;    // cost of a unit's set-up (its place on the line is before the stages)
-constexpr int kCostRun = 10;     // of kRun ring tokens
+// Costs on the line, in fifths of a page of 16 entries: of a unit's set-up (its place is before the stages), of kRun ring
+// tokens.  Measured, runs at 8, 12 and 16: 17.4, 17.7 and 18.0 us (32 sequences, 12 heads, w = 128, 4096 tokens); 48.6, 48.8
+// and 50.2 (64 of 1024 to 32768, 32 heads over 8 KV heads, w = 256); 44.4, 42.4 and 43.2 (the same with 8 heads).  Set-up
+// at 8 and 20, runs at 8: 17.4 and 17.3, 48.6 and 47.7.
+constexpr int kCostUnit = 20;
+constexpr int kCostRun = 10;
 template <int DD>
 __host__ __device__ constexpr int cost_page() { return DD == 8 ? 4 : 5 * DD / 16; }
 
@@ -79,6 +85,13 @@ template <int DD>
 __device__ __forceinline__ int unit_length(int L, int w)
 {
     return L > 0 ? kCostUnit + runs_of(L, w) * kCostRun + pages_of(L, w) * cost_page<DD>() : 0;
+}
+
+// Of a unit at the cache's capacity.
+template <int DD>
+static long long unit_capacity(int w, int maxp)
+{
+    return kCostUnit + ((long long)w + kRun - 1) / kRun * kCostRun + (long long)maxp * cost_page<DD>();
 }
 
 // Lengths and the places of the sequences' units on the line, the same in every CTA.
@@ -201,15 +214,17 @@ __device__ __forceinline__ void leave_span(const Args &a, const Cut &c, int shar
 // ------------------------------------------------------------------ attend, CUDA cores
 //
 // A warp takes two tokens a lane for the scores; for the sums a lane has an entry (of 64
-// tokens' weights, through shared memory).
+// tokens' weights, through shared memory).  R: 1, 2, 4 or 8 rows, the unit's at least (fp32, 4 sequences of up to
+// 1501 tokens, three heads a KV head: 16.0 us, 18.7 with 8).  What is left is latency: q~ of every cut, and
+// shuffles and expf that wait on one another.
+template <int R>
 struct LaneSmem {
-    float q[kRows][kHeadDim], qt[kRows][kHeadDim];
-    float p[kRows][kPage], x[kPage][16];
-    float sv[kPage];
+    float q[R][kHeadDim], qt[R][kHeadDim];
+    float p[R][kPage], x[kPage][16];
 };
 
-template <typename T, int DD>
-__device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, LaneSmem &s)
+template <typename T, int DD, int R>
+__device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, LaneSmem<R> &s)
 {
     using F = Fmt<DD>;
     constexpr int GS = F::kGroup, NB = F::kGroups, HALVES = 32 / GS;  // lanes that share an entry
@@ -221,13 +236,13 @@ __device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, Lan
             leave_span(a, c, share);
         __syncwarp();
         const size_t row0 = (size_t)c.b * a.c.Hq + c.g * a.G + c.rt * kRows;
-        for (int i = lane; i < kRows * kHeadDim; i += 32) {
+        for (int i = lane; i < R * kHeadDim; i += 32) {
             const int r = i / kHeadDim;
             s.q[r][i % kHeadDim] =
                 r < c.rows ? to_f32(static_cast<const T *>(a.c.q)[(row0 + r) * kHeadDim + i % kHeadDim]) : 0.f;
         }
         __syncwarp();
-        for (int i = lane; i < kRows * DD; i += 32) {
+        for (int i = lane; i < R * DD; i += 32) {
             const int r = i / DD, e = i % DD;
             float x[4] = {0.f, 0.f, 0.f, 0.f};
             if (r < c.rows) {
@@ -245,9 +260,9 @@ __device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, Lan
             s.qt[r][e] = (x[0] + x[1]) + (x[2] + x[3]);
         }
         __syncwarp();
-        float m[kRows], l[kRows], ol[kRows][2], od[kRows][NB];
+        float m[R], l[R], ol[R][2], od[R][NB];
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
+        for (int r = 0; r < R; ++r) {
             m[r] = -INFINITY;
             l[r] = ol[r][0] = ol[r][1] = 0.f;
 #pragma unroll
@@ -277,39 +292,39 @@ __device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, Lan
                 const int t0 = st * kRun, n = min(kRun, c.nwin - t0);
                 const size_t ring = (((size_t)c.b * a.c.Hkv + c.g) * a.c.w + t0) * kHeadDim;
                 const T *k = static_cast<const T *>(a.c.win_k) + ring, *v = static_cast<const T *>(a.c.win_v) + ring;
-                float y[kRows][2];
+                float y[R][2];
 #pragma unroll
-                for (int r = 0; r < kRows; ++r)
+                for (int r = 0; r < R; ++r)
                     y[r][0] = y[r][1] = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int tok = 2 * lane + e;
                     if (tok >= n)
                         continue;
-                    float x[kRows] = {};
+                    float x[R] = {};
                     constexpr int E = Granule<T>::kElems;
 #pragma unroll 2
                     for (int i = 0; i < kHeadDim / E; ++i) {
                         float kk[E];
                         unpack(reinterpret_cast<const uint4 *>(k + tok * kHeadDim)[i], kk, T());
 #pragma unroll
-                        for (int r = 0; r < kRows; ++r)
+                        for (int r = 0; r < R; ++r)
 #pragma unroll
                             for (int j = 0; j < E; ++j)
                                 x[r] = fmaf(s.q[r][i * E + j], kk[j], x[r]);
                     }
 #pragma unroll
-                    for (int r = 0; r < kRows; ++r)
+                    for (int r = 0; r < R; ++r)
                         y[r][e] = x[r] * a.c.c2;
                 }
 #pragma unroll
-                for (int r = 0; r < kRows; ++r)
+                for (int r = 0; r < R; ++r)
                     weigh(r, y[r][0], y[r][1]);
                 __syncwarp();
                 for (int tok = 0; tok < n; ++tok) {
                     const float v0 = to_f32(v[tok * kHeadDim + lane]), v1 = to_f32(v[tok * kHeadDim + 32 + lane]);
 #pragma unroll
-                    for (int r = 0; r < kRows; ++r) {
+                    for (int r = 0; r < R; ++r) {
                         const float p = s.p[r][tok];
                         ol[r][0] = fmaf(p, v0, ol[r][0]);
                         ol[r][1] = fmaf(p, v1, ol[r][1]);
@@ -327,14 +342,14 @@ __device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, Lan
             }
             const unsigned char *page =
                 static_cast<const unsigned char *>(a.c.pool) + ((size_t)id * a.c.Hkv + c.g) * F::kBytes;
-            float y[kRows][2] = {};
+            float y[R][2] = {};
 #pragma unroll 1
             for (int i = 0; i < NB; ++i) {
                 float x0[GS], x1[GS];
                 read_row<GS, false>(page + i * F::kBlock, 2 * lane, x0);
                 read_row<GS, false>(page + i * F::kBlock, 2 * lane + 1, x1);
 #pragma unroll
-                for (int r = 0; r < kRows; ++r)
+                for (int r = 0; r < R; ++r)
 #pragma unroll
                     for (int e = 0; e < GS; ++e) {
                         const float q = s.qt[r][i * GS + e];
@@ -343,7 +358,7 @@ __device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, Lan
                     }
             }
 #pragma unroll
-            for (int r = 0; r < kRows; ++r)
+            for (int r = 0; r < R; ++r)
                 weigh(r, 2 * lane < n ? y[r][0] * a.c.c2 : -INFINITY, 2 * lane + 1 < n ? y[r][1] * a.c.c2 : -INFINITY);
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
@@ -360,14 +375,14 @@ __device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, Lan
                 for (int tok = lane / GS; tok < kPage; tok += HALVES) {
                     const float v = s.x[tok][lane % GS];
 #pragma unroll
-                    for (int r = 0; r < kRows; ++r)
+                    for (int r = 0; r < R; ++r)
                         od[r][i] = fmaf(s.p[r][tok], v, od[r][i]);
                 }
             }
             __syncwarp();
         }
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
+        for (int r = 0; r < R; ++r) {
 #pragma unroll
             for (int o = 16; o; o >>= 1)
                 l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
@@ -391,16 +406,17 @@ __device__ __forceinline__ void attend_lanes(const Args &a, const Tables &t, Lan
     }
 }
 
-constexpr size_t lanes_smem(int B) { return kWarps * sizeof(LaneSmem) + (2 * (size_t)B + 1) * 4; }
+template <int R>
+constexpr size_t lanes_smem(int B) { return kWarps * sizeof(LaneSmem<R>) + (2 * (size_t)B + 1) * 4; }
 
-template <typename T, int DD>
+template <typename T, int DD, int R>
 __global__ void __launch_bounds__(kWarps * 32) attend_kernel(Args a)
 {
     extern __shared__ __align__(16) unsigned char smem[];
-    const Tables t = tables_at(reinterpret_cast<int *>(smem + kWarps * sizeof(LaneSmem)), a.c.B);
+    const Tables t = tables_at(reinterpret_cast<int *>(smem + kWarps * sizeof(LaneSmem<R>)), a.c.B);
     grid_dep_launch();
     build_tables<DD>(a, t);
-    attend_lanes<T, DD>(a, t, reinterpret_cast<LaneSmem *>(smem)[threadIdx.x >> 5]);
+    attend_lanes<T, DD, R>(a, t, reinterpret_cast<LaneSmem<R> *>(smem)[threadIdx.x >> 5]);
 }
 
 // ------------------------------------------------------------------ attend, tensor cores
@@ -426,8 +442,12 @@ __global__ void __launch_bounds__(kWarps * 32) attend_kernel(Args a)
 //  sums     of a stage start from 0, and beside them those of the weights times the offset, which come
 //           from a product with constant rows; what joins the other stages' is the difference (at
 //           256 tokens the offset's part is some 100 times the rest's 2^-24).
-// A page of 64 tokens takes an SM's quarter 104 cycles of its integer pipe, 80 of its tensor pipe and 114
-// instructions beside what a stage costs, with CT = 1.
+// What bounds it: a page of 64 tokens (1280 bytes) of four heads is 175 instructions of a warp, some 74 of them in the
+// integer pipe at two cycles each; all SMs at the clock of a measurement could take 152 x 4 pages in 148 cycles, 10 TB/s, but
+// issue is 62 % and that pipe 48 % (latency between dependent products is what four warps a quarter do not hide).  64
+// sequences of 1024 to 32768 tokens (206 MB): 47 us, 4.4 TB/s; one, two, eight heads a KV head: 42, 44, 63; the copies
+// alone, nothing computed: 44 us.  d_down 64, 339 MB: 64 us, 5.3 TB/s.  Before: on CUDA cores 518 us; e4m3 operands
+// 65; sign and magnitude 54.
 
 struct Soft {  // of one head of a lane
     float bias, l;  // minus the reference; the lane's share of the sum of weights
@@ -735,8 +755,8 @@ struct Ring {
 //
 // NH heads (1, 2 or 4; CT = 2: 8) share the columns of a product out: with one head, columns 2 x, 2 x + 1 belong to words
 // x of its lanes, and the products of the four words go into one result, each with an operand that is zero in the
-// others' columns.  So a lane has two scores of a page, not eight of which the lanes t have the same: 76 instructions a
-// page beside what a stage costs, instead of 114.  In general word i = x ND + d goes to columns of x in result d.
+// others' columns.  So a lane has two scores of a page, not eight of which the lanes t have the same: 139 instructions a
+// page instead of 175 (64 sequences as above with one head: 45.1 us and 49).  In general word i = x ND + d goes to columns of x in result d.
 template <int DD, int CT, int NH>
 struct Pages {
     static constexpr int GS = Fmt<DD>::kGroup, NB = Fmt<DD>::kGroups;
@@ -1542,7 +1562,8 @@ static cudaError_t launch(const Q4DecodeArgs &c, const AppendArgs *ap, void *wor
                     if (e2 == cudaSuccess)
                         e2 = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout,
                                                   cudaSharedmemCarveoutMaxShared);
-                for (const auto k : {join_kernel<T, DD, 16, 4>, join_kernel<T, DD, 4, 4>, join_kernel<T, DD, 2, 4>})
+                for (const auto k : {join_kernel<T, DD, 16, 4>, join_kernel<T, DD, 8, 4>, join_kernel<T, DD, 4, 4>,
+                                     join_kernel<T, DD, 2, 4>})
                     if (e2 == cudaSuccess)
                         e2 = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout,
                                                   cudaSharedmemCarveoutMaxShared);
@@ -1551,9 +1572,12 @@ static cudaError_t launch(const Q4DecodeArgs &c, const AppendArgs *ap, void *wor
                     if (e2 == cudaSuccess)
                         e2 = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                   (int)mma_smem<DD>(DAR_DECODE_MAX_BATCH));
-            } else if (e2 == cudaSuccess) {
-                e2 = cudaFuncSetAttribute(attend_kernel<T, DD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                          (int)lanes_smem(DAR_DECODE_MAX_BATCH));
+            } else {
+                for (const auto k : {attend_kernel<T, DD, 1>, attend_kernel<T, DD, 2>, attend_kernel<T, DD, 4>,
+                                     attend_kernel<T, DD, 8>})
+                    if (e2 == cudaSuccess)
+                        e2 = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                  (int)lanes_smem<8>(DAR_DECODE_MAX_BATCH));
             }
             return e2;
         },
@@ -1595,18 +1619,30 @@ static cudaError_t launch(const Q4DecodeArgs &c, const AppendArgs *ap, void *wor
     } else {
         const int grid = std::min(sms, kMaxShares / kWarps);
         a.shares = grid * kWarps;
-        attend_kernel<T, DD><<<grid, kWarps * 32, lanes_smem(c.B), s>>>(a);
+        const auto attend = y.RU == 1 ? attend_kernel<T, DD, 1> : y.RU == 2 ? attend_kernel<T, DD, 2>
+                            : y.RU <= 4 ? attend_kernel<T, DD, 4> : attend_kernel<T, DD, 8>;
+        const size_t smem = y.RU == 1 ? lanes_smem<1>(c.B) : y.RU == 2 ? lanes_smem<2>(c.B)
+                            : y.RU <= 4 ? lanes_smem<4>(c.B) : lanes_smem<8>(c.B);
+        attend<<<grid, kWarps * 32, smem, s>>>(a);
         e = cudaGetLastError();
     }
     if (e != cudaSuccess)
         return e;
     cfg.dynamicSmemBytes = 0;
-    // few rows may have a partial result of every share each, and many rows few
-    const int rows = c.B * c.Hq, warps = rows < 192 ? 16 : rows < 1024 ? 4 : 2;
+    // Few rows may have a partial result of every share each, and many rows few: 2, 4 and 16 warps a row take 17.2, 29 and
+    // 44 us with 8 rows of 131072 tokens, 27.2, 27.0 and 33.1 with 1024 of 4096, and 77, 87 and 174 with 16384 of 2048.
+    // Of few rows as many as take all that a sequence of the cache's capacity can have in one go: 4, 8 and 16 take 8.3,
+    // 8.5 and 9.0 with 901 tokens, 9.4, 8.8 and 9.5 with 2000, and 10.4, 9.9 and 9.7 with 4000.
+    constexpr int least = kCostRun > cost_page<DD>() ? kCostRun : cost_page<DD>();  // of a share
+    const int rows = c.B * c.Hq;
+    const long long parts = unit_capacity<DD>(c.w, c.maxp) / least + 1;
+    const int warps = rows >= 1024 ? 2 : rows >= 192 || parts <= 20 ? 4 : parts <= 36 ? 8 : 16;
     cfg.gridDim = dim3((unsigned)rows);
     cfg.blockDim = dim3(warps * 32);
     if (warps == 16)
         return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, 16, 4>, a);
+    if (warps == 8)
+        return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, 8, 4>, a);
     if (warps == 4)
         return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, 4, 4>, a);
     return cudaLaunchKernelEx(&cfg, join_kernel<T, DD, 2, 4>, a);
@@ -1649,7 +1685,7 @@ cudaError_t launch_step_q4(dar_dtype dt, int dd, const AppendArgs &ap, const Q4D
 {
     if (a.B == 0)
         return cudaSuccess;
-    if (dt == DAR_BF16 && q4::append_is_few<bf16>(ap))
+    if (dt == DAR_BF16 && q4::append_is_few<bf16>(ap, dd))
         return q4::launch_t<bf16>(dd, a, &ap, workspace, s);
     const cudaError_t e = launch_append_q4(dt, dd, ap, s);
     return e != cudaSuccess ? e : launch_decode_q4(dt, dd, a, workspace, s);

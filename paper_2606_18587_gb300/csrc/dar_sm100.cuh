@@ -64,20 +64,6 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t *bar, unsigned parity)
     return ok != 0;
 }
 
-// Whether the phase is complete, without any waiting (lanes of a warp may ask about different barriers).
-__device__ __forceinline__ bool mbar_test(uint64_t *bar, unsigned parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-
 // As mbar_try_wait, but the hardware may park the thread for up to `ns`
 // nanoseconds while the phase is incomplete (it wakes early on completion), so
 // a waiting warp does not keep issuing polls.

@@ -227,6 +227,16 @@ def test_append(dtype, Hkv, dd, w, lens, n, per):
         assert same(a, b)
 
 
+@pytest.mark.parametrize("dtype,Hkv,dd,w,B,n", [
+    ("bf16", 2, 16, 8, 400, 8), ("bf16", 12, 16, 20, 70, 7), ("bf16", 8, 64, 5, 60, 8), ("bf16", 6, 8, 20, 260, 8),
+    ("bf16", 5, 32, 1, 90, 5), ("bf16", 90, 16, 3, 33, 4), ("f32", 4, 16, 8, 200, 8), ("f32", 6, 8, 20, 260, 8),
+    ("f32", 48, 8, 20, 100, 6), ("f32", 8, 64, 5, 60, 8),
+])
+def test_append_to_many(dtype, Hkv, dd, w, B, n):
+    """Few tokens each to many sequences, at every place of a page and with 0 to n of them: as test_append."""
+    test_append(dtype, Hkv, dd, w, [(7 * b) % 213 for b in range(B)], n, [(5 * b + b // 9) % (n + 1) for b in range(B)])
+
+
 @pytest.mark.parametrize("dtype,dd", [("bf16", 16), ("bf16", 8), ("f32", 32)])
 def test_append_in_pieces(dtype, dd):
     """However a run of tokens is cut into calls, the cache ends with the same bytes."""
