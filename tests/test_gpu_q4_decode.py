@@ -112,6 +112,20 @@ def test_scale_and_output():
     Q.check_outputs("bf16", Q.read_back(dar, c4), full, q, Uk, Uv, out, scale=0.3)
 
 
+@pytest.mark.parametrize("Hq", [2, 8, 16])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size,scale", [(1e-30, 0.125), (1e-30, 1e-30), (1.0, 1e-38), (1e-38, 1e-38), (0.0, 1e-38)])
+def test_scores_that_vanish(dtype, size, scale, Hq):
+    """Queries and scales whose product is no fp32 number: all weights are the same, and rows behind the last token
+    still have none."""
+    c, full = R.filled_cache(dar, 5, dtype, 2, 16, 20, [300, 21, 5])
+    c4 = Q.beside(dar, c)
+    dar.dar_cache_pack_q4(c, c4)
+    q, Uk, Uv = R.operands(6, dtype, 3, Hq, 2, 16)
+    q *= size
+    Q.check_outputs(dtype, Q.read_back(dar, c4), full, q, Uk, Uv, decode(c4, q, Uk, Uv, scale=scale), scale=scale)
+
+
 @pytest.mark.parametrize("std", [0.02, 12.0, 40.0])
 @pytest.mark.parametrize("Hq", [2, 16])
 def test_flat_and_peaked_scores(std, Hq):
