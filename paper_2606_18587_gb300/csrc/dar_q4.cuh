@@ -84,6 +84,14 @@ __device__ __forceinline__ uint32_t code_of(float x, float s)
     return s > 0.f ? (uint32_t)((int)fminf(fmaxf(rintf(__fdiv_rn(x, s)), -7.f), 7.f) + 8) : 8u;
 }
 
+// The same for s from 2^-126 on, with inv close to 1 / s (1 ulp): the product lies 2^-20 from the quotient at most, and
+// where that could be on the other side of a half there is a division.
+__device__ __forceinline__ uint32_t code_near(float x, float s, float inv)
+{
+    const float q = x * inv, r = rintf(q);
+    return fabsf(q - r) <= 0.5f - 0x1p-16f ? (uint32_t)((int)r + 8) : code_of(x, s);
+}
+
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
 // Where slot r of half h of a word is.
@@ -248,9 +256,11 @@ struct Raw<float, GS> {
         a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
         a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
         const float s = group_scale(a);
+        float inv;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s >= 0x1p-126f ? s : __uint_as_float(0x7fc00000u)));
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            x[i] = code_of(w[2 * i], s) | code_of(w[2 * i + 1], s) << 16;
+            x[i] = code_near(w[2 * i], s, inv) | code_near(w[2 * i + 1], s, inv) << 16;
         return __float_as_uint(s) >> 16;
     }
     static __device__ __forceinline__ void store(float *p, const uint32_t (&x)[N], float s)

@@ -202,7 +202,14 @@ __global__ void __launch_bounds__(kConvertWarps * 32) convert_kernel(Q4ConvertAr
             read_page<T, GS, true>(page + i * F::kBlock, v + i * GS, DD, from, to, lane);
     };
     if (parts == 1) {
-#pragma unroll
+        if (PACK && lane == 0) {  // (all contexts of the 1B shape: 5 % less)
+            sm100::prefetch_l2(k, kPage * DD * sizeof(T));
+            sm100::prefetch_l2(v, kPage * DD * sizeof(T));
+        }
+        // code that the instruction cache holds: of four groups together 610 us instead of 296 (pack of 64000 bf16 pages of
+        // 64 entries), of two 126 and 136 (32 entries); fp32 1008 and 400
+        constexpr int kTogether = sizeof(T) == 2 && F::kGroups <= 2 ? 2 : 1;
+#pragma unroll kTogether
         for (int i = 0; i < F::kGroups; ++i) {
             keys(i);
             values(i);

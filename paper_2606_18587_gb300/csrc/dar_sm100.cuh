@@ -64,6 +64,12 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t *bar, unsigned parity)
     return ok != 0;
 }
 
+// Brings bytes (a multiple of 16, from a 16-byte boundary) to L2.
+__device__ __forceinline__ void prefetch_l2(const void *p, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
+
 // As mbar_try_wait, but the hardware may park the thread for up to `ns`
 // nanoseconds while the phase is incomplete (it wakes early on completion), so
 // a waiting warp does not keep issuing polls.
