@@ -770,8 +770,8 @@ struct Pages {
     Soft page[CT];
     float od[NB][2 * CT];    // times 2^-24, entries e of the heads and then e + 2 (see Sums)
 
-    // Words of a lane that the first kernel leaves of a unit, [unit][word][lane].
-    static constexpr int kWords = NB * (TB * 2 + 2) + CT;
+    // Words of a lane that the first kernel leaves of a unit, [unit][word][lane]: of its groups, and the factors.
+    static constexpr int kGroupWords = TB * 2 + 2, kWords = NB * kGroupWords + CT;
     template <typename F>
     __device__ __forceinline__ void each_word(const F &f)
     {
@@ -790,10 +790,16 @@ struct Pages {
         for (int k = 0; k < CT; ++k)
             f(i++, cq[k]);
     }
-    __device__ __forceinline__ void save(const Args &a, int unit, int lane)
+    // As group j of n.
+    __device__ __forceinline__ void save(const Args &a, int unit, int j, int n, int lane)
     {
-        uint32_t *p = a.prep + (size_t)unit * kWords * 32 + lane;
-        each_word([&](int i, auto &x) { p[i * 32] = *reinterpret_cast<const uint32_t *>(&x); });
+        static_assert(NB == 1, "a group");
+        uint32_t *p = a.prep + (size_t)unit * (n * kGroupWords + CT) * 32 + lane;
+        each_word([&](int i, auto &x) {
+            const int at = i < kGroupWords ? j * kGroupWords + i : n * kGroupWords + (i - kGroupWords);
+            if (i < kGroupWords || j == 0)
+                p[at * 32] = *reinterpret_cast<const uint32_t *>(&x);
+        });
     }
     __device__ __forceinline__ void load(const Args &a, int unit, int lane)
     {
@@ -821,14 +827,17 @@ struct Pages {
                 od[j][o] = 0.f;
     }
 
-    // q~^T = Uk q^T with Uk in three bf16 terms (products exact but for 2^-24).
-    __device__ __forceinline__ void make(const Args &a, const Cut &c, const uint32_t (&q)[4][2], int lane)
+    // q~^T = Uk q^T of a group's rows uk, with Uk in three bf16 terms (products exact but for 2^-24).  most: takes the
+    // largest magnitudes of the group's entries to those of all groups'.
+    template <typename F>
+    __device__ __forceinline__ void make(const Args &a, const float *uk, const uint32_t (&q)[4][2], int lane, const F &most)
     {
+        static_assert(NB == 1, "a group");
         const int i0 = lane >> 2, c0 = lane & 3;
         float x[NB][4];  // entries 16 j + i0 (+ 8) of heads c0 mod NH, and + 4: [0] i0 c0, [1] i0 c0 + 4, [2], [3] i0 + 8
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            const float *u = a.c.Uk + ((size_t)c.g * DD + 16 * j + i0) * kHeadDim + 2 * c0;
+            const float *u = uk + i0 * kHeadDim + 2 * c0;
             float z[3][4] = {};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -852,15 +861,18 @@ struct Pages {
         }
         // the largest entry of each head, and the power of two that brings it to [2^14, 2^15)
         float up[CT];
+        uint32_t tops[CT];
 #pragma unroll
         for (int k = 0; k < CT; ++k) {
-            uint32_t top = 0u;
-#pragma unroll
-            for (int j = 0; j < NB; ++j)
-                top = max(top, max(magnitude(x[j][k]), magnitude(x[j][2 + k])));
+            tops[k] = max(magnitude(x[0][k]), magnitude(x[0][2 + k]));
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1)
-                top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                tops[k] = max(tops[k], __shfl_xor_sync(0xffffffffu, tops[k], o));
+        }
+        most(tops);
+#pragma unroll
+        for (int k = 0; k < CT; ++k) {
+            const uint32_t top = tops[k];
             const int e = max((int)(top >> 23) - 127, -100);
             up[k] = __uint_as_float((uint32_t)(127 + 14 - e) << 23);  // e <= 127: 2^-113 at least
             // infinite or NaN: so are all scores.  Not 0: no token's score is minus infinity before it is multiplied
@@ -1267,10 +1279,17 @@ struct Pages {
     }
 };
 
-// q~ of every unit, a warp each, as the next kernel's lanes want it.
-template <int DD, int CT, int NH>
-__device__ __forceinline__ void prep_unit(const Args &a, int unit, int lane)
+// q~ of the units from `first` on, a warp for each group of 16 entries, as the next kernel's lanes want it; all threads of
+// a block of WARPS warps.  (A warp for all four groups of 64 entries takes 5 us, during which it keeps attending blocks off
+// its SM.)
+template <int DD, int CT, int NH, int WARPS>
+__device__ __forceinline__ void prep_units(const Args &a, int first, int units)
 {
+    constexpr int NB = Fmt<DD>::kGroups;
+    using Group = Pages<(DD < 16 ? DD : 16), CT, NH>;
+    __shared__ uint32_t tops[WARPS][CT][4];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j = warp % NB;
+    const int unit = min(first + warp / NB, units - 1);  // (the last one once more)
     Cut c;
     c.b = unit / (a.c.Hkv * a.RT);
     c.g = unit / a.RT % a.c.Hkv;
@@ -1278,31 +1297,50 @@ __device__ __forceinline__ void prep_unit(const Args &a, int unit, int lane)
     c.rows = min(kRows, a.G - c.rt * kRows);
     uint32_t q[4][2];
     queries_of<NH>(a, c, lane, q);
-    Pages<DD, CT, NH> h;
-    h.make(a, c, q, lane);
-    h.save(a, unit, lane);
+    Group h;
+    h.make(a, a.c.Uk + ((size_t)c.g * DD + 16 * j) * kHeadDim, q, lane, [&](uint32_t (&top)[CT]) {
+        if constexpr (NB > 1) {
+#pragma unroll
+            for (int k = 0; k < CT; ++k)
+                if (lane < 4)
+                    tops[warp][k][lane] = top[k];
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < CT; ++k)
+#pragma unroll
+                for (int i = 0; i < NB; ++i)
+                    top[k] = max(top[k], tops[warp - j + i][k][lane & 3]);
+        }
+    });
+    if (first + warp / NB < units)
+        h.save(a, unit, j, NB, lane);
 }
 
 constexpr int kPrepWarps = 4;
+template <int DD, int WARPS>
+static int prep_blocks(int units)
+{
+    constexpr int per = WARPS / Fmt<DD>::kGroups;
+    return (units + per - 1) / per;
+}
+
 template <int DD, int CT, int NH>
 __global__ void __launch_bounds__(kPrepWarps * 32) prep_kernel(const Args a, int units)
 {
     grid_dep_launch();
-    const int unit = blockIdx.x * kPrepWarps + (threadIdx.x >> 5);
-    if (unit < units)
-        prep_unit<DD, CT, NH>(a, unit, threadIdx.x & 31);
+    prep_units<DD, CT, NH, kPrepWarps>(a, (int)blockIdx.x * (kPrepWarps / Fmt<DD>::kGroups), units);
 }
 
 // The first kernel of a step of few tokens: the append's blocks, and the same.
 template <int DD, int CT, int NH>
 __global__ void __launch_bounds__(kFewThreads) front_kernel(AppendArgs ap, const Args a, int units)
 {
+    constexpr int kPer = kFewThreads / 32;
     grid_dep_launch();
-    const int unit = ((int)blockIdx.x - ap.B) * (kFewThreads / 32) + (int)(threadIdx.x >> 5);
     if ((int)blockIdx.x < ap.B)
         append_few<bf16, DD>(ap);
-    else if (unit < units)
-        prep_unit<DD, CT, NH>(a, unit, threadIdx.x & 31);
+    else
+        prep_units<DD, CT, NH, kPer>(a, ((int)blockIdx.x - ap.B) * (kPer / Fmt<DD>::kGroups), units);
 }
 
 template <int DD>
@@ -1603,11 +1641,10 @@ static cudaError_t launch(const Q4DecodeArgs &c, const AppendArgs *ap, void *wor
         if (ap) {
             const auto front = y.RU == 1 ? front_kernel<DD, 1, 1> : y.RU == 2 ? front_kernel<DD, 1, 2>
                                : y.RU <= 4 ? front_kernel<DD, 1, 4> : front_kernel<DD, 2, 4>;
-            constexpr int per = kFewThreads / 32;
-            front<<<ap->B + (units + per - 1) / per, kFewThreads, few_smem<T>(ap->Hkv), s>>>(*ap, a, units);
+            front<<<ap->B + prep_blocks<DD, kFewThreads / 32>(units), kFewThreads, few_smem<T>(ap->Hkv), s>>>(*ap, a, units);
             e = cudaGetLastError();
         } else {
-            prep<<<(units + kPrepWarps - 1) / kPrepWarps, kPrepWarps * 32, 0, s>>>(a, units);
+            prep<<<prep_blocks<DD, kPrepWarps>(units), kPrepWarps * 32, 0, s>>>(a, units);
             e = cudaGetLastError();
         }
         if (e != cudaSuccess)
