@@ -345,6 +345,8 @@ dar_status convert_q4(const dar_cache *t, const dar_cache_q4 *c, bool pack, cons
     if (t->dtype != c->dtype || t->B != c->B || t->Hkv != c->Hkv || t->d_down != c->d_down || t->w != c->w)
         return fail(DAR_ERR_INVALID_ARG, "the caches differ: dtype %d/%d B=%d/%d Hkv=%d/%d d_down=%d/%d w=%d/%d",
                     t->dtype, c->dtype, t->B, c->B, t->Hkv, c->Hkv, t->d_down, c->d_down, t->w, c->w);
+    if (t->B > 65535)
+        return fail(DAR_ERR_UNSUPPORTED, "batch %d > 65535", t->B);
     const int pages = t->max_pages_per_seq < c->max_pages_per_seq ? t->max_pages_per_seq : c->max_pages_per_seq;
     if ((double)pages * t->Hkv >= 2147483647.0)
         return fail(DAR_ERR_UNSUPPORTED, "%d pages of %d heads a sequence are too many blocks", pages, t->Hkv);

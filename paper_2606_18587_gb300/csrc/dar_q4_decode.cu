@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(kWarps * 32) attend_kernel(Args a)
 // integer pipe at two cycles each; all SMs at the clock of a measurement could take 152 x 4 pages in 148 cycles, 10 TB/s, but
 // issue is 62 % and that pipe 48 % (latency between dependent products is what four warps a quarter do not hide).  64
 // sequences of 1024 to 32768 tokens (206 MB): 47 us, 4.4 TB/s; one, two, eight heads a KV head: 42, 44, 63; the copies
-// alone, nothing computed: 44 us.  d_down 64, 339 MB: 64 us, 5.3 TB/s.  Before: on CUDA cores 518 us; e4m3 operands
+// alone, nothing computed: 44 us.  d_down 64, 339 MB: 62 us, 5.5 TB/s.  Before: on CUDA cores 518 us; e4m3 operands
 // 65; sign and magnitude 54.
 
 struct Soft {  // of one head of a lane

@@ -93,6 +93,13 @@ def test_convert_refuses(lib):
     assert L.dar_cache_unpack_q4(None, None, ctypes.byref(plain(lib)), None) == 1
 
 
+def test_convert_refuses_a_batch_beyond_a_grid(lib):
+    L, big = lib.load_library(), dict(B=65536)
+    t, c = plain(lib, **big), cache(lib, **big)
+    assert L.dar_cache_pack_q4(ctypes.byref(t), None, ctypes.byref(c), None) == 2
+    assert L.dar_cache_unpack_q4(ctypes.byref(c), None, ctypes.byref(t), None) == 2
+
+
 def test_decode_refuses(lib):
     L = lib.load_library()
 
