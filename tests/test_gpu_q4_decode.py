@@ -242,3 +242,31 @@ def test_step_equals_append_and_decode(dtype, n, per):
     assert torch.equal(got, want) and torch.equal(a.pool, b.pool) and torch.equal(a.seq_lens, b.seq_lens)
     assert a.device_status() == 0 and b.device_status() == 0
     Q.check_outputs(dtype, Q.read_back(dar, b), full, q, Uk, Uv, got)
+
+
+@pytest.mark.parametrize("dd", [8, 16, 32, 64])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (6, 3), (6, 2), (10, 2), (17, 1)])
+def test_step_of_one_token(dd, Hq, Hkv):
+    """Every width and number of heads, and units that leave warps of the first kernel over."""
+    lens, w = [300, 0, 39, 168, 40], 40
+    c, full = R.filled_cache(dar, 2, "bf16", Hkv, dd, w, [L + 1 for L in lens])
+    c.seq_lens.copy_(ints(lens))
+    a, b = (dar.DarCacheQ4(5, Hkv, dd, w, c.max_pages_per_seq, c.num_pages, block_table=c.block_table.cpu())
+            for _ in range(2))
+    for x in (a, b):
+        x.pool.random_(0, 256)
+        for t, u in ((x.win_k, c.win_k), (x.win_v, c.win_v), (x.seq_lens, c.seq_lens)):
+            t.copy_(u)
+        dar.dar_cache_pack_q4(c, x)
+    b.pool.copy_(a.pool)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn((5, Hkv, 1, 64), device="cuda", generator=g).bfloat16() for _ in range(2))
+    Dk, Dv = (torch.randn((Hkv, 64, dd), device="cuda", generator=g) / 8 for _ in range(2))
+    q, Uk, Uv = R.operands(4, "bf16", 5, Hq, Hkv, dd)
+    dar.dar_cache_append_q4(a, k, v, Dk, Dv)
+    want = decode(a, q, Uk, Uv)
+    got = dar.dar_decode_step_q4(b, k, v, Dk, Dv, q, Uk, Uv, dar.decode_q4_workspace(b, Hq))
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(a.pool, b.pool) and torch.equal(a.seq_lens, b.seq_lens)
+    assert a.device_status() == 0 and b.device_status() == 0
+    Q.check_outputs("bf16", Q.read_back(dar, b), full, q, Uk, Uv, got)
