@@ -1209,7 +1209,10 @@ struct Pages {
             scales(vm[k / CT], k, s0, s1);
             top = max3(top, p[k][0] * s0, p[k][1] * s1);
         }
-        if (__any_sync(0xffffffffu, fmaxf(l[0], l[1]) > kFarSum || top > kFar)) {
+        // without a reference yet these weights are infinite, or NaN in rows that do not count: the first one is not read off
+        // them (sums of both kinds of rows are NaN, and so is an infinite weight times a scale of 0)
+        const bool unset = page[0].bias == INFINITY || page[CT - 1].bias == INFINITY;
+        if (__any_sync(0xffffffffu, unset || fmaxf(l[0], l[1]) > kFarSum || top > kFar)) {
 #pragma unroll
             for (int k = 0; k < CT; ++k) {
                 top = -INFINITY;  // of p s_v, and of 2^-80 p
