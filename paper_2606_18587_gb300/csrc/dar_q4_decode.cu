@@ -1209,10 +1209,9 @@ struct Pages {
             scales(vm[k / CT], k, s0, s1);
             top = max3(top, p[k][0] * s0, p[k][1] * s1);
         }
-        // without a reference yet these weights are infinite, or NaN in rows that do not count: the first one is not read off
-        // them (sums of both kinds of rows are NaN, and so is an infinite weight times a scale of 0)
-        const bool unset = page[0].bias == INFINITY || page[CT - 1].bias == INFINITY;
-        if (__any_sync(0xffffffffu, unset || fmaxf(l[0], l[1]) > kFarSum || top > kFar)) {
+        // Without a reference yet the weights of rows that count are infinite and the others' NaN, and so is each of a lane's
+        // sums (top may miss it: an infinite weight times a scale of 0): what is not known to be small asks for one.
+        if (__any_sync(0xffffffffu, !(l[0] <= kFarSum && l[1] <= kFarSum && top <= kFar))) {
 #pragma unroll
             for (int k = 0; k < CT; ++k) {
                 top = -INFINITY;  // of p s_v, and of 2^-80 p
