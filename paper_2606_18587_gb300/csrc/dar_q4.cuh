@@ -328,6 +328,19 @@ __device__ __forceinline__ void even_codes(const Raw<T, GS> (&raw)[2], int from,
     }
 }
 
+// Writes the bits `mask` of a word of codes.  Sequences that list a page together write rows of the same word at the same
+// time, each those that it has: two atomic operations on its own bits lose nobody's (bits of a row that two of them have
+// come out alike in any order, since both write the same).
+__device__ __forceinline__ void put_word(uint32_t *p, uint32_t x, uint32_t mask)
+{
+    if (mask == ~0u) {
+        *p = x;
+    } else if (mask) {
+        atomicAnd(p, x | ~mask);
+        atomicOr(p, x & mask);
+    }
+}
+
 // Quantises rows [first, end) of a page into a block; row r's entries are at vec + r * stride.
 template <typename T, int GS, bool VALUES>
 __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, int stride, int first, int end, int lane)
@@ -397,8 +410,7 @@ __device__ __forceinline__ void write_page(unsigned char *block, const T *vec, i
                 const int row = row0 + (GS == 16 ? 4 : 8) * i + word_row<GS, VALUES>(VALUES ? 0 : 4 * (g & 1), r, h);
                 mask |= row >= first && row < end ? 15u << slot_shift(r, h) : 0u;
             }
-        if (mask)
-            words[i] = (words[i] & ~mask) | (w[GS == 16 ? i : 2 * i + 1] & mask);
+        put_word(words + i, w[GS == 16 ? i : 2 * i + 1], mask);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
