@@ -322,6 +322,8 @@ size_t dar_q4_page_bytes(int32_t d_down);
 /*
  * As dar_cache_append, with the vectors of the tokens that leave the window held in 4
  * bits.  Tokens of a page that were there before keep their codes.
+ * Several sequences may list a page and write it in one call, other tokens or the same
+ * ones (of which all write the same).
  */
 dar_status dar_cache_append_q4(const dar_cache_q4 *cache, const void *k_new, const void *v_new,
                                int32_t n, const int32_t *n_per_seq, const float *Dk,

@@ -78,9 +78,8 @@ struct FewWords {
             return;
         const int row0 = row & ~(GS == 16 ? 3 : 7);
         auto put = [&](int j, uint32_t x, uint32_t mask) {
-            uint32_t *p = reinterpret_cast<uint32_t *>(
-                block + (values ? kPage * GS / 2 + word_offset<GS, true>(row0, j) : word_offset<GS, false>(row0, j)));
-            *p = (*p & ~mask) | x;
+            put_word(reinterpret_cast<uint32_t *>(block + (values ? kPage * GS / 2 + word_offset<GS, true>(row0, j)
+                                                                  : word_offset<GS, false>(row0, j))), x, mask);
         };
         if (block) {
             if (values) {

@@ -97,3 +97,35 @@ def test_append_of_many_tokens(dtype, Hkv, dd):
     B, n = 48, 70
     lens = [(29 * b) % (W + 64 * PAGES - n + 1) for b in range(B)]
     appended(dtype, B, Hkv, dd, n, lens, [n - (5 * b) % 23 for b in range(B)])
+
+
+@pytest.mark.parametrize("dtype,B,Hkv,dd,n", [
+    ("bf16", 64, 2, 16, 3), ("bf16", 400, 2, 16, 8), ("bf16", 260, 6, 8, 8), ("bf16", 64, 1, 64, 2), ("bf16", 90, 5, 32, 5),
+    ("f32", 200, 4, 16, 8), ("f32", 64, 1, 8, 2),
+])
+def test_append_of_few_tokens(dtype, B, Hkv, dd, n):
+    """Sequences one or a few tokens apart, which write neighbouring rows of the same words."""
+    lens = [W + 30 + b % 7 + 64 * (b // 7 % 2) for b in range(B)]
+    appended(dtype, B, Hkv, dd, n, lens, [n - b % 3 % n for b in range(B)])
+
+
+@pytest.mark.parametrize("dd,Hq", [(16, 2), (16, 16), (8, 8), (64, 8)])
+def test_steps_of_sequences_that_share(dd, Hq):
+    """Steps of sequences a token or two apart on one text: each attends as one that has the pages to itself."""
+    B, Hkv, n = 12, 2, 1
+    lens = [W + 37 + b % 4 for b in range(B)]
+    g = torch.Generator(device="cuda").manual_seed(8)
+    text = [torch.randn((Hkv, W + 64 * PAGES, 64), device="cuda", generator=g).bfloat16() for _ in range(2)]
+    Dk, Dv = (torch.randn((Hkv, 64, dd), device="cuda", generator=g) / 8 for _ in range(2))
+    both = []
+    for table in (torch.tensor([[2, 0, 1]], dtype=torch.int32).repeat(B, 1), None):
+        c4 = dar.DarCacheQ4(B, Hkv, dd, W, PAGES, B * PAGES, block_table=table)
+        dar.dar_cache_append_q4(c4, *[t[None, :, :max(lens)].repeat(B, 1, 1, 1) for t in text], Dk, Dv,
+                                n_per_seq=ints(lens))
+        both.append((c4, dar.decode_q4_workspace(c4, Hq)))
+    q, Uk, Uv = R.operands(3, "bf16", B, Hq, Hkv, dd)
+    for i in range(40):
+        new = [torch.stack([t[:, L + i:L + i + 1] for L in lens]) for t in text]
+        a, b = (dar.dar_decode_step_q4(c4, *new, Dk, Dv, q, Uk, Uv, ws) for c4, ws in both)
+        assert torch.equal(a, b), i
+    assert all(c4.device_status() == 0 for c4, _ in both)
