@@ -367,8 +367,9 @@ dar_status dar_attn_decode_q4(const dar_cache_q4 *cache, int32_t Hq, const void 
 /*
  * One serving step: dar_cache_append_q4 and then dar_attn_decode_q4, with the arguments,
  * requirements and results of the two calls in turn; all arguments of both are checked
- * before anything is launched.  Of up to eight tokens a sequence (bf16) it is a launch less:
- * the query-side set-up runs beside the append, which writes neither q nor Uk.
+ * before anything is launched.  Of few tokens (bf16; one or two a sequence, and up to eight
+ * the more sequences there are) it is a launch less: the query-side set-up runs beside the
+ * append, which writes neither q nor Uk.  Of more it is the launches of both calls.
  */
 dar_status dar_decode_step_q4(const dar_cache_q4 *cache, const void *k_new, const void *v_new, int32_t n,
                               const int32_t *n_per_seq, const float *Dk, const float *Dv, int32_t Hq,
