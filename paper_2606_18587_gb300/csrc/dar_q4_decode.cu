@@ -435,10 +435,12 @@ __global__ void __launch_bounds__(kWarps * 32) attend_kernel(Args a)
 //           the second one is the other column's.  CT = 2: a product of its own.  A d_down of 8:
 //           the two halves of a product's 16 entries.  The sum starts from
 //           minus 8 times theirs.  Rows with c = 1 are in slots 1 and 3: their scores are 16 times as large.
-//  weights  p s_v as fp16 (2^-11) relative to a reference of the row that keeps the largest at
-//           2^8 when it is set.  It is raised where a weight overflows, which shows in the sums of a stage:
-//           the stage is done again, page by page with the weights looked at first.  (bf16 operands need
-//           two terms for the same error, twice the conversions and transpositions.)
+//  weights  p s_v as fp16 (2^-11) relative to a reference of the row, one for all groups, that keeps the
+//           largest at 2^8 when it is set: half a step of the smallest fp16 numbers is 2^-33 of that one, and
+//           what lies 2^-22 below it has fewer bits (a group of much smaller values too).  It is raised where a
+//           weight overflows, which shows in the sums of a stage: the stage is done again, page by page with the
+//           weights looked at first.  (bf16 operands need two terms for the same error, twice the conversions
+//           and transpositions; a reference of each group, a multiplication for each weight.)
 //  sums     of a stage start from 0, and beside them those of the weights times the offset, which come
 //           from a product with constant rows; what joins the other stages' is the difference (at
 //           256 tokens the offset's part is some 100 times the rest's 2^-24).
