@@ -355,7 +355,8 @@ dar_status dar_cache_unpack_q4(const dar_cache_q4 *src, const int32_t *first, co
  * more 2^-33 of the row's largest such product: a product 2^-22 of the largest one, of
  * whatever token and group, begins to lose bits).  That holds for pages whose values lie
  * between 2^-77 and 2^100 in magnitude (0 aside); at 2^-90 the 2^-33 are 2^-20, and farther
- * off weights lose more.  Arguments, alignment (pool too), limits and errors as
+ * off weights lose more.  Scores lie within 2^25 in magnitude; of larger ones out may be
+ * NaN.  Arguments, alignment (pool too), limits and errors as
  * dar_attn_decode, and Hkv * dar_q4_page_bytes(d_down) < 2^31; workspace of
  * dar_decode_q4_workspace_bytes(cache, Hq) bytes, no initialisation; calls that share one
  * must not overlap on the device.  Three kernels (fp32: two) in order on `stream`, the

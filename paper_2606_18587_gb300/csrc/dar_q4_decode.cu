@@ -877,9 +877,11 @@ struct Pages {
             const uint32_t top = tops[k];
             const int e = max((int)(top >> 23) - 127, -100);
             up[k] = __uint_as_float((uint32_t)(127 + 14 - e) << 23);  // e <= 127: 2^-113 at least
-            // infinite or NaN: so are all scores.  Not 0: no token's score is minus infinity before it is multiplied
-            cq[k] = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u)
-                                       : fmaxf(a.c.c2 * __uint_as_float((uint32_t)(127 + e) << 23) * 1024.f, 0x1p-120f);
+            // infinite or NaN: so are all scores.  Not 0: no token's score is minus infinity before it is multiplied.  Nor
+            // infinite: the scores of keys of zero stay 0
+            cq[k] = top >= 0x7f800000u
+                        ? __uint_as_float(0x7fc00000u)
+                        : fminf(fmaxf(a.c.c2 * __uint_as_float((uint32_t)(127 + e) << 23) * 1024.f, 0x1p-120f), 0x1p126f);
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 x[j][k] *= up[k];

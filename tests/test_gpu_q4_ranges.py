@@ -49,3 +49,37 @@ def test_groups_far_apart(dtype, dd, Hq, step):
                 tol[h] += n * 7 * 2.0 ** -33 * largest * Uv[g].cpu().double().abs().sum(0)
         err = (got[b].cpu().double() - out).abs()
         assert (err <= tol).all(), (b, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("Hq", [2, 4, 16])
+@pytest.mark.parametrize("dtype,dd", [("bf16", 8), ("bf16", 16), ("bf16", 64), ("f32", 16)])
+@pytest.mark.parametrize("size,scale,best", [
+    (1e30, 0.125, None), (1e36, 0.125, None), (1e30, 1e7, None), (1e3, 1e34, None),
+    (1e5, 0.125, 5), (1e-5, 1e9, 5), (3e4, 0.4, 5),
+])
+def test_large_queries(dtype, dd, Hq, size, scale, best):
+    """Queries times scale up to 2^125: keys of zero have equal weights.  Scores of up to 2^25: the one token whose score
+    is positive, the others' being its negative, has all of the weight."""
+    w, lens = 20, [300, 33, 84]
+    c, full = R.filled_cache(dar, 3, dtype, 2, dd, w, lens)
+    q, Uk, Uv = R.operands(4, dtype, 3, Hq, 2, dd)
+    q = q.abs().clamp(0.25, 2.0).mul(size).contiguous()
+    Uk = Uk.abs() + 0.1
+    key = 0.0 if best is None else -1.0
+    c.pool_kd.copy_(torch.where(c.pool_kd.isnan(), c.pool_kd, key))
+    c.win_k.copy_(torch.where(c.win_k.isnan(), c.win_k, key))
+    if best is not None:
+        for b in range(3):
+            c.pool_kd[full[b][0], :, best] = 1.0
+    c4 = Q.beside(dar, c)
+    dar.dar_cache_pack_q4(c, c4)
+    back = Q.read_back(dar, c4)
+    got = decode(c4, q, Uk, Uv, scale=scale)
+    for b in range(3):
+        out, _, mag, top = R.attend(q[b].cpu().double(), *R.contents(back, full, b), Uk.cpu().double(),
+                                    Uv.cpu().double(), scale)
+        assert top < 2.0 ** 25
+        # equal scores are exactly equal, and the others are so far apart that errors of theirs change no weight
+        tol = Q.tolerances(dtype, out, mag, 0.0)
+        err = (got[b].cpu().double() - out).abs()
+        assert (err <= tol).all(), (b, float((err / tol).max()))
