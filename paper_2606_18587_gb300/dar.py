@@ -439,7 +439,7 @@ class DarCacheQ4:
     :class:`DarCache`; ``pool`` is uint8 ``[num_pages, Hkv, dar_q4_page_bytes(d_down)]``.
 
     ``share`` (a :class:`DarCache` of the same sizes): its ring, block table, lengths and status word are this
-    cache's too (see :meth:`beside`)."""
+    cache's too, and the pool lies on its device (see :meth:`beside`)."""
 
     def __init__(self, B, Hkv, d_down, w, max_pages_per_seq, num_pages=None, dtype=torch.bfloat16,
                  block_table=None, device="cuda", d=64, share=None):
@@ -452,6 +452,15 @@ class DarCacheQ4:
         nbytes = dar_q4_page_bytes(d_down)
         if nbytes == 0:
             raise DarError(DAR_ERR_UNSUPPORTED, f"d_down={d_down} (built: 8, 16, 32, 64)")
+        if share is not None:
+            mine, theirs = ((dtype, B, Hkv, d, w, max_pages_per_seq),
+                            (share.dtype, share.B, share.Hkv, share.d, share.w, share.max_pages_per_seq))
+            if mine != theirs:
+                raise ValueError(f"the shared cache has other sizes: dtype, B, Hkv, d, w, max_pages_per_seq {theirs}, "
+                                 f"not {mine}")
+            if block_table is not None:
+                raise ValueError("a shared cache has its own block table")
+            device = share.win_k.device
         self.pool = torch.zeros((max(num_pages, 1), Hkv, nbytes), dtype=torch.uint8, device=device)
         if share is not None:
             self.win_k, self.win_v = share.win_k, share.win_v
