@@ -471,6 +471,9 @@ class DarCacheQ4:
             if block_table is None:
                 block_table = torch.arange(B * max_pages_per_seq, dtype=torch.int32).reshape(B, max_pages_per_seq)
             self.block_table = torch.as_tensor(block_table, dtype=torch.int32).to(device).contiguous()
+            if self.block_table.numel() < B * max_pages_per_seq:
+                raise ValueError(f"block_table has shape {tuple(self.block_table.shape)}, expected "
+                                 f"{(B, max_pages_per_seq)}")
             if self.block_table.numel() == 0:
                 self.block_table = torch.full((max(B, 1), 1), -1, dtype=torch.int32, device=device)
             self.seq_lens = torch.zeros(B, dtype=torch.int32, device=device)

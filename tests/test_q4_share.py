@@ -1,5 +1,5 @@
-"""A cache in 4 bits that shares an ordinary one's ring, table and lengths takes no other sizes: the kernels would read
-and write beyond what is shared."""
+"""A cache in 4 bits takes only a ring, table and lengths of its own sizes, shared or its own: the kernels would read and
+write beyond smaller ones."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -32,3 +32,13 @@ def test_refuses_other_sizes(dar, kw):
     dar.DarCacheQ4(**args)
     with pytest.raises(ValueError):
         dar.DarCacheQ4(**{**args, **kw})
+
+
+def test_refuses_a_short_block_table(dar):
+    """Every sequence has max_pages_per_seq entries, which kernels read."""
+    for shape in ((3, 3), (2, 4), (0,)):
+        with pytest.raises(ValueError):
+            dar.DarCacheQ4(3, 2, 16, 8, 4, block_table=torch.zeros(shape, dtype=torch.int32), device="cpu")
+    dar.DarCacheQ4(3, 2, 16, 8, 4, block_table=torch.zeros((3, 4), dtype=torch.int32), device="cpu")
+    dar.DarCacheQ4(3, 2, 16, 8, 0, block_table=torch.zeros((3, 0), dtype=torch.int32), num_pages=1, device="cpu")
+    dar.DarCacheQ4(0, 2, 16, 8, 4, device="cpu")
