@@ -19,7 +19,7 @@
 //   row      r of a page is token 4 i + 2 c + o of 16 t ..: t = r / 16, i = r / 4 mod 4, c = r / 2 mod 2, o = r mod 2
 //   keys     lane (g, u) = 4 g + u has rows with 2 t + o = g: word i, slots c and 2 + c, are
 //            entries 4 u, 4 u + 1 and 4 u + 2, 4 u + 3 in the two halves
-//   values   lane (g, t): word i, slots 2 c and 2 c + 1, are entries g and g + 8 in half o
+//   values   lane (g, t): word i, slots 2 c and 2 c + 1, are entries e = 4 (g / 2) + g mod 2 and e + 2 in half o
 //   scales   of row r at (2 t + o) * 8 + 2 i + c
 // With 8 entries, two rows' words are one: word i / 2, slots 2 (i mod 2) + c, are entries
 // 2 u, 2 u + 1 of a key in the two halves, or entry g of a value in half o.

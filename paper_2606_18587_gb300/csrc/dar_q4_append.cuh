@@ -32,7 +32,7 @@ inline size_t few_smem(int Hkv)
 // many sequences as SMs no longer; the tiles of dar_q4_cache.cu take 6.4 us up to 8 tokens and more with every CTA.
 // Here and there, d_down 16, us (B, Hkv, n): 1, 12, 1: 5.0 and 6.4; 1, 12, 4: 8.6 and 6.6; 32, 1, 4: 7.4 and 7.0; 32, 12, 8:
 // 13.0 and 13.6; 32, 32, 4: 15.6 and 18.3; 32, 32, 8: 25 and 19; 128, 12, 8: 13.2 and 25.4; of 64 entries 32, 8, 4: 13.3 and
-// 17.3; 32, 8, 8: 20.8 and 18.0.
+// 17.3; 32, 8, 8: 20.8 and 18.0.  (Of these the rule gives 32, 12, 8 to the tiles.)
 template <typename T>
 inline bool append_is_few(const AppendArgs &a, int dd)
 {

@@ -247,7 +247,9 @@ static cudaError_t append_t(int dd, const AppendArgs &a, cudaStream_t s)
         // 2048: 15.3 and 16.8), and from bf16 in tiles of two pages once these fill the chip a few times over (12 KV
         // heads, d_down 16, 32 x 2048: 111 and 128; 32 x 64, 768 tiles: 13.9 and 15.5; 4 x 512, 480 tiles: 13.5 and
         // 11.3).  fp32 rows are twice as long: 212 and 210 at 32 x 2048.  d_down 8: 62 and 63, but 14.7 and 13.1 at 4 x
-        // 2048.  Four rows, or tiles of four pages: between 2 % less and 40 % more.
+        // 2048.  Not used: four rows a thread (64 entries in tiles of two pages 229 and 246 at 32 x 2048, 242 and 254 at 64 x
+        // 1024, but 19.4 and 15.6 at 4 x 512; else 4 % less to twice as long), tiles of four pages (32 entries 133 and 142 at
+        // 32 x 2048, but 22 and 17 at 32 x 64; 16 entries 2 % less there and 24 % more here; else longer).
         if constexpr (DD == 64) {
             return append_tiles<T, DD, 2, kPage / 2>(a, s);
         } else {
@@ -266,7 +268,9 @@ static cudaError_t convert_t(int dd, const Q4ConvertArgs &a, cudaStream_t s)
 {
     return by_width(dd, [&](auto width) {
         // 72 pages of fp32 vectors of 32 entries: 22 us a page to a warp, 7 a group; all contexts of the 1B shape (133 thousand
-        // pages, bf16): 158 and 192
+        // pages, bf16): 158 and 192.  Pages are counted by capacity, since lengths and `first` are on the device: the last 128
+        // tokens of 64 sequences of 8 heads take 3.2 us in a cache with room for no more, 8.5 with room for 3840 and 38 for
+        // 32512, most of them of warps that find nothing to do.
         const long long pages = (long long)std::min(a.maxp, a.maxp4) * a.Hkv;
         const int parts = pages * a.B < kSplitPages ? 2 * Fmt<decltype(width)::value>::kGroups : 1;
         const long long items = pages * parts;

@@ -42,7 +42,7 @@ template <int DD>
 __host__ __device__ constexpr int mma_warps() { return DD <= 16 ? 16 : 12; }
 template <int DD>
 __host__ __device__ constexpr int mma_slots() { return DD <= 16 ? 2 : 3; }
-// Registers of a thread: without spills, and for one or two heads of narrow vectors such that blocks of the first kernel
+// Registers of a thread: without spills (eight heads: 30 bytes at most), and for one or two heads of narrow vectors such that blocks of the first kernel
 // fit beside on an SM (else half the blocks start 1 us later; with four heads the spills cost more: 46.9 and 48.7 us).
 template <int DD, int NH>
 __host__ __device__ constexpr int mma_registers() { return DD > 16 ? 168 : NH < 4 ? 112 : 128; }
@@ -1676,7 +1676,8 @@ static cudaError_t launch(const Q4DecodeArgs &c, const AppendArgs *ap, void *wor
     // Few rows may have a partial result of every share each, and many rows few: 2, 4 and 16 warps a row take 17.2, 29 and
     // 44 us with 8 rows of 131072 tokens, 27.2, 27.0 and 33.1 with 1024 of 4096, and 77, 87 and 174 with 16384 of 2048.
     // Of few rows as many as take all that a sequence of the cache's capacity can have in one go: 4, 8 and 16 take 8.3,
-    // 8.5 and 9.0 with 901 tokens, 9.4, 8.8 and 9.5 with 2000, and 10.4, 9.9 and 9.7 with 4000.
+    // 8.5 and 9.0 with 901 tokens, 9.4, 8.8 and 9.5 with 2000, and 10.4, 9.9 and 9.7 with 4000.  (By capacity, since
+    // lengths are on the device: 901 tokens in a cache with room for 4096 or more take 8.8 to 9.0.)
     constexpr int least = kCostRun > cost_page<DD>() ? kCostRun : cost_page<DD>();  // of a share
     const int rows = c.B * c.Hq;
     const long long parts = unit_capacity<DD>(c.w, c.maxp) / least + 1;
